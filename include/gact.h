@@ -292,6 +292,137 @@ int gact_compress_footprint_noalloc(const void *d_x, gact_dtype dtype, int64_t n
                                     void *stream);
 
 /*
+ * Global norm of a list of gradient buffers, and clipping by it.
+ *     norm = sqrt(sum g^2)  (GACT_NORM_2)   or   max |g|  (GACT_NORM_INF), over all buffers together,
+ *     out  = g * min(1, max_norm / (norm + 1e-6)),   rounded once to the buffer's type,
+ * the squares added in binary64 in an order that depends on the list's sizes and types only.  A NaN among the
+ * gradients gives a NaN norm and NaN outputs; an infinity gives an infinite norm and outputs 0 (NaN at its place).
+ *   gact_grad_norm     d_norm receives the norm
+ *   gact_grad_clip     the same, and the scaled gradients in two launches
+ *   gact_grad_clip_by  scales by the norm in d_norm: one that several ranks have agreed on, or the square root
+ *                      of gact_grad_stats_update's d_out[0]
+ *   h_bufs       host array of K buffers of any alignment that their type has; g and out of n elements of `dtype`.
+ *                out may be g (then nothing is written where nothing has to be scaled); otherwise no output may
+ *                overlap an input, and no two outputs overlap (GACT_E_ARG): a buffer listed twice is refused
+ *                by the calls that scale.  gact_grad_norm ignores out and counts a buffer as often as it is listed.
+ *   max_norm     finite, >= 0
+ *   d_norm       device double[1]
+ *   d_workspace  device scratch, >= gact_grad_norm_workspace_bytes(K), 16-byte aligned; in use until the enqueued
+ *                kernels have run.  Calls that share one must not overlap in time.
+ * K == 0 or all n == 0 writes the norm 0.
+ * HIP graphs: all three calls can be captured, whatever K: a list of more than 136 non-empty buffers, whose table is
+ * uploaded otherwise, travels in the arguments of small kernels of its own then.  A replay uses the pointers, sizes
+ * and max_norm of the captured call and its workspace.
+ */
+typedef enum { GACT_NORM_2 = 0, GACT_NORM_INF = 1 } gact_norm_kind;
+
+typedef struct {
+    const void *g;
+    void       *out;
+    int64_t     n;
+    int32_t     dtype;     /* gact_dtype of g and out */
+    int32_t     reserved;
+} gact_grad_buf;
+
+size_t gact_grad_norm_workspace_bytes(int K);
+
+int gact_grad_norm(const gact_grad_buf *h_bufs, int K, int kind, double *d_norm, void *d_workspace,
+                   size_t workspace_bytes, void *stream);
+
+int gact_grad_clip(const gact_grad_buf *h_bufs, int K, int kind, double max_norm, double *d_norm,
+                   void *d_workspace, size_t workspace_bytes, void *stream);
+
+int gact_grad_clip_by(const gact_grad_buf *h_bufs, int K, double max_norm, const double *d_norm,
+                      void *d_workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Norms of queries and keys for each head with the position rotation in the same pass, whose context (x, the queries
+ * or keys before the norm) can leave the same pass compressed, and the gradients, taken from the compressed
+ * context without decompressing it to memory.  A tensor is [batch, tokens, heads, head_dim], its heads' elements
+ * consecutive, every other stride its own.  For each head of each token
+ *     r = 1 / sqrt(mean x^2 + eps),   n = x * r * w,
+ *     y_a = n_a * cos - n_b * sin,   y_b = n_b * cos + n_a * sin
+ * for the rot_dim / 2 pairs (a, b) of its first rot_dim elements, (i, i + rot_dim/2) or, `interleaved`,
+ * (2i, 2i + 1); y = n from rot_dim on.  Backward, with dn = dy rotated back,
+ *     dx = r * (dn * w - x * r^2 * mean(dn * w * x)),   dw = sum over heads and tokens of dn * x * r.
+ * Arithmetic in binary32, dw's sums over blocks in binary64 and in a fixed order; outputs rounded once.
+ *
+ * Context.  With bits in {1, 2, 4, 8} the forward pass writes what gact_compress gives for x laid out
+ * contiguously as [batch, tokens, heads, head_dim] with the same group_size, bits and seed, byte for byte, and the backward
+ * pass uses codes * step + minimum (in binary32, not rounded to the tensor's type) for x.  r is not taken from these:
+ * the forward pass leaves it in rstd, so that dw is linear in the compressed x and stays unbiased.  With
+ * GACT_BITS_UNCOMPRESSED nothing is compressed and the backward pass reads x.
+ *
+ *   h_parts      host array of 1 or 2 tensors (queries and keys), which go into one launch where their bits agree.
+ *     forward:   reads x; writes y, rstd (batch * tokens * heads floats; NULL without a backward pass, only with
+ *                bits == GACT_BITS_UNCOMPRESSED) and, compressing, packed (16-byte aligned), gmin and gscale.  y may be x
+ *                itself with x's strides; nothing else may overlap an output.
+ *     backward:  reads dy, rstd and packed, gmin, gscale (compressed) or x; writes dx and, where dw is not NULL, dw.
+ *                dx may be dy itself with dy's strides.
+ *     w, dw      head_dim weights and their gradients, of w_dtype; w NULL: no weights (dw must be NULL)
+ *     strides    in elements: batch, token, head
+ *     heads      may differ between the parts
+ *   h_rotation   what the parts share:
+ *     cos, sin   tables [n_positions, rot_dim / 2] in binary32; unused with rot_dim 0
+ *     positions  device int64 [batch * tokens], or NULL: a token's place in its sequence.  A token whose position is
+ *                outside [0, n_positions) gets NaN in its rotated elements (and in the gradients they reach); nothing
+ *                is read outside the tables.
+ *     head_dim   a multiple of 8 in [8, 512];  rot_dim a multiple of 16 in [0, head_dim]
+ *     group_size of a context: a power of two in [32, 512] that divides head_dim, or a multiple of 32 that is head_dim *
+ *                1, 2, 4, ... , at most 64 lanes of eight elements (a head occupies head_dim / 8 lanes rounded up to a
+ *                power of two); heads * head_dim must be a multiple of it.  GACT_E_GROUP otherwise: gact_compress takes
+ *                such a tensor.
+ *   batch * tokens * heads must be below 2^31.
+ *   d_workspace  backward: device scratch, >= gact_head_norm_rotate_workspace_bytes(head_dim), 16-byte aligned, in use
+ *                until the enqueued kernels have run; calls that share one must not overlap in time.  Not used (NULL) when
+ *                no dw is asked for.
+ * An empty tensor (batch or tokens 0) is GACT_OK; its dw is 0.  Both calls can be captured into a HIP graph.
+ */
+typedef struct {
+    const void *x;
+    void       *y;
+    const void *dy;
+    void       *dx;
+    const void *w;
+    void       *dw;
+    float      *rstd;
+    void       *packed;
+    float      *gmin;
+    float      *gscale;
+    int64_t     x_stride[3];
+    int64_t     y_stride[3];
+    int64_t     dy_stride[3];
+    int64_t     dx_stride[3];
+    uint64_t    seed;
+    int32_t     heads;
+    int32_t     bits;
+} gact_heads;
+
+typedef struct {
+    int64_t        batch;
+    int64_t        tokens;
+    const float   *cos;
+    const float   *sin;
+    const int64_t *positions;
+    int64_t        n_positions;
+    int32_t        head_dim;
+    int32_t        rot_dim;
+    int32_t        interleaved;
+    int32_t        dtype;       /* gact_dtype of x, y, dy, dx */
+    int32_t        w_dtype;     /* gact_dtype of w, dw */
+    int32_t        group_size;  /* of the contexts */
+    float          eps;         /* > 0; forward only */
+    int32_t        reserved;
+} gact_rotation;
+
+size_t gact_head_norm_rotate_workspace_bytes(int head_dim);
+
+int gact_head_norm_rotate(const gact_heads *h_parts, int n_parts, const gact_rotation *h_rotation, void *stream);
+
+int gact_head_norm_rotate_backward(const gact_heads *h_parts, int n_parts, const gact_rotation *h_rotation,
+                                   void *d_workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Variance alert (host only): V(b) = sum_l c_l S(b_l) (Thm. 2) against the
  * gradient variance.  Writes V / grad_var to *h_ratio (may be NULL) and
  * returns 1 if it exceeds `threshold`, 0 if not, a negative code on error.

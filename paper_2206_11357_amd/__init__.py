@@ -8,7 +8,9 @@ shared library cannot be loaded the import fails.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import math
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -29,6 +31,8 @@ GACT_E_HIP = -5
 GACT_E_CAPTURE = -6
 GACT_E_SCRATCH = -7
 GACT_NOALLOC_SCRATCH_BYTES = 2 << 20
+GACT_NORM_2 = 0
+GACT_NORM_INF = 1
 
 EXPORTS = (
     "gact_num_groups", "gact_packed_bytes", "gact_error_string", "gact_compress",
@@ -37,6 +41,8 @@ EXPORTS = (
     "gact_sensitivity", "gact_grad_stats_update", "gact_variance_alert",
     "gact_allocate_bits_levels", "gact_footprint", "gact_compress_footprint",
     "gact_compress_footprint_workspace_bytes", "gact_compress_footprint_noalloc", "gact_copy_bounded",
+    "gact_grad_norm_workspace_bytes", "gact_grad_norm", "gact_grad_clip", "gact_grad_clip_by",
+    "gact_head_norm_rotate_workspace_bytes", "gact_head_norm_rotate", "gact_head_norm_rotate_backward",
 )
 GACT_BITS_UNCOMPRESSED = 32
 
@@ -65,6 +71,30 @@ class GradStat(ctypes.Structure):
     """Mirror of gact_grad_stat."""
     _fields_ = [("g", ctypes.c_void_p), ("mean", ctypes.c_void_p), ("n", ctypes.c_int64),
                 ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class GradBuf(ctypes.Structure):
+    """Mirror of gact_grad_buf."""
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class Heads(ctypes.Structure):
+    """Mirror of gact_heads."""
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("dy", ctypes.c_void_p), ("dx", ctypes.c_void_p),
+                ("w", ctypes.c_void_p), ("dw", ctypes.c_void_p), ("rstd", ctypes.c_void_p), ("packed", ctypes.c_void_p),
+                ("gmin", ctypes.c_void_p), ("gscale", ctypes.c_void_p), ("x_stride", ctypes.c_int64 * 3),
+                ("y_stride", ctypes.c_int64 * 3), ("dy_stride", ctypes.c_int64 * 3), ("dx_stride", ctypes.c_int64 * 3),
+                ("seed", ctypes.c_uint64), ("heads", ctypes.c_int32), ("bits", ctypes.c_int32)]
+
+
+class Rotation(ctypes.Structure):
+    """Mirror of gact_rotation."""
+    _fields_ = [("batch", ctypes.c_int64), ("tokens", ctypes.c_int64), ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("n_positions", ctypes.c_int64), ("head_dim", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("w_dtype", ctypes.c_int32), ("group_size", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
 
 
 def _load() -> ctypes.CDLL:
@@ -113,6 +143,20 @@ def _load() -> ctypes.CDLL:
     lib.gact_copy_bounded.restype = i32
     lib.gact_variance_alert.argtypes = [vp, vp, i32, ctypes.c_double, ctypes.c_double, vp]
     lib.gact_variance_alert.restype = i32
+    lib.gact_grad_norm_workspace_bytes.argtypes = [i32]
+    lib.gact_grad_norm_workspace_bytes.restype = sz
+    lib.gact_grad_norm.argtypes = [vp, i32, i32, vp, vp, sz, vp]
+    lib.gact_grad_norm.restype = i32
+    lib.gact_grad_clip.argtypes = [vp, i32, i32, ctypes.c_double, vp, vp, sz, vp]
+    lib.gact_grad_clip.restype = i32
+    lib.gact_grad_clip_by.argtypes = [vp, i32, ctypes.c_double, vp, vp, sz, vp]
+    lib.gact_grad_clip_by.restype = i32
+    lib.gact_head_norm_rotate_workspace_bytes.argtypes = [i32]
+    lib.gact_head_norm_rotate_workspace_bytes.restype = sz
+    lib.gact_head_norm_rotate.argtypes = [vp, i32, vp, vp]
+    lib.gact_head_norm_rotate.restype = i32
+    lib.gact_head_norm_rotate_backward.argtypes = [vp, i32, vp, vp, sz, vp]
+    lib.gact_head_norm_rotate_backward.restype = i32
     return lib
 
 
@@ -470,3 +514,323 @@ def gact_variance_alert(sensitivity, bits, grad_var: float, threshold: float):
     if rc < 0:
         raise GactError(rc, "gact_variance_alert")
     return bool(rc), ratio.value
+
+
+# ------------------------------------------------- gradient norm and clipping
+def _enqueue(fn, name: str, device: torch.device, stream, *args) -> None:
+    """fn(*args, stream) on the tensors' device, whichever is current."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream(stream))
+    else:
+        rc = fn(*args, _stream(stream))
+    if rc != GACT_OK:
+        raise GactError(rc, name)
+
+
+def _allocating_for(stream, device: torch.device):
+    """Where a call on `stream` allocates its outputs and scratch: under that stream, so that the allocator hands their
+    memory out again only behind the call."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if type(stream) is int:
+        stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
+
+
+def _same_device(tensors) -> torch.device:
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("gact needs device tensors")
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError("the tensors of a call lie on different devices")
+    return device if device is not None else torch.device("cuda", torch.cuda.current_device())
+
+
+def _dense(t: torch.Tensor) -> bool:
+    return (t.is_contiguous() or (t.dim() == 4 and t.is_contiguous(memory_format=torch.channels_last))
+            or (t.dim() == 5 and t.is_contiguous(memory_format=torch.channels_last_3d)))
+
+
+def gact_grad_norm_workspace_bytes(K: int) -> int:
+    return int(lib.gact_grad_norm_workspace_bytes(K))
+
+
+def make_grad_bufs(g: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None):
+    """ctypes array of gact_grad_buf (reusable across calls while the buffers live); without `outs` in place."""
+    g = list(g)
+    outs = g if outs is None else list(outs)
+    if len(outs) != len(g):
+        raise ValueError("g and outs must list the same buffers")
+    _same_device(g + outs if outs is not g else g)
+    arr = (GradBuf * max(len(g), 1))()
+    for k, (a, o) in enumerate(zip(g, outs)):
+        if not _dense(a):
+            raise ValueError("buffer %d: gact needs contiguous tensors" % k)
+        if o is not a and (o.dtype != a.dtype or o.shape != a.shape or o.stride() != a.stride()):
+            raise ValueError("buffer %d: g and its output differ in size, dtype or strides" % k)
+        arr[k].g, arr[k].out, arr[k].n, arr[k].dtype = a.data_ptr(), o.data_ptr(), a.numel(), dtype_code(a.dtype)
+    return arr
+
+
+def _norm_kind(norm_type: float) -> int:
+    if norm_type == 2:
+        return GACT_NORM_2
+    if norm_type == math.inf:
+        return GACT_NORM_INF
+    raise ValueError("norm_type must be 2 or inf, got %r" % (norm_type,))
+
+
+def _norm_call(g, outs, norm, workspace, stream, bufs):
+    """What the three calls share: (K, table, device, norm, workspace)."""
+    g = list(g)
+    arr = bufs if bufs is not None else make_grad_bufs(g, outs)
+    if len(arr) < len(g):
+        raise ValueError("bufs lists fewer buffers than g")
+    device = _same_device(g[:1])
+    if norm is None or workspace is None:
+        with _allocating_for(stream, device):
+            if norm is None:
+                norm = torch.empty(1, dtype=torch.float64, device=device)
+            if workspace is None:
+                workspace = torch.empty(gact_grad_norm_workspace_bytes(len(g)), dtype=torch.uint8, device=device)
+    if norm.dtype != torch.float64 or norm.numel() != 1:
+        raise ValueError("the norm is one float64 element")
+    if _same_device([norm, workspace]) != device:
+        raise ValueError("the tensors of a call lie on different devices")
+    return len(g), arr, device, norm, workspace
+
+
+def gact_grad_norm(g: Sequence[torch.Tensor], norm_type: float = 2.0, out: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None, bufs=None) -> torch.Tensor:
+    """Norm over all buffers together, 2 or inf -> device float64[1].  `bufs` (from make_grad_bufs) skips
+    re-marshalling the list."""
+    kind = _norm_kind(norm_type)
+    K, arr, device, out, workspace = _norm_call(g, None, out, workspace, stream, bufs)
+    _enqueue(lib.gact_grad_norm, "gact_grad_norm", device, stream, ctypes.addressof(arr), K, kind, out.data_ptr(),
+             workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return out
+
+
+def gact_grad_clip(g: Sequence[torch.Tensor], max_norm: float, norm_type: float = 2.0,
+                   outs: Optional[Sequence[torch.Tensor]] = None, norm: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None, bufs=None) -> torch.Tensor:
+    """Scales the buffers by min(1, max_norm / (norm + 1e-6)), in place or into `outs`; returns their norm before,
+    device float64[1]."""
+    kind = _norm_kind(norm_type)
+    K, arr, device, norm, workspace = _norm_call(g, outs, norm, workspace, stream, bufs)
+    _enqueue(lib.gact_grad_clip, "gact_grad_clip", device, stream, ctypes.addressof(arr), K, kind, float(max_norm),
+             norm.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return norm
+
+
+def gact_grad_clip_by(g: Sequence[torch.Tensor], max_norm: float, norm: torch.Tensor,
+                      outs: Optional[Sequence[torch.Tensor]] = None, workspace: Optional[torch.Tensor] = None,
+                      stream=None, bufs=None) -> None:
+    """gact_grad_clip by a norm that is known already (device float64[1])."""
+    K, arr, device, norm, workspace = _norm_call(g, outs, norm, workspace, stream, bufs)
+    _enqueue(lib.gact_grad_clip_by, "gact_grad_clip_by", device, stream, ctypes.addressof(arr), K, float(max_norm),
+             norm.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+# ---------------------------------------------- norms of heads and rotation
+class HeadContext:
+    """What the forward pass keeps of one tensor (queries or keys) for its gradient: rstd, and the compressed
+    context where bits is not GACT_BITS_UNCOMPRESSED."""
+    __slots__ = ("bits", "group_size", "seed", "rstd", "packed", "gmin", "gscale")
+
+    def __init__(self, bits, group_size, seed, rstd, packed=None, gmin=None, gscale=None):
+        self.bits, self.group_size, self.seed, self.rstd = bits, group_size, seed, rstd
+        self.packed, self.gmin, self.gscale = packed, gmin, gscale
+
+
+def make_head_context(x: torch.Tensor, bits: int = GACT_BITS_UNCOMPRESSED, group_size: int = 0, seed: int = 0,
+                      stream=None) -> HeadContext:
+    """Buffers for the context of x, [batch, tokens, heads, head_dim] or [tokens, heads, head_dim]."""
+    with _allocating_for(stream, x.device):
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        if bits == GACT_BITS_UNCOMPRESSED:
+            return HeadContext(bits, group_size, seed, rstd)
+        return HeadContext(bits, group_size, seed, rstd, *alloc_compressed(x.numel(), max(group_size, 1), bits, x.device))
+
+
+def head_context_fits(group_size: int, head_dim: int, *heads: int) -> bool:
+    """Whether the forward pass can compress the context of heads of this size in groups of group_size (gact.h)."""
+    if group_size < 32 or group_size % 32 or head_dim % 8 or not 8 <= head_dim <= 512:
+        return False
+    lanes = 1 << (head_dim // 8 - 1).bit_length()
+    n = group_size // head_dim
+    fits = (head_dim % group_size == 0 and group_size & (group_size - 1) == 0 if group_size < head_dim
+            else group_size % head_dim == 0 and n & (n - 1) == 0 and n * lanes <= 64)
+    return fits and all(h * head_dim % group_size == 0 for h in heads)
+
+
+def gact_head_norm_rotate_workspace_bytes(head_dim: int) -> int:
+    return int(lib.gact_head_norm_rotate_workspace_bytes(head_dim))
+
+
+def _head_shape(x: torch.Tensor):
+    if x.dim() not in (3, 4):
+        raise ValueError("gact needs [batch, tokens, heads, head_dim] or [tokens, heads, head_dim]")
+    return tuple(x.shape) if x.dim() == 4 else (1,) + tuple(x.shape)
+
+
+def _head_strides(x: torch.Tensor):
+    if x.shape[-1] > 1 and x.stride(-1) != 1:
+        raise ValueError("a head's elements must be consecutive")
+    return x.stride()[:3] if x.dim() == 4 else (0,) + x.stride()[:2]
+
+
+def _rotation(x: torch.Tensor, cos, sin, positions, interleaved: bool, weights) -> Rotation:
+    """The record that queries and keys share, from one of them."""
+    B, S, _, D = _head_shape(x)
+    r = Rotation()
+    r.batch, r.tokens, r.head_dim, r.dtype, r.interleaved = B, S, D, dtype_code(x.dtype), int(bool(interleaved))
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin belong together")
+    if cos is not None:
+        if cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32 \
+                or not cos.is_contiguous() or not sin.is_contiguous():
+            raise ValueError("cos and sin must be contiguous float32 tables [positions, rot_dim / 2]")
+        r.n_positions, r.rot_dim = cos.shape[0], 2 * cos.shape[1]
+        r.cos, r.sin = cos.data_ptr(), sin.data_ptr()
+        if positions is not None:
+            if positions.dtype != torch.int64 or positions.numel() != B * S or not positions.is_contiguous():
+                raise ValueError("positions must be contiguous int64, one per token")
+            r.positions = positions.data_ptr()
+        elif S > r.n_positions:
+            raise ValueError("the tables hold fewer positions than a sequence has tokens")
+    types = {w.dtype for w in weights if w is not None}
+    if len(types) > 1:
+        raise ValueError("the weights must have one type")
+    r.w_dtype = dtype_code(types.pop()) if types else GACT_F32
+    return r
+
+
+def _head_part(h: Heads, field: str, t: torch.Tensor, like: torch.Tensor) -> None:
+    if _head_shape(t) != _head_shape(like) or t.dtype != like.dtype:
+        raise ValueError("%s: shape or dtype differ" % field)
+    setattr(h, field, t.data_ptr())
+    setattr(h, field + "_stride", (ctypes.c_int64 * 3)(*_head_strides(t)))
+
+
+def _head_weights(h: Heads, w, D: int) -> None:
+    if w is not None:
+        if w.numel() != D or not w.is_contiguous():
+            raise ValueError("the weights must be contiguous, one per element of a head")
+        h.w = w.data_ptr()
+
+
+def _head_context(h: Heads, c: Optional[HeadContext], shape, r: Rotation) -> None:
+    h.heads, h.bits = shape[2], GACT_BITS_UNCOMPRESSED
+    if c is None:
+        return
+    n = shape[0] * shape[1] * shape[2]
+    if c.rstd.numel() != n or c.rstd.dtype != torch.float32 or not c.rstd.is_contiguous():
+        raise ValueError("the context was made for another shape")
+    h.rstd, h.bits, h.seed = c.rstd.data_ptr(), c.bits, c.seed & (2**64 - 1)
+    if c.bits != GACT_BITS_UNCOMPRESSED:
+        n *= shape[3]
+        groups = gact_num_groups(n, c.group_size)
+        if c.packed.numel() < gact_packed_bytes(n, c.bits) or c.gmin.numel() < groups or c.gscale.numel() < groups:
+            raise ValueError("the context was made for another shape")
+        if r.group_size not in (0, c.group_size):
+            raise ValueError("the contexts of a call must have one group size")
+        r.group_size = c.group_size
+        h.packed, h.gmin, h.gscale = c.packed.data_ptr(), c.gmin.data_ptr(), c.gscale.data_ptr()
+
+
+def _forward_record(q, k, cos, sin, wq, wk, positions, eps, interleaved, out, context):
+    """(parts, number of parts, rotation) of a forward call into `out`."""
+    xs = [q] if k is None else [q, k]
+    ws, ctxs = (wq, wk), context if context is not None else (None, None)
+    _same_device(xs + [cos, sin, wq, wk, positions] + list(out))
+    if k is not None and (_head_shape(k)[:2] != _head_shape(q)[:2] or k.shape[-1] != q.shape[-1] or k.dtype != q.dtype):
+        raise ValueError("queries and keys differ in batch, tokens, head_dim or dtype")
+    r = _rotation(q, cos, sin, positions, interleaved, ws[:len(xs)])
+    r.eps = eps
+    parts = (Heads * 2)()
+    for h, x, y, w, c in zip(parts, xs, out, ws, ctxs):
+        _head_part(h, "x", x, x)
+        _head_part(h, "y", y, x)
+        _head_weights(h, w, x.shape[-1])
+        _head_context(h, c, _head_shape(x), r)
+    return parts, len(xs), r
+
+
+def gact_head_norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], cos: Optional[torch.Tensor],
+                          sin: Optional[torch.Tensor], wq: Optional[torch.Tensor] = None,
+                          wk: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                          eps: float = 1e-6, interleaved: bool = False, out=None, context=None, stream=None):
+    """RMS norm of every head of q and k ([batch, tokens, heads, head_dim], any strides but the last) with its weights,
+    then the position rotation; returns (yq, yk).  cos, sin: float32 tables [positions, rot_dim / 2], or None for no
+    rotation; positions: int64 per token, or None for a token's place in its sequence; out: tensors of the same shapes
+    (a transposed view lets the result lie head by head); context: two HeadContexts that the pass fills."""
+    device = _same_device([q, k])
+    if out is None:
+        with _allocating_for(stream, device):
+            out = tuple(None if x is None else torch.empty(x.shape, dtype=x.dtype, device=device) for x in (q, k))
+    parts, n, r = _forward_record(q, k, cos, sin, wq, wk, positions, eps, interleaved, out, context)
+    _enqueue(lib.gact_head_norm_rotate, "gact_head_norm_rotate", device, stream, ctypes.addressof(parts), n,
+             ctypes.addressof(r))
+    return out
+
+
+def prepare_head_norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], cos, sin, wq=None, wk=None, positions=None,
+                             eps: float = 1e-6, interleaved: bool = False, *, out, context=None) -> PreparedCall:
+    """gact_head_norm_rotate(...) into `out`, as a PreparedCall."""
+    parts, n, r = _forward_record(q, k, cos, sin, wq, wk, positions, eps, interleaved, out, context)
+    vp = ctypes.c_void_p
+    args = (vp(ctypes.addressof(parts)), n, vp(ctypes.addressof(r)))
+    return PreparedCall(lib.gact_head_norm_rotate, "gact_head_norm_rotate", args,
+                        (parts, r, q, k, cos, sin, wq, wk, positions, out, context))
+
+
+def gact_head_norm_rotate_backward(dyq: Optional[torch.Tensor], dyk: Optional[torch.Tensor], cos, sin, wq=None, wk=None,
+                                   positions=None, *, context, x=None, interleaved: bool = False, out=None,
+                                   weight_grads=(True, True), workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of gact_head_norm_rotate from dyq, dyk (any strides but the last) and the contexts it has filled; x =
+    (q, k) where these are not compressed.  Returns (dq, dk, dwq, dwk); None for a part without dy, without weights or
+    whose weight gradient is not wanted."""
+    dys, ws = (dyq, dyk), (wq, wk)
+    live = [i for i in (0, 1) if dys[i] is not None]
+    if not live:
+        return None, None, None, None
+    xs = x if x is not None else (None, None)
+    device = _same_device([dyq, dyk, cos, sin, wq, wk, positions] + list(xs) + [context[i].rstd for i in live])
+    first = dys[live[0]]
+    D = first.shape[-1]
+    if len(live) == 2 and (_head_shape(dyk)[:2] != _head_shape(dyq)[:2] or dyk.shape[-1] != D or dyk.dtype != dyq.dtype):
+        raise ValueError("queries and keys differ in batch, tokens, head_dim or dtype")
+    r = _rotation(first, cos, sin, positions, interleaved, [ws[i] for i in live])
+    wanted = [ws[i] is not None and bool(weight_grads[i]) for i in (0, 1)]
+    dxs, dws = [None, None], [None, None]
+    with _allocating_for(stream, device):
+        for i in live:
+            dxs[i] = out[i] if out is not None else torch.empty(dys[i].shape, dtype=dys[i].dtype, device=device)
+            if wanted[i]:
+                dws[i] = torch.empty(ws[i].shape, dtype=ws[i].dtype, device=device)
+        if any(wanted[i] for i in live) and workspace is None:
+            workspace = torch.empty(gact_head_norm_rotate_workspace_bytes(D), dtype=torch.uint8, device=device)
+    _same_device([first, workspace] + dxs)
+    parts = (Heads * 2)()
+    for h, i in zip(parts, live):
+        _head_part(h, "dy", dys[i], dys[i])
+        _head_part(h, "dx", dxs[i], dys[i])
+        _head_weights(h, ws[i], D)
+        if dws[i] is not None:
+            h.dw = dws[i].data_ptr()
+        _head_context(h, context[i], _head_shape(dys[i]), r)
+        if context[i].bits == GACT_BITS_UNCOMPRESSED:
+            if xs[i] is None:
+                raise ValueError("the context is not compressed: x is needed")
+            _head_part(h, "x", xs[i], dys[i])
+    _enqueue(lib.gact_head_norm_rotate_backward, "gact_head_norm_rotate_backward", device, stream, ctypes.addressof(parts),
+             len(live), ctypes.addressof(r), workspace.data_ptr() if workspace is not None else None,
+             workspace.numel() * workspace.element_size() if workspace is not None else 0)
+    return dxs[0], dxs[1], dws[0], dws[1]

@@ -14,6 +14,8 @@
 
 #include "gact.h"
 #include "gact_device.h"
+#include "gact_heads.h"
+#include "gact_norm.h"
 #include "gact_sum.h"
 
 // Scratch area of gact_compress_footprint_noalloc: device memory that is part
@@ -395,6 +397,217 @@ int compress_footprint(const void* d_x, gact_dtype dtype, int64_t n, int group_s
                                         d_footprint, stream) == 0 ? GACT_OK : GACT_E_HIP;
 }
 
+// ------------------------------------------------------------- gradient norm
+size_t norm_table_bytes(int K) {
+    return ((size_t)K * sizeof(gact::NormBuffer) + (size_t)(K + 1) * sizeof(uint32_t) + 15) / 16 * 16;
+}
+constexpr size_t kNormPartials = gact::kNormBlocks * sizeof(double);
+
+// Whether an output overlaps another one, or an input that is not its own buffer in place.
+bool outputs_overlap(const std::vector<gact::NormBuffer>& bufs, size_t f32) {
+    struct Range { uintptr_t begin, end; bool out; };
+    std::vector<Range> ranges;
+    ranges.reserve(2 * bufs.size());
+    for (size_t k = 0; k < bufs.size(); ++k) {
+        const uintptr_t bytes = (uintptr_t)bufs[k].n * (k < f32 ? 4 : 2);
+        const uintptr_t in = (uintptr_t)bufs[k].in, out = (uintptr_t)bufs[k].out;
+        ranges.push_back(Range{out, out + bytes, true});
+        if (in != out) ranges.push_back(Range{in, in + bytes, false});
+    }
+    std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+    uintptr_t any_end = 0, out_end = 0;
+    for (const Range& r : ranges) {
+        if (r.begin < (r.out ? any_end : out_end)) return true;
+        any_end = std::max(any_end, r.end);
+        if (r.out) out_end = std::max(out_end, r.end);
+    }
+    return false;
+}
+
+// What the three calls share: checks, the buffers' table (in *table, or in the workspace where it is too long for
+// the arguments), the launch's blocks.
+int stage_norm(const gact_grad_buf* bufs, int K, bool scale, const double* d_norm, void* d_workspace, size_t workspace_bytes,
+               void* stream, gact::NormTable* table, gact::NormArgs* a, bool* is_inline) {
+    if (K < 0 || (K > 0 && !bufs) || !d_norm || !aligned(d_norm, 8)) return GACT_E_ARG;
+    if (!d_workspace || !aligned(d_workspace, 16) || workspace_bytes < gact_grad_norm_workspace_bytes(K)) return GACT_E_ARG;
+    std::vector<gact::NormBuffer> live;
+    live.reserve((size_t)K);
+    std::vector<uint32_t> first;
+    first.reserve((size_t)K + 1);
+    uint64_t chunks = 0;
+    for (const int dtype : {GACT_F32, GACT_BF16}) {
+        for (int k = 0; k < K; ++k) {
+            const gact_grad_buf& b = bufs[k];
+            if (!dtype_ok(b.dtype) || b.n < 0) return GACT_E_ARG;
+            if (b.dtype != dtype || b.n == 0) continue;
+            const size_t size = dtype == GACT_F32 ? 4 : 2;
+            if (!b.g || !aligned(b.g, size) || (scale && (!b.out || !aligned(b.out, size)))) return GACT_E_ARG;
+            live.push_back(gact::NormBuffer{b.g, b.out, b.n});
+            first.push_back((uint32_t)chunks);
+            chunks += ((uint64_t)b.n - 1) / (uint64_t)gact::norm_chunk_elems(dtype) + 1;
+            if (chunks > 0x7FFFFFFFull) return GACT_E_ARG;
+        }
+        if (dtype == GACT_F32) a->f32 = (uint32_t)live.size();
+    }
+    first.push_back((uint32_t)chunks);
+    if (scale && outputs_overlap(live, a->f32)) return GACT_E_ARG;
+    a->K = (uint32_t)live.size();
+    a->chunks = (uint32_t)chunks;
+    a->blocks = (uint32_t)std::min<uint64_t>(chunks, gact::kNormBlocks);
+    a->partial = (double*)d_workspace;
+    a->norm = const_cast<double*>(d_norm);
+    *is_inline = a->K <= (uint32_t)gact::kInlineNorm;
+    if (*is_inline) {
+        std::memcpy(table->t, live.data(), live.size() * sizeof(gact::NormBuffer));
+        std::memcpy(table->first, first.data(), first.size() * sizeof(uint32_t));
+        return GACT_OK;
+    }
+    unsigned char* base = (unsigned char*)d_workspace + kNormPartials;
+    const size_t tb = live.size() * sizeof(gact::NormBuffer), bytes = tb + first.size() * sizeof(uint32_t);
+    a->table = (const gact::NormBuffer*)base;
+    a->first = (const uint32_t*)(base + tb);
+    std::vector<unsigned char> image(bytes);
+    std::memcpy(image.data(), live.data(), tb);
+    std::memcpy(image.data() + tb, first.data(), first.size() * sizeof(uint32_t));
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing((hipStream_t)stream, &status) != hipSuccess) return GACT_E_HIP;
+    if (status == hipStreamCaptureStatusNone) return upload(base, image.data(), bytes, stream);
+    for (size_t at = 0; at < bytes; at += gact::kTablePiece) {
+        gact::TablePiece piece{};
+        const size_t part = std::min<size_t>(gact::kTablePiece, bytes - at);
+        std::memcpy(piece.w, image.data() + at, part);
+        if (gact_launch_table_piece(base + at, &piece, (unsigned)(part / 4), stream) != 0) return GACT_E_HIP;
+    }
+    return GACT_OK;
+}
+
+int run_norm(const gact_grad_buf* bufs, int K, int kind, bool scale, bool given, double max_norm, const double* d_norm,
+             void* d_workspace, size_t workspace_bytes, void* stream) {
+    if (kind != GACT_NORM_2 && kind != GACT_NORM_INF) return GACT_E_ARG;
+    if (scale && !(max_norm >= 0.0 && std::isfinite(max_norm))) return GACT_E_ARG;
+    gact::NormTable table;
+    gact::NormArgs a{};
+    a.max_norm = max_norm;
+    bool is_inline = false;
+    if (const int rc = stage_norm(bufs, K, scale, d_norm, d_workspace, workspace_bytes, stream, &table, &a, &is_inline)) return rc;
+    const gact::NormTable* t = is_inline ? &table : nullptr;
+    scale = scale && a.blocks != 0;
+    if (!given && gact_launch_grad_norm(t, &a, kind, !scale, stream) != 0) return GACT_E_HIP;
+    if (scale && gact_launch_grad_clip(t, &a, kind, given, stream) != 0) return GACT_E_HIP;
+    return GACT_OK;
+}
+
+// -------------------------------------------------- norms of heads and rotation
+int log2_up(int v) {
+    int s = 0;
+    while ((1 << s) < v) ++s;
+    return s;
+}
+
+// How a context's groups lie in the heads; false if they do not.
+bool group_of_heads(int G, int dim, gact::HeadArgs* a) {
+    if (G < 32 || G % 32 != 0) return false;
+    if (G < dim) {
+        if ((G & (G - 1)) != 0 || dim % G != 0) return false;
+        a->group_lanes = G / 8;
+        a->groups_per_row = dim / G;
+        a->group_shift = log2_up(G);
+        return true;
+    }
+    const int heads = G / dim;
+    if (G % dim != 0 || (heads & (heads - 1)) != 0 || (heads << a->lanes_shift) > 64) return false;
+    a->group_lanes = heads << a->lanes_shift;
+    a->groups_per_row = 0;
+    a->row_shift = log2_up(heads);
+    return true;
+}
+
+gact::HeadTensor head_tensor(const void* p, const int64_t (&stride)[3]) {
+    return gact::HeadTensor{const_cast<void*>(p), stride[0], stride[1], stride[2]};
+}
+
+// Checks a call and fills what its parts share, then the parts.  `bits` of part k goes to part_bits[k], 0 without a context.
+int stage_heads(const gact_heads* parts, int n_parts, const gact_rotation* r, bool backward, gact::HeadArgs* a, int* part_bits) {
+    if (!parts || n_parts < 1 || n_parts > gact::kHeadParts || !r) return GACT_E_ARG;
+    if (!dtype_ok(r->dtype) || !dtype_ok(r->w_dtype) || r->batch < 0 || r->tokens < 0) return GACT_E_ARG;
+    const int dim = r->head_dim;
+    if (dim < 8 || dim > gact::kMaxHeadDim || dim % 8 != 0 || r->rot_dim < 0 || r->rot_dim > dim || r->rot_dim % 16 != 0)
+        return GACT_E_ARG;
+    if (!backward && !(r->eps > 0.0f && std::isfinite(r->eps))) return GACT_E_ARG;
+    if (r->batch > 0x7FFFFFFFll || r->tokens > 0x7FFFFFFFll || r->batch * r->tokens > 0x7FFFFFFFll) return GACT_E_ARG;
+    const int64_t tokens = r->batch * r->tokens;
+    if (r->rot_dim > 0 && tokens > 0 &&
+        (!r->cos || !r->sin || !aligned(r->cos, 4) || !aligned(r->sin, 4) || !aligned(r->positions, 8) || r->n_positions < 0))
+        return GACT_E_ARG;
+    const size_t size = r->dtype == GACT_F32 ? 4 : 2, w_size = r->w_dtype == GACT_F32 ? 4 : 2;
+    a->cos = r->cos;
+    a->sin = r->sin;
+    a->positions = r->positions;
+    a->n_positions = r->n_positions;
+    a->seq = (uint32_t)r->tokens;
+    a->by_seq = gact::divisor(a->seq);
+    a->eps = r->eps;
+    a->inv_dim = 1.0f / (float)dim;
+    a->dim = dim;
+    a->lanes_shift = log2_up(dim / 8);
+    a->rot_lanes = r->rot_dim / 8;
+    a->w_f32 = r->w_dtype == GACT_F32;
+    const uint32_t rows_per_pass = 64u >> a->lanes_shift;
+    for (int k = 0; k < n_parts; ++k) {
+        const gact_heads& h = parts[k];
+        gact::HeadPart& p = a->part[k];
+        if (h.bits != GACT_BITS_UNCOMPRESSED && !bits_ok(h.bits)) return GACT_E_BITS;
+        part_bits[k] = h.bits == GACT_BITS_UNCOMPRESSED ? 0 : h.bits;
+        if (h.heads < 1 || tokens * h.heads > 0x7FFFFFFFll) return GACT_E_ARG;
+        if (part_bits[k] != 0 && (!group_of_heads(r->group_size, dim, a) || ((int64_t)h.heads * dim) % r->group_size != 0))
+            return GACT_E_GROUP;
+        if (!aligned(h.w, w_size) || (backward && h.dw && (!h.w || !aligned(h.dw, w_size)))) return GACT_E_ARG;
+        const void* in = backward ? h.dy : h.x;
+        void* out = backward ? h.dx : h.y;
+        const bool read_x = backward && part_bits[k] == 0;
+        if (tokens > 0) {
+            if (!in || !out || !aligned(in, size) || !aligned(out, size) || !aligned(h.rstd, 4)) return GACT_E_ARG;
+            if (!h.rstd && (backward || part_bits[k] != 0)) return GACT_E_ARG;
+            if (read_x && (!h.x || !aligned(h.x, size))) return GACT_E_ARG;
+            if (part_bits[k] != 0 && (!h.packed || !h.gmin || !h.gscale || !aligned(h.packed, 16) || !aligned(h.gmin, 4) ||
+                                      !aligned(h.gscale, 4)))
+                return GACT_E_ARG;
+        }
+        p.in = backward ? head_tensor(h.dy, h.dy_stride) : head_tensor(h.x, h.x_stride);
+        p.out = backward ? head_tensor(h.dx, h.dx_stride) : head_tensor(h.y, h.y_stride);
+        p.x = head_tensor(h.x, h.x_stride);
+        p.w = h.w;
+        p.dw = backward ? h.dw : nullptr;
+        p.rstd = h.rstd;
+        p.packed = (uint8_t*)h.packed;
+        p.gmin = h.gmin;
+        p.gscale = h.gscale;
+        p.rows = (uint32_t)(tokens * h.heads);
+        p.heads = (uint32_t)h.heads;
+        p.by_heads = gact::divisor(p.heads);
+        p.seed_lo = (uint32_t)h.seed;
+        p.seed_hi = (uint32_t)(h.seed >> 32);
+        p.passes = (p.rows + rows_per_pass - 1) / rows_per_pass;
+    }
+    return GACT_OK;
+}
+
+// The launches of a staged call: one where the parts have the same kind of context, else one for each.
+int launch_heads(const gact::HeadArgs& a, int n_parts, const int* part_bits, const gact_rotation* r, bool backward, void* stream) {
+    const int halves = r->interleaved == 0;
+    const bool together = n_parts == 1 || part_bits[0] == part_bits[1];
+    for (int k = 0; k < (together ? 1 : n_parts); ++k) {
+        gact::HeadArgs one = a;
+        if (!together) {
+            one.part[0] = a.part[k];
+            one.part[1].blocks = 0;
+        }
+        if (one.part[0].blocks + one.part[1].blocks == 0) continue;
+        if (gact_launch_heads(&one, r->dtype, part_bits[k], halves, backward, stream) != 0) return GACT_E_HIP;
+    }
+    return GACT_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -548,6 +761,60 @@ int gact_compress_footprint_noalloc(const void* d_x, gact_dtype dtype, int64_t n
     if (const int rc = scratch_of_current_device(&area)) return rc;
     return compress_footprint(d_x, dtype, n, group_size, bits, seed, d_packed, d_gmin, d_gscale,
                               n_samples, d_footprint, area, GACT_NOALLOC_SCRATCH_BYTES, true, stream);
+}
+
+// ------------------------------------------------ gradient norm, clipping
+size_t gact_grad_norm_workspace_bytes(int K) { return K < 0 ? 0 : kNormPartials + norm_table_bytes(K); }
+
+int gact_grad_norm(const gact_grad_buf* h_bufs, int K, int kind, double* d_norm, void* d_workspace, size_t workspace_bytes,
+                   void* stream) {
+    return run_norm(h_bufs, K, kind, false, false, 0.0, d_norm, d_workspace, workspace_bytes, stream);
+}
+
+int gact_grad_clip(const gact_grad_buf* h_bufs, int K, int kind, double max_norm, double* d_norm, void* d_workspace,
+                   size_t workspace_bytes, void* stream) {
+    return run_norm(h_bufs, K, kind, true, false, max_norm, d_norm, d_workspace, workspace_bytes, stream);
+}
+
+int gact_grad_clip_by(const gact_grad_buf* h_bufs, int K, double max_norm, const double* d_norm, void* d_workspace,
+                      size_t workspace_bytes, void* stream) {
+    return run_norm(h_bufs, K, GACT_NORM_2, true, true, max_norm, d_norm, d_workspace, workspace_bytes, stream);
+}
+
+// ---------------------------------------------- norms of heads and rotation
+size_t gact_head_norm_rotate_workspace_bytes(int head_dim) {
+    if (head_dim < 8 || head_dim > gact::kMaxHeadDim || head_dim % 8 != 0) return 0;
+    return (size_t)gact::kHeadBackwardBlocks * (size_t)head_dim * sizeof(float);
+}
+
+int gact_head_norm_rotate(const gact_heads* h_parts, int n_parts, const gact_rotation* h_rotation, void* stream) {
+    gact::HeadArgs a{};
+    int bits[gact::kHeadParts] = {};
+    if (const int rc = stage_heads(h_parts, n_parts, h_rotation, false, &a, bits)) return rc;
+    gact::plan_heads(&a, n_parts);
+    return launch_heads(a, n_parts, bits, h_rotation, false, stream);
+}
+
+int gact_head_norm_rotate_backward(const gact_heads* h_parts, int n_parts, const gact_rotation* h_rotation, void* d_workspace,
+                                   size_t workspace_bytes, void* stream) {
+    gact::HeadArgs a{};
+    int bits[gact::kHeadParts] = {};
+    if (const int rc = stage_heads(h_parts, n_parts, h_rotation, true, &a, bits)) return rc;
+    gact::plan_heads_backward(&a, n_parts);
+    bool any_dw = false;
+    float* partial = (float*)d_workspace;
+    for (int k = 0; k < n_parts; ++k) {
+        if (!a.part[k].dw) continue;
+        any_dw = true;
+        a.part[k].partial = partial;
+        partial += (size_t)a.part[k].blocks * (size_t)a.dim;
+    }
+    if (any_dw && (!d_workspace || !aligned(d_workspace, 16) ||
+                   workspace_bytes < gact_head_norm_rotate_workspace_bytes(h_rotation->head_dim)))
+        return GACT_E_ARG;
+    if (const int rc = launch_heads(a, n_parts, bits, h_rotation, true, stream)) return rc;
+    if (any_dw && gact_launch_heads_dw(&a, n_parts, stream) != 0) return GACT_E_HIP;
+    return GACT_OK;
 }
 
 }  // extern "C"

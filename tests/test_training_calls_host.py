@@ -1,0 +1,211 @@
+"""Argument checks of the gradient norm, clipping and head norm calls, on the host: nothing is launched.  The kernels' divisions
+by variables, compiled for the host."""
+import ctypes
+import math
+import os
+import subprocess
+
+import pytest
+import torch
+
+import paper_2206_11357_amd as gact
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2206_11357_amd", "csrc")
+BUF = (ctypes.c_char * (1 << 16))()
+P = (ctypes.addressof(BUF) + 255) // 256 * 256
+
+
+def bufs(*entries):
+    arr = (gact.GradBuf * max(len(entries), 1))()
+    for b, (g, out, n, dtype) in zip(arr, entries):
+        b.g, b.out, b.n, b.dtype = g, out, n, dtype
+    return arr
+
+
+def clip(arr, K, kind=0, max_norm=1.0, norm=P + 32768, ws=P + 49152, size=None):
+    size = gact.gact_grad_norm_workspace_bytes(K) if size is None else size
+    return gact.lib.gact_grad_clip(ctypes.addressof(arr) if arr is not None else None, K, kind, max_norm, norm, ws, size, None)
+
+
+def test_norm_and_clip_refusals():
+    E = gact.GACT_E_ARG
+    ok = bufs((P, P, 64, 0), (P + 1024, P + 1024, 64, 1))
+    assert clip(ok, -1) == E and clip(None, 2) == E
+    assert clip(ok, 2, kind=2) == E and clip(ok, 2, kind=-1) == E
+    for bad in (-1.0, math.nan, math.inf, -math.inf):
+        assert clip(ok, 2, max_norm=bad) == E
+    assert clip(ok, 2, norm=None) == E and clip(ok, 2, norm=P + 4) == E
+    assert clip(ok, 2, ws=None) == E and clip(ok, 2, ws=P + 8) == E
+    assert clip(ok, 2, size=gact.gact_grad_norm_workspace_bytes(2) - 1) == E
+    for entry in ((None, P, 64, 0), (P, None, 64, 0), (P + 2, P + 2, 64, 0), (P, P + 1, 64, 1), (P, P, -1, 0), (P, P, 64, 2)):
+        assert clip(bufs(entry), 1) == E, entry
+    assert gact.lib.gact_grad_norm(ctypes.addressof(ok), 2, 5, P + 32768, P + 49152, 16000, None) == E
+    assert gact.lib.gact_grad_norm(ctypes.addressof(ok), 2, 0, P + 32768, P + 49152, 8, None) == E
+    assert gact.lib.gact_grad_clip_by(ctypes.addressof(ok), 2, -1.0, P + 32768, P + 49152, 16000, None) == E
+    assert gact.gact_grad_norm_workspace_bytes(-1) == 0
+    # more chunks than a launch takes
+    assert clip(bufs((P, P, 1 << 62, 0)), 1) == E
+
+
+def test_overlapping_outputs_are_refused():
+    """A buffer listed twice, outputs that touch each other or an input that is not their own, also where a long one spans
+    several short ones."""
+    E = gact.GACT_E_ARG
+    for entries in (((P, P, 64, 0), (P, P, 64, 0)),
+                    ((P, P, 64, 0), (P + 252, P + 252, 64, 0)),
+                    ((P, P + 4096, 64, 0), (P + 8192, P + 4096 + 255 // 4 * 4, 4, 0)),
+                    ((P, P + 128, 64, 0),),
+                    ((P, P + 1024, 64, 0), (P + 1024, P + 2048, 64, 0)),
+                    ((P, P, 1000, 1), (P + 100, P + 8192, 10, 1)),
+                    ((P, P + 8192, 10, 0), (P + 16384, P + 16384, 10, 0), (P + 20, P + 10, 300, 1))):
+        assert clip(bufs(*entries), len(entries)) == E, entries
+
+
+def record(**over):
+    parts, r = (gact.Heads * 2)(), gact.Rotation()
+    D = over.get("head_dim", 64)
+    for k, h in enumerate(parts):
+        h.heads, h.bits = 4, 4
+        for f in ("x", "y", "dy", "dx", "w", "dw", "rstd", "packed", "gmin", "gscale"):
+            setattr(h, f, P + 1024 * (k + 1))
+        for f in ("x_stride", "y_stride", "dy_stride", "dx_stride"):
+            setattr(h, f, (ctypes.c_int64 * 3)(8 * 4 * D, 4 * D, D))
+    r.batch, r.tokens, r.head_dim, r.rot_dim, r.dtype, r.w_dtype, r.group_size, r.eps = 2, 8, D, D // 16 * 16, 1, 0, 64, 1e-6
+    r.cos, r.sin, r.positions, r.n_positions = P, P, P, 8
+    n_parts = over.pop("n_parts", 2)
+    for key, v in over.items():
+        if hasattr(r, key):
+            setattr(r, key, v)
+        else:
+            setattr(parts[1 if n_parts == 2 else 0], key, v)
+    return parts, n_parts, r
+
+
+def forward(**over):
+    parts, n, r = record(**over)
+    return gact.lib.gact_head_norm_rotate(ctypes.addressof(parts), n, ctypes.addressof(r), None)
+
+
+def backward(ws=P, size=1 << 30, **over):
+    parts, n, r = record(**over)
+    return gact.lib.gact_head_norm_rotate_backward(ctypes.addressof(parts), n, ctypes.addressof(r), ws, size, None)
+
+
+BOTH = [dict(n_parts=0), dict(n_parts=3), dict(head_dim=0), dict(head_dim=12), dict(head_dim=520), dict(rot_dim=8),
+        dict(rot_dim=80), dict(rot_dim=-16), dict(dtype=2), dict(w_dtype=7), dict(batch=-1), dict(tokens=-1),
+        dict(batch=1 << 40), dict(batch=1 << 20, tokens=1 << 12), dict(batch=1 << 16, tokens=1 << 14, heads=4),
+        dict(heads=0), dict(cos=None), dict(sin=P + 2), dict(positions=P + 4), dict(n_positions=-1), dict(rstd=None),
+        dict(rstd=P + 2), dict(packed=None), dict(packed=P + 8), dict(gmin=None), dict(gscale=P + 1), dict(w=P + 2)]
+
+
+@pytest.mark.parametrize("over", BOTH, ids=str)
+def test_head_calls_refuse_what_neither_takes(over):
+    assert forward(**dict(over)) == gact.GACT_E_ARG
+    assert backward(**dict(over)) == gact.GACT_E_ARG
+
+
+def test_head_calls_refuse_their_own():
+    E = gact.GACT_E_ARG
+    for over in (dict(eps=0.0), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(x=None), dict(x=P + 1), dict(y=None)):
+        assert forward(**over) == E, over
+    for over in (dict(dy=None), dict(dx=None), dict(dx=P + 1), dict(dw=P + 2), dict(w=None), dict(bits=32, x=None),
+                 dict(ws=None), dict(ws=P + 8), dict(size=gact.gact_head_norm_rotate_workspace_bytes(64) - 1)):
+        assert backward(**over) == E, over
+    assert gact.lib.gact_head_norm_rotate(None, 1, P, None) == E and gact.lib.gact_head_norm_rotate(P, 1, None, None) == E
+    for bits in (0, 3, 16, -1):
+        assert forward(bits=bits) == gact.GACT_E_BITS and backward(bits=bits) == gact.GACT_E_BITS
+    assert [gact.gact_head_norm_rotate_workspace_bytes(d) for d in (0, 4, 12, 520, -8)] == [0] * 5
+
+
+def test_groups_that_do_not_fit_heads():
+    """The binding's rule and the library's are the same one."""
+    for D in range(8, 520, 8):
+        for G in (0, 16, 32, 64, 80, 96, 128, 160, 192, 256, 320, 384, 512, 640, 768, 1024):
+            for heads in (1, 2, 3, 4, 8):
+                fits = gact.head_context_fits(G, D, heads)
+                # a call that is refused behind the group check where the group fits
+                rc = forward(head_dim=D, group_size=G, heads=heads, n_parts=1, w=P + 2)
+                assert rc == (gact.GACT_E_ARG if fits else gact.GACT_E_GROUP), (D, G, heads)
+    assert gact.head_context_fits(256, 64, 16) and not gact.head_context_fits(1024, 64, 16)
+    assert not gact.head_context_fits(256, 64, 2)
+
+
+def test_empty_calls_need_no_tensors():
+    parts, n, r = record(batch=0)
+    for h in parts:
+        for f in ("x", "y", "dy", "dx", "w", "dw", "rstd", "packed", "gmin", "gscale"):
+            setattr(h, f, None)
+    assert gact.lib.gact_head_norm_rotate(ctypes.addressof(parts), n, ctypes.addressof(r), None) == gact.GACT_OK
+    assert gact.lib.gact_head_norm_rotate_backward(ctypes.addressof(parts), n, ctypes.addressof(r), None, 0, None) == gact.GACT_OK
+
+
+def test_the_binding_refuses_tensors_the_kernels_cannot_take():
+    x = torch.zeros(2, 3, 4, 64)
+    with pytest.raises(ValueError):
+        gact.gact_head_norm_rotate(x, None, None, None)                     # host memory
+    with pytest.raises(ValueError):
+        gact.make_grad_bufs([x])
+    with pytest.raises(ValueError):
+        gact.gact_grad_norm([x], norm_type=1.0)
+    with pytest.raises(ValueError):
+        gact._head_strides(x.transpose(2, 3))
+    with pytest.raises(ValueError):
+        gact._head_shape(x[0, 0])
+    t = torch.zeros(3, 32)
+    for cos, sin, pos in ((t, None, None), (t.double(), t.double(), None), (t, t[:2], None), (t.t(), t.t(), None),
+                          (t, t, torch.zeros(6, dtype=torch.int32)), (t, t, torch.zeros(5, dtype=torch.int64)), (t[:2], t[:2], None)):
+        with pytest.raises(ValueError):
+            gact._rotation(x, cos, sin, pos, False, ())
+    with pytest.raises(ValueError):
+        gact._rotation(x, t, t, None, False, (torch.zeros(64), torch.zeros(64, dtype=torch.bfloat16)))
+    with pytest.raises(TypeError):
+        gact._rotation(x.half(), t, t, None, False, ())
+
+
+PROGRAM = r"""
+#include <cstdio>
+#include "gact_heads.h"
+#include "gact_norm.h"
+int main() {
+    int failed = 0;
+    uint64_t z = 88172645463325252ull;
+    const auto next = [&]() { z ^= z << 13; z ^= z >> 7; z ^= z << 17; return z; };
+    for (int i = 0; i < 400000; ++i) {
+        const uint32_t d = i < 3000 ? (uint32_t)i + 1 : (uint32_t)(next() % 0x7FFFFFFF) >> (i % 31) | 1u;
+        const gact::Divisor m = gact::divisor(d);
+        const uint32_t top = 0x7FFFFFFFu / d * d;
+        const uint32_t xs[] = {0u, 1u, d - 1, d, top - 1, top, 0x7FFFFFFFu, (uint32_t)next() >> 1};
+        for (uint32_t x : xs) {
+            if (x > 0x7FFFFFFFu) continue;
+            const uint32_t q = m.magic == 0 ? x : (uint32_t)(((uint64_t)x * m.magic) >> 32) >> m.shift;
+            if (q != x / d) { std::printf("%u / %u = %u\n", x, d, q); failed = 1; }
+        }
+    }
+    // the backward launch's blocks, whatever the parts' sizes
+    for (int i = 0; i < 200000; ++i) {
+        gact::HeadArgs a{};
+        for (auto& p : a.part) p.passes = (uint32_t)(next() % 0x7FFFFFFF) >> (next() % 31);
+        gact::plan_heads_backward(&a, 2);
+        if (a.part[0].blocks + a.part[1].blocks > gact::kHeadBackwardBlocks) { std::printf("blocks\n"); failed = 1; }
+        for (auto& p : a.part)
+            if ((uint64_t)p.blocks * gact::kHeadWaves * p.run < p.passes) { std::printf("passes\n"); failed = 1; }
+        gact::plan_heads(&a, 2);
+        for (auto& p : a.part) {
+            const uint64_t taken = (uint64_t)p.blocks * gact::kHeadWaves * p.run;
+            if (taken < p.passes || taken >= (uint64_t)p.passes + gact::kHeadWaves * p.run) { std::printf("run\n"); failed = 1; }
+            if (!gact::launchable((uint64_t)a.part[0].blocks + a.part[1].blocks, 64 * gact::kHeadWaves)) { std::printf("threads\n"); failed = 1; }
+        }
+    }
+    return failed;
+}
+"""
+
+
+def test_divisions_and_launch_plans(tmp_path):
+    src = tmp_path / "plans.cpp"
+    src.write_text(PROGRAM)
+    exe = tmp_path / "plans"
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-I", CSRC, str(src), "-o", str(exe)])
+    out = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert out.returncode == 0, out.stdout[:500]

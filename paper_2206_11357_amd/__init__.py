@@ -12,6 +12,7 @@ import contextlib
 import ctypes
 import math
 import os
+import struct
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
@@ -79,22 +80,11 @@ class GradBuf(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
-class Heads(ctypes.Structure):
-    """Mirror of gact_heads."""
-    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("dy", ctypes.c_void_p), ("dx", ctypes.c_void_p),
-                ("w", ctypes.c_void_p), ("dw", ctypes.c_void_p), ("rstd", ctypes.c_void_p), ("packed", ctypes.c_void_p),
-                ("gmin", ctypes.c_void_p), ("gscale", ctypes.c_void_p), ("x_stride", ctypes.c_int64 * 3),
-                ("y_stride", ctypes.c_int64 * 3), ("dy_stride", ctypes.c_int64 * 3), ("dx_stride", ctypes.c_int64 * 3),
-                ("seed", ctypes.c_uint64), ("heads", ctypes.c_int32), ("bits", ctypes.c_int32)]
-
-
-class Rotation(ctypes.Structure):
-    """Mirror of gact_rotation."""
-    _fields_ = [("batch", ctypes.c_int64), ("tokens", ctypes.c_int64), ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p),
-                ("positions", ctypes.c_void_p), ("n_positions", ctypes.c_int64), ("head_dim", ctypes.c_int32),
-                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("dtype", ctypes.c_int32),
-                ("w_dtype", ctypes.c_int32), ("group_size", ctypes.c_int32), ("eps", ctypes.c_float),
-                ("reserved", ctypes.c_int32)]
+# gact_heads: x, y, dy, dx, w, dw, rstd, packed, gmin, gscale; strides of x, y, dy, dx; seed; heads, bits.
+_HEADS = struct.Struct("10P12qQ2i")
+# gact_rotation: batch, tokens; cos, sin, positions; n_positions; head_dim, rot_dim, interleaved, dtype, w_dtype,
+# group_size; eps, reserved.
+_ROTATION = struct.Struct("2q3Pq6ifi")
 
 
 def _load() -> ctypes.CDLL:
@@ -517,39 +507,44 @@ def gact_variance_alert(sensitivity, bits, grad_var: float, threshold: float):
 
 
 # ------------------------------------------------- gradient norm and clipping
-def _enqueue(fn, name: str, device: torch.device, stream, *args) -> None:
+# The current device's index without torch's check whether a device has been set up: a tensor on one is at hand.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _enqueue(fn, name: str, device: int, stream, *args) -> None:
     """fn(*args, stream) on the tensors' device, whichever is current."""
-    if device.index != torch.cuda.current_device():
+    if device != _current_device():
         with torch.cuda.device(device):
             rc = fn(*args, _stream(stream))
+    elif stream is None and _raw_stream is not None:
+        rc = fn(*args, _raw_stream(device))
     else:
         rc = fn(*args, _stream(stream))
     if rc != GACT_OK:
         raise GactError(rc, name)
 
 
-def _allocating_for(stream, device: torch.device):
+def _allocating_for(stream, device: int):
     """Where a call on `stream` allocates its outputs and scratch: under that stream, so that the allocator hands their
     memory out again only behind the call."""
-    if stream is None:
-        return contextlib.nullcontext()
     if type(stream) is int:
         stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
     return torch.cuda.stream(stream)
 
 
-def _same_device(tensors) -> torch.device:
-    device = None
+def _same_device(*tensors) -> int:
+    """Index of the device that all of them (None aside) lie on; -2 without tensors."""
+    device = -2                          # get_device() of host memory is -1
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("gact needs device tensors")
-        if device is None:
-            device = t.device
-        elif t.device != device:
-            raise ValueError("the tensors of a call lie on different devices")
-    return device if device is not None else torch.device("cuda", torch.cuda.current_device())
+        if t is not None:
+            d = t.get_device()
+            if d != device:
+                if d < 0:
+                    raise ValueError("gact needs device tensors")
+                if device >= 0:
+                    raise ValueError("the tensors of a call lie on different devices")
+                device = d
+    return device
 
 
 def _dense(t: torch.Tensor) -> bool:
@@ -567,14 +562,15 @@ def make_grad_bufs(g: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tens
     outs = g if outs is None else list(outs)
     if len(outs) != len(g):
         raise ValueError("g and outs must list the same buffers")
-    _same_device(g + outs if outs is not g else g)
+    if _same_device(*g) != _same_device(*outs):
+        raise ValueError("the tensors of a call lie on different devices")
     arr = (GradBuf * max(len(g), 1))()
-    for k, (a, o) in enumerate(zip(g, outs)):
+    for b, a, o in zip(arr, g, outs):
         if not _dense(a):
-            raise ValueError("buffer %d: gact needs contiguous tensors" % k)
+            raise ValueError("gact needs contiguous tensors")
         if o is not a and (o.dtype != a.dtype or o.shape != a.shape or o.stride() != a.stride()):
-            raise ValueError("buffer %d: g and its output differ in size, dtype or strides" % k)
-        arr[k].g, arr[k].out, arr[k].n, arr[k].dtype = a.data_ptr(), o.data_ptr(), a.numel(), dtype_code(a.dtype)
+            raise ValueError("a buffer and its output differ in size, dtype or strides")
+        b.g, b.out, b.n, b.dtype = a.data_ptr(), o.data_ptr(), a.numel(), dtype_code(a.dtype)
     return arr
 
 
@@ -586,34 +582,42 @@ def _norm_kind(norm_type: float) -> int:
     raise ValueError("norm_type must be 2 or inf, got %r" % (norm_type,))
 
 
+def _norm_scratch(K: int, norm, workspace, device: int):
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float64, device=device)
+    if workspace is None:
+        workspace = torch.empty(gact_grad_norm_workspace_bytes(K), dtype=torch.uint8, device=device)
+    return norm, workspace
+
+
 def _norm_call(g, outs, norm, workspace, stream, bufs):
-    """What the three calls share: (K, table, device, norm, workspace)."""
-    g = list(g)
+    """What the three calls share: (number of buffers, table, device, norm, workspace).  The table lives as long as the
+    caller holds it."""
     arr = bufs if bufs is not None else make_grad_bufs(g, outs)
-    if len(arr) < len(g):
+    K = len(g)
+    if len(arr) < K:
         raise ValueError("bufs lists fewer buffers than g")
-    device = _same_device(g[:1])
+    device = g[0].get_device() if K else _current_device()
     if norm is None or workspace is None:
-        with _allocating_for(stream, device):
-            if norm is None:
-                norm = torch.empty(1, dtype=torch.float64, device=device)
-            if workspace is None:
-                workspace = torch.empty(gact_grad_norm_workspace_bytes(len(g)), dtype=torch.uint8, device=device)
+        if stream is None:
+            norm, workspace = _norm_scratch(K, norm, workspace, device)
+        else:
+            with _allocating_for(stream, device):
+                norm, workspace = _norm_scratch(K, norm, workspace, device)
     if norm.dtype != torch.float64 or norm.numel() != 1:
         raise ValueError("the norm is one float64 element")
-    if _same_device([norm, workspace]) != device:
+    if norm.get_device() != device or workspace.get_device() != device:
         raise ValueError("the tensors of a call lie on different devices")
-    return len(g), arr, device, norm, workspace
+    return K, arr, device, norm, workspace
 
 
 def gact_grad_norm(g: Sequence[torch.Tensor], norm_type: float = 2.0, out: Optional[torch.Tensor] = None,
                    workspace: Optional[torch.Tensor] = None, stream=None, bufs=None) -> torch.Tensor:
     """Norm over all buffers together, 2 or inf -> device float64[1].  `bufs` (from make_grad_bufs) skips
     re-marshalling the list."""
-    kind = _norm_kind(norm_type)
-    K, arr, device, out, workspace = _norm_call(g, None, out, workspace, stream, bufs)
-    _enqueue(lib.gact_grad_norm, "gact_grad_norm", device, stream, ctypes.addressof(arr), K, kind, out.data_ptr(),
-             workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    K, table, device, out, workspace = _norm_call(g, None, out, workspace, stream, bufs)
+    _enqueue(lib.gact_grad_norm, "gact_grad_norm", device, stream, table, K, _norm_kind(norm_type), out.data_ptr(),
+             workspace.data_ptr(), workspace.nbytes)
     return out
 
 
@@ -621,11 +625,10 @@ def gact_grad_clip(g: Sequence[torch.Tensor], max_norm: float, norm_type: float 
                    outs: Optional[Sequence[torch.Tensor]] = None, norm: Optional[torch.Tensor] = None,
                    workspace: Optional[torch.Tensor] = None, stream=None, bufs=None) -> torch.Tensor:
     """Scales the buffers by min(1, max_norm / (norm + 1e-6)), in place or into `outs`; returns their norm before,
-    device float64[1]."""
-    kind = _norm_kind(norm_type)
-    K, arr, device, norm, workspace = _norm_call(g, outs, norm, workspace, stream, bufs)
-    _enqueue(lib.gact_grad_clip, "gact_grad_clip", device, stream, ctypes.addressof(arr), K, kind, float(max_norm),
-             norm.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    device float64[1].  `bufs` (from make_grad_bufs, with its outputs) skips re-marshalling the list."""
+    K, table, device, norm, workspace = _norm_call(g, outs, norm, workspace, stream, bufs)
+    _enqueue(lib.gact_grad_clip, "gact_grad_clip", device, stream, table, K, _norm_kind(norm_type), float(max_norm),
+             norm.data_ptr(), workspace.data_ptr(), workspace.nbytes)
     return norm
 
 
@@ -633,30 +636,65 @@ def gact_grad_clip_by(g: Sequence[torch.Tensor], max_norm: float, norm: torch.Te
                       outs: Optional[Sequence[torch.Tensor]] = None, workspace: Optional[torch.Tensor] = None,
                       stream=None, bufs=None) -> None:
     """gact_grad_clip by a norm that is known already (device float64[1])."""
-    K, arr, device, norm, workspace = _norm_call(g, outs, norm, workspace, stream, bufs)
-    _enqueue(lib.gact_grad_clip_by, "gact_grad_clip_by", device, stream, ctypes.addressof(arr), K, float(max_norm),
-             norm.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    K, table, device, norm, workspace = _norm_call(g, outs, norm, workspace, stream, bufs)
+    _enqueue(lib.gact_grad_clip_by, "gact_grad_clip_by", device, stream, table, K, float(max_norm), norm.data_ptr(),
+             workspace.data_ptr(), workspace.nbytes)
 
 
 # ---------------------------------------------- norms of heads and rotation
 class HeadContext:
-    """What the forward pass keeps of one tensor (queries or keys) for its gradient: rstd, and the compressed
-    context where bits is not GACT_BITS_UNCOMPRESSED."""
-    __slots__ = ("bits", "group_size", "seed", "rstd", "packed", "gmin", "gscale")
+    """What the forward pass keeps of one tensor (queries or keys) for its gradient, in one buffer: rstd, float32 of x's
+    shape without head_dim, and, where bits is not GACT_BITS_UNCOMPRESSED, packed, gmin and gscale as gact_compress
+    lays them out."""
+    __slots__ = ("bits", "group_size", "seed", "shape", "blob", "groups", "off")
 
-    def __init__(self, bits, group_size, seed, rstd, packed=None, gmin=None, gscale=None):
-        self.bits, self.group_size, self.seed, self.rstd = bits, group_size, seed, rstd
-        self.packed, self.gmin, self.gscale = packed, gmin, gscale
+    def __init__(self, x: torch.Tensor, bits: int, group_size: int, seed: int):
+        self.bits, self.group_size, self.seed, self.shape = bits, group_size, seed & (2**64 - 1), x.shape
+        n = x.numel()
+        packed = self.groups = meta = 0
+        if bits != GACT_BITS_UNCOMPRESSED:
+            packed = (n * bits + 127 >> 7) * 16
+            self.groups = -(-n // group_size) if group_size > 0 else 0
+            meta = (self.groups + 3 >> 2) * 16
+        self.off = (0, packed, packed + meta, packed + 2 * meta)           # of packed, gmin, gscale, rstd
+        rows = n // x.shape[-1] if n else 0
+        self.blob = torch.empty(packed + 2 * meta + 4 * rows, dtype=torch.uint8, device=x.device)
+
+    @property
+    def packed(self) -> torch.Tensor:
+        return self.blob[:self.off[1]]
+
+    def _floats(self, k: int, count: int) -> torch.Tensor:
+        return self.blob[self.off[k]:self.off[k] + 4 * count].view(torch.float32)
+
+    @property
+    def gmin(self) -> torch.Tensor:
+        return self._floats(1, self.groups)
+
+    @property
+    def gscale(self) -> torch.Tensor:
+        return self._floats(2, self.groups)
+
+    @property
+    def rstd(self) -> torch.Tensor:
+        return self.blob[self.off[3]:].view(torch.float32).view(self.shape[:-1])
+
+    def addresses(self):
+        """Of rstd, packed, gmin, gscale."""
+        a = self.blob.data_ptr()
+        if self.bits == GACT_BITS_UNCOMPRESSED:
+            return a, 0, 0, 0
+        off = self.off
+        return a + off[3], a, a + off[1], a + off[2]
 
 
 def make_head_context(x: torch.Tensor, bits: int = GACT_BITS_UNCOMPRESSED, group_size: int = 0, seed: int = 0,
                       stream=None) -> HeadContext:
     """Buffers for the context of x, [batch, tokens, heads, head_dim] or [tokens, heads, head_dim]."""
-    with _allocating_for(stream, x.device):
-        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-        if bits == GACT_BITS_UNCOMPRESSED:
-            return HeadContext(bits, group_size, seed, rstd)
-        return HeadContext(bits, group_size, seed, rstd, *alloc_compressed(x.numel(), max(group_size, 1), bits, x.device))
+    if stream is None:
+        return HeadContext(x, bits, group_size, seed)
+    with _allocating_for(stream, x.get_device()):
+        return HeadContext(x, bits, group_size, seed)
 
 
 def head_context_fits(group_size: int, head_dim: int, *heads: int) -> bool:
@@ -674,93 +712,113 @@ def gact_head_norm_rotate_workspace_bytes(head_dim: int) -> int:
     return int(lib.gact_head_norm_rotate_workspace_bytes(head_dim))
 
 
-def _head_shape(x: torch.Tensor):
-    if x.dim() not in (3, 4):
+_NO_STRIDES = (0, 0, 0)
+
+
+def _head_strides(x: torch.Tensor) -> tuple:
+    """Of batch, token and head, in elements."""
+    st = x.stride()
+    if len(st) == 4:
+        a, b, c, last = st
+    elif len(st) == 3:
+        a, (b, c, last) = 0, st
+    else:
         raise ValueError("gact needs [batch, tokens, heads, head_dim] or [tokens, heads, head_dim]")
-    return tuple(x.shape) if x.dim() == 4 else (1,) + tuple(x.shape)
-
-
-def _head_strides(x: torch.Tensor):
-    if x.shape[-1] > 1 and x.stride(-1) != 1:
+    if last != 1 and x.shape[-1] > 1:
         raise ValueError("a head's elements must be consecutive")
-    return x.stride()[:3] if x.dim() == 4 else (0,) + x.stride()[:2]
+    return a, b, c
 
 
-def _rotation(x: torch.Tensor, cos, sin, positions, interleaved: bool, weights) -> Rotation:
-    """The record that queries and keys share, from one of them."""
-    B, S, _, D = _head_shape(x)
-    r = Rotation()
-    r.batch, r.tokens, r.head_dim, r.dtype, r.interleaved = B, S, D, dtype_code(x.dtype), int(bool(interleaved))
-    if (cos is None) != (sin is None):
-        raise ValueError("cos and sin belong together")
-    if cos is not None:
-        if cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32 \
+def _rotation(x: torch.Tensor, cos, sin, positions, interleaved, w_dtype, group_size: int, eps: float) -> bytes:
+    """gact_rotation of queries and keys, from one of them."""
+    shape = x.shape
+    B = shape[0] if len(shape) == 4 else 1
+    S, D = shape[-3], shape[-1]
+    a_cos = a_sin = a_pos = n_positions = rot = 0
+    if cos is not None and sin is not None:
+        n_positions, half = cos.shape
+        if cos.shape != sin.shape or cos.dtype is not torch.float32 or sin.dtype is not torch.float32 \
                 or not cos.is_contiguous() or not sin.is_contiguous():
             raise ValueError("cos and sin must be contiguous float32 tables [positions, rot_dim / 2]")
-        r.n_positions, r.rot_dim = cos.shape[0], 2 * cos.shape[1]
-        r.cos, r.sin = cos.data_ptr(), sin.data_ptr()
+        rot, a_cos, a_sin = 2 * half, cos.data_ptr(), sin.data_ptr()
         if positions is not None:
-            if positions.dtype != torch.int64 or positions.numel() != B * S or not positions.is_contiguous():
+            if positions.dtype is not torch.int64 or positions.numel() != B * S or not positions.is_contiguous():
                 raise ValueError("positions must be contiguous int64, one per token")
-            r.positions = positions.data_ptr()
-        elif S > r.n_positions:
+            a_pos = positions.data_ptr()
+        elif S > n_positions:
             raise ValueError("the tables hold fewer positions than a sequence has tokens")
-    types = {w.dtype for w in weights if w is not None}
-    if len(types) > 1:
-        raise ValueError("the weights must have one type")
-    r.w_dtype = dtype_code(types.pop()) if types else GACT_F32
-    return r
+    elif cos is not None or sin is not None:
+        raise ValueError("cos and sin belong together")
+    return _ROTATION.pack(B, S, a_cos, a_sin, a_pos, n_positions, D, rot, 1 if interleaved else 0, dtype_code(x.dtype),
+                          GACT_F32 if w_dtype is None else dtype_code(w_dtype), group_size, eps, 0)
 
 
-def _head_part(h: Heads, field: str, t: torch.Tensor, like: torch.Tensor) -> None:
-    if _head_shape(t) != _head_shape(like) or t.dtype != like.dtype:
-        raise ValueError("%s: shape or dtype differ" % field)
-    setattr(h, field, t.data_ptr())
-    setattr(h, field + "_stride", (ctypes.c_int64 * 3)(*_head_strides(t)))
+def _weights_dtype(weights, D: int):
+    """The one type of those that are given; None if none is."""
+    dtype = None
+    for w in weights:
+        if w is not None:
+            if w.numel() != D or not w.is_contiguous():
+                raise ValueError("the weights must be contiguous, one per element of a head")
+            if dtype is not None and w.dtype is not dtype:
+                raise ValueError("the weights must have one type")
+            dtype = w.dtype
+    return dtype
 
 
-def _head_weights(h: Heads, w, D: int) -> None:
-    if w is not None:
-        if w.numel() != D or not w.is_contiguous():
-            raise ValueError("the weights must be contiguous, one per element of a head")
-        h.w = w.data_ptr()
+def _check_like(y: torch.Tensor, x: torch.Tensor) -> None:
+    if y.shape != x.shape or y.dtype is not x.dtype:
+        raise ValueError("shape or dtype differ: %s %s, %s %s" % (tuple(y.shape), y.dtype, tuple(x.shape), x.dtype))
 
 
-def _head_context(h: Heads, c: Optional[HeadContext], shape, r: Rotation) -> None:
-    h.heads, h.bits = shape[2], GACT_BITS_UNCOMPRESSED
-    if c is None:
-        return
-    n = shape[0] * shape[1] * shape[2]
-    if c.rstd.numel() != n or c.rstd.dtype != torch.float32 or not c.rstd.is_contiguous():
-        raise ValueError("the context was made for another shape")
-    h.rstd, h.bits, h.seed = c.rstd.data_ptr(), c.bits, c.seed & (2**64 - 1)
-    if c.bits != GACT_BITS_UNCOMPRESSED:
-        n *= shape[3]
-        groups = gact_num_groups(n, c.group_size)
-        if c.packed.numel() < gact_packed_bytes(n, c.bits) or c.gmin.numel() < groups or c.gscale.numel() < groups:
-            raise ValueError("the context was made for another shape")
-        if r.group_size not in (0, c.group_size):
-            raise ValueError("the contexts of a call must have one group size")
-        r.group_size = c.group_size
-        h.packed, h.gmin, h.gscale = c.packed.data_ptr(), c.gmin.data_ptr(), c.gscale.data_ptr()
+def _check_pair(q: torch.Tensor, k: torch.Tensor) -> None:
+    a, b = q.shape, k.shape
+    if len(a) != len(b) or a[:-2] != b[:-2] or a[-1] != b[-1] or q.dtype is not k.dtype:
+        raise ValueError("queries and keys differ in batch, tokens, head_dim or dtype")
+
+
+def _contexts_group(context, xs) -> int:
+    """The one group size of the compressed contexts; 0 if none is."""
+    G = 0
+    for c, x in zip(context, xs):
+        if c is not None:
+            if c.shape != x.shape or c.blob.get_device() != x.get_device():
+                raise ValueError("the context was made for another shape or device")
+            if c.bits != GACT_BITS_UNCOMPRESSED:
+                if G and c.group_size != G:
+                    raise ValueError("the contexts of a call must have one group size")
+                G = c.group_size
+    return G
+
+
+_NO_CONTEXT = (None, None)
 
 
 def _forward_record(q, k, cos, sin, wq, wk, positions, eps, interleaved, out, context):
-    """(parts, number of parts, rotation) of a forward call into `out`."""
-    xs = [q] if k is None else [q, k]
-    ws, ctxs = (wq, wk), context if context is not None else (None, None)
-    _same_device(xs + [cos, sin, wq, wk, positions] + list(out))
-    if k is not None and (_head_shape(k)[:2] != _head_shape(q)[:2] or k.shape[-1] != q.shape[-1] or k.dtype != q.dtype):
-        raise ValueError("queries and keys differ in batch, tokens, head_dim or dtype")
-    r = _rotation(q, cos, sin, positions, interleaved, ws[:len(xs)])
-    r.eps = eps
-    parts = (Heads * 2)()
-    for h, x, y, w, c in zip(parts, xs, out, ws, ctxs):
-        _head_part(h, "x", x, x)
-        _head_part(h, "y", y, x)
-        _head_weights(h, w, x.shape[-1])
-        _head_context(h, c, _head_shape(x), r)
-    return parts, len(xs), r
+    """(device, parts, number of parts, rotation) of a forward call into `out`."""
+    context = context if context is not None else _NO_CONTEXT
+    if k is None:
+        device = _same_device(q, out[0], wq, cos, sin, positions)
+        w_dtype, triples = _weights_dtype((wq,), q.shape[-1]), ((q, out[0], wq, context[0]),)
+    else:
+        _check_pair(q, k)
+        device = _same_device(q, k, out[0], out[1], wq, wk, cos, sin, positions)
+        w_dtype = _weights_dtype((wq, wk), q.shape[-1])
+        triples = ((q, out[0], wq, context[0]), (k, out[1], wk, context[1]))
+    rotation = _rotation(q, cos, sin, positions, interleaved, w_dtype, _contexts_group(context, (q, k)), eps)
+    parts = b""
+    for x, y, w, c in triples:
+        if y is not x:
+            _check_like(y, x)
+        rstd, packed, gmin, gscale = c.addresses() if c is not None else (0, 0, 0, 0)
+        parts += _HEADS.pack(x.data_ptr(), y.data_ptr(), 0, 0, 0 if w is None else w.data_ptr(), 0, rstd, packed, gmin, gscale,
+                             *_head_strides(x), *_head_strides(y), *_NO_STRIDES, *_NO_STRIDES, 0 if c is None else c.seed,
+                             x.shape[-2], GACT_BITS_UNCOMPRESSED if c is None else c.bits)
+    return device, parts, len(triples), rotation
+
+
+def _empty_heads(*like) -> tuple:
+    return tuple(None if x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in like)
 
 
 def gact_head_norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], cos: Optional[torch.Tensor],
@@ -771,24 +829,26 @@ def gact_head_norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], cos: Optio
     then the position rotation; returns (yq, yk).  cos, sin: float32 tables [positions, rot_dim / 2], or None for no
     rotation; positions: int64 per token, or None for a token's place in its sequence; out: tensors of the same shapes
     (a transposed view lets the result lie head by head); context: two HeadContexts that the pass fills."""
-    device = _same_device([q, k])
     if out is None:
-        with _allocating_for(stream, device):
-            out = tuple(None if x is None else torch.empty(x.shape, dtype=x.dtype, device=device) for x in (q, k))
-    parts, n, r = _forward_record(q, k, cos, sin, wq, wk, positions, eps, interleaved, out, context)
-    _enqueue(lib.gact_head_norm_rotate, "gact_head_norm_rotate", device, stream, ctypes.addressof(parts), n,
-             ctypes.addressof(r))
+        if stream is None:
+            out = _empty_heads(q, k)
+        else:
+            with _allocating_for(stream, q.get_device()):
+                out = _empty_heads(q, k)
+    device, parts, n, rotation = _forward_record(q, k, cos, sin, wq, wk, positions, eps, interleaved, out, context)
+    _enqueue(lib.gact_head_norm_rotate, "gact_head_norm_rotate", device, stream, parts, n, rotation)
     return out
 
 
 def prepare_head_norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], cos, sin, wq=None, wk=None, positions=None,
                              eps: float = 1e-6, interleaved: bool = False, *, out, context=None) -> PreparedCall:
     """gact_head_norm_rotate(...) into `out`, as a PreparedCall."""
-    parts, n, r = _forward_record(q, k, cos, sin, wq, wk, positions, eps, interleaved, out, context)
+    _, parts, n, rotation = _forward_record(q, k, cos, sin, wq, wk, positions, eps, interleaved, out, context)
     vp = ctypes.c_void_p
-    args = (vp(ctypes.addressof(parts)), n, vp(ctypes.addressof(r)))
+    keep = (ctypes.create_string_buffer(parts, len(parts)), ctypes.create_string_buffer(rotation, len(rotation)))
+    args = (vp(ctypes.addressof(keep[0])), n, vp(ctypes.addressof(keep[1])))
     return PreparedCall(lib.gact_head_norm_rotate, "gact_head_norm_rotate", args,
-                        (parts, r, q, k, cos, sin, wq, wk, positions, out, context))
+                        (keep, q, k, cos, sin, wq, wk, positions, out, context))
 
 
 def gact_head_norm_rotate_backward(dyq: Optional[torch.Tensor], dyk: Optional[torch.Tensor], cos, sin, wq=None, wk=None,
@@ -797,40 +857,41 @@ def gact_head_norm_rotate_backward(dyq: Optional[torch.Tensor], dyk: Optional[to
     """Gradients of gact_head_norm_rotate from dyq, dyk (any strides but the last) and the contexts it has filled; x =
     (q, k) where these are not compressed.  Returns (dq, dk, dwq, dwk); None for a part without dy, without weights or
     whose weight gradient is not wanted."""
-    dys, ws = (dyq, dyk), (wq, wk)
-    live = [i for i in (0, 1) if dys[i] is not None]
+    dys, ws, xs = (dyq, dyk), (wq, wk), x if x is not None else _NO_CONTEXT
+    live = tuple(i for i in (0, 1) if dys[i] is not None)
     if not live:
         return None, None, None, None
-    xs = x if x is not None else (None, None)
-    device = _same_device([dyq, dyk, cos, sin, wq, wk, positions] + list(xs) + [context[i].rstd for i in live])
+    if len(live) == 2:
+        _check_pair(dyq, dyk)
+    device = _same_device(dyq, dyk, cos, sin, wq, wk, positions, xs[0], xs[1], workspace)
     first = dys[live[0]]
     D = first.shape[-1]
-    if len(live) == 2 and (_head_shape(dyk)[:2] != _head_shape(dyq)[:2] or dyk.shape[-1] != D or dyk.dtype != dyq.dtype):
-        raise ValueError("queries and keys differ in batch, tokens, head_dim or dtype")
-    r = _rotation(first, cos, sin, positions, interleaved, [ws[i] for i in live])
-    wanted = [ws[i] is not None and bool(weight_grads[i]) for i in (0, 1)]
-    dxs, dws = [None, None], [None, None]
-    with _allocating_for(stream, device):
+    w_dtype = _weights_dtype([ws[i] for i in live], D)
+    rotation = _rotation(first, cos, sin, positions, interleaved, w_dtype,
+                         _contexts_group([context[i] for i in live], [dys[i] for i in live]), 0.0)
+    with _allocating_for(stream, device) if stream is not None else contextlib.nullcontext():
+        dxs = list(_empty_heads(dyq, dyk)) if out is None else [out[0], out[1]]
+        dws = [None, None]
         for i in live:
-            dxs[i] = out[i] if out is not None else torch.empty(dys[i].shape, dtype=dys[i].dtype, device=device)
-            if wanted[i]:
-                dws[i] = torch.empty(ws[i].shape, dtype=ws[i].dtype, device=device)
-        if any(wanted[i] for i in live) and workspace is None:
-            workspace = torch.empty(gact_head_norm_rotate_workspace_bytes(D), dtype=torch.uint8, device=device)
-    _same_device([first, workspace] + dxs)
-    parts = (Heads * 2)()
-    for h, i in zip(parts, live):
-        _head_part(h, "dy", dys[i], dys[i])
-        _head_part(h, "dx", dxs[i], dys[i])
-        _head_weights(h, ws[i], D)
-        if dws[i] is not None:
-            h.dw = dws[i].data_ptr()
-        _head_context(h, context[i], _head_shape(dys[i]), r)
-        if context[i].bits == GACT_BITS_UNCOMPRESSED:
-            if xs[i] is None:
+            if ws[i] is not None and weight_grads[i]:
+                dws[i] = torch.empty(ws[i].shape, dtype=w_dtype, device=first.device)
+        if workspace is None and (dws[0] is not None or dws[1] is not None):
+            workspace = torch.empty(gact_head_norm_rotate_workspace_bytes(D), dtype=torch.uint8, device=first.device)
+    if out is not None:
+        _same_device(first, *dxs)
+    parts = b""
+    for i in live:
+        dy, dx, w, dw, c, xi = dys[i], dxs[i], ws[i], dws[i], context[i], xs[i]
+        _check_like(dx, dy)
+        a_x, x_strides = 0, _NO_STRIDES
+        if c.bits == GACT_BITS_UNCOMPRESSED:
+            if xi is None:
                 raise ValueError("the context is not compressed: x is needed")
-            _head_part(h, "x", xs[i], dys[i])
-    _enqueue(lib.gact_head_norm_rotate_backward, "gact_head_norm_rotate_backward", device, stream, ctypes.addressof(parts),
-             len(live), ctypes.addressof(r), workspace.data_ptr() if workspace is not None else None,
-             workspace.numel() * workspace.element_size() if workspace is not None else 0)
+            _check_like(xi, dy)
+            a_x, x_strides = xi.data_ptr(), _head_strides(xi)
+        parts += _HEADS.pack(a_x, 0, dy.data_ptr(), dx.data_ptr(), 0 if w is None else w.data_ptr(),
+                             0 if dw is None else dw.data_ptr(), *c.addresses(), *x_strides, *_NO_STRIDES, *_head_strides(dy),
+                             *_head_strides(dx), c.seed, dy.shape[-2], c.bits)
+    _enqueue(lib.gact_head_norm_rotate_backward, "gact_head_norm_rotate_backward", device, stream, parts, len(live), rotation,
+             None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes)
     return dxs[0], dxs[1], dws[0], dws[1]

@@ -16,6 +16,32 @@ BUF = (ctypes.c_char * (1 << 16))()
 P = (ctypes.addressof(BUF) + 255) // 256 * 256
 
 
+
+class Heads(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("x", "y", "dy", "dx", "w", "dw", "rstd", "packed", "gmin", "gscale")] + \
+        [(f, ctypes.c_int64 * 3) for f in ("x_stride", "y_stride", "dy_stride", "dx_stride")] + \
+        [("seed", ctypes.c_uint64), ("heads", ctypes.c_int32), ("bits", ctypes.c_int32)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("tokens", ctypes.c_int64), ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("n_positions", ctypes.c_int64)] + \
+        [(f, ctypes.c_int32) for f in ("head_dim", "rot_dim", "interleaved", "dtype", "w_dtype", "group_size")] + \
+        [("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+def test_the_binding_packs_the_records_of_the_interface():
+    assert gact._HEADS.size == ctypes.sizeof(Heads) and gact._ROTATION.size == ctypes.sizeof(Rotation)
+    h = Heads.from_buffer_copy(gact._HEADS.pack(*range(1, 11), *range(11, 23), 2**64 - 1, 5, 4))
+    assert [getattr(h, f) for f in ("x", "y", "dy", "dx", "w", "dw", "rstd", "packed", "gmin", "gscale")] == list(range(1, 11))
+    assert list(h.x_stride) + list(h.dx_stride) == [11, 12, 13, 20, 21, 22] and (h.seed, h.heads, h.bits) == (2**64 - 1, 5, 4)
+    t = torch.zeros(9, 16)
+    r = Rotation.from_buffer_copy(gact._rotation(torch.zeros(2, 3, 4, 64), t, t, torch.zeros(6, dtype=torch.int64), True,
+                                                 torch.bfloat16, 64, 0.5))
+    assert (r.batch, r.tokens, r.head_dim, r.rot_dim, r.n_positions, r.interleaved, r.dtype, r.w_dtype, r.group_size, r.eps,
+            r.cos) == (2, 3, 64, 32, 9, 1, 0, 1, 64, 0.5, t.data_ptr())
+
+
 def bufs(*entries):
     arr = (gact.GradBuf * max(len(entries), 1))()
     for b, (g, out, n, dtype) in zip(arr, entries):
@@ -63,7 +89,7 @@ def test_overlapping_outputs_are_refused():
 
 
 def record(**over):
-    parts, r = (gact.Heads * 2)(), gact.Rotation()
+    parts, r = (Heads * 2)(), Rotation()
     D = over.get("head_dim", 64)
     for k, h in enumerate(parts):
         h.heads, h.bits = 4, 4
@@ -147,20 +173,23 @@ def test_the_binding_refuses_tensors_the_kernels_cannot_take():
     with pytest.raises(ValueError):
         gact.make_grad_bufs([x])
     with pytest.raises(ValueError):
-        gact.gact_grad_norm([x], norm_type=1.0)
-    with pytest.raises(ValueError):
-        gact._head_strides(x.transpose(2, 3))
-    with pytest.raises(ValueError):
-        gact._head_shape(x[0, 0])
+        gact._norm_kind(1.0)
+    for strided in (x.transpose(2, 3), x[0, 0], x[:, :, :, ::2]):
+        with pytest.raises(ValueError):
+            gact._head_strides(strided)
     t = torch.zeros(3, 32)
     for cos, sin, pos in ((t, None, None), (t.double(), t.double(), None), (t, t[:2], None), (t.t(), t.t(), None),
                           (t, t, torch.zeros(6, dtype=torch.int32)), (t, t, torch.zeros(5, dtype=torch.int64)), (t[:2], t[:2], None)):
         with pytest.raises(ValueError):
-            gact._rotation(x, cos, sin, pos, False, ())
-    with pytest.raises(ValueError):
-        gact._rotation(x, t, t, None, False, (torch.zeros(64), torch.zeros(64, dtype=torch.bfloat16)))
+            gact._rotation(x, cos, sin, pos, False, None, 0, 1e-6)
     with pytest.raises(TypeError):
-        gact._rotation(x.half(), t, t, None, False, ())
+        gact._rotation(x.half(), t, t, None, False, None, 0, 1e-6)
+    for weights in ((torch.zeros(64), torch.zeros(64, dtype=torch.bfloat16)), (torch.zeros(63),), (torch.zeros(128)[::2],)):
+        with pytest.raises(ValueError):
+            gact._weights_dtype(weights, 64)
+    for other in (x[:1], x[:, :2], x[..., :32], x.bfloat16(), x[0]):
+        with pytest.raises(ValueError):
+            gact._check_pair(x, other)
 
 
 PROGRAM = r"""

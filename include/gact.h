@@ -411,7 +411,7 @@ typedef struct {
     int32_t        dtype;       /* gact_dtype of x, y, dy, dx */
     int32_t        w_dtype;     /* gact_dtype of w, dw */
     int32_t        group_size;  /* of the contexts */
-    float          eps;         /* > 0; forward only */
+    float          eps;         /* a normal number > 0; forward only */
     int32_t        reserved;
 } gact_rotation;
 

@@ -34,10 +34,6 @@ typedef hf4 hf4_any __attribute__((aligned(4)));
 
 constexpr int kHeadThreads = 64 * kHeadWaves;
 
-__device__ __forceinline__ uint32_t divided(uint32_t x, const Divisor& d) {
-    return d.magic == 0 ? x : (uint32_t)(((uint64_t)x * d.magic) >> 32) >> d.shift;
-}
-
 // ------------------------------------------------------------------ lane moves
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
@@ -61,14 +57,28 @@ __device__ __forceinline__ float add_over(float v, int lanes) {
     if (lanes > 32) { float a, b; swap_halves(v, a, b); v = a + b; }
     return v;
 }
+// Minimum and maximum of a group, over four lanes or more.
 __device__ __forceinline__ void minmax_over(float& mn, float& mx, int lanes) {
-    group_minmax_pow2(mn, mx, lanes);
-    if (lanes > 32) {
-        float a, b;
-        swap_halves(mn, a, b);
-        mn = fmin2(a, b);
-        swap_halves(mx, a, b);
-        mx = fmax2(a, b);
+    mn = min_xor2(min_xor1(mn));
+    mx = max_xor2(max_xor1(mx));
+    if (lanes > 4) {
+        mn = min_half_mirror(mn);
+        mx = max_half_mirror(mx);
+        if (lanes > 8) {
+            mn = min_mirror(mn);
+            mx = max_mirror(mx);
+            if (lanes > 16) {
+                mn = fmin2(mn, swizzle_xor16(mn));
+                mx = fmax2(mx, swizzle_xor16(mx));
+                if (lanes > 32) {
+                    float a, b;
+                    swap_halves(mn, a, b);
+                    mn = fmin2(a, b);
+                    swap_halves(mx, a, b);
+                    mx = fmax2(a, b);
+                }
+            }
+        }
     }
 }
 
@@ -78,14 +88,17 @@ struct Raw {
     h4 w[DT == GACT_DT_F32 ? 2 : 1];
 };
 template <int DT>
-__device__ __forceinline__ Raw<DT> load8(const void* base, int64_t e) {
+constexpr int kSize = DT == GACT_DT_F32 ? 4 : 2;
+// Addresses are a base of the wavefront's and an offset of the lane's, in bytes: 32 bits where the part is steady, which a load
+// takes as they are.
+template <int DT, typename OFFSET>
+__device__ __forceinline__ Raw<DT> load8(const uint8_t* base, OFFSET at) {
     Raw<DT> r;
     if (DT == GACT_DT_F32) {
-        const float* p = (const float*)base + e;
-        r.w[0] = __builtin_bit_cast(h4, *(const hf4_any*)p);
-        r.w[DT == GACT_DT_F32 ? 1 : 0] = __builtin_bit_cast(h4, *(const hf4_any*)(p + 4));
+        r.w[0] = __builtin_bit_cast(h4, *(const hf4_any*)(base + at));
+        r.w[DT == GACT_DT_F32 ? 1 : 0] = __builtin_bit_cast(h4, *(const hf4_any*)(base + at + 16));
     } else {
-        r.w[0] = *(const h4_any*)((const uint16_t*)base + e);
+        r.w[0] = *(const h4_any*)(base + at);
     }
     return r;
 }
@@ -104,118 +117,186 @@ __device__ __forceinline__ void widen8(const Raw<DT>& r, float (&v)[8]) {
         }
     }
 }
-template <int DT>
-__device__ __forceinline__ void store8(void* base, int64_t e, const float (&v)[8]) {
+template <int DT, typename OFFSET>
+__device__ __forceinline__ void store8(uint8_t* base, OFFSET at, const float (&v)[8]) {
     if (DT == GACT_DT_F32) {
-        float* p = (float*)base + e;
-        *(hf4_any*)p = hf4{v[0], v[1], v[2], v[3]};
-        *(hf4_any*)(p + 4) = hf4{v[4], v[5], v[6], v[7]};
+        *(hf4_any*)(base + at) = hf4{v[0], v[1], v[2], v[3]};
+        *(hf4_any*)(base + at + 16) = hf4{v[4], v[5], v[6], v[7]};
     } else {
-        *(h4_any*)((uint16_t*)base + e) = h4{bf16_pair_rne(v[0], v[1]), bf16_pair_rne(v[2], v[3]),
+        *(h4_any*)(base + at) = h4{bf16_pair_rne(v[0], v[1]), bf16_pair_rne(v[2], v[3]),
                                              bf16_pair_rne(v[4], v[5]), bf16_pair_rne(v[6], v[7])};
     }
 }
-__device__ __forceinline__ float load_weight(const void* w, int w_f32, int d) {
-    if (w_f32) return ((const float*)w)[d];
-    return __builtin_bit_cast(float, (uint32_t)((const uint16_t*)w)[d] << 16);
-}
 
 // ------------------------------------------------------------------- rotation
+// How a part's passes lie in its tensors (heads_mode on the host).
+//   kAny      any number of heads: each lane finds its row's token and addresses for itself
+//   kSteady   a token's heads are a multiple of a pass's rows, or they divide them and the passes of a sequence come out
+//             even: the addresses are the wavefront's, counted on from pass to pass, and what a lane adds to them is the
+//             same in every pass
+//   3 .. 5    the same, and the log2 of a head's lanes, all of which hold elements (heads of 64, 128, 256): no lane is ever
+//             idle, and row sums are so many lane moves without a question
+// Us, bf16, kAny | kSteady | the last: 8192 tokens of 32 + 8 heads of 128 34.2 | 30.6 | 29.6; 32768 tokens with 4-bit contexts
+// 198 | 180 | 172, backward 194 | 165 | 150; backward of 8192 tokens of 16 + 16 of 64, 20.1 | 18.4 | 16.1.
+constexpr bool steady(int mode) { return mode != kAny; }
+constexpr bool full(int mode) { return mode >= kFullModes; }
+template <int MODE>
+__device__ __forceinline__ int lanes_shift(const HeadArgs& a) { return full(MODE) ? MODE : a.lanes_shift; }
+
 // A lane's place: of the 64 >> lanes_shift rows of a pass, the one that it works on, and its elements d .. d + 7.
+template <int MODE>
 struct Place {
-    int lane, row, j, d;
+    int lane, row, j, d, shift;
     bool in_head;                                      // d is one of the head's elements
     __device__ __forceinline__ Place(const HeadArgs& a) {
+        shift = lanes_shift<MODE>(a);
         lane = threadIdx.x & 63;
-        row = lane >> a.lanes_shift;
-        j = lane & ((1 << a.lanes_shift) - 1);
+        row = lane >> shift;
+        j = lane & ((1 << shift) - 1);
         d = j * 8;
-        in_head = d < a.dim;
+        in_head = full(MODE) || d < a.dim;
+    }
+    // whether the lane holds elements of a pass that begins with row `first`
+    __device__ __forceinline__ bool holds(const HeadPart& p, uint32_t first) const {
+        return full(MODE) || (in_head && (steady(MODE) || first + (uint32_t)row < p.rows));
+    }
+    // the lane's weights; 1 without
+    __device__ __forceinline__ void weights(const HeadArgs& a, const HeadPart& p, float (&w)[8]) const {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = 1.0f;
+        if (!p.w || !in_head) return;
+        if (a.w_f32) widen8<GACT_DT_F32>(load8<GACT_DT_F32>((const uint8_t*)p.w, (uint32_t)d * 4u), w);
+        else widen8<GACT_DT_BF16>(load8<GACT_DT_BF16>((const uint8_t*)p.w, (uint32_t)d * 2u), w);
     }
 };
 
-// A row's token and head, and where its elements begin in a tensor.
-struct Row {
-    uint32_t token, head, batch, at;                   // at: the token's place in its sequence
-    __device__ __forceinline__ Row(const HeadArgs& a, const HeadPart& p, uint32_t row) {
-        token = divided(row, p.by_heads);
-        head = row - token * p.heads;
-        batch = divided(token, a.by_seq);
-        at = token - batch * a.seq;
+// Where a unit begins, in the first TENSORS tensors of its part.
+template <int MODE, int TENSORS>
+struct Unit {
+    UnitPlace at;
+    int64_t   first[TENSORS];                          // elements in front of the rows
+    __device__ __forceinline__ Unit(const HeadArgs& a, const HeadPart& p, const Place<MODE>& place, uint32_t unit)
+        : at(unit_place(a, p, steady(MODE), unit, (uint32_t)place.row, place.shift)) {
+#pragma unroll
+        for (int k = 0; k < TENSORS; ++k) first[k] = unit_first(p.t[k], steady(MODE), at);
     }
-    __device__ __forceinline__ int64_t in(const HeadTensor& t) const {
-        return (int64_t)batch * t.batch + (int64_t)at * t.token + (int64_t)head * t.head;
+};
+// kAny: the whole of what is in front of a lane's row is its own
+template <int MODE>
+struct LaneOffset {
+    typedef uint32_t type;
+};
+template <>
+struct LaneOffset<kAny> {
+    typedef int64_t type;
+};
+
+// Where the lane's elements stand in the rotation.
+template <bool HALVES>
+struct Turn {
+    bool  turned, second;                              // the lane's elements are rotated; HALVES: are of the second half
+    int   partner, first;                              // HALVES: the lane with the elements' partners; the first angle
+    template <typename PLACE>
+    __device__ __forceinline__ Turn(const HeadArgs& a, const PLACE& at) {
+        const int half = a.rot_lanes >> 1;
+        turned = at.j < a.rot_lanes;
+        second = at.j >= half;
+        partner = !turned ? at.lane : second ? at.lane - half : at.lane + half;
+        first = HALVES ? 8 * (second ? at.j - half : at.j) : 4 * at.j;
     }
 };
 
-// Cosines and sines of the lane's elements at one position.  HALVES: pairs (i, i + rot/2), eight angles a lane, the same
-// in the lane that holds the partners; else pairs (2i, 2i + 1), four angles.  A position outside the table reads
-// nothing and turns by NaN.
+// Cosines and sines of the lane's elements at one position.  HALVES: pairs (i, i + rot/2), eight angles a lane, the same in
+// the lane that holds the partners, the sine with the sign that the forward pass gives the partner; else pairs (2i, 2i + 1),
+// four angles.  Behind rot the angles are 0.  A position outside the tables reads nothing and turns by NaN.
 template <bool HALVES>
 struct Angles {
     static constexpr int N = HALVES ? 8 : 4;
     float c[N], s[N];
-    int partner = 0;                                   // HALVES: the lane with the elements' partners
-    float sign = 1.0f;                                 // HALVES: of the sine, in the lane's own element
-    bool turned = false;
-    __device__ __forceinline__ Angles(const HeadArgs& a, const Place& at) {
+    __device__ __forceinline__ Angles() {
 #pragma unroll
         for (int k = 0; k < N; ++k) { c[k] = 1.0f; s[k] = 0.0f; }
-        turned = at.j < a.rot_lanes;
-        if (HALVES) {
-            const int half = a.rot_lanes >> 1;
-            const bool second = at.j >= half;
-            partner = turned ? (second ? at.lane - half : at.lane + half) : at.lane;
-            sign = second ? 1.0f : -1.0f;
-        }
     }
-    __device__ __forceinline__ void load(const HeadArgs& a, const Place& at, const Row& r) {
-        if (!turned) return;
-        const int64_t position = a.positions ? a.positions[r.token] : (int64_t)r.at;
-        const int half = a.rot_lanes >> 1;
-        const int first = HALVES ? 8 * (at.j < half ? at.j : at.j - half) : 4 * at.j;
-        if ((uint64_t)position < (uint64_t)a.n_positions) {
-            const int64_t o = position * (a.rot_lanes * 4) + first;
+    template <int MODE, int TENSORS>
+    __device__ __forceinline__ void load(const HeadArgs& a, const HeadPart& p, const Turn<HALVES>& turn,
+                                         const Unit<MODE, TENSORS>& u, uint32_t lane_token) {
+        if (a.rot_lanes == 0) return;
+        int64_t position = (int64_t)(u.at.at + lane_token);
+        if (a.positions) {
+            // nothing writes them while the kernel runs: a scalar load where the token is the wavefront's
+            if (steady(MODE) && p.tokens_per_pass == 1)
+                position = ((const __attribute__((address_space(4))) int64_t*)(uintptr_t)a.positions)[u.at.token];
+            else position = a.positions[u.at.token + lane_token];
+        }
+        if (!turn.turned) return;
+        const bool inside = (uint64_t)position < (uint64_t)a.n_positions;
+        const int64_t o = position * (a.rot_lanes * 4) + turn.first;
+        const float nan = __builtin_nanf("");
 #pragma unroll
-            for (int k = 0; k < N; k += 4) {
-                const hf4 cc = *(const hf4_any*)(a.cos + o + k), ss = *(const hf4_any*)(a.sin + o + k);
+        for (int k = 0; k < N; k += 4) {
+            hf4 cc = {nan, nan, nan, nan}, ss = cc;
+            if (inside) { cc = *(const hf4_any*)(a.cos + o + k); ss = *(const hf4_any*)(a.sin + o + k); }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { c[k + i] = cc[i]; s[k + i] = ss[i]; }
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k) c[k] = s[k] = __builtin_nanf("");
+            for (int i = 0; i < 4; ++i) { c[k + i] = cc[i]; s[k + i] = HALVES && !turn.second ? -ss[i] : ss[i]; }
         }
     }
     // v turned by the angles (BACK: by their negatives)
     template <bool BACK>
-    __device__ __forceinline__ void turn(float (&v)[8]) const {
+    __device__ __forceinline__ void turn(float (&v)[8], int partner) const {
         if (HALVES) {
-            const float sg = BACK ? -sign : sign;
             float p[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) p[k] = lane_read(v[k], partner);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float t = __builtin_fmaf(p[k], sg * s[k % N], v[k] * c[k % N]);
-                v[k] = turned ? t : v[k];
-            }
+            for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(BACK ? -p[k] : p[k], s[k % N], v[k] * c[k % N]);
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float x = v[2 * k], y = v[2 * k + 1], sn = BACK ? -s[k] : s[k];
-                const float tx = __builtin_fmaf(-y, sn, x * c[k]), ty = __builtin_fmaf(x, sn, y * c[k]);
-                v[2 * k] = turned ? tx : x;
-                v[2 * k + 1] = turned ? ty : y;
+                const float x = v[2 * k], y = v[2 * k + 1];
+                v[2 * k] = __builtin_fmaf(BACK ? y : -y, s[k], x * c[k]);
+                v[2 * k + 1] = __builtin_fmaf(BACK ? -x : x, s[k], y * c[k]);
             }
         }
     }
 };
 
 // ------------------------------------------------------------------- context
-// Group of element d of row `row`.
-__device__ __forceinline__ int64_t group_of(const HeadArgs& a, uint32_t row, int d) {
-    return a.groups_per_row ? (int64_t)row * a.groups_per_row + (d >> a.group_shift) : (int64_t)(row >> a.row_shift);
+// Where a pass's context lies: rows, and blocks of eight elements, each `bits` bytes of the packed string and one of noise.
+template <int BITS>
+struct Spot {
+    float*   rstd;
+    uint8_t* packed;
+    float*   gmin;
+    float*   gscale;
+    uint64_t block;
+    uint32_t row;
+    int      blocks, groups, rows;                     // of a pass
+    __device__ __forceinline__ Spot(const HeadArgs& a, const HeadPart& p, uint32_t pass, int shift) {
+        rows = 64 >> shift;
+        blocks = rows * (a.dim >> 3);
+        groups = a.groups_per_row ? rows * a.groups_per_row : rows >> a.row_shift;
+        row = pass * (uint32_t)rows;
+        rstd = p.rstd + row;
+        block = (uint64_t)pass * (uint32_t)blocks;
+        packed = p.packed + block * BITS;
+        gmin = p.gmin + (int64_t)pass * groups;
+        gscale = p.gscale + (int64_t)pass * groups;
+    }
+    __device__ __forceinline__ void next() {
+        row += (uint32_t)rows;
+        rstd += rows;
+        block += (uint32_t)blocks;
+        packed += blocks * BITS;
+        gmin += groups;
+        gscale += groups;
+    }
+};
+// The lane's own in it.
+template <typename PLACE>
+__device__ __forceinline__ uint32_t lane_block(const HeadArgs& a, const PLACE& at) { return at.row * (a.dim >> 3) + at.j; }
+template <typename PLACE>
+__device__ __forceinline__ uint32_t lane_group(const HeadArgs& a, const PLACE& at) {
+    return a.groups_per_row ? at.row * a.groups_per_row + (at.d >> a.group_shift) : at.row >> a.row_shift;
 }
 
 // Codes of eight elements, the first in the low bits: compress_tile's rounding (its comment derives it) of one
@@ -270,29 +351,30 @@ __device__ __forceinline__ uint64_t codes8(const float (&v)[8], float mn, float 
 }
 
 template <int BITS>
-__device__ __forceinline__ void store_codes(uint8_t* packed, int64_t e, uint64_t codes) {
-    uint8_t* p = packed + (e >> 3) * BITS;
+__device__ __forceinline__ void store_codes(uint8_t* p, uint64_t codes) {
     if (BITS == 1) *p = (uint8_t)codes;
     if (BITS == 2) *(uint16_t*)p = (uint16_t)codes;
     if (BITS == 4) *(uint32_t*)p = (uint32_t)codes;
     if (BITS == 8) *(uint64_t*)p = codes;
 }
 template <int BITS>
-__device__ __forceinline__ uint64_t load_codes(const uint8_t* packed, int64_t e) {
-    const uint8_t* p = packed + (e >> 3) * BITS;
+__device__ __forceinline__ uint64_t load_codes(const uint8_t* p) {
     if (BITS == 1) return *p;
     if (BITS == 2) return *(const uint16_t*)p;
     if (BITS == 4) return *(const uint32_t*)p;
     return *(const uint64_t*)p;
 }
 
-// Leaves the context of a pass: v holds the lane's elements of row `row`, e the first one's index.
-template <int BITS>
-__device__ __forceinline__ void compress_pass(const HeadArgs& a, const HeadPart& p, const Place& at, uint32_t row,
-                                              bool active, const float (&v)[8]) {
-    const int64_t e = (int64_t)row * a.dim + at.d;
+// Leaves the context of a pass, whose elements v holds.
+template <int BITS, typename PLACE>
+__device__ __forceinline__ void compress_pass(const HeadArgs& a, const HeadPart& p, const PLACE& at, const Spot<BITS>& spot,
+                                              uint32_t my_block, uint32_t my_group, bool active, const float (&v)[8]) {
     uint32_t r[4];
-    philox_head_any((uint64_t)e >> 3, p.seed_lo, p.seed_hi, r);
+    // the high word of the block's number is the wavefront's, unless the low one wraps in this pass
+    if (__builtin_expect((uint32_t)spot.block <= 0xFFFFFFFFu - 64u, 1))
+        philox_head_uniform((uint32_t)spot.block + my_block,
+                            PhiloxUniform((uint32_t)(spot.block >> 32), p.seed_lo, p.seed_hi), p.seed_lo, p.seed_hi, r);
+    else philox_head_any((uint64_t)spot.block + my_block, p.seed_lo, p.seed_hi, r);
     philox_rounds<3>(r[0], r[1], r[2], r[3], p.seed_lo, p.seed_hi);
     float mn = fmin3(v[0], v[1], v[2]), mx = fmax3(v[0], v[1], v[2]);
     mn = fmin3(mn, v[3], v[4]); mx = fmax3(mx, v[3], v[4]);
@@ -306,11 +388,10 @@ __device__ __forceinline__ void compress_pass(const HeadArgs& a, const HeadPart&
     if (range >= 0x1p-100f) { inv = (float)((1u << BITS) - 1u) / range; step = div_levels<BITS>(range); }
     const uint64_t codes = codes8<BITS>(v, mn, inv, r);
     if (!active) return;
-    store_codes<BITS>(p.packed, e, codes);
+    store_codes<BITS>(spot.packed + my_block * BITS, codes);
     if ((at.lane & (a.group_lanes - 1)) == 0) {
-        const int64_t g = group_of(a, row, at.d);
-        p.gmin[g] = mn;
-        p.gscale[g] = step;
+        spot.gmin[my_group] = mn;
+        spot.gscale[my_group] = step;
     }
 }
 
@@ -329,128 +410,206 @@ __device__ __forceinline__ int part_of(const HeadArgs& a, uint32_t& block) {
     block -= a.part[0].blocks;
     return 1;
 }
+__device__ __forceinline__ uint32_t wave_of_block() { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 
-template <int DT, int BITS, bool HALVES>
+template <int DT, int BITS, bool HALVES, int MODE>
+__device__ __forceinline__ void heads_run(const HeadArgs& a, const HeadPart& p, uint32_t unit) {
+    const Place<MODE> at(a);
+    const uint32_t my_token = lane_token(p, steady(MODE), (uint32_t)at.row);
+    typedef typename LaneOffset<MODE>::type Offset;
+    const auto mine = [&](const HeadTensor& t) {
+        return (Offset)((lane_first(p, t, steady(MODE), (uint32_t)at.row, my_token) + at.d) * kSize<DT>);
+    };
+    // a tensor's elements from `first` on: kAny adds them to the lane's offset instead
+    const auto base = [&](const HeadTensor& t, int64_t first) { return (uint8_t*)t.p + (steady(MODE) ? first * kSize<DT> : 0); };
+    const auto lane_at = [&](Offset lane, int64_t first) { return steady(MODE) ? lane : (Offset)(lane + first * kSize<DT>); };
+    const Offset in_lane = mine(p.t[kIn]), out_lane = mine(p.t[kOut]);
+    const int lanes = 1 << at.shift;
+    const uint32_t my_group = BITS != 0 ? lane_group(a, at) : 0, my_block = lane_block(a, at);
+    float w[8];
+    at.weights(a, p, w);
+    const Turn<HALVES> turn(a, at);
+    Angles<HALVES> angles;
+    const auto fetch = [&](int64_t from, uint32_t row) {
+        Raw<DT> raw = {};
+        if (at.holds(p, row)) raw = load8<DT>(base(p.t[kIn], from), lane_at(in_lane, from));
+        return raw;
+    };
+    const uint32_t passes = steady(MODE) ? p.run : 1;
+    const bool keep = p.rstd != nullptr;
+    Unit<MODE, 2> u(a, p, at, unit);
+    Raw<DT> ahead = fetch(u.first[kIn], unit * passes << (6 - at.shift));
+    for (;;) {
+        angles.load(a, p, turn, u, my_token);
+        // behind the wavefront's last unit the same once more, which no HBM traffic follows: so that a pass's elements are
+        // always on their way, without a branch, while the one before is worked on
+        const uint32_t following = p.units - unit > p.waves ? unit + p.waves : unit;
+        const Unit<MODE, 2> next(a, p, at, following);
+        int64_t in = u.first[kIn], out = u.first[kOut];
+        Spot<BITS> spot(a, p, unit * passes, at.shift);
+        for (uint32_t i = 1; i <= passes; ++i) {
+            const Raw<DT> raw = ahead;
+            in += p.t[kIn].pass;
+            const bool last = i == passes;
+            ahead = fetch(last ? next.first[kIn] : in, last ? following * passes << (6 - at.shift) : spot.row + (uint32_t)spot.rows);
+            const bool active = at.holds(p, spot.row);
+            float v[8], n[8], ss = 0.0f;
+            widen8<DT>(raw, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                ss = __builtin_fmaf(v[k], v[k], ss);
+                n[k] = v[k] * w[k];
+            }
+            angles.template turn<false>(n, turn.partner);
+            ss = add_over(ss, lanes);
+            const float rstd = __builtin_amdgcn_rsqf(__builtin_fmaf(ss, a.inv_dim, a.eps));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) n[k] *= rstd;
+            if (active) store8<DT>(base(p.t[kOut], out), lane_at(out_lane, out), n);
+            if (active && keep && at.j == 0) spot.rstd[(uint32_t)at.row] = rstd;
+            if constexpr (BITS != 0) compress_pass<BITS>(a, p, at, spot, my_block, my_group, active, v);
+            out += p.t[kOut].pass;
+            spot.next();
+        }
+        if (following == unit) return;
+        unit = following;
+        u = next;
+    }
+}
+
+template <int DT, int BITS, bool HALVES, int MODE>
 __global__ __launch_bounds__(kHeadThreads) void heads_kernel(HeadArgs a) {
     uint32_t block;
     const HeadPart& p = a.part[part_of(a, block)];
-    const Place at(a);
-    const uint32_t wave = block * kHeadWaves + (threadIdx.x >> 6);
-    const uint32_t first = wave * p.run;
-    if (first >= p.passes) return;
-    const uint32_t end = first + p.run < p.passes ? first + p.run : p.passes;
-    float w[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = p.w && at.in_head ? load_weight(p.w, a.w_f32, at.d + k) : 1.0f;
-    Angles<HALVES> angles(a, at);
-    uint32_t token = 0xFFFFFFFFu;
-    const int lanes = 1 << a.lanes_shift, rows = 64 >> a.lanes_shift;
-    for (uint32_t pass = first; pass < end; ++pass) {
-        const uint32_t row = pass * (uint32_t)rows + (uint32_t)at.row;
-        const bool active = at.in_head && row < p.rows;
-        const Row r(a, p, row < p.rows ? row : p.rows - 1);
-        Raw<DT> raw = {};
-        if (active) raw = load8<DT>(p.in.p, r.in(p.in) + at.d);
-        if (__any(r.token != token)) {
-            token = r.token;
-            angles.load(a, at, r);
-        }
-        float v[8];
-        widen8<DT>(raw, v);
-        float ss = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) ss = __builtin_fmaf(v[k], v[k], ss);
-        ss = add_over(ss, lanes);
-        const float rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(ss, a.inv_dim, a.eps));
-        float n[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) n[k] = v[k] * rstd * w[k];
-        angles.template turn<false>(n);
-        if (active) store8<DT>(p.out.p, r.in(p.out) + at.d, n);
-        if (active && p.rstd && at.j == 0) p.rstd[row] = rstd;
-        if constexpr (BITS != 0) compress_pass<BITS>(a, p, at, row, active, v);
-    }
+    const uint32_t unit = block * kHeadWaves + wave_of_block();
+    if (unit >= p.units) return;
     if constexpr (BITS != 0)
-        if (end == p.passes) zero_pad<BITS>(a, p, at.lane);
+        if (unit == 0) zero_pad<BITS>(a, p, (int)threadIdx.x);
+    heads_run<DT, BITS, HALVES, MODE>(a, p, unit);
 }
 
-template <int DT, int BITS, bool HALVES>
+// x of eight elements from their codes.
+template <int BITS>
+__device__ __forceinline__ void decompress8(uint64_t codes, float mn, float step, float (&x)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        // a nibble of every byte of a word, so that the bytes convert in place
+        const uint32_t word = BITS == 8 && k >= 4 ? (uint32_t)(codes >> 32) : (uint32_t)codes;
+        const uint32_t q = BITS == 8 ? word >> (8 * (k & 3)) & 0xFFu
+                         : BITS == 4 ? ((k & 1 ? word >> 4 : word) & 0x0F0F0F0Fu) >> (8 * (k >> 1)) & 0xFFu
+                         : word >> (k * BITS) & ((1u << BITS) - 1u);
+        const float t = (float)q * step;
+        x[k] = t + mn;
+    }
+}
+
+template <int DT, int BITS, bool HALVES, int MODE>
+__device__ __forceinline__ void backward_run(const HeadArgs& a, const HeadPart& p, const Place<MODE>& at, uint32_t unit,
+                                             float (&dw)[8]) {
+    constexpr int kTensors = BITS == 0 ? 3 : 2;
+    const uint32_t my_token = lane_token(p, steady(MODE), (uint32_t)at.row);
+    typedef typename LaneOffset<MODE>::type Offset;
+    const auto mine = [&](const HeadTensor& t) {
+        return (Offset)((lane_first(p, t, steady(MODE), (uint32_t)at.row, my_token) + at.d) * kSize<DT>);
+    };
+    // a tensor's elements from `first` on: kAny adds them to the lane's offset instead
+    const auto base = [&](const HeadTensor& t, int64_t first) { return (uint8_t*)t.p + (steady(MODE) ? first * kSize<DT> : 0); };
+    const auto lane_at = [&](Offset lane, int64_t first) { return steady(MODE) ? lane : (Offset)(lane + first * kSize<DT>); };
+    const Offset in_lane = mine(p.t[kIn]), out_lane = mine(p.t[kOut]);
+    const Offset x_lane = BITS == 0 ? mine(p.t[kX]) : 0;
+    const int lanes = 1 << at.shift;
+    const uint32_t my_group = BITS != 0 ? lane_group(a, at) : 0, my_block = lane_block(a, at);
+    float w[8];
+    at.weights(a, p, w);
+    const Turn<HALVES> turn(a, at);
+    Angles<HALVES> angles;
+    struct Input {
+        Raw<DT> dy, x;
+        uint64_t codes;
+        float mn, step, rstd;
+    };
+    const auto fetch = [&](int64_t dy, int64_t x, const Spot<BITS>& from) {
+        Input in = {};
+        if (at.holds(p, from.row)) {
+            in.dy = load8<DT>(base(p.t[kIn], dy), lane_at(in_lane, dy));
+            in.rstd = from.rstd[(uint32_t)at.row];
+            if constexpr (BITS != 0) {
+                in.codes = load_codes<BITS>(from.packed + my_block * BITS);
+                in.mn = from.gmin[my_group];
+                in.step = from.gscale[my_group];
+            } else {
+                in.x = load8<DT>(base(p.t[kX], x), lane_at(x_lane, x));
+            }
+        }
+        return in;
+    };
+    const uint32_t passes = steady(MODE) ? p.run : 1;
+    Unit<MODE, kTensors> u(a, p, at, unit);
+    Spot<BITS> spot(a, p, unit * passes, at.shift);
+    Input ahead = fetch(u.first[kIn], u.first[kTensors - 1], spot);
+    for (;;) {
+        angles.load(a, p, turn, u, my_token);
+        const uint32_t following = p.units - unit > p.waves ? unit + p.waves : unit;       // as in heads_run
+        const Unit<MODE, kTensors> next(a, p, at, following);
+        const Spot<BITS> next_spot(a, p, following * passes, at.shift);
+        int64_t dy = u.first[kIn], out = u.first[kOut], xs = u.first[kTensors - 1];
+        for (uint32_t i = 1; i <= passes; ++i) {
+            const Input in = ahead;
+            const bool active = at.holds(p, spot.row);
+            dy += p.t[kIn].pass;
+            xs += p.t[kTensors - 1].pass;
+            spot.next();
+            const bool last = i == passes;
+            if (last) spot = next_spot;
+            ahead = fetch(last ? next.first[kIn] : dy, last ? next.first[kTensors - 1] : xs, spot);
+            float dn[8], x[8], s = 0.0f;
+            widen8<DT>(in.dy, dn);
+            if constexpr (BITS != 0) decompress8<BITS>(in.codes, in.mn, in.step, x);
+            else widen8<DT>(in.x, x);
+            angles.template turn<true>(dn, turn.partner);
+            // r g and r mean(g x)
+            float g[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                dn[k] *= in.rstd;
+                g[k] = dn[k] * w[k];
+                s = __builtin_fmaf(g[k], x[k], s);
+            }
+            s = add_over(s, lanes) * a.inv_dim * (in.rstd * in.rstd);
+            if (active) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    dw[k] = __builtin_fmaf(dn[k], x[k], dw[k]);
+                    g[k] = __builtin_fmaf(-x[k], s, g[k]);
+                }
+                store8<DT>(base(p.t[kOut], out), lane_at(out_lane, out), g);
+            }
+            out += p.t[kOut].pass;
+        }
+        if (following == unit) return;
+        unit = following;
+        u = next;
+    }
+}
+
+template <int DT, int BITS, bool HALVES, int MODE>
 __global__ __launch_bounds__(kHeadThreads) void heads_backward_kernel(HeadArgs a) {
     __shared__ float lds[kHeadWaves][64 * 8];
     uint32_t block;
     const HeadPart& p = a.part[part_of(a, block)];
-    const Place at(a);
-    const uint32_t wave = block * kHeadWaves + (threadIdx.x >> 6);
-    const uint32_t first = wave * p.run < p.passes ? wave * p.run : p.passes;
-    const uint32_t end = p.passes - first > p.run ? first + p.run : p.passes;
-    float w[8], dw[8];
+    const uint32_t unit = block * kHeadWaves + wave_of_block();
+    const Place<MODE> at(a);
+    float dw[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        w[k] = p.w && at.in_head ? load_weight(p.w, a.w_f32, at.d + k) : 1.0f;
-        dw[k] = 0.0f;
-    }
-    Angles<HALVES> angles(a, at);
-    uint32_t token = 0xFFFFFFFFu;
-    const int lanes = 1 << a.lanes_shift, rows = 64 >> a.lanes_shift;
-    for (uint32_t pass = first; pass < end; ++pass) {
-        const uint32_t row = pass * (uint32_t)rows + (uint32_t)at.row;
-        const bool active = at.in_head && row < p.rows;
-        const Row r(a, p, row < p.rows ? row : p.rows - 1);
-        Raw<DT> raw = {}, raw_x = {};
-        uint64_t codes = 0;
-        float mn = 0.0f, step = 0.0f, rstd = 0.0f;
-        if (active) {
-            raw = load8<DT>(p.in.p, r.in(p.in) + at.d);
-            rstd = p.rstd[row];
-            if constexpr (BITS != 0) {
-                codes = load_codes<BITS>(p.packed, (int64_t)row * a.dim + at.d);
-                const int64_t g = group_of(a, row, at.d);
-                mn = p.gmin[g];
-                step = p.gscale[g];
-            } else {
-                raw_x = load8<DT>(p.x.p, r.in(p.x) + at.d);
-            }
-        }
-        if (__any(r.token != token)) {
-            token = r.token;
-            angles.load(a, at, r);
-        }
-        float dn[8], x[8];
-        widen8<DT>(raw, dn);
-        if constexpr (BITS != 0) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const uint32_t q = (uint32_t)(codes >> (k * BITS)) & ((1u << BITS) - 1u);
-                const float t = (float)q * step;
-                x[k] = t + mn;
-            }
-        } else {
-            widen8<DT>(raw_x, x);
-        }
-        angles.template turn<true>(dn);
-        float s = 0.0f, g[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            x[k] *= rstd;
-            g[k] = dn[k] * w[k];
-            s = __builtin_fmaf(g[k], x[k], s);
-        }
-        s = add_over(s, lanes) * a.inv_dim;
-        if (active) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                dw[k] = __builtin_fmaf(dn[k], x[k], dw[k]);
-                g[k] = rstd * __builtin_fmaf(-x[k], s, g[k]);
-            }
-            store8<DT>(p.out.p, r.in(p.out) + at.d, g);
-        }
-    }
+    for (int k = 0; k < 8; ++k) dw[k] = 0.0f;
+    if (unit < p.units) backward_run<DT, BITS, HALVES, MODE>(a, p, at, unit, dw);
     if (!p.partial) return;
     // over the wavefront's rows, then over the block's wavefronts
     float* mine = lds[threadIdx.x >> 6];
 #pragma unroll
     for (int k = 0; k < 8; ++k) mine[k * 64 + at.lane] = dw[k];
     __syncthreads();
+    const int lanes = 1 << at.shift, rows = 64 >> at.shift;
     for (int d = (int)threadIdx.x; d < a.dim; d += kHeadThreads) {
         float sum = 0.0f;
         for (int v = 0; v < kHeadWaves; ++v)
@@ -459,60 +618,80 @@ __global__ __launch_bounds__(kHeadThreads) void heads_backward_kernel(HeadArgs a
     }
 }
 
-// dw of one part: its blocks' sums, 32 elements a block of 16 x 32 threads, added in binary64 and in a fixed order.
-constexpr int kDwRows = 16, kDwColumns = 32;
-__global__ __launch_bounds__(kDwRows * kDwColumns) void heads_dw_kernel(HeadArgs a) {
-    __shared__ double lds[kDwRows][kDwColumns];
+// dw of one part: its blocks' sums, eight elements a block of 8 x 128 threads, added in binary64 and in a fixed order.
+constexpr int kDwColumns = 8, kDwRows = 128, kDwThreads = kDwColumns * kDwRows;
+__global__ __launch_bounds__(kDwThreads) void heads_dw_kernel(HeadArgs a) {
+    __shared__ double lds[kDwThreads / 64][kDwColumns];
     const HeadPart& p = a.part[blockIdx.y];
     if (!p.dw) return;
     const int col = threadIdx.x % kDwColumns, row = threadIdx.x / kDwColumns, d = blockIdx.x * kDwColumns + col;
+    constexpr int kEach = (int)(kHeadBackwardBlocks + kDwRows - 1) / kDwRows;
+    float v[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const uint32_t i = (uint32_t)(k * kDwRows + row);
+        v[k] = i < p.blocks ? p.partial[i * (uint32_t)a.dim + (uint32_t)d] : 0.0f;
+    }
     double sum = 0.0;
-    if (d < a.dim)
-        for (uint32_t b = row; b < p.blocks; b += kDwRows) sum += (double)p.partial[(size_t)b * a.dim + d];
-    lds[row][col] = sum;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) sum += (double)v[k];
+#pragma unroll
+    for (int m = 32; m >= kDwColumns; m >>= 1) sum += __shfl_xor(sum, m);
+    if ((threadIdx.x & 63) < kDwColumns) lds[threadIdx.x >> 6][col] = sum;
     __syncthreads();
-    if (row != 0 || d >= a.dim) return;
-    for (int k = 1; k < kDwRows; ++k) sum += lds[k][col];
+    if (threadIdx.x >= kDwColumns) return;
+    sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < kDwThreads / 64; ++k) sum += lds[k][threadIdx.x];
     if (a.w_f32) ((float*)p.dw)[d] = (float)sum;
     else ((uint16_t*)p.dw)[d] = (uint16_t)bf16_pair_rne((float)sum, 0.0f);
 }
 
 // ------------------------------------------------------------- host launchers
-template <int DT, int BITS, bool HALVES>
+template <int DT, int BITS, bool HALVES, int MODE>
 static void launch(bool backward, const HeadArgs& a, unsigned blocks, hipStream_t s) {
-    if (backward) hipLaunchKernelGGL((heads_backward_kernel<DT, BITS, HALVES>), dim3(blocks), dim3(kHeadThreads), 0, s, a);
-    else hipLaunchKernelGGL((heads_kernel<DT, BITS, HALVES>), dim3(blocks), dim3(kHeadThreads), 0, s, a);
+    if (backward) hipLaunchKernelGGL((heads_backward_kernel<DT, BITS, HALVES, MODE>), dim3(blocks), dim3(kHeadThreads), 0, s, a);
+    else hipLaunchKernelGGL((heads_kernel<DT, BITS, HALVES, MODE>), dim3(blocks), dim3(kHeadThreads), 0, s, a);
 }
-template <int DT, bool HALVES>
-static void launch_bits(bool backward, const HeadArgs& a, int bits, unsigned blocks, hipStream_t s) {
-    switch (bits) {
-        case 0: launch<DT, 0, HALVES>(backward, a, blocks, s); break;
-        case 1: launch<DT, 1, HALVES>(backward, a, blocks, s); break;
-        case 2: launch<DT, 2, HALVES>(backward, a, blocks, s); break;
-        case 4: launch<DT, 4, HALVES>(backward, a, blocks, s); break;
-        default: launch<DT, 8, HALVES>(backward, a, blocks, s); break;
+template <int DT, int BITS, bool HALVES>
+static void launch_mode(bool backward, const HeadArgs& a, int mode, unsigned blocks, hipStream_t s) {
+    switch (mode) {
+        case kAny: launch<DT, BITS, HALVES, kAny>(backward, a, blocks, s); break;
+        case kSteady: launch<DT, BITS, HALVES, kSteady>(backward, a, blocks, s); break;
+        case 3: launch<DT, BITS, HALVES, 3>(backward, a, blocks, s); break;
+        case 4: launch<DT, BITS, HALVES, 4>(backward, a, blocks, s); break;
+        default: launch<DT, BITS, HALVES, 5>(backward, a, blocks, s); break;
     }
 }
-static int launch_any(bool backward, const HeadArgs& a, int dtype, int bits, int halves, hipStream_t s) {
+template <int DT, bool HALVES>
+static void launch_bits(bool backward, const HeadArgs& a, int mode, int bits, unsigned blocks, hipStream_t s) {
+    switch (bits) {
+        case 0: launch_mode<DT, 0, HALVES>(backward, a, mode, blocks, s); break;
+        case 1: launch_mode<DT, 1, HALVES>(backward, a, mode, blocks, s); break;
+        case 2: launch_mode<DT, 2, HALVES>(backward, a, mode, blocks, s); break;
+        case 4: launch_mode<DT, 4, HALVES>(backward, a, mode, blocks, s); break;
+        default: launch_mode<DT, 8, HALVES>(backward, a, mode, blocks, s); break;
+    }
+}
+static int launch_any(bool backward, const HeadArgs& a, int mode, int dtype, int bits, int halves, hipStream_t s) {
     const unsigned blocks = a.part[0].blocks + a.part[1].blocks;
     if (dtype == GACT_DT_F32) {
-        if (halves) launch_bits<GACT_DT_F32, true>(backward, a, bits, blocks, s);
-        else launch_bits<GACT_DT_F32, false>(backward, a, bits, blocks, s);
+        if (halves) launch_bits<GACT_DT_F32, true>(backward, a, mode, bits, blocks, s);
+        else launch_bits<GACT_DT_F32, false>(backward, a, mode, bits, blocks, s);
     } else {
-        if (halves) launch_bits<GACT_DT_BF16, true>(backward, a, bits, blocks, s);
-        else launch_bits<GACT_DT_BF16, false>(backward, a, bits, blocks, s);
+        if (halves) launch_bits<GACT_DT_BF16, true>(backward, a, mode, bits, blocks, s);
+        else launch_bits<GACT_DT_BF16, false>(backward, a, mode, bits, blocks, s);
     }
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 }  // namespace gact
 
-extern "C" int gact_launch_heads(const gact::HeadArgs* a, int dtype, int bits, int halves, int backward, void* stream) {
-    return gact::launch_any(backward != 0, *a, dtype, bits, halves, (hipStream_t)stream);
+extern "C" int gact_launch_heads(const gact::HeadArgs* a, int mode, int dtype, int bits, int halves, int backward, void* stream) {
+    return gact::launch_any(backward != 0, *a, mode, dtype, bits, halves, (hipStream_t)stream);
 }
 
 extern "C" int gact_launch_heads_dw(const gact::HeadArgs* a, int parts, void* stream) {
-    hipLaunchKernelGGL(gact::heads_dw_kernel, dim3((a->dim + gact::kDwColumns - 1) / gact::kDwColumns, parts),
-                       dim3(gact::kDwRows * gact::kDwColumns), 0, (hipStream_t)stream, *a);
+    hipLaunchKernelGGL(gact::heads_dw_kernel, dim3(a->dim / gact::kDwColumns, parts), dim3(gact::kDwThreads), 0, (hipStream_t)stream, *a);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }

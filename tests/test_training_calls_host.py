@@ -194,6 +194,7 @@ def test_the_binding_refuses_tensors_the_kernels_cannot_take():
 
 PROGRAM = r"""
 #include <cstdio>
+#include <vector>
 #include "gact_heads.h"
 #include "gact_norm.h"
 int main() {
@@ -211,20 +212,70 @@ int main() {
             if (q != x / d) { std::printf("%u / %u = %u\n", x, d, q); failed = 1; }
         }
     }
-    // the backward launch's blocks, whatever the parts' sizes
-    for (int i = 0; i < 200000; ++i) {
-        gact::HeadArgs a{};
-        for (auto& p : a.part) p.passes = (uint32_t)(next() % 0x7FFFFFFF) >> (next() % 31);
-        gact::plan_heads_backward(&a, 2);
-        if (a.part[0].blocks + a.part[1].blocks > gact::kHeadBackwardBlocks) { std::printf("blocks\n"); failed = 1; }
-        for (auto& p : a.part)
-            if ((uint64_t)p.blocks * gact::kHeadWaves * p.run < p.passes) { std::printf("passes\n"); failed = 1; }
-        gact::plan_heads(&a, 2);
-        for (auto& p : a.part) {
-            const uint64_t taken = (uint64_t)p.blocks * gact::kHeadWaves * p.run;
-            if (taken < p.passes || taken >= (uint64_t)p.passes + gact::kHeadWaves * p.run) { std::printf("run\n"); failed = 1; }
-            if (!gact::launchable((uint64_t)a.part[0].blocks + a.part[1].blocks, 64 * gact::kHeadWaves)) { std::printf("threads\n"); failed = 1; }
+    // the launches' plans, whatever the parts' sizes
+    for (uint32_t passes = 1; passes < 5000; ++passes) {
+        for (const uint32_t most : {1u, 2u, 3u, 8u}) {
+            const uint32_t run = gact::head_run(passes, most);
+            if (run < 1 || run > most || passes % run != 0 || (passes <= most && run != passes)) { std::printf("run\n"); failed = 1; }
         }
+    }
+    for (int i = 0; i < 100000; ++i) {
+        gact::HeadArgs a{};
+        for (auto& p : a.part) {
+            p.run = 1 + (uint32_t)(next() % 8);
+            p.units = (i < 3000 ? (uint32_t)(next() % 60000) : (uint32_t)(next() % 0x7FFFFFFF) >> (next() % 31)) / p.run;
+        }
+        for (const uint32_t all : {gact::kHeadBackwardBlocks, gact::kHeadForwardBlocks}) {
+            gact::plan_heads(a.part, 2, all);
+            if (a.part[0].blocks + a.part[1].blocks > all) { std::printf("blocks\n"); failed = 1; }
+            for (auto& p : a.part) {
+                if ((p.units != 0) != (p.blocks != 0) || p.waves != p.blocks * gact::kHeadWaves) { std::printf("waves\n"); failed = 1; }
+                if (p.blocks != 0 && (uint64_t)(p.blocks - 1) * gact::kHeadWaves >= p.units) { std::printf("idle block\n"); failed = 1; }
+            }
+        }
+    }
+    // every row of a part is taken once, by a lane that has its token and its address, however the part is laid out
+    for (int i = 0; i < 4000; ++i) {
+        gact::HeadArgs a{};
+        a.lanes_shift = (int)(next() % 7);
+        a.dim = a.lanes_shift == 0 ? 8 : (4 << a.lanes_shift) + 8 + (int)(next() % (1 << a.lanes_shift)) / 2 * 8;
+        if (i % 2) a.dim = 8 << a.lanes_shift;
+        a.seq = 1 + (uint32_t)(next() % 9);
+        a.by_seq = gact::divisor(a.seq);
+        const uint32_t batch = 1 + (uint32_t)(next() % 5), in_pass = 64u >> a.lanes_shift;
+        gact::HeadPart& p = a.part[0];
+        p.heads = 1 + (uint32_t)(next() % (i % 3 ? 20 : 200));
+        p.rows = batch * a.seq * p.heads;
+        p.row_by_heads = gact::divisor(p.heads);
+        gact::HeadTensor& t = p.t[gact::kIn];
+        const int64_t far = i % 5 == 0 ? 1ll << 31 : 100000, offset = i % 7 == 0 ? far / 2 : 0;      // too far for 32 bits; negative
+        t.batch = (int64_t)(next() % 100000) - 50000;
+        t.token = (int64_t)(next() % far) - offset;
+        t.head = (int64_t)(next() % far) - offset;
+        const int size = i % 2 ? 2 : 4;
+        const int mode = gact::lay_out_heads(a, &p, i % 4 == 3 ? 0 : 1 + (uint32_t)(next() % 8), size);
+        if ((i % 4 == 3 || t.token < 0 || t.head < 0) && mode != gact::kAny) { std::printf("mode\n"); failed = 1; }
+        gact::plan_heads(a.part, 1, 8);
+        const bool steady = mode != gact::kAny;
+        std::vector<int> taken(p.rows);
+        for (uint32_t w = 0; w < p.waves; ++w)
+            for (uint32_t unit = w; unit < p.units; unit += p.waves)
+                for (uint32_t lane = 0; lane < in_pass; ++lane) {
+                    const gact::UnitPlace u = gact::unit_place(a, p, steady, unit, lane, a.lanes_shift);
+                    const uint32_t more = gact::lane_token(p, steady, lane);
+                    const int64_t mine = gact::lane_first(p, t, steady, lane, more);
+                    if (steady && (mine < 0 || (mine + a.dim) * size > 0xFFFFFFFFll)) { std::printf("offset\n"); failed = 1; }
+                    int64_t at = gact::unit_first(t, steady, u) + mine;
+                    for (uint32_t pass = 0; pass < p.run; ++pass, at += t.pass) {
+                        const uint64_t row = ((uint64_t)unit * p.run + pass) * in_pass + lane;
+                        if (row >= p.rows) { if (steady) { std::printf("row\n"); failed = 1; } continue; }
+                        const uint32_t token = (uint32_t)(row / p.heads), head = (uint32_t)(row % p.heads);
+                        const int64_t want = (int64_t)(token / a.seq) * t.batch + (int64_t)(token % a.seq) * t.token + (int64_t)head * t.head;
+                        if (at != want || u.token + more != token || u.at + more != token % a.seq) { std::printf("place\n"); failed = 1; }
+                        ++taken[row];
+                    }
+                }
+        for (int n : taken) if (n != 1) { std::printf("taken\n"); failed = 1; break; }
     }
     return failed;
 }

@@ -409,8 +409,8 @@ bool outputs_overlap(const std::vector<gact::NormBuffer>& bufs, size_t f32) {
     std::vector<Range> ranges;
     ranges.reserve(2 * bufs.size());
     for (size_t k = 0; k < bufs.size(); ++k) {
-        const uintptr_t bytes = (uintptr_t)bufs[k].n * (k < f32 ? 4 : 2);
-        const uintptr_t in = (uintptr_t)bufs[k].in, out = (uintptr_t)bufs[k].out;
+        const uintptr_t size = k < f32 ? 4 : 2, bytes = (uintptr_t)(bufs[k].n + bufs[k].head) * size;
+        const uintptr_t in = (uintptr_t)bufs[k].in - bufs[k].head * size, out = (uintptr_t)bufs[k].out - bufs[k].head * size;
         ranges.push_back(Range{out, out + bytes, true});
         if (in != out) ranges.push_back(Range{in, in + bytes, false});
     }
@@ -427,7 +427,7 @@ bool outputs_overlap(const std::vector<gact::NormBuffer>& bufs, size_t f32) {
 // What the three calls share: checks, the buffers' table (in *table, or in the workspace where it is too long for
 // the arguments), the launch's blocks.
 int stage_norm(const gact_grad_buf* bufs, int K, bool scale, const double* d_norm, void* d_workspace, size_t workspace_bytes,
-               void* stream, gact::NormTable* table, gact::NormArgs* a, bool* is_inline) {
+               void* stream, gact::NormTable* table, gact::NormArgs* a, bool* is_inline, uint64_t* bytes) {
     if (K < 0 || (K > 0 && !bufs) || !d_norm || !aligned(d_norm, 8)) return GACT_E_ARG;
     if (!d_workspace || !aligned(d_workspace, 16) || workspace_bytes < gact_grad_norm_workspace_bytes(K)) return GACT_E_ARG;
     std::vector<gact::NormBuffer> live;
@@ -442,9 +442,18 @@ int stage_norm(const gact_grad_buf* bufs, int K, bool scale, const double* d_nor
             if (b.dtype != dtype || b.n == 0) continue;
             const size_t size = dtype == GACT_F32 ? 4 : 2;
             if (!b.g || !aligned(b.g, size) || (scale && (!b.out || !aligned(b.out, size)))) return GACT_E_ARG;
-            live.push_back(gact::NormBuffer{b.g, b.out, b.n});
+            if (b.n > (int64_t)1 << 48) return GACT_E_ARG;
+            const int64_t head = std::min<int64_t>(b.n, (int64_t)((0 - (uintptr_t)b.g & 15) / size));
+            gact::NormBuffer nb{};
+            nb.in = (const unsigned char*)b.g + head * size;
+            nb.out = scale ? (unsigned char*)b.out + head * size : nullptr;
+            nb.n = b.n - head;
+            nb.head = head;
+            live.push_back(nb);
+            *bytes += (uint64_t)b.n * size;
             first.push_back((uint32_t)chunks);
-            chunks += ((uint64_t)b.n - 1) / (uint64_t)gact::norm_chunk_elems(dtype) + 1;
+            // one at least, which has the elements in front
+            chunks += std::max<uint64_t>(1, ((uint64_t)nb.n + gact::norm_chunk_elems(dtype) - 1) / (uint64_t)gact::norm_chunk_elems(dtype));
             if (chunks > 0x7FFFFFFFull) return GACT_E_ARG;
         }
         if (dtype == GACT_F32) a->f32 = (uint32_t)live.size();
@@ -463,18 +472,18 @@ int stage_norm(const gact_grad_buf* bufs, int K, bool scale, const double* d_nor
         return GACT_OK;
     }
     unsigned char* base = (unsigned char*)d_workspace + kNormPartials;
-    const size_t tb = live.size() * sizeof(gact::NormBuffer), bytes = tb + first.size() * sizeof(uint32_t);
+    const size_t tb = live.size() * sizeof(gact::NormBuffer), size = tb + first.size() * sizeof(uint32_t);
     a->table = (const gact::NormBuffer*)base;
     a->first = (const uint32_t*)(base + tb);
-    std::vector<unsigned char> image(bytes);
+    std::vector<unsigned char> image(size);
     std::memcpy(image.data(), live.data(), tb);
     std::memcpy(image.data() + tb, first.data(), first.size() * sizeof(uint32_t));
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
     if (hipStreamIsCapturing((hipStream_t)stream, &status) != hipSuccess) return GACT_E_HIP;
-    if (status == hipStreamCaptureStatusNone) return upload(base, image.data(), bytes, stream);
-    for (size_t at = 0; at < bytes; at += gact::kTablePiece) {
+    if (status == hipStreamCaptureStatusNone) return upload(base, image.data(), size, stream);
+    for (size_t at = 0; at < size; at += gact::kTablePiece) {
         gact::TablePiece piece{};
-        const size_t part = std::min<size_t>(gact::kTablePiece, bytes - at);
+        const size_t part = std::min<size_t>(gact::kTablePiece, size - at);
         std::memcpy(piece.w, image.data() + at, part);
         if (gact_launch_table_piece(base + at, &piece, (unsigned)(part / 4), stream) != 0) return GACT_E_HIP;
     }
@@ -489,10 +498,13 @@ int run_norm(const gact_grad_buf* bufs, int K, int kind, bool scale, bool given,
     gact::NormArgs a{};
     a.max_norm = max_norm;
     bool is_inline = false;
-    if (const int rc = stage_norm(bufs, K, scale, d_norm, d_workspace, workspace_bytes, stream, &table, &a, &is_inline)) return rc;
+    uint64_t bytes = 0;
+    if (const int rc = stage_norm(bufs, K, scale, d_norm, d_workspace, workspace_bytes, stream, &table, &a, &is_inline, &bytes)) return rc;
     const gact::NormTable* t = is_inline ? &table : nullptr;
     scale = scale && a.blocks != 0;
-    if (!given && gact_launch_grad_norm(t, &a, kind, !scale, stream) != 0) return GACT_E_HIP;
+    const bool once = bytes >= (scale ? gact::kClipOnceBytes : gact::kNormOnceBytes);
+    a.clip_blocks = given || once ? std::min(a.chunks, gact::kClipBlocks) : a.blocks;
+    if (!given && gact_launch_grad_norm(t, &a, kind, once, !scale, stream) != 0) return GACT_E_HIP;
     if (scale && gact_launch_grad_clip(t, &a, kind, given, stream) != 0) return GACT_E_HIP;
     return GACT_OK;
 }

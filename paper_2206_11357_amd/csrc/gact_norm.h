@@ -12,15 +12,24 @@ namespace gact {
 constexpr int kNormWaves = 8, kNormThreads = 64 * kNormWaves;
 constexpr int kNormPieces = 2;                    // of 16 bytes, per thread and chunk
 constexpr int64_t norm_chunk_elems(int dtype) { return kNormThreads * kNormPieces * (dtype == GACT_DT_F32 ? 4 : 8); }
-// Blocks of a launch, each of which takes a run of neighbouring chunks and leaves one result.
+// Blocks of a norm's launch, each of which takes a run of neighbouring chunks and leaves one result.
 constexpr uint32_t kNormBlocks = 1024;
-static_assert(kNormBlocks <= 2 * kNormThreads, "two results a thread when a block adds them up");
+// Lists of this many bytes and more do not stay in the 256 MB cache from one launch to the next: a norm alone reads them as data
+// that nobody wants again, and clipping, which reads them twice, from the larger bound on.  Clipping has then eight times the blocks
+// (each adds up the norm's results first), as it has by a given norm.  Us, norm alone, ordinary | as said: 201 MB bf16 32.0 | 33.4,
+// 608 MB 108 | 99; clipping fp32, norm + scaling: 50 MB 27 | 31, 101 MB 49 | 57, 202 MB 95 | 102, 403 MB 193 | 199, 503 MB 244 | 241, 604 MB 301 | 294,
+// 1.2 GB 632 | 610.
+constexpr uint64_t kNormOnceBytes = 256ull << 20, kClipOnceBytes = 440ull << 20;
+constexpr uint32_t kClipBlocks = 8192;
 
+// A buffer from the first 16-byte line of the input on.  (Loads of 16 bytes that begin anywhere take a quarter longer.)
 struct NormBuffer {
     const void* in;
     void*       out;                              // null: norm only
-    int64_t     n;
+    int64_t     n : 56;                           // from there on
+    int64_t     head : 8;                         // elements in front, up to 7
 };
+static_assert(sizeof(NormBuffer) == 24, "three words of a table");
 // A table small enough to travel in the kernel arguments: the buffers of one type behind those of the other
 // (f32 of them are fp32), then the first chunk of each.
 constexpr int kInlineNorm = 136;
@@ -31,7 +40,7 @@ struct NormTable {
 struct NormArgs {
     const NormBuffer* table;                      // device memory; null: the inline table
     const uint32_t*   first;
-    uint32_t K, f32, chunks, blocks;
+    uint32_t K, f32, chunks, blocks, clip_blocks;
     double*  partial;                             // one a block
     double*  norm;
     double   max_norm;
@@ -46,7 +55,7 @@ struct TablePiece {
 
 }  // namespace gact
 
-extern "C" int gact_launch_grad_norm(const gact::NormTable* t, const gact::NormArgs* a, int kind, int finish, void* stream);
+extern "C" int gact_launch_grad_norm(const gact::NormTable* t, const gact::NormArgs* a, int kind, int once, int finish, void* stream);
 extern "C" int gact_launch_grad_clip(const gact::NormTable* t, const gact::NormArgs* a, int kind, int given, void* stream);
 extern "C" int gact_launch_table_piece(void* dst, const gact::TablePiece* piece, unsigned words, void* stream);
 

@@ -67,42 +67,23 @@ __device__ __forceinline__ double join_block(double v) {
 template <int KIND>
 __device__ __forceinline__ double root(double v) { return KIND == kNorm2 ? __builtin_sqrt(v) : v; }
 
-// The chunks of a block's run, buffer by buffer.
-struct Walk {
-    const NormBuffer* table;
-    const uint32_t* first;
-    uint32_t k, begin, end;                          // buffer; chunks of the run that are left
-    __device__ __forceinline__ Walk(const NormBuffer* buffers, const uint32_t* firsts, const NormArgs& a, bool from_end)
-        : table(buffers), first(firsts) {
-        begin = (uint32_t)((uint64_t)a.chunks * blockIdx.x / a.blocks);
-        end = (uint32_t)((uint64_t)a.chunks * (blockIdx.x + 1) / a.blocks);
-        const uint32_t at = from_end ? end - 1 : begin;
-        uint32_t lo = 0, hi = a.K;
-        while (hi - lo > 1) {
-            const uint32_t mid = (lo + hi) >> 1;
-            if (first[mid] <= at) lo = mid; else hi = mid;
-        }
-        k = lo;
-    }
-};
-
-template <int DT, bool FULL>
-__device__ __forceinline__ n4 load_piece(const void* in, int64_t e, int64_t n) {
-    constexpr int P = DT == GACT_DT_F32 ? 4 : 8;
-    n4 w = {0u, 0u, 0u, 0u};
-    if (FULL || e + P <= n) {
-        if (DT == GACT_DT_F32) w = *(const n4_f32*)((const uint32_t*)in + e);
-        else w = *(const n4_bf16*)((const uint16_t*)in + e);
-    } else if (e < n) {
-        uint32_t t[4] = {0u, 0u, 0u, 0u};
-        for (int j = 0; j < P; ++j)
-            if (e + j < n) {
-                if (DT == GACT_DT_F32) t[j & 3] = ((const uint32_t*)in)[e + j];
-                else t[j >> 1] |= (uint32_t)((const uint16_t*)in)[e + j] << (16 * (j & 1));
-            }
-        w = n4{t[0], t[1], t[2], t[3]};
-    }
-    return w;
+// A 16-byte piece.  ONCE: it is not wanted in a cache (norm_streams, clip_run).
+template <int DT, bool ONCE>
+__device__ __forceinline__ n4 load_piece(const uint8_t* p) {
+    if (DT == GACT_DT_F32) return ONCE ? __builtin_nontemporal_load((const n4_f32*)p) : *(const n4_f32*)p;
+    return ONCE ? __builtin_nontemporal_load((const n4_bf16*)p) : *(const n4_bf16*)p;
+}
+template <int DT>
+__device__ __forceinline__ void store_piece(uint8_t* p, n4 w) {
+    if (DT == GACT_DT_F32) __builtin_nontemporal_store(w, (n4_f32*)p);
+    else __builtin_nontemporal_store(w, (n4_bf16*)p);
+}
+template <int DT>
+constexpr int kSize = DT == GACT_DT_F32 ? 4 : 2;
+template <int DT>
+__device__ __forceinline__ float load_element(const uint8_t* p) {
+    if (DT == GACT_DT_F32) return *(const float*)p;
+    return __builtin_bit_cast(float, (uint32_t)*(const uint16_t*)p << 16);
 }
 template <int DT>
 __device__ __forceinline__ void widen(const n4 w, float (&v)[8]) {
@@ -114,47 +95,104 @@ __device__ __forceinline__ void widen(const n4 w, float (&v)[8]) {
     }
 }
 
-template <int KIND, int DT, bool FULL>
-__device__ __forceinline__ void norm_chunk(const NormBuffer& b, int64_t chunk, Acc<KIND>& acc) {
-    constexpr int P = DT == GACT_DT_F32 ? 4 : 8;
-    n4 w[kNormPieces];
-#pragma unroll
-    for (int i = 0; i < kNormPieces; ++i)
-        w[i] = load_piece<DT, FULL>(b.in, chunk * norm_chunk_elems(DT) + (i * kNormThreads + (int)threadIdx.x) * P, b.n);
-#pragma unroll
-    for (int i = 0; i < kNormPieces; ++i) {
-        float v[8];
-        widen<DT>(w[i], v);
-#pragma unroll
-        for (int j = 0; j < P; ++j) acc.add(v[j]);
+constexpr int kChunkBytes = kNormThreads * kNormPieces * 16;
+constexpr int kTogether = 2;                        // chunks whose loads are out together
+
+// A run of neighbouring chunks [begin, end), buffer by buffer, forwards or (BACK) from the end: part(buffer, number of its first
+// chunk, number of chunks) for each.  Chunks are whole but for a buffer's last.
+template <bool BACK, typename PART>
+__device__ __forceinline__ void each_part(const NormBuffer* table, const uint32_t* first, uint32_t K, uint32_t begin, uint32_t end,
+                                          const PART& part) {
+    uint32_t lo = 0, hi = K;
+    const uint32_t at = BACK ? end - 1 : begin;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (first[mid] <= at) lo = mid; else hi = mid;
+    }
+    if (!BACK) {
+        for (uint32_t k = lo; begin < end; ++k) {
+            const uint32_t stop = first[k + 1] < end ? first[k + 1] : end;
+            part(k, begin - first[k], stop - begin);
+            begin = stop;
+        }
+    } else {
+        for (uint32_t k = lo; begin < end; --k) {
+            const uint32_t start = first[k] > begin ? first[k] : begin;
+            part(k, start - first[k], end - start);
+            end = start;
+        }
     }
 }
 
-template <int KIND>
-__device__ __forceinline__ void norm_run(Walk walk, const NormArgs& a) {
-    Acc<KIND> acc;
-    for (uint32_t c = walk.begin; c < walk.end; ++c) {
-        while (walk.first[walk.k + 1] <= c) ++walk.k;
-        const NormBuffer b = walk.table[walk.k];
-        const int64_t chunk = c - walk.first[walk.k];
-        if (walk.k < a.f32) {
-            if ((chunk + 1) * norm_chunk_elems(GACT_DT_F32) <= b.n) norm_chunk<KIND, GACT_DT_F32, true>(b, chunk, acc);
-            else norm_chunk<KIND, GACT_DT_F32, false>(b, chunk, acc);
-        } else {
-            if ((chunk + 1) * norm_chunk_elems(GACT_DT_BF16) <= b.n) norm_chunk<KIND, GACT_DT_BF16, true>(b, chunk, acc);
-            else norm_chunk<KIND, GACT_DT_BF16, false>(b, chunk, acc);
+template <int KIND, bool ONCE, int DT>
+__device__ __forceinline__ void norm_part(const NormBuffer& b, uint32_t chunk, uint32_t chunks, Acc<KIND>& acc) {
+    constexpr int P = 16 / kSize<DT>;
+    if (chunk == 0 && threadIdx.x < (uint32_t)b.head)
+        acc.add(load_element<DT>((const uint8_t*)b.in - (threadIdx.x + 1) * kSize<DT>));
+    const uint8_t* p = (const uint8_t*)b.in + (int64_t)chunk * kChunkBytes;
+    const uint32_t mine = threadIdx.x * 16;
+    const int64_t left = b.n - (int64_t)chunk * norm_chunk_elems(DT);
+    const uint32_t whole = left >= (int64_t)chunks * norm_chunk_elems(DT) ? chunks : chunks - 1;
+    uint32_t i = 0;
+    for (; i + kTogether <= whole; i += kTogether, p += kTogether * kChunkBytes) {
+        n4 w[kTogether * kNormPieces];
+#pragma unroll
+        for (int k = 0; k < kTogether * kNormPieces; ++k) w[k] = load_piece<DT, ONCE>((p + k * kNormThreads * 16) + mine);
+#pragma unroll
+        for (int k = 0; k < kTogether * kNormPieces; ++k) {
+            float v[8];
+            widen<DT>(w[k], v);
+#pragma unroll
+            for (int j = 0; j < P; ++j) acc.add(v[j]);
         }
     }
+    for (; i < whole; ++i, p += kChunkBytes) {
+        n4 w[kNormPieces];
+#pragma unroll
+        for (int k = 0; k < kNormPieces; ++k) w[k] = load_piece<DT, ONCE>((p + k * kNormThreads * 16) + mine);
+#pragma unroll
+        for (int k = 0; k < kNormPieces; ++k) {
+            float v[8];
+            widen<DT>(w[k], v);
+#pragma unroll
+            for (int j = 0; j < P; ++j) acc.add(v[j]);
+        }
+    }
+    if (whole == chunks) return;
+    // the buffer's last chunk: pieces up to the one that its end cuts, whose elements go to a lane each
+    const uint32_t rest = (uint32_t)(left - (int64_t)whole * norm_chunk_elems(DT)), in_pieces = rest & ~(uint32_t)(P - 1);
+#pragma unroll
+    for (int k = 0; k < kNormPieces; ++k) {
+        const uint32_t e = (k * kNormThreads + threadIdx.x) * P;
+        if (e >= in_pieces) continue;
+        float v[8];
+        widen<DT>(load_piece<DT, ONCE>(p + e * kSize<DT>), v);
+#pragma unroll
+        for (int j = 0; j < P; ++j) acc.add(v[j]);
+    }
+    if (threadIdx.x < rest - in_pieces) acc.add(load_element<DT>(p + (in_pieces + threadIdx.x) * kSize<DT>));
+}
+
+template <int KIND, bool ONCE>
+__device__ __forceinline__ void norm_run(const NormBuffer* table, const uint32_t* first, const NormArgs& a) {
+    const uint32_t begin = (uint32_t)((uint64_t)a.chunks * blockIdx.x / a.blocks);
+    const uint32_t end = (uint32_t)((uint64_t)a.chunks * (blockIdx.x + 1) / a.blocks);
+    Acc<KIND> acc;
+    each_part<false>(table, first, a.K, begin, end, [&](uint32_t k, uint32_t chunk, uint32_t chunks) {
+        const NormBuffer b = table[k];
+        if (k < a.f32) norm_part<KIND, ONCE, GACT_DT_F32>(b, chunk, chunks, acc);
+        else norm_part<KIND, ONCE, GACT_DT_BF16>(b, chunk, chunks, acc);
+    });
     const double v = join_block<KIND>(acc.value());
     if (threadIdx.x == 0) a.partial[blockIdx.x] = v;
 }
-template <int KIND>
+template <int KIND, bool ONCE>
 __global__ __launch_bounds__(kNormThreads) void grad_norm_kernel(NormArgs a) {
-    norm_run<KIND>(Walk(a.table, a.first, a, false), a);
+    norm_run<KIND, ONCE>(a.table, a.first, a);
 }
-template <int KIND>
+template <int KIND, bool ONCE>
 __global__ __launch_bounds__(kNormThreads) void grad_norm_inline_kernel(NormArgs a, NormTable t) {
-    norm_run<KIND>(Walk(t.t, t.first, a, false), a);
+    norm_run<KIND, ONCE>(t.t, t.first, a);
 }
 
 // The results of all blocks, in every thread.
@@ -173,43 +211,74 @@ __global__ __launch_bounds__(kNormThreads) void norm_finish_kernel(NormArgs a) {
     if (threadIdx.x == 0) *a.norm = norm;
 }
 
-template <int DT, bool FULL>
-__device__ __forceinline__ void clip_chunk(const NormBuffer& b, int64_t chunk, double c) {
-    constexpr int P = DT == GACT_DT_F32 ? 4 : 8;
-    n4 w[kNormPieces];
-    const int64_t e0 = chunk * norm_chunk_elems(DT) + (int)threadIdx.x * P;
+// c times a piece, in binary64, so that a binary32 result is rounded once.  (A bf16 result goes by way of binary32, which
+// moves the half of a step by 2^-24 of the value.)
+template <int DT>
+__device__ __forceinline__ n4 scaled(const n4 w, double c) {
+    constexpr int P = 16 / kSize<DT>;
+    float v[8];
+    widen<DT>(w, v);
 #pragma unroll
-    for (int i = 0; i < kNormPieces; ++i) w[i] = load_piece<DT, FULL>(b.in, e0 + i * kNormThreads * P, b.n);
+    for (int j = 0; j < P; ++j) v[j] = (float)((double)v[j] * c);
+    if (DT == GACT_DT_F32)
+        return n4{__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1]), __builtin_bit_cast(uint32_t, v[2]),
+                  __builtin_bit_cast(uint32_t, v[3])};
+    return n4{bf16_pair_rne(v[0], v[1]), bf16_pair_rne(v[2], v[3]), bf16_pair_rne(v[4], v[5]), bf16_pair_rne(v[6], v[7])};
+}
+
+template <int DT>
+__device__ __forceinline__ void clip_element(const uint8_t* in, uint8_t* out, double c) {
+    const float v = (float)((double)load_element<DT>(in) * c);
+    if (DT == GACT_DT_F32) *(float*)out = v;
+    else *(uint16_t*)out = (uint16_t)bf16_pair_rne(v, 0.0f);
+}
+
+template <int DT, bool ONCE, int CHUNKS>
+__device__ __forceinline__ void clip_chunks(const uint8_t* in, uint8_t* out, uint32_t mine, double c) {
+    n4 w[CHUNKS * kNormPieces];
 #pragma unroll
-    for (int i = 0; i < kNormPieces; ++i) {
-        const int64_t e = e0 + i * kNormThreads * P;
-        float v[8];
-        widen<DT>(w[i], v);
-        // in binary64, so that a binary32 result is rounded once
+    for (int k = 0; k < CHUNKS * kNormPieces; ++k) w[k] = load_piece<DT, ONCE>((in + k * kNormThreads * 16) + mine);
 #pragma unroll
-        for (int j = 0; j < P; ++j) v[j] = (float)((double)v[j] * c);
-        n4 o;
-        if (DT == GACT_DT_F32)
-            o = n4{__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1]), __builtin_bit_cast(uint32_t, v[2]),
-                   __builtin_bit_cast(uint32_t, v[3])};
-        else
-            o = n4{bf16_pair_rne(v[0], v[1]), bf16_pair_rne(v[2], v[3]), bf16_pair_rne(v[4], v[5]), bf16_pair_rne(v[6], v[7])};
-        if (FULL || e + P <= b.n) {
-            if (DT == GACT_DT_F32) *(n4_f32*)((uint32_t*)b.out + e) = o;
-            else *(n4_bf16*)((uint16_t*)b.out + e) = o;
-        } else if (e < b.n) {
-            for (int j = 0; j < P; ++j)
-                if (e + j < b.n) {
-                    if (DT == GACT_DT_F32) ((uint32_t*)b.out)[e + j] = o[j & 3];
-                    else ((uint16_t*)b.out)[e + j] = (uint16_t)(o[j >> 1] >> (16 * (j & 1)));
-                }
+    for (int k = 0; k < CHUNKS * kNormPieces; ++k) store_piece<DT>((out + k * kNormThreads * 16) + mine, scaled<DT>(w[k], c));
+}
+
+template <int DT, bool ONCE>
+__device__ __forceinline__ void clip_part(const NormBuffer& b, uint32_t chunk, uint32_t chunks, double c) {
+    constexpr int P = 16 / kSize<DT>;
+    if (chunk == 0 && threadIdx.x < (uint32_t)b.head) {
+        const uint32_t back = (threadIdx.x + 1) * kSize<DT>;
+        clip_element<DT>((const uint8_t*)b.in - back, (uint8_t*)b.out - back, c);
+    }
+    const uint8_t* in = (const uint8_t*)b.in + (int64_t)chunk * kChunkBytes;
+    uint8_t* out = (uint8_t*)b.out + (int64_t)chunk * kChunkBytes;
+    const uint32_t mine = threadIdx.x * 16;
+    const int64_t left = b.n - (int64_t)chunk * norm_chunk_elems(DT);
+    const uint32_t whole = left >= (int64_t)chunks * norm_chunk_elems(DT) ? chunks : chunks - 1;
+    if (whole != chunks) {                           // as in norm_part
+        const int64_t o = (int64_t)whole * kChunkBytes;
+        const uint32_t rest = (uint32_t)(left - (int64_t)whole * norm_chunk_elems(DT)), in_pieces = rest & ~(uint32_t)(P - 1);
+#pragma unroll
+        for (int k = 0; k < kNormPieces; ++k) {
+            const uint32_t e = (k * kNormThreads + threadIdx.x) * P;
+            if (e < in_pieces) store_piece<DT>(out + o + e * kSize<DT>, scaled<DT>(load_piece<DT, ONCE>(in + o + e * kSize<DT>), c));
+        }
+        if (threadIdx.x < rest - in_pieces) {
+            const int64_t at = o + (in_pieces + threadIdx.x) * kSize<DT>;
+            clip_element<DT>(in + at, out + at, c);
         }
     }
+    uint32_t i = whole;
+    for (; i >= kTogether; i -= kTogether)
+        clip_chunks<DT, ONCE, kTogether>(in + (int64_t)(i - kTogether) * kChunkBytes, out + (int64_t)(i - kTogether) * kChunkBytes, mine, c);
+    for (; i > 0; --i) clip_chunks<DT, ONCE, 1>(in + (int64_t)(i - 1) * kChunkBytes, out + (int64_t)(i - 1) * kChunkBytes, mine, c);
 }
 
 // GIVEN: the norm is there; else it comes from the blocks' results, and block 0 leaves it.
+// What comes out is not wanted in a cache, where it would push out what is still to be read: 100 M bf16 elements by a
+// given norm 84 us with ordinary stores, 62; 100 M fp32 behind their norm 139, 124.  Nor is what is read a second time (fp32,
+// 100 M: 152 us with ordinary loads, 124), but by a given norm it may well be there from what has made it (78, 62).
 template <int KIND, bool GIVEN>
-__device__ __forceinline__ void clip_run(const NormBuffer* buffers, const uint32_t* firsts, const NormArgs& a) {
+__device__ __forceinline__ void clip_run(const NormBuffer* table, const uint32_t* first, const NormArgs& a) {
     double norm;
     if (GIVEN) norm = *a.norm;
     else {
@@ -218,21 +287,15 @@ __device__ __forceinline__ void clip_run(const NormBuffer* buffers, const uint32
     }
     double c = a.max_norm / (norm + 1e-6);
     c = c > 1.0 ? 1.0 : c;                           // a NaN stays
+    const uint32_t begin = (uint32_t)((uint64_t)a.chunks * blockIdx.x / a.clip_blocks);
+    const uint32_t end = (uint32_t)((uint64_t)a.chunks * (blockIdx.x + 1) / a.clip_blocks);
     // Backwards: what the norm's launch has read last may still be in a cache.
-    Walk walk(buffers, firsts, a, true);
-    for (uint32_t i = walk.end; i > walk.begin; --i) {
-        while (walk.first[walk.k] > i - 1) --walk.k;
-        const NormBuffer b = walk.table[walk.k];
-        if (c == 1.0 && b.in == b.out) continue;
-        const int64_t chunk = i - 1 - walk.first[walk.k];
-        if (walk.k < a.f32) {
-            if ((chunk + 1) * norm_chunk_elems(GACT_DT_F32) <= b.n) clip_chunk<GACT_DT_F32, true>(b, chunk, c);
-            else clip_chunk<GACT_DT_F32, false>(b, chunk, c);
-        } else {
-            if ((chunk + 1) * norm_chunk_elems(GACT_DT_BF16) <= b.n) clip_chunk<GACT_DT_BF16, true>(b, chunk, c);
-            else clip_chunk<GACT_DT_BF16, false>(b, chunk, c);
-        }
-    }
+    each_part<true>(table, first, a.K, begin, end, [&](uint32_t k, uint32_t chunk, uint32_t chunks) {
+        const NormBuffer b = table[k];
+        if (c == 1.0 && b.in == b.out) return;
+        if (k < a.f32) clip_part<GACT_DT_F32, !GIVEN>(b, chunk, chunks, c);
+        else clip_part<GACT_DT_BF16, !GIVEN>(b, chunk, chunks, c);
+    });
 }
 
 template <int KIND, bool GIVEN>
@@ -252,26 +315,28 @@ __global__ void table_piece_kernel(uint32_t* __restrict__ dst, TablePiece piece,
 }  // namespace gact
 
 namespace gact {
-template <int KIND>
+template <int KIND, bool ONCE>
 static void launch_norm(const NormTable* t, const NormArgs& a, hipStream_t s) {
-    if (t) hipLaunchKernelGGL(grad_norm_inline_kernel<KIND>, dim3(a.blocks), dim3(kNormThreads), 0, s, a, *t);
-    else hipLaunchKernelGGL(grad_norm_kernel<KIND>, dim3(a.blocks), dim3(kNormThreads), 0, s, a);
+    if (t) hipLaunchKernelGGL((grad_norm_inline_kernel<KIND, ONCE>), dim3(a.blocks), dim3(kNormThreads), 0, s, a, *t);
+    else hipLaunchKernelGGL((grad_norm_kernel<KIND, ONCE>), dim3(a.blocks), dim3(kNormThreads), 0, s, a);
 }
 template <int KIND, bool GIVEN>
 static void launch_clip(const NormTable* t, const NormArgs& a, hipStream_t s) {
-    if (t) hipLaunchKernelGGL((grad_clip_inline_kernel<KIND, GIVEN>), dim3(a.blocks), dim3(kNormThreads), 0, s, a, *t);
-    else hipLaunchKernelGGL((grad_clip_kernel<KIND, GIVEN>), dim3(a.blocks), dim3(kNormThreads), 0, s, a);
+    if (t) hipLaunchKernelGGL((grad_clip_inline_kernel<KIND, GIVEN>), dim3(a.clip_blocks), dim3(kNormThreads), 0, s, a, *t);
+    else hipLaunchKernelGGL((grad_clip_kernel<KIND, GIVEN>), dim3(a.clip_blocks), dim3(kNormThreads), 0, s, a);
 }
 }  // namespace gact
 
 // `t` where the table travels in the arguments, else null.  finish: a launch behind it adds the results up and
 // leaves the norm.
-extern "C" int gact_launch_grad_norm(const gact::NormTable* t, const gact::NormArgs* a, int kind, int finish, void* stream) {
+extern "C" int gact_launch_grad_norm(const gact::NormTable* t, const gact::NormArgs* a, int kind, int once, int finish, void* stream) {
     using namespace gact;
     hipStream_t s = (hipStream_t)stream;
     if (a->blocks != 0) {
-        if (kind == kNorm2) launch_norm<kNorm2>(t, *a, s);
-        else launch_norm<kNormInf>(t, *a, s);
+        if (kind == kNorm2 && once) launch_norm<kNorm2, true>(t, *a, s);
+        else if (kind == kNorm2) launch_norm<kNorm2, false>(t, *a, s);
+        else if (once) launch_norm<kNormInf, true>(t, *a, s);
+        else launch_norm<kNormInf, false>(t, *a, s);
         if (hipGetLastError() != hipSuccess) return -1;
     }
     if (!finish) return 0;

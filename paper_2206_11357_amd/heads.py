@@ -1,0 +1,70 @@
+"""Differentiable form of ``gact_head_norm_rotate``: RMS norms of queries and
+keys for each head with the position rotation, one launch forward, whose context
+(queries and keys before the norm) is kept compressed (arXiv 2206.11357, Sec. 3.1:
+the context Q(h) that the backward pass uses) and never written out decompressed.
+No arithmetic here: every step runs in the library's kernels."""
+from __future__ import annotations
+
+from typing import Optional, Sequence
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import (GACT_BITS_UNCOMPRESSED, gact_head_norm_rotate, gact_head_norm_rotate_backward, make_head_context)
+
+
+def _empty_by_head(x: torch.Tensor) -> torch.Tensor:
+    """Of x's shape [..., tokens, heads, head_dim], laid out head by head."""
+    shape = x.shape
+    return torch.empty(*shape[:-3], shape[-2], shape[-3], shape[-1], dtype=x.dtype, device=x.device).transpose(-3, -2)
+
+
+def _consecutive(dy: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    return dy if dy is None or dy.stride(-1) == 1 else dy.contiguous()
+
+
+class _HeadNormRotate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, wq, wk, cos, sin, positions, eps, interleaved, by_head, bits, group_size, seeds, own):
+        ctx.set_materialize_grads(False)
+        context = tuple(make_head_context(x, b, group_size if b != GACT_BITS_UNCOMPRESSED else 0, s)
+                        for x, b, s in zip((q, k), bits, seeds))
+        out = (_empty_by_head(q), _empty_by_head(k)) if by_head else None
+        yq, yk = gact_head_norm_rotate(q, k, cos, sin, wq, wk, positions, eps, interleaved, out=out, context=context)
+        # What is not compressed goes through autograd (and whatever hooks are set), or, `own`, is kept as it is.
+        raw = tuple(x.detach() if b == GACT_BITS_UNCOMPRESSED else None for x, b in zip((q, k), bits))
+        ctx.kept = tuple((x, x._version) for x in raw if x is not None) if own else ()
+        ctx.raw = raw if own else None
+        saved = (q if bits[0] == GACT_BITS_UNCOMPRESSED else None, k if bits[1] == GACT_BITS_UNCOMPRESSED else None)
+        ctx.save_for_backward(*(saved if not own else (None, None)), wq, wk, cos, sin, positions)
+        ctx.context, ctx.interleaved = context, interleaved
+        return yq, yk
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dyq, dyk):
+        q, k, wq, wk, cos, sin, positions = ctx.saved_tensors
+        for x, version in ctx.kept:
+            if x._version != version:
+                raise RuntimeError("queries or keys kept for the backward pass were modified in place")
+        need = ctx.needs_input_grad
+        grads = gact_head_norm_rotate_backward(
+            _consecutive(dyq), _consecutive(dyk), cos, sin, wq, wk, positions, context=ctx.context,
+            x=ctx.raw if ctx.raw is not None else (q, k), interleaved=ctx.interleaved, weight_grads=need[2:4])
+        return (*(g if n else None for g, n in zip(grads, need)), *(None,) * 10)
+
+
+def head_norm_rotate(q: torch.Tensor, k: torch.Tensor, cos: Optional[torch.Tensor], sin: Optional[torch.Tensor],
+                     wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None,
+                     positions: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                     by_head: bool = False, bits: Sequence[int] = (GACT_BITS_UNCOMPRESSED, GACT_BITS_UNCOMPRESSED),
+                     group_size: int = 0, seeds: Sequence[int] = (0, 0), _own: bool = False):
+    """``gact_head_norm_rotate`` with gradients for q, k, wq and wk.  by_head: the results lie head by head
+    ([..., heads, tokens, head_dim] in memory, of q's shape), as attention reads them.  bits: widths of the contexts of q
+    and k, in groups of group_size with the noise of `seeds`; GACT_BITS_UNCOMPRESSED keeps the tensor itself through
+    autograd.  ``Controller.head_norm_rotate`` chooses them from its scheme."""
+    if not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, wq, wk))):
+        out = (_empty_by_head(q), _empty_by_head(k)) if by_head else None
+        return gact_head_norm_rotate(q, k, cos, sin, wq, wk, positions, eps, interleaved, out=out)
+    return _HeadNormRotate.apply(q, k, wq, wk, cos, sin, positions, eps, interleaved, by_head, tuple(bits), group_size,
+                                 tuple(seeds), _own)

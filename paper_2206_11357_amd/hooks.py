@@ -17,15 +17,16 @@ from the ``Controller``.
 from __future__ import annotations
 
 import ctypes
-from typing import Callable, Dict, List, Optional, Sequence
+from typing import Callable, Dict, Iterable, List, Optional, Sequence
 
 import numpy as np
 import torch
 from torch.multiprocessing.reductions import StorageWeakRef
 
 from . import (GACT_BITS_UNCOMPRESSED, GACT_OK, GactError, TensorDesc, dtype_code, gact_allocate_bits_levels,
-               gact_copy_bounded,
+               gact_copy_bounded, gact_grad_clip, gact_grad_norm_workspace_bytes, head_context_fits,
                gact_multi_workspace_bytes, gact_num_groups, gact_packed_bytes, gact_sensitivity, lib)
+from .heads import head_norm_rotate
 
 _MASK64 = (1 << 64) - 1
 _MAX_BATCH = 64            # a launch table of at most 64 tensors travels in the kernel arguments
@@ -50,6 +51,14 @@ def _side_streams():
     if dev not in _SIDE_STREAMS:
         _SIDE_STREAMS[dev] = (torch.cuda.Stream(), torch.cuda.Stream())
     return _SIDE_STREAMS[dev]
+
+
+def clip_grad_norm_(params: Iterable[torch.Tensor], max_norm: float, norm_type: float = 2.0,
+                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Scales the parameters' gradients in place so that their norm together, 2 or inf, is at most max_norm; returns the
+    norm before, a device float64 scalar (``gact_grad_clip``: nothing waits for it)."""
+    grads = [p.grad.detach() for p in dict.fromkeys(params) if p.grad is not None]
+    return gact_grad_clip(grads, max_norm, norm_type, workspace=workspace).view(())
 
 
 class _Packed:
@@ -172,6 +181,7 @@ class Controller:
         self._out_inflight: List[_Batch] = []     # swap mode: swap-out enqueued, device copy still held
         self._descs = (TensorDesc * _MAX_BATCH)()
         self._ws: Optional[torch.Tensor] = None
+        self._norm_ws: Optional[torch.Tensor] = None
         # swap-out and swap-in each on a stream of their own (Sec. 5.3), both at default priority
         self._out_stream, self._in_stream = _side_streams() if swap else (None, None)
         # pinned host memory for the swapped batches: one arena, handed out front to back within
@@ -280,6 +290,40 @@ class Controller:
     def hooks(self):
         """Context manager: ``with controller.hooks(): loss = model(x)``."""
         return torch.autograd.graph.saved_tensors_hooks(self.pack, self.unpack)
+
+    # ----------------------------------------------- operators of its own
+    def head_norm_rotate(self, q: torch.Tensor, k: torch.Tensor, cos, sin, wq=None, wk=None, positions=None,
+                         eps: float = 1e-6, interleaved: bool = False, by_head: bool = False):
+        """``heads.head_norm_rotate`` whose context is part of the scheme: q and k before the norm are context tensors l
+        like those of the hooks, with widths b_l, seeds r_l and a place in Alg. 1 and Eq. (ilp), but compressed by the
+        forward kernel itself and read by the backward kernel as codes.  Their buffers stay on the device (they are
+        not swapped).  Heads that the controller's group size does not fit (``head_context_fits``), and tensors that the
+        hooks would not compress, are left to autograd, with or without hooks."""
+        bits, seeds, own = [GACT_BITS_UNCOMPRESSED] * 2, [0, 0], []
+        for j, x in enumerate((q, k)):
+            if (torch.is_grad_enabled() and x.is_cuda and x.requires_grad and x.numel() >= self.min_numel
+                    and x.dtype in (torch.float32, torch.bfloat16)
+                    and head_context_fits(self.group_size, x.shape[-1], x.shape[-2])):
+                own.append(j)
+        if len(own) < 2:                             # one launch with one kind of context, or none
+            return head_norm_rotate(q, k, cos, sin, wq, wk, positions, eps, interleaved, by_head)
+        for j in own:
+            index = len(self._handles)
+            self._handles.append(None)
+            self.numel.append((q, k)[j].numel())
+            bits[j], seeds[j] = self.bits_of(index), self.seed_of(index)
+        return head_norm_rotate(q, k, cos, sin, wq, wk, positions, eps, interleaved, by_head, bits, self.group_size, seeds,
+                                _own=True)
+
+    def clip_grad_norm_(self, params: Iterable[torch.Tensor], max_norm: float, norm_type: float = 2.0) -> torch.Tensor:
+        """``clip_grad_norm_`` with a workspace that the controller keeps.  (The compressor's noise adds V(b) of Thm. 2 to
+        the gradient's variance, and with it to the norm.)"""
+        params = list(dict.fromkeys(params))
+        need = gact_grad_norm_workspace_bytes(len(params))
+        device = next((p.grad.device for p in params if p.grad is not None), None)
+        if device is not None and (self._norm_ws is None or self._norm_ws.numel() < need or self._norm_ws.device != device):
+            self._norm_ws = torch.empty(need, dtype=torch.uint8, device=device)
+        return clip_grad_norm_(params, max_norm, norm_type, self._norm_ws if device is not None else None)
 
     # ------------------------------------------------------------ compression
     def _workspace(self, device) -> torch.Tensor:

@@ -345,7 +345,8 @@ int gact_grad_clip_by(const gact_grad_buf *h_bufs, int K, double max_norm, const
  * for the rot_dim / 2 pairs (a, b) of its first rot_dim elements, (i, i + rot_dim/2) or, `interleaved`,
  * (2i, 2i + 1); y = n from rot_dim on.  Backward, with dn = dy rotated back,
  *     dx = r * (dn * w - x * r^2 * mean(dn * w * x)),   dw = sum over heads and tokens of dn * x * r.
- * Arithmetic in binary32, dw's sums over blocks in binary64 and in a fixed order; outputs rounded once.
+ * Arithmetic in binary32 (the squares of x are added in it: |x| < 2^59), dw's sums over blocks in binary64 and in a fixed
+ * order; outputs rounded once.  A head's values reach no other head's.
  *
  * Context.  With bits in {1, 2, 4, 8} the forward pass writes what gact_compress gives for x laid out
  * contiguously as [batch, tokens, heads, head_dim] with the same group_size, bits and seed, byte for byte, and the backward

@@ -8,8 +8,8 @@ shared library cannot be loaded the import fails.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 import math
 import os
 import struct
@@ -552,6 +552,7 @@ def _dense(t: torch.Tensor) -> bool:
             or (t.dim() == 5 and t.is_contiguous(memory_format=torch.channels_last_3d)))
 
 
+@functools.lru_cache(maxsize=64)
 def gact_grad_norm_workspace_bytes(K: int) -> int:
     return int(lib.gact_grad_norm_workspace_bytes(K))
 
@@ -597,6 +598,8 @@ def _norm_call(g, outs, norm, workspace, stream, bufs):
     K = len(g)
     if len(arr) < K:
         raise ValueError("bufs lists fewer buffers than g")
+    if bufs is not None and K and (arr[0].g != g[0].data_ptr() or (outs is not None and arr[0].out != outs[0].data_ptr())):
+        raise ValueError("bufs was made for other buffers")
     device = g[0].get_device() if K else _current_device()
     if norm is None or workspace is None:
         if stream is None:
@@ -658,7 +661,7 @@ class HeadContext:
             meta = (self.groups + 3 >> 2) * 16
         self.off = (0, packed, packed + meta, packed + 2 * meta)           # of packed, gmin, gscale, rstd
         rows = n // x.shape[-1] if n else 0
-        self.blob = torch.empty(packed + 2 * meta + 4 * rows, dtype=torch.uint8, device=x.device)
+        self.blob = x.new_empty(packed + 2 * meta + 4 * rows, dtype=torch.uint8)
 
     @property
     def packed(self) -> torch.Tensor:
@@ -708,6 +711,7 @@ def head_context_fits(group_size: int, head_dim: int, *heads: int) -> bool:
     return fits and all(h * head_dim % group_size == 0 for h in heads)
 
 
+@functools.lru_cache(maxsize=64)
 def gact_head_norm_rotate_workspace_bytes(head_dim: int) -> int:
     return int(lib.gact_head_norm_rotate_workspace_bytes(head_dim))
 
@@ -810,15 +814,18 @@ def _forward_record(q, k, cos, sin, wq, wk, positions, eps, interleaved, out, co
     for x, y, w, c in triples:
         if y is not x:
             _check_like(y, x)
-        rstd, packed, gmin, gscale = c.addresses() if c is not None else (0, 0, 0, 0)
-        parts += _HEADS.pack(x.data_ptr(), y.data_ptr(), 0, 0, 0 if w is None else w.data_ptr(), 0, rstd, packed, gmin, gscale,
-                             *_head_strides(x), *_head_strides(y), *_NO_STRIDES, *_NO_STRIDES, 0 if c is None else c.seed,
-                             x.shape[-2], GACT_BITS_UNCOMPRESSED if c is None else c.bits)
+        w = 0 if w is None else w.data_ptr()
+        if c is None:
+            parts += _HEADS.pack(x.data_ptr(), y.data_ptr(), 0, 0, w, 0, 0, 0, 0, 0, *_head_strides(x), *_head_strides(y),
+                                 0, 0, 0, 0, 0, 0, 0, x.shape[-2], GACT_BITS_UNCOMPRESSED)
+        else:
+            parts += _HEADS.pack(x.data_ptr(), y.data_ptr(), 0, 0, w, 0, *c.addresses(), *_head_strides(x), *_head_strides(y),
+                                 0, 0, 0, 0, 0, 0, c.seed, x.shape[-2], c.bits)
     return device, parts, len(triples), rotation
 
 
-def _empty_heads(*like) -> tuple:
-    return tuple(None if x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in like)
+def _empty_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor]) -> tuple:
+    return None if q is None else q.new_empty(q.shape), None if k is None else k.new_empty(k.shape)
 
 
 def gact_head_norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], cos: Optional[torch.Tensor],
@@ -857,41 +864,56 @@ def gact_head_norm_rotate_backward(dyq: Optional[torch.Tensor], dyk: Optional[to
     """Gradients of gact_head_norm_rotate from dyq, dyk (any strides but the last) and the contexts it has filled; x =
     (q, k) where these are not compressed.  Returns (dq, dk, dwq, dwk); None for a part without dy, without weights or
     whose weight gradient is not wanted."""
-    dys, ws, xs = (dyq, dyk), (wq, wk), x if x is not None else _NO_CONTEXT
-    live = tuple(i for i in (0, 1) if dys[i] is not None)
-    if not live:
+    xq, xk = x if x is not None else _NO_CONTEXT
+    device = _same_device(dyq, dyk, cos, sin, wq, wk, positions, xq, xk, workspace)
+    oq, ok = out if out is not None else _NO_CONTEXT
+    todo = []                            # (dy, x, w, context, output, whether the weights' gradient is wanted) of each part
+    if dyq is not None:
+        todo.append((dyq, xq, wq, context[0], oq, wq is not None and weight_grads[0]))
+    if dyk is not None:
+        todo.append((dyk, xk, wk, context[1], ok, wk is not None and weight_grads[1]))
+        if dyq is not None:
+            _check_pair(dyq, dyk)
+    if not todo:
         return None, None, None, None
-    if len(live) == 2:
-        _check_pair(dyq, dyk)
-    device = _same_device(dyq, dyk, cos, sin, wq, wk, positions, xs[0], xs[1], workspace)
-    first = dys[live[0]]
+    first = todo[0][0]
     D = first.shape[-1]
-    w_dtype = _weights_dtype([ws[i] for i in live], D)
+    w_dtype = _weights_dtype([t[2] for t in todo], D)
     rotation = _rotation(first, cos, sin, positions, interleaved, w_dtype,
-                         _contexts_group([context[i] for i in live], [dys[i] for i in live]), 0.0)
-    with _allocating_for(stream, device) if stream is not None else contextlib.nullcontext():
-        dxs = list(_empty_heads(dyq, dyk)) if out is None else [out[0], out[1]]
-        dws = [None, None]
-        for i in live:
-            if ws[i] is not None and weight_grads[i]:
-                dws[i] = torch.empty(ws[i].shape, dtype=w_dtype, device=first.device)
-        if workspace is None and (dws[0] is not None or dws[1] is not None):
-            workspace = torch.empty(gact_head_norm_rotate_workspace_bytes(D), dtype=torch.uint8, device=first.device)
+                         _contexts_group([t[3] for t in todo], [t[0] for t in todo]), 0.0)
+    if stream is None:
+        made, workspace = _backward_buffers(todo, workspace, D)
+    else:
+        with _allocating_for(stream, device):
+            made, workspace = _backward_buffers(todo, workspace, D)
     if out is not None:
-        _same_device(first, *dxs)
+        _same_device(first, oq, ok)
     parts = b""
-    for i in live:
-        dy, dx, w, dw, c, xi = dys[i], dxs[i], ws[i], dws[i], context[i], xs[i]
+    for (dy, xi, w, c, _, _), (dx, dw) in zip(todo, made):
         _check_like(dx, dy)
-        a_x, x_strides = 0, _NO_STRIDES
+        a_x = 0
+        x_strides = _NO_STRIDES
         if c.bits == GACT_BITS_UNCOMPRESSED:
             if xi is None:
                 raise ValueError("the context is not compressed: x is needed")
             _check_like(xi, dy)
             a_x, x_strides = xi.data_ptr(), _head_strides(xi)
         parts += _HEADS.pack(a_x, 0, dy.data_ptr(), dx.data_ptr(), 0 if w is None else w.data_ptr(),
-                             0 if dw is None else dw.data_ptr(), *c.addresses(), *x_strides, *_NO_STRIDES, *_head_strides(dy),
+                             0 if dw is None else dw.data_ptr(), *c.addresses(), *x_strides, 0, 0, 0, *_head_strides(dy),
                              *_head_strides(dx), c.seed, dy.shape[-2], c.bits)
-    _enqueue(lib.gact_head_norm_rotate_backward, "gact_head_norm_rotate_backward", device, stream, parts, len(live), rotation,
-             None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes)
-    return dxs[0], dxs[1], dws[0], dws[1]
+    _enqueue(lib.gact_head_norm_rotate_backward, "gact_head_norm_rotate_backward", device, stream, parts, len(todo), rotation,
+             *(workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0))
+    if len(made) == 2:
+        return made[0][0], made[1][0], made[0][1], made[1][1]
+    return (made[0][0], None, made[0][1], None) if dyq is not None else (None, made[0][0], None, made[0][1])
+
+
+def _backward_buffers(todo, workspace, D: int):
+    """(dx, dw) of each part, and the workspace where there is a dw."""
+    made, any_dw = [], False
+    for dy, _, w, _, dx, want in todo:
+        any_dw = any_dw or want
+        made.append((dx if dx is not None else dy.new_empty(dy.shape), w.new_empty(w.shape) if want else None))
+    if any_dw and workspace is None:
+        workspace = todo[0][0].new_empty(gact_head_norm_rotate_workspace_bytes(D), dtype=torch.uint8)
+    return made, workspace

@@ -7,6 +7,7 @@
 #include <chrono>
 #include <cmath>
 #include <cstring>
+#include <exception>
 #include <mutex>
 #include <queue>
 #include <algorithm>
@@ -509,6 +510,16 @@ int run_norm(const gact_grad_buf* bufs, int K, int kind, bool scale, bool given,
     return GACT_OK;
 }
 
+// No exception leaves a C entry: a list that the host has no room for is an argument that is too large.
+int norm_call(const gact_grad_buf* bufs, int K, int kind, bool scale, bool given, double max_norm, const double* d_norm,
+              void* d_workspace, size_t workspace_bytes, void* stream) {
+    try {
+        return run_norm(bufs, K, kind, scale, given, max_norm, d_norm, d_workspace, workspace_bytes, stream);
+    } catch (const std::exception&) {
+        return GACT_E_ARG;
+    }
+}
+
 // -------------------------------------------------- norms of heads and rotation
 int log2_up(int v) {
     int s = 0;
@@ -795,17 +806,17 @@ size_t gact_grad_norm_workspace_bytes(int K) { return K < 0 ? 0 : kNormPartials 
 
 int gact_grad_norm(const gact_grad_buf* h_bufs, int K, int kind, double* d_norm, void* d_workspace, size_t workspace_bytes,
                    void* stream) {
-    return run_norm(h_bufs, K, kind, false, false, 0.0, d_norm, d_workspace, workspace_bytes, stream);
+    return norm_call(h_bufs, K, kind, false, false, 0.0, d_norm, d_workspace, workspace_bytes, stream);
 }
 
 int gact_grad_clip(const gact_grad_buf* h_bufs, int K, int kind, double max_norm, double* d_norm, void* d_workspace,
                    size_t workspace_bytes, void* stream) {
-    return run_norm(h_bufs, K, kind, true, false, max_norm, d_norm, d_workspace, workspace_bytes, stream);
+    return norm_call(h_bufs, K, kind, true, false, max_norm, d_norm, d_workspace, workspace_bytes, stream);
 }
 
 int gact_grad_clip_by(const gact_grad_buf* h_bufs, int K, double max_norm, const double* d_norm, void* d_workspace,
                       size_t workspace_bytes, void* stream) {
-    return run_norm(h_bufs, K, GACT_NORM_2, true, true, max_norm, d_norm, d_workspace, workspace_bytes, stream);
+    return norm_call(h_bufs, K, GACT_NORM_2, true, true, max_norm, d_norm, d_workspace, workspace_bytes, stream);
 }
 
 // ---------------------------------------------- norms of heads and rotation

@@ -166,3 +166,31 @@ def test_streams_and_repeated_calls(gact):
     assert torch.equal(a, want) and torch.equal(b, want)
     for _ in range(3):
         assert torch.equal(gact.gact_grad_norm(g), want)
+
+
+def test_a_buffer_of_more_than_2_31_elements(gact):
+    n = 2 ** 31 + 12345
+    area = torch.ones(n + 1, dtype=torch.bfloat16, device="cuda")
+    g = [area[1:], torch.ones(5, device="cuda")]
+    area[-1] = 3.0
+    norm = gact.gact_grad_clip(g, 0.5 * math.sqrt(n + 13), 2.0)
+    assert abs(float(norm) - math.sqrt(n + 13)) <= 1e-11 * math.sqrt(n)
+    c = 0.5 * math.sqrt(n + 13) / (math.sqrt(n + 13) + 1e-6)
+    want = torch.tensor(c).to(torch.bfloat16)
+    assert area[0] == 1.0 and (area[1:-1] == want).all() and area[-1] == torch.tensor(3 * c).to(torch.bfloat16)
+    assert float(gact.gact_grad_norm(g, math.inf)) == float(area[-1])
+
+
+def test_bufs_of_other_gradients_are_noticed(gact):
+    g = grads((100, 200), ("f32",), 7)
+    bufs = gact.make_grad_bufs(g)
+    with pytest.raises(ValueError):
+        gact.gact_grad_norm([t.clone() for t in g], bufs=bufs)
+    with pytest.raises(ValueError):
+        gact.gact_grad_clip(g, 1.0, outs=[torch.empty_like(t) for t in g], bufs=bufs)
+    with pytest.raises(ValueError):
+        gact.gact_grad_norm(g + g, bufs=bufs)
+    with pytest.raises(gact.GactError):
+        gact.gact_grad_clip([g[0], g[0]], 1.0)                                   # the same buffer twice
+    twice, once = float(gact.gact_grad_norm([g[0], g[0]])), float(gact.gact_grad_norm([g[0]]))
+    assert abs(twice - math.sqrt(2) * once) <= 1e-11 * twice                     # counted as often as it is listed

@@ -357,3 +357,34 @@ def test_nothing_is_written_outside_the_outputs(gact):
         assert torch.equal(o, w)
         o.fill_(7.0)
         assert (a == 7.0).all()
+
+
+@pytest.mark.parametrize("D,Hq,Hk", [(64, 8, 8), (80, 3, 1)])
+def test_offsets_beyond_32_bits(gact, D, Hq, Hk):
+    """Tokens so far apart that the last ones lie 6 GB behind the first, in the wavefront's addresses and in the lanes' own;
+    heads too far apart for 32-bit offsets in a lane."""
+    S = 24
+    far = 134_217_728 + 8                              # elements between tokens: S of them reach 6.4 GB
+    area = torch.empty(S * far, dtype=torch.bfloat16, device="cuda")
+    q = area.as_strided((1, S, Hq, D), (0, far, D, 1))
+    k = area.as_strided((1, S, Hk, D), (0, far, D, 1), Hq * D)
+    q.copy_(randn(1, *q.shape)), k.copy_(randn(2, *k.shape))
+    out = tuple(area.as_strided(x.shape, x.stride(), o) for x, o in ((q, 4096), (k, 8192)))
+    cos, sin = tables(S, 64)
+    w = randn(3, D) * 0.1 + 1
+    args = (cos, sin, w, w)
+    ctx, near_ctx = ([gact.make_head_context(x) for x in (q, k)] for _ in range(2))
+    gact.gact_head_norm_rotate(q, k, *args, out=out, context=ctx)
+    near = gact.gact_head_norm_rotate(q.contiguous(), k.contiguous(), *args, context=near_ctx)
+    assert all(torch.equal(a, b) for a, b in zip(out, near))
+    dy = tuple(randn(4 + j, *x.shape, dtype=x.dtype) for j, x in enumerate((q, k)))
+    want = gact.gact_head_norm_rotate_backward(*dy, *args, context=near_ctx, x=(q.contiguous(), k.contiguous()))
+    for a, b in zip(out, dy):
+        a.copy_(b)
+    got = gact.gact_head_norm_rotate_backward(*out, *args, context=ctx, x=(q, k), out=out)        # dx in place of dy
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    # heads of one token 400 M elements apart
+    wide = area.as_strided((1, 2, 8, D), (0, 4096, 400_000_008, 1))
+    wide.copy_(randn(7, *wide.shape))
+    y, _ = gact.gact_head_norm_rotate(wide, None, *args)
+    assert torch.equal(y, gact.gact_head_norm_rotate(wide.contiguous(), None, *args)[0])

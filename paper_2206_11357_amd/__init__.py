@@ -649,10 +649,11 @@ class HeadContext:
     """What the forward pass keeps of one tensor (queries or keys) for its gradient, in one buffer: rstd, float32 of x's
     shape without head_dim, and, where bits is not GACT_BITS_UNCOMPRESSED, packed, gmin and gscale as gact_compress
     lays them out."""
-    __slots__ = ("bits", "group_size", "seed", "shape", "blob", "groups", "off")
+    __slots__ = ("bits", "group_size", "seed", "shape", "device", "blob", "groups", "off")
 
     def __init__(self, x: torch.Tensor, bits: int, group_size: int, seed: int):
-        self.bits, self.group_size, self.seed, self.shape = bits, group_size, seed & (2**64 - 1), x.shape
+        self.bits, self.group_size, self.seed, self.device = bits, group_size, seed & (2**64 - 1), x.get_device()
+        self.shape = shape = x.shape
         n = x.numel()
         packed = self.groups = meta = 0
         if bits != GACT_BITS_UNCOMPRESSED:
@@ -660,7 +661,7 @@ class HeadContext:
             self.groups = -(-n // group_size) if group_size > 0 else 0
             meta = (self.groups + 3 >> 2) * 16
         self.off = (0, packed, packed + meta, packed + 2 * meta)           # of packed, gmin, gscale, rstd
-        rows = n // x.shape[-1] if n else 0
+        rows = n // shape[-1] if n else 0
         self.blob = x.new_empty(packed + 2 * meta + 4 * rows, dtype=torch.uint8)
 
     @property
@@ -683,12 +684,15 @@ class HeadContext:
         return self.blob[self.off[3]:].view(torch.float32).view(self.shape[:-1])
 
     def addresses(self):
-        """Of rstd, packed, gmin, gscale."""
+        """Addresses of rstd, packed, gmin, gscale; seed; bits."""
         a = self.blob.data_ptr()
         if self.bits == GACT_BITS_UNCOMPRESSED:
-            return a, 0, 0, 0
+            return a, 0, 0, 0, 0, GACT_BITS_UNCOMPRESSED
         off = self.off
-        return a + off[3], a, a + off[1], a + off[2]
+        return a + off[3], a, a + off[1], a + off[2], self.seed, self.bits
+
+
+_NO_CONTEXT = (0, 0, 0, 0, 0, GACT_BITS_UNCOMPRESSED)
 
 
 def make_head_context(x: torch.Tensor, bits: int = GACT_BITS_UNCOMPRESSED, group_size: int = 0, seed: int = 0,
@@ -733,18 +737,26 @@ def _head_strides(x: torch.Tensor) -> tuple:
     return a, b, c
 
 
-def _rotation(x: torch.Tensor, cos, sin, positions, interleaved, w_dtype, group_size: int, eps: float) -> bytes:
-    """gact_rotation of queries and keys, from one of them."""
+def _head_shape(x: torch.Tensor) -> tuple:
+    """(batch, tokens, heads, head_dim)"""
     shape = x.shape
-    B = shape[0] if len(shape) == 4 else 1
-    S, D = shape[-3], shape[-1]
+    if len(shape) == 4:
+        return shape
+    if len(shape) == 3:
+        return (1, *shape)
+    raise ValueError("gact needs [batch, tokens, heads, head_dim] or [tokens, heads, head_dim]")
+
+
+def _rotation(B: int, S: int, D: int, dtype, cos, sin, positions, interleaved, w_dtype, group_size: int, eps: float) -> bytes:
+    """gact_rotation of queries and keys."""
     a_cos = a_sin = a_pos = n_positions = rot = 0
     if cos is not None and sin is not None:
-        n_positions, half = cos.shape
-        if cos.shape != sin.shape or cos.dtype is not torch.float32 or sin.dtype is not torch.float32 \
+        shape = cos.shape
+        if len(shape) != 2 or sin.shape != shape or cos.dtype is not torch.float32 or sin.dtype is not torch.float32 \
                 or not cos.is_contiguous() or not sin.is_contiguous():
             raise ValueError("cos and sin must be contiguous float32 tables [positions, rot_dim / 2]")
-        rot, a_cos, a_sin = 2 * half, cos.data_ptr(), sin.data_ptr()
+        n_positions = shape[0]
+        rot, a_cos, a_sin = 2 * shape[1], cos.data_ptr(), sin.data_ptr()
         if positions is not None:
             if positions.dtype is not torch.int64 or positions.numel() != B * S or not positions.is_contiguous():
                 raise ValueError("positions must be contiguous int64, one per token")
@@ -753,20 +765,21 @@ def _rotation(x: torch.Tensor, cos, sin, positions, interleaved, w_dtype, group_
             raise ValueError("the tables hold fewer positions than a sequence has tokens")
     elif cos is not None or sin is not None:
         raise ValueError("cos and sin belong together")
-    return _ROTATION.pack(B, S, a_cos, a_sin, a_pos, n_positions, D, rot, 1 if interleaved else 0, dtype_code(x.dtype),
+    return _ROTATION.pack(B, S, a_cos, a_sin, a_pos, n_positions, D, rot, 1 if interleaved else 0, dtype_code(dtype),
                           GACT_F32 if w_dtype is None else dtype_code(w_dtype), group_size, eps, 0)
 
 
-def _weights_dtype(weights, D: int):
+def _weights_dtype(wq, wk, D: int):
     """The one type of those that are given; None if none is."""
     dtype = None
-    for w in weights:
+    for w in (wq, wk):
         if w is not None:
             if w.numel() != D or not w.is_contiguous():
                 raise ValueError("the weights must be contiguous, one per element of a head")
-            if dtype is not None and w.dtype is not dtype:
+            if dtype is None:
+                dtype = w.dtype
+            elif w.dtype is not dtype:
                 raise ValueError("the weights must have one type")
-            dtype = w.dtype
     return dtype
 
 
@@ -775,53 +788,49 @@ def _check_like(y: torch.Tensor, x: torch.Tensor) -> None:
         raise ValueError("shape or dtype differ: %s %s, %s %s" % (tuple(y.shape), y.dtype, tuple(x.shape), x.dtype))
 
 
-def _check_pair(q: torch.Tensor, k: torch.Tensor) -> None:
-    a, b = q.shape, k.shape
-    if len(a) != len(b) or a[:-2] != b[:-2] or a[-1] != b[-1] or q.dtype is not k.dtype:
-        raise ValueError("queries and keys differ in batch, tokens, head_dim or dtype")
+def _check_context(c: HeadContext, x: torch.Tensor, device: int, group_size: int) -> int:
+    """The group size of the contexts looked at so far, and this one; 0 while none is compressed."""
+    if c.shape != x.shape or c.device != device:
+        raise ValueError("the context was made for another shape or device")
+    if c.bits == GACT_BITS_UNCOMPRESSED:
+        return group_size
+    if group_size and c.group_size != group_size:
+        raise ValueError("the contexts of a call must have one group size")
+    return c.group_size
 
 
-def _contexts_group(context, xs) -> int:
-    """The one group size of the compressed contexts; 0 if none is."""
-    G = 0
-    for c, x in zip(context, xs):
-        if c is not None:
-            if c.shape != x.shape or c.blob.get_device() != x.get_device():
-                raise ValueError("the context was made for another shape or device")
-            if c.bits != GACT_BITS_UNCOMPRESSED:
-                if G and c.group_size != G:
-                    raise ValueError("the contexts of a call must have one group size")
-                G = c.group_size
-    return G
-
-
-_NO_CONTEXT = (None, None)
+_NONE = (None, None)
 
 
 def _forward_record(q, k, cos, sin, wq, wk, positions, eps, interleaved, out, context):
     """(device, parts, number of parts, rotation) of a forward call into `out`."""
-    context = context if context is not None else _NO_CONTEXT
+    yq, yk = out
+    cq, ck = context if context is not None else _NONE
+    B, S, H, D = _head_shape(q)
+    dtype, G = q.dtype, 0
     if k is None:
-        device = _same_device(q, out[0], wq, cos, sin, positions)
-        w_dtype, triples = _weights_dtype((wq,), q.shape[-1]), ((q, out[0], wq, context[0]),)
-    else:
-        _check_pair(q, k)
-        device = _same_device(q, k, out[0], out[1], wq, wk, cos, sin, positions)
-        w_dtype = _weights_dtype((wq, wk), q.shape[-1])
-        triples = ((q, out[0], wq, context[0]), (k, out[1], wk, context[1]))
-    rotation = _rotation(q, cos, sin, positions, interleaved, w_dtype, _contexts_group(context, (q, k)), eps)
-    parts = b""
-    for x, y, w, c in triples:
-        if y is not x:
-            _check_like(y, x)
-        w = 0 if w is None else w.data_ptr()
-        if c is None:
-            parts += _HEADS.pack(x.data_ptr(), y.data_ptr(), 0, 0, w, 0, 0, 0, 0, 0, *_head_strides(x), *_head_strides(y),
-                                 0, 0, 0, 0, 0, 0, 0, x.shape[-2], GACT_BITS_UNCOMPRESSED)
-        else:
-            parts += _HEADS.pack(x.data_ptr(), y.data_ptr(), 0, 0, w, 0, *c.addresses(), *_head_strides(x), *_head_strides(y),
-                                 0, 0, 0, 0, 0, 0, c.seed, x.shape[-2], c.bits)
-    return device, parts, len(triples), rotation
+        yk = wk = ck = None
+    device = _same_device(q, k, yq, yk, wq, wk, cos, sin, positions)
+    w_dtype = _weights_dtype(wq, wk, D)
+    if yq is not q:
+        _check_like(yq, q)
+    a_q = _NO_CONTEXT
+    if cq is not None:
+        G, a_q = _check_context(cq, q, device, G), cq.addresses()
+    parts = _HEADS.pack(q.data_ptr(), yq.data_ptr(), 0, 0, 0 if wq is None else wq.data_ptr(), 0, *a_q[:4], *_head_strides(q),
+                        *_head_strides(yq), 0, 0, 0, 0, 0, 0, a_q[4], H, a_q[5])
+    if k is not None:
+        Bk, Sk, Hk, Dk = _head_shape(k)
+        if Bk != B or Sk != S or Dk != D or k.dtype is not dtype:
+            raise ValueError("queries and keys differ in batch, tokens, head_dim or dtype")
+        if yk is not k:
+            _check_like(yk, k)
+        a_k = _NO_CONTEXT
+        if ck is not None:
+            G, a_k = _check_context(ck, k, device, G), ck.addresses()
+        parts += _HEADS.pack(k.data_ptr(), yk.data_ptr(), 0, 0, 0 if wk is None else wk.data_ptr(), 0, *a_k[:4], *_head_strides(k),
+                             *_head_strides(yk), 0, 0, 0, 0, 0, 0, a_k[4], Hk, a_k[5])
+    return device, parts, 1 if k is None else 2, _rotation(B, S, D, dtype, cos, sin, positions, interleaved, w_dtype, G, eps)
 
 
 def _empty_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor]) -> tuple:
@@ -864,56 +873,79 @@ def gact_head_norm_rotate_backward(dyq: Optional[torch.Tensor], dyk: Optional[to
     """Gradients of gact_head_norm_rotate from dyq, dyk (any strides but the last) and the contexts it has filled; x =
     (q, k) where these are not compressed.  Returns (dq, dk, dwq, dwk); None for a part without dy, without weights or
     whose weight gradient is not wanted."""
-    xq, xk = x if x is not None else _NO_CONTEXT
+    if dyq is None or dyk is None:
+        return _backward_of_one(dyq, dyk, cos, sin, wq, wk, positions, context, x, interleaved, out, weight_grads, workspace, stream)
+    xq, xk = x if x is not None else _NONE
     device = _same_device(dyq, dyk, cos, sin, wq, wk, positions, xq, xk, workspace)
-    oq, ok = out if out is not None else _NO_CONTEXT
-    todo = []                            # (dy, x, w, context, output, whether the weights' gradient is wanted) of each part
-    if dyq is not None:
-        todo.append((dyq, xq, wq, context[0], oq, wq is not None and weight_grads[0]))
-    if dyk is not None:
-        todo.append((dyk, xk, wk, context[1], ok, wk is not None and weight_grads[1]))
-        if dyq is not None:
-            _check_pair(dyq, dyk)
-    if not todo:
-        return None, None, None, None
-    first = todo[0][0]
-    D = first.shape[-1]
-    w_dtype = _weights_dtype([t[2] for t in todo], D)
-    rotation = _rotation(first, cos, sin, positions, interleaved, w_dtype,
-                         _contexts_group([t[3] for t in todo], [t[0] for t in todo]), 0.0)
+    B, S, H, D = _head_shape(dyq)
+    Bk, Sk, Hk, Dk = _head_shape(dyk)
+    dtype = dyq.dtype
+    if Bk != B or Sk != S or Dk != D or dyk.dtype is not dtype:
+        raise ValueError("queries and keys differ in batch, tokens, head_dim or dtype")
+    w_dtype = _weights_dtype(wq, wk, D)
+    want = (wq is not None and weight_grads[0], wk is not None and weight_grads[1])
     if stream is None:
-        made, workspace = _backward_buffers(todo, workspace, D)
+        dq, dk, dwq, dwk, workspace = _backward_buffers(dyq, dyk, wq, wk, want, out, workspace, D)
     else:
         with _allocating_for(stream, device):
-            made, workspace = _backward_buffers(todo, workspace, D)
+            dq, dk, dwq, dwk, workspace = _backward_buffers(dyq, dyk, wq, wk, want, out, workspace, D)
     if out is not None:
-        _same_device(first, oq, ok)
-    parts = b""
-    for (dy, xi, w, c, _, _), (dx, dw) in zip(todo, made):
-        _check_like(dx, dy)
-        a_x = 0
-        x_strides = _NO_STRIDES
-        if c.bits == GACT_BITS_UNCOMPRESSED:
-            if xi is None:
-                raise ValueError("the context is not compressed: x is needed")
-            _check_like(xi, dy)
-            a_x, x_strides = xi.data_ptr(), _head_strides(xi)
-        parts += _HEADS.pack(a_x, 0, dy.data_ptr(), dx.data_ptr(), 0 if w is None else w.data_ptr(),
-                             0 if dw is None else dw.data_ptr(), *c.addresses(), *x_strides, 0, 0, 0, *_head_strides(dy),
-                             *_head_strides(dx), c.seed, dy.shape[-2], c.bits)
-    _enqueue(lib.gact_head_norm_rotate_backward, "gact_head_norm_rotate_backward", device, stream, parts, len(todo), rotation,
+        _same_device(dyq, dq, dk)
+        _check_like(dq, dyq)
+        _check_like(dk, dyk)
+    G = _check_context(context[1], dyk, device, _check_context(context[0], dyq, device, 0))
+    parts = _backward_part(dyq, xq, dq, wq, dwq, context[0], H) + _backward_part(dyk, xk, dk, wk, dwk, context[1], Hk)
+    rotation = _rotation(B, S, D, dtype, cos, sin, positions, interleaved, w_dtype, G, 0.0)
+    if workspace is None:
+        _enqueue(lib.gact_head_norm_rotate_backward, "gact_head_norm_rotate_backward", device, stream, parts, 2, rotation, None, 0)
+    else:
+        _enqueue(lib.gact_head_norm_rotate_backward, "gact_head_norm_rotate_backward", device, stream, parts, 2, rotation,
+                 workspace.data_ptr(), workspace.nbytes)
+    return dq, dk, dwq, dwk
+
+
+def _backward_of_one(dyq, dyk, cos, sin, wq, wk, positions, context, x, interleaved, out, weight_grads, workspace, stream):
+    """Where only one of the two has a gradient to pass on."""
+    if dyq is None and dyk is None:
+        return None, None, None, None
+    i = 0 if dyq is not None else 1
+    dy, w, c, xi = (dyq, dyk)[i], (wq, wk)[i], context[i], x[i] if x is not None else None
+    device = _same_device(dy, cos, sin, w, positions, xi, workspace)
+    B, S, H, D = _head_shape(dy)
+    w_dtype = _weights_dtype(w, None, D)
+    want = (w is not None and weight_grads[i], False)
+    one = None if out is None else (out[i], None)
+    if stream is None:
+        dx, _, dw, _, workspace = _backward_buffers(dy, None, w, None, want, one, workspace, D)
+    else:
+        with _allocating_for(stream, device):
+            dx, _, dw, _, workspace = _backward_buffers(dy, None, w, None, want, one, workspace, D)
+    _same_device(dy, dx)
+    _check_like(dx, dy)
+    parts = _backward_part(dy, xi, dx, w, dw, c, H)
+    rotation = _rotation(B, S, D, dy.dtype, cos, sin, positions, interleaved, w_dtype, _check_context(c, dy, device, 0), 0.0)
+    _enqueue(lib.gact_head_norm_rotate_backward, "gact_head_norm_rotate_backward", device, stream, parts, 1, rotation,
              *(workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0))
-    if len(made) == 2:
-        return made[0][0], made[1][0], made[0][1], made[1][1]
-    return (made[0][0], None, made[0][1], None) if dyq is not None else (None, made[0][0], None, made[0][1])
+    return (dx, None, dw, None) if i == 0 else (None, dx, None, dw)
 
 
-def _backward_buffers(todo, workspace, D: int):
-    """(dx, dw) of each part, and the workspace where there is a dw."""
-    made, any_dw = [], False
-    for dy, _, w, _, dx, want in todo:
-        any_dw = any_dw or want
-        made.append((dx if dx is not None else dy.new_empty(dy.shape), w.new_empty(w.shape) if want else None))
-    if any_dw and workspace is None:
-        workspace = todo[0][0].new_empty(gact_head_norm_rotate_workspace_bytes(D), dtype=torch.uint8)
-    return made, workspace
+def _backward_buffers(dyq, dyk, wq, wk, want, out, workspace, D: int):
+    """(dq, dk, dwq, dwk, workspace): those that are wanted and not given."""
+    dq, dk = out if out is not None else _empty_heads(dyq, dyk)
+    dwq = wq.new_empty(wq.shape) if want[0] else None
+    dwk = wk.new_empty(wk.shape) if want[1] else None
+    if workspace is None and (want[0] or want[1]):
+        workspace = dyq.new_empty(gact_head_norm_rotate_workspace_bytes(D), dtype=torch.uint8)
+    return dq, dk, dwq, dwk, workspace
+
+
+def _backward_part(dy, x, dx, w, dw, c: HeadContext, H: int) -> bytes:
+    a_x, strides = 0, _NO_STRIDES
+    rstd, packed, gmin, gscale, seed, bits = c.addresses()
+    if bits == GACT_BITS_UNCOMPRESSED:
+        if x is None:
+            raise ValueError("the context is not compressed: x is needed")
+        _check_like(x, dy)
+        a_x, strides = x.data_ptr(), _head_strides(x)
+    return _HEADS.pack(a_x, 0, dy.data_ptr(), dx.data_ptr(), 0 if w is None else w.data_ptr(), 0 if dw is None else dw.data_ptr(),
+                       rstd, packed, gmin, gscale, *strides, 0, 0, 0, *_head_strides(dy), *_head_strides(dx), seed, H, bits)

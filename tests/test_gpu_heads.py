@@ -388,3 +388,32 @@ def test_offsets_beyond_32_bits(gact, D, Hq, Hk):
     wide.copy_(randn(7, *wide.shape))
     y, _ = gact.gact_head_norm_rotate(wide, None, *args)
     assert torch.equal(y, gact.gact_head_norm_rotate(wide.contiguous(), None, *args)[0])
+
+
+def test_calls_whose_tensors_do_not_belong_together(gact):
+    q, k, cos, sin, wq, wk, pos = args = inputs((2, 8, 4, 2, 64, 64, "bf16", "f32", False))
+    ctx = [gact.make_head_context(x, 4, 64, 1) for x in (q, k)]
+    gact.gact_head_norm_rotate(*args, context=ctx)
+    for bad in (k[:1], k[:, :4], k[..., :32], k.float(), k[0]):
+        with pytest.raises(ValueError):
+            gact.gact_head_norm_rotate(q, bad, *args[2:])
+        with pytest.raises(ValueError):
+            gact.gact_head_norm_rotate_backward(q, bad, *args[2:], context=ctx)
+    other = gact.make_head_context(k, 4, 128, 1)
+    for context in ((ctx[0], ctx[0]), (ctx[0], other)):
+        with pytest.raises(ValueError):
+            gact.gact_head_norm_rotate(*args, context=context)
+        with pytest.raises(ValueError):
+            gact.gact_head_norm_rotate_backward(q, k, *args[2:], context=context)
+    with pytest.raises(ValueError):
+        gact.gact_head_norm_rotate(*args, out=(q, q))
+    with pytest.raises(ValueError):
+        gact.gact_head_norm_rotate_backward(q, k, *args[2:], context=ctx, out=(q, q))
+    with pytest.raises(ValueError):
+        gact.gact_head_norm_rotate_backward(q, k, *args[2:], context=[gact.make_head_context(x) for x in (q, k)])      # no x
+    with pytest.raises(ValueError):
+        gact.gact_head_norm_rotate(q, k, cos.cpu(), sin, wq, wk, pos)
+    with pytest.raises(gact.GactError):
+        gact.gact_head_norm_rotate(*args, context=[gact.make_head_context(x, 4, 256, 1) for x in (q, k)])              # 2 * 64 < 256
+    with pytest.raises(gact.GactError):
+        gact.gact_head_norm_rotate(*args, eps=0.0)

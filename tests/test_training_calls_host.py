@@ -36,7 +36,7 @@ def test_the_binding_packs_the_records_of_the_interface():
     assert [getattr(h, f) for f in ("x", "y", "dy", "dx", "w", "dw", "rstd", "packed", "gmin", "gscale")] == list(range(1, 11))
     assert list(h.x_stride) + list(h.dx_stride) == [11, 12, 13, 20, 21, 22] and (h.seed, h.heads, h.bits) == (2**64 - 1, 5, 4)
     t = torch.zeros(9, 16)
-    r = Rotation.from_buffer_copy(gact._rotation(torch.zeros(2, 3, 4, 64), t, t, torch.zeros(6, dtype=torch.int64), True,
+    r = Rotation.from_buffer_copy(gact._rotation(2, 3, 64, torch.float32, t, t, torch.zeros(6, dtype=torch.int64), True,
                                                  torch.bfloat16, 64, 0.5))
     assert (r.batch, r.tokens, r.head_dim, r.rot_dim, r.n_positions, r.interleaved, r.dtype, r.w_dtype, r.group_size, r.eps,
             r.cos) == (2, 3, 64, 32, 9, 1, 0, 1, 64, 0.5, t.data_ptr())
@@ -181,15 +181,15 @@ def test_the_binding_refuses_tensors_the_kernels_cannot_take():
     for cos, sin, pos in ((t, None, None), (t.double(), t.double(), None), (t, t[:2], None), (t.t(), t.t(), None),
                           (t, t, torch.zeros(6, dtype=torch.int32)), (t, t, torch.zeros(5, dtype=torch.int64)), (t[:2], t[:2], None)):
         with pytest.raises(ValueError):
-            gact._rotation(x, cos, sin, pos, False, None, 0, 1e-6)
+            gact._rotation(2, 3, 64, x.dtype, cos, sin, pos, False, None, 0, 1e-6)
     with pytest.raises(TypeError):
-        gact._rotation(x.half(), t, t, None, False, None, 0, 1e-6)
-    for weights in ((torch.zeros(64), torch.zeros(64, dtype=torch.bfloat16)), (torch.zeros(63),), (torch.zeros(128)[::2],)):
+        gact._rotation(2, 3, 64, torch.float16, t, t, None, False, None, 0, 1e-6)
+    for weights in ((torch.zeros(64), torch.zeros(64, dtype=torch.bfloat16)), (torch.zeros(63), None), (None, torch.zeros(128)[::2])):
         with pytest.raises(ValueError):
-            gact._weights_dtype(weights, 64)
-    for other in (x[:1], x[:, :2], x[..., :32], x.bfloat16(), x[0]):
+            gact._weights_dtype(*weights, 64)
+    for bad in (x[0, 0], x[None]):
         with pytest.raises(ValueError):
-            gact._check_pair(x, other)
+            gact._head_shape(bad)
 
 
 PROGRAM = r"""

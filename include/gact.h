@@ -357,9 +357,12 @@ int gact_grad_clip_by(const gact_grad_buf *h_bufs, int K, double max_norm, const
  *   h_parts      host array of 1 or 2 tensors (queries and keys), which go into one launch where their bits agree.
  *     forward:   reads x; writes y, rstd (batch * tokens * heads floats; NULL without a backward pass, only with
  *                bits == GACT_BITS_UNCOMPRESSED) and, compressing, packed (16-byte aligned), gmin and gscale.  y may be x
- *                itself with x's strides; nothing else may overlap an output.
+ *                itself with x's strides.
  *     backward:  reads dy, rstd and packed, gmin, gscale (compressed) or x; writes dx and, where dw is not NULL, dw.
  *                dx may be dy itself with dy's strides.
+ *     Nothing else may overlap an output.  GACT_E_ARG for what pointers and strides show of it: a buffer given twice, in
+ *     place with other strides, an output's rows that share memory (each stride of an axis longer than 1 has to pass what
+ *     the smaller ones span).
  *     w, dw      head_dim weights and their gradients, of w_dtype; w NULL: no weights (dw must be NULL)
  *     strides    in elements: batch, token, head
  *     heads      may differ between the parts

@@ -545,6 +545,46 @@ bool group_of_heads(int G, int dim, gact::HeadArgs* a) {
     return true;
 }
 
+// Whether two rows of a tensor can share memory: unless, in the order of their sizes, each stride passes what lies below it.
+bool rows_overlap(const int64_t (&stride)[3], const gact_rotation* r, int heads) {
+    struct Axis { uint64_t stride, n; };
+    const auto axis = [](int64_t s, int64_t n) { return Axis{s < 0 ? 0 - (uint64_t)s : (uint64_t)s, (uint64_t)n}; };
+    Axis axes[3] = {axis(stride[0], r->batch), axis(stride[1], r->tokens), axis(stride[2], heads)};
+    std::sort(axes, axes + 3, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+    uint64_t extent = (uint64_t)r->head_dim;
+    for (const Axis& x : axes) {
+        if (x.n < 2) continue;
+        if (x.stride < extent || x.stride >= (uint64_t)1 << 48) return true;      // (behind that products would wrap)
+        extent += x.stride * (x.n - 1);
+    }
+    return false;
+}
+bool same_strides(const int64_t (&a)[3], const int64_t (&b)[3], const gact_rotation* r, int heads) {
+    return (a[0] == b[0] || r->batch < 2) && (a[1] == b[1] || r->tokens < 2) && (a[2] == b[2] || heads < 2);
+}
+// Whether the parts' outputs overlap themselves, each other or an input that is not their own, as far as pointers and strides
+// show it: a buffer given twice, in place with other strides, rows that share memory.
+bool head_outputs_overlap(const gact_heads* parts, int n_parts, const gact_rotation* r, bool backward) {
+    for (int k = 0; k < n_parts; ++k) {
+        const gact_heads& h = parts[k];
+        const void* out = backward ? h.dx : h.y;
+        const auto& strides = backward ? h.dx_stride : h.y_stride;
+        if (rows_overlap(strides, r, h.heads)) return true;
+        if (out == (backward ? h.dy : h.x) && !same_strides(strides, backward ? h.dy_stride : h.x_stride, r, h.heads)) return true;
+        for (int j = 0; j < n_parts; ++j) {
+            const gact_heads& o = parts[j];
+            if (backward && o.bits == GACT_BITS_UNCOMPRESSED && out == o.x) return true;
+            if (j == k) continue;
+            if (out == (backward ? o.dx : o.y) || out == (backward ? o.dy : o.x)) return true;
+            if (backward ? h.dw && h.dw == o.dw : h.rstd && h.rstd == o.rstd) return true;
+            if (!backward && h.bits != GACT_BITS_UNCOMPRESSED && o.bits != GACT_BITS_UNCOMPRESSED &&
+                (h.packed == o.packed || h.gmin == o.gmin || h.gscale == o.gscale))
+                return true;
+        }
+    }
+    return false;
+}
+
 // Checks a call and fills what its parts share, then the parts.  `bits` of part k goes to part_bits[k], 0 without a context.
 int stage_heads(const gact_heads* parts, int n_parts, const gact_rotation* r, bool backward, gact::HeadArgs* a, int* part_bits) {
     if (!parts || n_parts < 1 || n_parts > gact::kHeadParts || !r) return GACT_E_ARG;
@@ -609,7 +649,7 @@ int stage_heads(const gact_heads* parts, int n_parts, const gact_rotation* r, bo
         p.seed_lo = (uint32_t)h.seed;
         p.seed_hi = (uint32_t)(h.seed >> 32);
     }
-    return GACT_OK;
+    return tokens > 0 && head_outputs_overlap(parts, n_parts, r, backward) ? GACT_E_ARG : GACT_OK;
 }
 
 // The launches of a staged call: one where the parts have the same kind of context, in a mode that both have, else one for

@@ -548,8 +548,16 @@ def _same_device(*tensors) -> int:
 
 
 def _dense(t: torch.Tensor) -> bool:
-    return (t.is_contiguous() or (t.dim() == 4 and t.is_contiguous(memory_format=torch.channels_last))
-            or (t.dim() == 5 and t.is_contiguous(memory_format=torch.channels_last_3d)))
+    """Whether t's elements are numel() consecutive ones, in whatever order of its axes."""
+    if t.is_contiguous():
+        return True
+    extent = 1
+    for stride, size in sorted(zip(t.stride(), t.shape)):
+        if size != 1:
+            if stride != extent:
+                return False
+            extent *= size
+    return True
 
 
 @functools.lru_cache(maxsize=64)
@@ -611,6 +619,8 @@ def _norm_call(g, outs, norm, workspace, stream, bufs):
         raise ValueError("the norm is one float64 element")
     if norm.get_device() != device or workspace.get_device() != device:
         raise ValueError("the tensors of a call lie on different devices")
+    if not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
     return K, arr, device, norm, workspace
 
 
@@ -639,6 +649,8 @@ def gact_grad_clip_by(g: Sequence[torch.Tensor], max_norm: float, norm: torch.Te
                       outs: Optional[Sequence[torch.Tensor]] = None, workspace: Optional[torch.Tensor] = None,
                       stream=None, bufs=None) -> None:
     """gact_grad_clip by a norm that is known already (device float64[1])."""
+    if norm is None:
+        raise ValueError("the norm to clip by is missing")
     K, table, device, norm, workspace = _norm_call(g, outs, norm, workspace, stream, bufs)
     _enqueue(lib.gact_grad_clip_by, "gact_grad_clip_by", device, stream, table, K, float(max_norm), norm.data_ptr(),
              workspace.data_ptr(), workspace.nbytes)
@@ -934,7 +946,10 @@ def _backward_buffers(dyq, dyk, wq, wk, want, out, workspace, D: int):
     dq, dk = out if out is not None else _empty_heads(dyq, dyk)
     dwq = wq.new_empty(wq.shape) if want[0] else None
     dwk = wk.new_empty(wk.shape) if want[1] else None
-    if workspace is None and (want[0] or want[1]):
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("the workspace must be contiguous")
+    elif want[0] or want[1]:
         workspace = dyq.new_empty(gact_head_norm_rotate_workspace_bytes(D), dtype=torch.uint8)
     return dq, dk, dwq, dwk, workspace
 

@@ -17,14 +17,14 @@ from the ``Controller``.
 from __future__ import annotations
 
 import ctypes
-from typing import Callable, Dict, Iterable, List, Optional, Sequence
+from typing import Callable, Dict, Iterable, List, Optional, Sequence, Union
 
 import numpy as np
 import torch
 from torch.multiprocessing.reductions import StorageWeakRef
 
 from . import (GACT_BITS_UNCOMPRESSED, GACT_OK, GactError, TensorDesc, dtype_code, gact_allocate_bits_levels,
-               gact_copy_bounded, gact_grad_clip, gact_grad_norm_workspace_bytes, head_context_fits,
+               gact_copy_bounded, gact_grad_clip, head_context_fits,
                gact_multi_workspace_bytes, gact_num_groups, gact_packed_bytes, gact_sensitivity, lib)
 from .heads import head_norm_rotate
 
@@ -53,12 +53,15 @@ def _side_streams():
     return _SIDE_STREAMS[dev]
 
 
-def clip_grad_norm_(params: Iterable[torch.Tensor], max_norm: float, norm_type: float = 2.0,
+def clip_grad_norm_(params: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float, norm_type: float = 2.0,
                     workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Scales the parameters' gradients in place so that their norm together, 2 or inf, is at most max_norm; returns the
     norm before, a device float64 scalar (``gact_grad_clip``: nothing waits for it)."""
-    grads = [p.grad.detach() for p in dict.fromkeys(params) if p.grad is not None]
-    return gact_grad_clip(grads, max_norm, norm_type, workspace=workspace).view(())
+    params = dict.fromkeys([params] if isinstance(params, torch.Tensor) else params)
+    grads = [p.grad.detach() for p in params if p.grad is not None]
+    norm = gact_grad_clip(grads, max_norm, norm_type, workspace=workspace).view(())
+    torch.autograd.graph.increment_version(grads)      # the kernel writes behind autograd's back
+    return norm
 
 
 class _Packed:
@@ -181,7 +184,6 @@ class Controller:
         self._out_inflight: List[_Batch] = []     # swap mode: swap-out enqueued, device copy still held
         self._descs = (TensorDesc * _MAX_BATCH)()
         self._ws: Optional[torch.Tensor] = None
-        self._norm_ws: Optional[torch.Tensor] = None
         # swap-out and swap-in each on a stream of their own (Sec. 5.3), both at default priority
         self._out_stream, self._in_stream = _side_streams() if swap else (None, None)
         # pinned host memory for the swapped batches: one arena, handed out front to back within
@@ -315,15 +317,11 @@ class Controller:
         return head_norm_rotate(q, k, cos, sin, wq, wk, positions, eps, interleaved, by_head, bits, self.group_size, seeds,
                                 _own=True)
 
-    def clip_grad_norm_(self, params: Iterable[torch.Tensor], max_norm: float, norm_type: float = 2.0) -> torch.Tensor:
-        """``clip_grad_norm_`` with a workspace that the controller keeps.  (The compressor's noise adds V(b) of Thm. 2 to
-        the gradient's variance, and with it to the norm.)"""
-        params = list(dict.fromkeys(params))
-        need = gact_grad_norm_workspace_bytes(len(params))
-        device = next((p.grad.device for p in params if p.grad is not None), None)
-        if device is not None and (self._norm_ws is None or self._norm_ws.numel() < need or self._norm_ws.device != device):
-            self._norm_ws = torch.empty(need, dtype=torch.uint8, device=device)
-        return clip_grad_norm_(params, max_norm, norm_type, self._norm_ws if device is not None else None)
+    def clip_grad_norm_(self, params: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float,
+                        norm_type: float = 2.0) -> torch.Tensor:
+        """``clip_grad_norm_`` of the step.  (The compressor's noise adds V(b) of Thm. 2 to the gradient's variance, and with
+        it to the norm.)"""
+        return clip_grad_norm_(params, max_norm, norm_type)
 
     # ------------------------------------------------------------ compression
     def _workspace(self, device) -> torch.Tensor:

@@ -194,3 +194,26 @@ def test_bufs_of_other_gradients_are_noticed(gact):
         gact.gact_grad_clip([g[0], g[0]], 1.0)                                   # the same buffer twice
     twice, once = float(gact.gact_grad_norm([g[0], g[0]])), float(gact.gact_grad_norm([g[0]]))
     assert abs(twice - math.sqrt(2) * once) <= 1e-11 * twice                     # counted as often as it is listed
+
+
+def test_calls_whose_arguments_are_missing_or_strided(gact):
+    g = grads((100, 200), ("f32",), 8)
+    with pytest.raises(ValueError):
+        gact.gact_grad_clip_by(g, 1.0, None)
+    ws = torch.empty(2 * gact.gact_grad_norm_workspace_bytes(2), dtype=torch.uint8, device="cuda")
+    for bad in (ws[::2], ws[:1].expand(ws.numel())):
+        with pytest.raises(ValueError):
+            gact.gact_grad_norm(g, workspace=bad)
+    with pytest.raises(ValueError):
+        gact.gact_grad_norm([g[0].view(10, 10)[:, :5]])
+
+
+def test_gradients_in_another_order_of_axes(gact):
+    g = [t.view(4, 5, -1).permute(2, 0, 1) for t in grads((100, 2000), ("f32", "bf16"), 9)]
+    want = math.sqrt(sum(float((t.double() ** 2).sum()) for t in g))
+    before = [t.clone() for t in g]
+    norm = float(gact.gact_grad_clip(g, 0.25 * want))
+    assert abs(norm - want) <= 1e-11 * want
+    c = 0.25 * want / (want + 1e-6)
+    for t, b in zip(g, before):
+        assert ((t.double() - c * b.double()).abs() <= c * b.double().abs() * torch.finfo(t.dtype).eps / 2 * 1.01).all()

@@ -240,6 +240,52 @@ def test_clipping_by_the_norm_that_the_statistics_give(gact):
     assert all((x - y).abs().max() <= 2.0 ** -23 * y.abs().max() for x, y in zip(a, b))
 
 
+def test_clipping_that_is_captured_beside_eager_calls(gact, hooks):
+    """A captured call of a controller and eager ones of longer lists between its replays, whose workspaces differ: each finds
+    its own norm, with memory written over that the eager calls have given back."""
+    ctl = hooks.Controller(group_size=64, bits=4)
+
+    def params(seed, K):
+        out = [torch.nn.Parameter(rand(seed + j, 1000 + j)) for j in range(K)]
+        for j, p in enumerate(out):
+            p.grad = rand(seed + 1000 + j, *p.shape)
+        return out
+
+    def norm_of(ps):
+        return math.sqrt(sum(float((p.grad.double() ** 2).sum()) for p in ps))
+    few, many = params(1, 200), params(500, 300)
+    ctl.clip_grad_norm_(few, 1e9)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norm = ctl.clip_grad_norm_(few, 1e9)
+    for n in range(3):
+        eager = ctl.clip_grad_norm_(many, 1e9)
+        junk = [torch.full((1 << 14,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(8)]
+        few[n].grad.mul_(2.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert abs(float(norm) - norm_of(few)) <= 1e-11 * float(norm)
+        assert abs(float(eager) - norm_of(many)) <= 1e-11 * float(eager)
+        assert all((t == 0xFF).all() for t in junk)
+
+
+def test_clipping_as_autograd_sees_it(hooks):
+    """One parameter alone, one listed twice, and gradients that a graph of theirs still needs."""
+    p = torch.nn.Parameter(rand(1, 64))
+    p.grad = rand(2, 64)
+    want = float(p.grad.double().norm())
+    assert abs(float(hooks.clip_grad_norm_(p, 1e9)) - want) <= 1e-11 * want
+    assert abs(float(hooks.clip_grad_norm_([p, p], 1e9)) - want) <= 1e-11 * want
+    x = rand(3, 64).requires_grad_(True)
+    (x ** 3).sum().backward(create_graph=True)
+    y = (x.grad ** 2).sum()                            # keeps x.grad
+    hooks.clip_grad_norm_(x, 0.1)
+    with pytest.raises(RuntimeError):
+        y.backward()
+    x.grad = None
+
+
 def test_tensors_on_another_stream_and_a_captured_step(gact, heads, hooks):
     """Forward, backward and clipping captured together (a warm-up on a side stream first), replayed with new inputs against
     the same calls made eagerly."""

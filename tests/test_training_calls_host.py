@@ -144,6 +144,48 @@ def test_head_calls_refuse_their_own():
     assert [gact.gact_head_norm_rotate_workspace_bytes(d) for d in (0, 4, 12, 520, -8)] == [0] * 5
 
 
+def apart(k, bits=4):
+    """Part k of a call whose buffers are all different."""
+    h = Heads()
+    h.heads, h.bits = 4, bits
+    for i, f in enumerate(("x", "y", "dy", "dx", "w", "dw", "rstd", "packed", "gmin", "gscale")):
+        setattr(h, f, P + 8192 * (10 * k + i + 1))
+    for f in ("x_stride", "y_stride", "dy_stride", "dx_stride"):
+        setattr(h, f, (ctypes.c_int64 * 3)(8 * 4 * 64, 4 * 64, 64))
+    return h
+
+
+def refused(backward, change, bits=4):
+    parts = (Heads * 2)(apart(0, bits), apart(1, bits))
+    change(*parts)
+    _, _, r = record()
+    if backward:
+        rc = gact.lib.gact_head_norm_rotate_backward(ctypes.addressof(parts), 2, ctypes.addressof(r), P, 1 << 30, None)
+    else:
+        rc = gact.lib.gact_head_norm_rotate(ctypes.addressof(parts), 2, ctypes.addressof(r), None)
+    return rc == gact.GACT_E_ARG
+
+
+def test_outputs_of_heads_that_overlap_are_refused():
+    def to(field, value):
+        return lambda a, b: setattr(b, field, value(a, b) if callable(value) else value)
+
+    def strides(*s):
+        return (ctypes.c_int64 * 3)(*s)
+    for change in (to("y", lambda a, b: a.y), to("y", lambda a, b: a.x), to("rstd", lambda a, b: a.rstd),
+                   to("packed", lambda a, b: a.packed), to("gmin", lambda a, b: a.gmin), to("gscale", lambda a, b: a.gscale),
+                   to("y_stride", strides(2048, 256, 0)), to("y_stride", strides(0, 256, 64)),
+                   to("y_stride", strides(2048, 255, 64)), to("y_stride", strides(2048, 64, 64)),
+                   to("y_stride", strides(2048, 256, -63)), to("y_stride", strides(1 << 62, 256, 64)),
+                   lambda a, b: (to("y", b.x)(a, b), to("y_stride", strides(2048, 64, 512))(a, b))):
+        assert refused(False, change)
+    for bits, change in ((4, to("dx", lambda a, b: a.dx)), (4, to("dx", lambda a, b: a.dy)), (4, to("dw", lambda a, b: a.dw)),
+                         (32, to("dx", lambda a, b: b.x)), (32, to("dx", lambda a, b: a.x)),
+                         (4, to("dx_stride", strides(2048, 256, 0))),
+                         (4, lambda a, b: (to("dx", b.dy)(a, b), to("dx_stride", strides(2048, 64, 512))(a, b)))):
+        assert refused(True, change, bits)
+
+
 def test_groups_that_do_not_fit_heads():
     """The binding's rule and the library's are the same one."""
     for D in range(8, 520, 8):
@@ -172,6 +214,9 @@ def test_the_binding_refuses_tensors_the_kernels_cannot_take():
         gact.gact_head_norm_rotate(x, None, None, None)                     # host memory
     with pytest.raises(ValueError):
         gact.make_grad_bufs([x])
+    dense = [x, x.transpose(1, 3), x.permute(2, 0, 3, 1), x[:1, :1, :1], x[:0, ::2], torch.zeros(6, 5).t(), torch.zeros(())]
+    assert all(gact._dense(t) for t in dense)
+    assert not any(gact._dense(t) for t in (x[:, :2], x[:, :1, :1], x[..., ::2], x[:1].expand(2, 3, 4, 64), torch.zeros(6, 5).t()[1:]))
     with pytest.raises(ValueError):
         gact._norm_kind(1.0)
     for strided in (x.transpose(2, 3), x[0, 0], x[:, :, :, ::2]):

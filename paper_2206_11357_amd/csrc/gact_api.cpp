@@ -444,7 +444,7 @@ int stage_norm(const gact_grad_buf* bufs, int K, bool scale, const double* d_nor
             const size_t size = dtype == GACT_F32 ? 4 : 2;
             if (!b.g || !aligned(b.g, size) || (scale && (!b.out || !aligned(b.out, size)))) return GACT_E_ARG;
             if (b.n > (int64_t)1 << 48) return GACT_E_ARG;
-            const int64_t head = std::min<int64_t>(b.n, (int64_t)((0 - (uintptr_t)b.g & 15) / size));
+            const int64_t head = std::min<int64_t>(b.n, (int64_t)((0 - (uintptr_t)b.g & (gact::kNormLine - 1)) / size));
             gact::NormBuffer nb{};
             nb.in = (const unsigned char*)b.g + head * size;
             nb.out = scale ? (unsigned char*)b.out + head * size : nullptr;

@@ -16,6 +16,11 @@
 // backward pass takes x from the codes, which are never written out decompressed.  r is kept from the forward pass
 // in binary32: dn x^ r and the first term of dx are then linear in x^, so that the rounding noise leaves their
 // expectation where it is (Sec. 3.1 asks it of the compressor); from x^ itself r would be biased.
+//
+// Us and TB/s of what is read and written: 8192 tokens of 32 + 8 heads of 128, bf16, head by head 30.0 (5.6); with 4-bit
+// contexts, 32768 tokens 167 (4.6), backward 149 (5.2); 8192 tokens of 16 + 16 of 64, 21.1 (3.6) and 15.7 (4.9); fp32, 12608
+// of 16 + 16 of 64, 2 bits 45.8 (4.8) and 46.4 (4.8).  A large copy reaches 5.0.  The compressing forward pass in bf16 is bound
+// by its arithmetic, the noise and the rounding: without them 150 us of the 167.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -129,7 +134,7 @@ __device__ __forceinline__ void store8(uint8_t* base, OFFSET at, const float (&v
 }
 
 // ------------------------------------------------------------------- rotation
-// How a part's passes lie in its tensors (heads_mode on the host).
+// How a part's passes lie in its tensors (lay_out_heads on the host).
 //   kAny      any number of heads: each lane finds its row's token and addresses for itself
 //   kSteady   a token's heads are a multiple of a pass's rows, or they divide them and the passes of a sequence come out
 //             even: the addresses are the wavefront's, counted on from pass to pass, and what a lane adds to them is the

@@ -17,17 +17,19 @@ constexpr uint32_t kNormBlocks = 1024;
 // Lists of this many bytes and more do not stay in the 256 MB cache from one launch to the next: a norm alone reads them as data
 // that nobody wants again, and clipping, which reads them twice, from the larger bound on.  Clipping has then eight times the blocks
 // (each adds up the norm's results first), as it has by a given norm.  Us, norm alone, ordinary | as said: 201 MB bf16 32.0 | 33.4,
-// 608 MB 108 | 99; clipping fp32, norm + scaling: 50 MB 27 | 31, 101 MB 49 | 57, 202 MB 95 | 102, 403 MB 193 | 199, 503 MB 244 | 241, 604 MB 301 | 294,
+// 608 MB 108 | 95; clipping fp32, norm + scaling: 50 MB 27 | 31, 101 MB 49 | 57, 202 MB 95 | 102, 403 MB 193 | 199, 503 MB 244 | 241, 604 MB 301 | 294,
 // 1.2 GB 632 | 610.
 constexpr uint64_t kNormOnceBytes = 256ull << 20, kClipOnceBytes = 440ull << 20;
 constexpr uint32_t kClipBlocks = 8192;
 
-// A buffer from the first 16-byte line of the input on.  (Loads of 16 bytes that begin anywhere take a quarter longer.)
+// A buffer from the first cache line of the input on, so that a wavefront's loads are whole lines: 608 MB at odd addresses 124 us
+// from the first element on, 99 from the first 16 bytes, 95 from the first line.
+constexpr uintptr_t kNormLine = 128;
 struct NormBuffer {
     const void* in;
     void*       out;                              // null: norm only
     int64_t     n : 56;                           // from there on
-    int64_t     head : 8;                         // elements in front, up to 7
+    int64_t     head : 8;                         // elements in front, up to 63
 };
 static_assert(sizeof(NormBuffer) == 24, "three words of a table");
 // A table small enough to travel in the kernel arguments: the buffers of one type behind those of the other

@@ -659,14 +659,17 @@ struct HeadLaunches {
     bool together;
     int mode[gact::kHeadParts];
 };
-HeadLaunches arrange_heads(gact::HeadArgs* a, int n_parts, const int* part_bits, int size, bool backward) {
+HeadLaunches arrange_heads(gact::HeadArgs* a, int n_parts, const int* part_bits, int dtype, bool backward) {
     HeadLaunches l{};
-    const uint32_t run = backward ? gact::kHeadBackwardRun : gact::kHeadForwardRun;
+    const int size = dtype == GACT_F32 ? 4 : 2;
+    uint64_t rows = 0;
+    for (int k = 0; k < n_parts; ++k) rows += a->part[k].rows;
+    const uint32_t run = gact::head_most_run(rows >> (6 - a->lanes_shift), backward ? gact::kHeadBackwardRun : gact::kHeadForwardRun);
     for (int k = 0; k < n_parts; ++k) l.mode[k] = gact::lay_out_heads(*a, &a->part[k], run, size);
     l.together = n_parts == 1 || part_bits[0] == part_bits[1];
     if (l.together && n_parts > 1 && l.mode[0] != l.mode[1])
         for (int k = 0; k < n_parts; ++k) l.mode[k] = gact::lay_out_heads(*a, &a->part[k], 0, size);
-    const uint32_t blocks = backward ? gact::kHeadBackwardBlocks : gact::kHeadForwardBlocks;
+    const uint32_t blocks = backward ? gact::head_backward_blocks(dtype) : gact::kHeadForwardBlocks;
     if (l.together) gact::plan_heads(a->part, n_parts, blocks);
     else for (int k = 0; k < n_parts; ++k) gact::plan_heads(&a->part[k], 1, blocks);
     return l;
@@ -869,7 +872,7 @@ int gact_head_norm_rotate(const gact_heads* h_parts, int n_parts, const gact_rot
     gact::HeadArgs a{};
     int bits[gact::kHeadParts] = {};
     if (const int rc = stage_heads(h_parts, n_parts, h_rotation, false, &a, bits)) return rc;
-    const HeadLaunches l = arrange_heads(&a, n_parts, bits, h_rotation->dtype == GACT_F32 ? 4 : 2, false);
+    const HeadLaunches l = arrange_heads(&a, n_parts, bits, h_rotation->dtype, false);
     return launch_heads(a, n_parts, bits, l, h_rotation, false, stream);
 }
 
@@ -878,7 +881,7 @@ int gact_head_norm_rotate_backward(const gact_heads* h_parts, int n_parts, const
     gact::HeadArgs a{};
     int bits[gact::kHeadParts] = {};
     if (const int rc = stage_heads(h_parts, n_parts, h_rotation, true, &a, bits)) return rc;
-    const HeadLaunches l = arrange_heads(&a, n_parts, bits, h_rotation->dtype == GACT_F32 ? 4 : 2, true);
+    const HeadLaunches l = arrange_heads(&a, n_parts, bits, h_rotation->dtype, true);
     bool any_dw = false;
     float* partial = (float*)d_workspace;
     for (int k = 0; k < n_parts; ++k) {

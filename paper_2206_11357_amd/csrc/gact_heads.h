@@ -11,8 +11,17 @@ namespace gact {
 constexpr int kHeadParts = 2;           // queries and keys
 constexpr int kHeadWaves = 4;           // wavefronts of a block
 constexpr int kMaxHeadDim = 512;        // a head lies in one wavefront, eight elements a lane
-// Blocks of a backward launch: each leaves one sum of weight gradients per element of a head.
-constexpr uint32_t kHeadBackwardBlocks = 1280;
+// Blocks of a backward launch, each of which leaves one sum of weight gradients per element of a head: as many as the 256 compute
+// units hold at a time, a wavefront of each on every SIMD.  The kernels' registers are bounded to that, 96 for five and 128 for
+// four: in fp32 five spill where heads of other sizes than 64, 128, 256 are turned by halves.  More blocks than fit take a second,
+// short round.  Us, blocks and wavefronts a SIMD 1024, 4 | 1280, 5 | 1280, 4: 8192 tokens of 64 + 16 heads of 160, bf16 152 | 139 |
+// 209; 65536 of 12 + 1 of 80 118 | 106 | 149; 13107 of 32 + 8 of 128, 4 bits 68 | 65 | 65; fp32, 65536 of 8 + 4 of 192 364 | 383 |
+// 407, of 4 + 4 of 256 328 | 336 | 338.  With six a SIMD all spill.
+constexpr int head_backward_waves(int dtype) { return dtype == GACT_DT_F32 ? 4 : 5; }
+constexpr uint32_t head_backward_blocks(int dtype) { return 256u * (uint32_t)head_backward_waves(dtype); }
+constexpr uint32_t kHeadBackwardBlocks = 1280;          // the most
+static_assert(head_backward_blocks(GACT_DT_F32) <= kHeadBackwardBlocks && head_backward_blocks(GACT_DT_BF16) <= kHeadBackwardBlocks,
+              "room in the workspace");
 
 // x / d for x < 2^31, as a product: floor(2^(32+s) / d) + 1 with 2^(s+1) >= d (Granlund, Montgomery 1994, Thm. 4.2,
 // as group_divisor); magic 0 stands for d = 1.
@@ -90,6 +99,14 @@ struct HeadArgs {
 //    backward of the second  1  176     2  148     4  154     8  165; one of three passes (12 heads of 80)  1  13.0     3  9.0
 constexpr uint32_t kHeadForwardBlocks = 8192;
 constexpr uint32_t kHeadForwardRun = 8, kHeadBackwardRun = 3;
+// Shorter ones in calls that would not fill the GPU otherwise, until this many wavefronts have a unit.  Us, units of 8 | as said: 8
+// tokens of 32 + 8 heads of 128 5.2 | 3.0, with 4-bit contexts 7.9 | 3.7, of 64 + 16 of 160 10.4 | 4.4; 128 tokens of the last 11.0
+// | 6.9, 1024 of the first 6.5 | 5.5 and 10.1 | 8.5.  (1024 wavefronts: 128 tokens 8.2, 4096: 1024 tokens 8.9, 8192: 10.5.)
+constexpr uint32_t kHeadFill = 2048;
+inline uint32_t head_most_run(uint64_t passes, uint32_t most) {
+    const uint64_t fill = passes / kHeadFill;
+    return fill >= most ? most : fill > 1 ? (uint32_t)fill : 1;
+}
 // Passes of a unit where a token has `passes` of them: all up to `most`, else the most of these that divide them evenly.
 inline uint32_t head_run(uint32_t passes, uint32_t most) {
     uint32_t run = passes < most ? passes : most;

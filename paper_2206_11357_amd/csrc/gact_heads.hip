@@ -598,7 +598,7 @@ __device__ __forceinline__ void backward_run(const HeadArgs& a, const HeadPart& 
 }
 
 template <int DT, int BITS, bool HALVES, int MODE>
-__global__ __launch_bounds__(kHeadThreads) void heads_backward_kernel(HeadArgs a) {
+__global__ __launch_bounds__(kHeadThreads, head_backward_waves(DT)) void heads_backward_kernel(HeadArgs a) {
     __shared__ float lds[kHeadWaves][64 * 8];
     uint32_t block;
     const HeadPart& p = a.part[part_of(a, block)];

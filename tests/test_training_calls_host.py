@@ -264,13 +264,19 @@ int main() {
             if (run < 1 || run > most || passes % run != 0 || (passes <= most && run != passes)) { std::printf("run\n"); failed = 1; }
         }
     }
+    for (const uint64_t passes : {0ull, 1ull, 2047ull, 2048ull, 4095ull, 4096ull, 6144ull, 16384ull, 1ull << 31}) {
+        for (const uint32_t most : {3u, 8u}) {
+            const uint32_t run = gact::head_most_run(passes, most);
+            if (run < 1 || run > most || (run > 1 && passes / run < gact::kHeadFill)) { std::printf("most run\n"); failed = 1; }
+        }
+    }
     for (int i = 0; i < 100000; ++i) {
         gact::HeadArgs a{};
         for (auto& p : a.part) {
             p.run = 1 + (uint32_t)(next() % 8);
             p.units = (i < 3000 ? (uint32_t)(next() % 60000) : (uint32_t)(next() % 0x7FFFFFFF) >> (next() % 31)) / p.run;
         }
-        for (const uint32_t all : {gact::kHeadBackwardBlocks, gact::kHeadForwardBlocks}) {
+        for (const uint32_t all : {gact::head_backward_blocks(0), gact::head_backward_blocks(1), gact::kHeadForwardBlocks}) {
             gact::plan_heads(a.part, 2, all);
             if (a.part[0].blocks + a.part[1].blocks > all) { std::printf("blocks\n"); failed = 1; }
             for (auto& p : a.part) {

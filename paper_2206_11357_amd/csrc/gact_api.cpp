@@ -426,7 +426,7 @@ bool outputs_overlap(const std::vector<gact::NormBuffer>& bufs, size_t f32) {
 }
 
 // What the three calls share: checks, the buffers' table (in *table, or in the workspace where it is too long for
-// the arguments), the launch's blocks.
+// the arguments).
 int stage_norm(const gact_grad_buf* bufs, int K, bool scale, const double* d_norm, void* d_workspace, size_t workspace_bytes,
                void* stream, gact::NormTable* table, gact::NormArgs* a, bool* is_inline, uint64_t* bytes) {
     if (K < 0 || (K > 0 && !bufs) || !d_norm || !aligned(d_norm, 8)) return GACT_E_ARG;
@@ -463,7 +463,6 @@ int stage_norm(const gact_grad_buf* bufs, int K, bool scale, const double* d_nor
     if (scale && outputs_overlap(live, a->f32)) return GACT_E_ARG;
     a->K = (uint32_t)live.size();
     a->chunks = (uint32_t)chunks;
-    a->blocks = (uint32_t)std::min<uint64_t>(chunks, gact::kNormBlocks);
     a->partial = (double*)d_workspace;
     a->norm = const_cast<double*>(d_norm);
     *is_inline = a->K <= (uint32_t)gact::kInlineNorm;
@@ -502,8 +501,9 @@ int run_norm(const gact_grad_buf* bufs, int K, int kind, bool scale, bool given,
     uint64_t bytes = 0;
     if (const int rc = stage_norm(bufs, K, scale, d_norm, d_workspace, workspace_bytes, stream, &table, &a, &is_inline, &bytes)) return rc;
     const gact::NormTable* t = is_inline ? &table : nullptr;
-    scale = scale && a.blocks != 0;
+    scale = scale && a.chunks != 0;
     const bool once = bytes >= (scale ? gact::kClipOnceBytes : gact::kNormOnceBytes);
+    a.blocks = std::min(a.chunks, once ? gact::kNormBlocks : gact::kNormFit);
     a.clip_blocks = given || once ? std::min(a.chunks, gact::kClipBlocks) : a.blocks;
     if (!given && gact_launch_grad_norm(t, &a, kind, once, !scale, stream) != 0) return GACT_E_HIP;
     if (scale && gact_launch_grad_clip(t, &a, kind, given, stream) != 0) return GACT_E_HIP;

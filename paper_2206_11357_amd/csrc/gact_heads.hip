@@ -17,9 +17,9 @@
 // in binary32: dn x^ r and the first term of dx are then linear in x^, so that the rounding noise leaves their
 // expectation where it is (Sec. 3.1 asks it of the compressor); from x^ itself r would be biased.
 //
-// Us and TB/s of what is read and written: 8192 tokens of 32 + 8 heads of 128, bf16, head by head 30.0 (5.6); with 4-bit
-// contexts, 32768 tokens 167 (4.6), backward 149 (5.2); 8192 tokens of 16 + 16 of 64, 21.1 (3.6) and 15.7 (4.9); fp32, 12608
-// of 16 + 16 of 64, 2 bits 45.8 (4.8) and 46.4 (4.8).  A large copy reaches 5.0.  The compressing forward pass in bf16 is bound
+// Us and TB/s of what is read and written: 8192 tokens of 32 + 8 heads of 128, bf16, head by head 28.2 (5.9); with 4-bit
+// contexts, 32768 tokens 170 (4.5), backward 150 (5.2); 8192 tokens of 16 + 16 of 64, 21.5 (3.5) and 16.1 (4.8); fp32, 12608
+// of 16 + 16 of 64, 2 bits 45.6 (4.8) and 45.9 (4.8).  A large copy reaches 5.0.  The compressing forward pass in bf16 is bound
 // by its arithmetic, the noise and the rounding: without them 150 us of the 167.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -417,6 +417,15 @@ __device__ __forceinline__ int part_of(const HeadArgs& a, uint32_t& block) {
 }
 __device__ __forceinline__ uint32_t wave_of_block() { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 
+// What a wavefront loads behind its last unit, for nothing, so that no load stands behind a branch: the part's first unit, which
+// all take and a cache has, or, where arithmetic bounds the pass, its own once more.  Us, its own | the first: fp32, 8192 tokens
+// of 16 + 16 heads of 64 25.8 | 23.2, of 4 + 4 of 256 27.9 | 25.5, backward 40 | 39; bf16, 8192 of 32 + 8 of 128 29.4 | 28.2; with
+// 4-bit contexts, 65536 of 4 + 1 of 128 51 | 54, 13107 of 32 + 8 63 | 65, 16384 of 16 + 16 of 64 34.4 | 35.1.
+template <int DT, int BITS>
+__device__ __forceinline__ uint32_t behind_last(uint32_t unit) {
+    return DT == GACT_DT_BF16 && BITS != 0 ? unit : 0;
+}
+
 template <int DT, int BITS, bool HALVES, int MODE>
 __device__ __forceinline__ void heads_run(const HeadArgs& a, const HeadPart& p, uint32_t unit) {
     const Place<MODE> at(a);
@@ -446,9 +455,8 @@ __device__ __forceinline__ void heads_run(const HeadArgs& a, const HeadPart& p, 
     Raw<DT> ahead = fetch(u.first[kIn], unit * passes << (6 - at.shift));
     for (;;) {
         angles.load(a, p, turn, u, my_token);
-        // behind the wavefront's last unit the same once more, which no HBM traffic follows: so that a pass's elements are
-        // always on their way, without a branch, while the one before is worked on
-        const uint32_t following = p.units - unit > p.waves ? unit + p.waves : unit;
+        // a pass's elements are always on their way, without a branch, while the one before is worked on
+        const uint32_t following = p.units - unit > p.waves ? unit + p.waves : behind_last<DT, BITS>(unit);
         const Unit<MODE, 2> next(a, p, at, following);
         int64_t in = u.first[kIn], out = u.first[kOut];
         Spot<BITS> spot(a, p, unit * passes, at.shift);
@@ -476,7 +484,7 @@ __device__ __forceinline__ void heads_run(const HeadArgs& a, const HeadPart& p, 
             out += p.t[kOut].pass;
             spot.next();
         }
-        if (following == unit) return;
+        if (following <= unit) return;
         unit = following;
         u = next;
     }
@@ -554,7 +562,7 @@ __device__ __forceinline__ void backward_run(const HeadArgs& a, const HeadPart& 
     Input ahead = fetch(u.first[kIn], u.first[kTensors - 1], spot);
     for (;;) {
         angles.load(a, p, turn, u, my_token);
-        const uint32_t following = p.units - unit > p.waves ? unit + p.waves : unit;       // as in heads_run
+        const uint32_t following = p.units - unit > p.waves ? unit + p.waves : behind_last<DT, BITS>(unit);
         const Unit<MODE, kTensors> next(a, p, at, following);
         const Spot<BITS> next_spot(a, p, following * passes, at.shift);
         int64_t dy = u.first[kIn], out = u.first[kOut], xs = u.first[kTensors - 1];
@@ -591,7 +599,7 @@ __device__ __forceinline__ void backward_run(const HeadArgs& a, const HeadPart& 
             }
             out += p.t[kOut].pass;
         }
-        if (following == unit) return;
+        if (following <= unit) return;
         unit = following;
         u = next;
     }

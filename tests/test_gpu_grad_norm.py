@@ -217,3 +217,26 @@ def test_gradients_in_another_order_of_axes(gact):
     c = 0.25 * want / (want + 1e-6)
     for t, b in zip(g, before):
         assert ((t.double() - c * b.double()).abs() <= c * b.double().abs() * torch.finfo(t.dtype).eps / 2 * 1.01).all()
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_every_offset_in_a_cache_line(gact, dtype):
+    """Buffers that begin at every element of a line and end before, at and behind its end; what is between them stays."""
+    lengths = (1, 5, 31, 32, 63, 64, 65, 8300)
+    step = 8448                                        # whole lines
+    area = torch.randn(64 * len(lengths) * step, device="cuda", generator=torch.Generator("cuda").manual_seed(3)).to(dtype)
+    before = area.clone()
+    at = [(i * step + offset, n) for i, (offset, n) in enumerate((o, n) for o in range(64) for n in lengths)]
+    g = [area[a:a + n] for a, n in at]
+    inside = torch.zeros_like(area, dtype=torch.bool)
+    for a, n in at:
+        inside[a:a + n] = True
+    want = math.sqrt(float((before[inside].double() ** 2).sum()))
+    norm = float(gact.gact_grad_clip(g, 0.5 * want))
+    assert abs(norm - want) <= 1e-11 * want
+    assert torch.equal(area[~inside], before[~inside])
+    c = 0.5 * want / (want + 1e-6)
+    x, y = area[inside].double(), c * before[inside].double()
+    # half a step of the type; binary32 on the way to bf16
+    assert ((x - y).abs() <= (torch.finfo(dtype).eps / 2 * (1 + 2.0 ** -10)) * y.abs()).all()
+    assert float(gact.gact_grad_norm(g, math.inf)) == float(area[inside].abs().max())

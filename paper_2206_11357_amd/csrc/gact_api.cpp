@@ -652,30 +652,7 @@ int stage_heads(const gact_heads* parts, int n_parts, const gact_rotation* r, bo
     return tokens > 0 && head_outputs_overlap(parts, n_parts, r, backward) ? GACT_E_ARG : GACT_OK;
 }
 
-// The launches of a staged call: one where the parts have the same kind of context, in a mode that both have, else one for
-// each.  (Parts that lie differently in launches of their own, with all the blocks of one each, are no faster: 12 query
-// heads of 80 and one key head, 1021 tokens, forward 8.8 us, together 4.8; 28 and 7 of 128, 30001 tokens 112.6, 112.4.)
-struct HeadLaunches {
-    bool together;
-    int mode[gact::kHeadParts];
-};
-HeadLaunches arrange_heads(gact::HeadArgs* a, int n_parts, const int* part_bits, int dtype, bool backward) {
-    HeadLaunches l{};
-    const int size = dtype == GACT_F32 ? 4 : 2;
-    uint64_t rows = 0;
-    for (int k = 0; k < n_parts; ++k) rows += a->part[k].rows;
-    const uint32_t run = gact::head_most_run(rows >> (6 - a->lanes_shift), backward ? gact::kHeadBackwardRun : gact::kHeadForwardRun);
-    for (int k = 0; k < n_parts; ++k) l.mode[k] = gact::lay_out_heads(*a, &a->part[k], run, size);
-    l.together = n_parts == 1 || part_bits[0] == part_bits[1];
-    if (l.together && n_parts > 1 && l.mode[0] != l.mode[1])
-        for (int k = 0; k < n_parts; ++k) l.mode[k] = gact::lay_out_heads(*a, &a->part[k], 0, size);
-    const uint32_t blocks = backward ? gact::head_backward_blocks(dtype) : gact::kHeadForwardBlocks;
-    if (l.together) gact::plan_heads(a->part, n_parts, blocks);
-    else for (int k = 0; k < n_parts; ++k) gact::plan_heads(&a->part[k], 1, blocks);
-    return l;
-}
-
-int launch_heads(const gact::HeadArgs& a, int n_parts, const int* part_bits, const HeadLaunches& l, const gact_rotation* r,
+int launch_heads(const gact::HeadArgs& a, int n_parts, const int* part_bits, const gact::HeadLaunches& l, const gact_rotation* r,
                  bool backward, void* stream) {
     for (int k = 0; k < (l.together ? 1 : n_parts); ++k) {
         gact::HeadArgs one = a;
@@ -872,7 +849,7 @@ int gact_head_norm_rotate(const gact_heads* h_parts, int n_parts, const gact_rot
     gact::HeadArgs a{};
     int bits[gact::kHeadParts] = {};
     if (const int rc = stage_heads(h_parts, n_parts, h_rotation, false, &a, bits)) return rc;
-    const HeadLaunches l = arrange_heads(&a, n_parts, bits, h_rotation->dtype, false);
+    const gact::HeadLaunches l = gact::arrange_heads(&a, n_parts, bits, h_rotation->dtype, false);
     return launch_heads(a, n_parts, bits, l, h_rotation, false, stream);
 }
 
@@ -881,7 +858,7 @@ int gact_head_norm_rotate_backward(const gact_heads* h_parts, int n_parts, const
     gact::HeadArgs a{};
     int bits[gact::kHeadParts] = {};
     if (const int rc = stage_heads(h_parts, n_parts, h_rotation, true, &a, bits)) return rc;
-    const HeadLaunches l = arrange_heads(&a, n_parts, bits, h_rotation->dtype, true);
+    const gact::HeadLaunches l = gact::arrange_heads(&a, n_parts, bits, h_rotation->dtype, true);
     bool any_dw = false;
     float* partial = (float*)d_workspace;
     for (int k = 0; k < n_parts; ++k) {

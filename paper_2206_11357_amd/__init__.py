@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import math
+import operator
 import os
 import struct
 from typing import Optional, Sequence, Tuple
@@ -565,21 +566,59 @@ def gact_grad_norm_workspace_bytes(K: int) -> int:
     return int(lib.gact_grad_norm_workspace_bytes(K))
 
 
+class _GradTable(ctypes.Array):
+    """gact_grad_buf entries, the tensors that they describe (kept alive) and where these were."""
+    _type_, _length_ = GradBuf, 0
+
+    def describes(self, g: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]]) -> bool:
+        """Whether the first len(g) entries are those of g and, if given, outs."""
+        K = len(g)
+        if K > len(self.g):
+            return False
+        whole, copies = K == len(self.g), outs is not None and not (outs is g and self.outs is self.g)
+        # addresses first: a tensor can have been given other memory
+        if list(map(_address, g)) != (self.g_at if whole else self.g_at[:K]):
+            return False
+        if copies and list(map(_address, outs)) != (self.outs_at if whole else self.outs_at[:K]):
+            return False
+        if all(map(operator.is_, g, self.g)) and not (copies and not all(map(operator.is_, outs, self.outs))):
+            return True
+        return all(_dense(a) and a.numel() == b.numel() and a.dtype == b.dtype for a, b in zip(g, self.g)) and \
+            (outs is None or all(map(_alike, outs, g)))
+
+
+_address = torch.Tensor.data_ptr
+
+
+def _alike(o: torch.Tensor, a: torch.Tensor) -> bool:
+    return o is a or (o.dtype == a.dtype and o.shape == a.shape and o.stride() == a.stride())
+
+
+@functools.lru_cache(maxsize=64)
+def _grad_table_type(K: int):
+    return type("_GradTable%d" % K, (_GradTable,), {"_type_": GradBuf, "_length_": K})
+
+
 def make_grad_bufs(g: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None):
-    """ctypes array of gact_grad_buf (reusable across calls while the buffers live); without `outs` in place."""
+    """ctypes array of gact_grad_buf; without `outs` in place.  It can be used for any number of calls with the same buffers
+    and keeps the tensors alive."""
+    in_place = outs is None or outs is g
     g = list(g)
-    outs = g if outs is None else list(outs)
+    outs = g if in_place else list(outs)
     if len(outs) != len(g):
         raise ValueError("g and outs must list the same buffers")
     if _same_device(*g) != _same_device(*outs):
         raise ValueError("the tensors of a call lie on different devices")
-    arr = (GradBuf * max(len(g), 1))()
+    arr = _grad_table_type(len(g))()
+    arr.g, arr.outs = g, outs
     for b, a, o in zip(arr, g, outs):
         if not _dense(a):
             raise ValueError("gact needs contiguous tensors")
-        if o is not a and (o.dtype != a.dtype or o.shape != a.shape or o.stride() != a.stride()):
+        if not _alike(o, a):
             raise ValueError("a buffer and its output differ in size, dtype or strides")
         b.g, b.out, b.n, b.dtype = a.data_ptr(), o.data_ptr(), a.numel(), dtype_code(a.dtype)
+    arr.g_at = list(map(_address, g))
+    arr.outs_at = arr.g_at if outs is g else list(map(_address, outs))
     return arr
 
 
@@ -600,27 +639,32 @@ def _norm_scratch(K: int, norm, workspace, device: int):
 
 
 def _norm_call(g, outs, norm, workspace, stream, bufs):
-    """What the three calls share: (number of buffers, table, device, norm, workspace).  The table lives as long as the
-    caller holds it."""
-    arr = bufs if bufs is not None else make_grad_bufs(g, outs)
+    """What the three calls share: (number of buffers, table, device, norm, workspace).  outs: None if the call writes no
+    buffers.  The table lives as long as the caller holds it."""
     K = len(g)
-    if len(arr) < K:
-        raise ValueError("bufs lists fewer buffers than g")
-    if bufs is not None and K and (arr[0].g != g[0].data_ptr() or (outs is not None and arr[0].out != outs[0].data_ptr())):
-        raise ValueError("bufs was made for other buffers")
+    if bufs is None:
+        arr = make_grad_bufs(g, outs)
+    else:
+        arr = bufs
+        if not arr.describes(g, outs):
+            raise ValueError("bufs was made for other buffers")
     device = g[0].get_device() if K else _current_device()
+    if norm is not None:
+        if norm.dtype != torch.float64 or norm.numel() != 1:
+            raise ValueError("the norm is one float64 element")
+        if norm.get_device() != device:
+            raise ValueError("the tensors of a call lie on different devices")
+    if workspace is not None:
+        if workspace.get_device() != device:
+            raise ValueError("the tensors of a call lie on different devices")
+        if not workspace.is_contiguous():
+            raise ValueError("the workspace must be contiguous")
     if norm is None or workspace is None:
         if stream is None:
             norm, workspace = _norm_scratch(K, norm, workspace, device)
         else:
             with _allocating_for(stream, device):
                 norm, workspace = _norm_scratch(K, norm, workspace, device)
-    if norm.dtype != torch.float64 or norm.numel() != 1:
-        raise ValueError("the norm is one float64 element")
-    if norm.get_device() != device or workspace.get_device() != device:
-        raise ValueError("the tensors of a call lie on different devices")
-    if not workspace.is_contiguous():
-        raise ValueError("the workspace must be contiguous")
     return K, arr, device, norm, workspace
 
 
@@ -638,8 +682,8 @@ def gact_grad_clip(g: Sequence[torch.Tensor], max_norm: float, norm_type: float 
                    outs: Optional[Sequence[torch.Tensor]] = None, norm: Optional[torch.Tensor] = None,
                    workspace: Optional[torch.Tensor] = None, stream=None, bufs=None) -> torch.Tensor:
     """Scales the buffers by min(1, max_norm / (norm + 1e-6)), in place or into `outs`; returns their norm before,
-    device float64[1].  `bufs` (from make_grad_bufs, with its outputs) skips re-marshalling the list."""
-    K, table, device, norm, workspace = _norm_call(g, outs, norm, workspace, stream, bufs)
+    device float64[1].  `bufs` (from make_grad_bufs with the same g and outs) skips re-marshalling the list."""
+    K, table, device, norm, workspace = _norm_call(g, g if outs is None else outs, norm, workspace, stream, bufs)
     _enqueue(lib.gact_grad_clip, "gact_grad_clip", device, stream, table, K, _norm_kind(norm_type), float(max_norm),
              norm.data_ptr(), workspace.data_ptr(), workspace.nbytes)
     return norm
@@ -651,7 +695,7 @@ def gact_grad_clip_by(g: Sequence[torch.Tensor], max_norm: float, norm: torch.Te
     """gact_grad_clip by a norm that is known already (device float64[1])."""
     if norm is None:
         raise ValueError("the norm to clip by is missing")
-    K, table, device, norm, workspace = _norm_call(g, outs, norm, workspace, stream, bufs)
+    K, table, device, norm, workspace = _norm_call(g, g if outs is None else outs, norm, workspace, stream, bufs)
     _enqueue(lib.gact_grad_clip_by, "gact_grad_clip_by", device, stream, table, K, float(max_norm), norm.data_ptr(),
              workspace.data_ptr(), workspace.nbytes)
 

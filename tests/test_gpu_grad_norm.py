@@ -240,3 +240,50 @@ def test_every_offset_in_a_cache_line(gact, dtype):
     # half a step of the type; binary32 on the way to bf16
     assert ((x - y).abs() <= (torch.finfo(dtype).eps / 2 * (1 + 2.0 ** -10)) * y.abs()).all()
     assert float(gact.gact_grad_norm(g, math.inf)) == float(area[inside].abs().max())
+
+
+def test_a_table_is_looked_at_to_its_end(gact):
+    """Whatever of the list has changed since the table was made, in its last buffer only: nothing is read or written by the old
+    addresses, sizes or types."""
+    g = grads((100, 200, 300), ("f32", "bf16"), 7)
+    outs = [torch.zeros_like(t) for t in g]
+    norm = gact.gact_grad_norm(g)
+    in_place, copies = gact.make_grad_bufs(g), gact.make_grad_bufs(g, outs)
+    flat = g[2].clone()
+    wrong = [g[:2] + [g[2].clone()], g[:2] + [g[2][:299]], g[:2] + [g[2].view(torch.int16).view(torch.bfloat16)[:300]],
+             g[:2] + [flat], [g[0], g[2], g[1]], g + [flat], g[:2] + [torch.as_strided(g[2], (300,), (0,))]]
+    before = [t.clone() for t in g]
+    for other in wrong:
+        for call in (lambda: gact.gact_grad_norm(other, bufs=in_place), lambda: gact.gact_grad_clip(other, 1e-3, bufs=in_place),
+                     lambda: gact.gact_grad_clip_by(other, 1e-3, norm, bufs=in_place),
+                     lambda: gact.gact_grad_clip(other, 1e-3, outs=outs, bufs=copies)):
+            with pytest.raises(ValueError):
+                call()
+    # outputs: others in the last place, too few, and none where the table has some
+    for other in (outs[:2] + [flat], outs[:2], None, g):
+        with pytest.raises(ValueError):
+            gact.gact_grad_clip(g, 1e-3, outs=other, bufs=copies)
+        with pytest.raises(ValueError):
+            gact.gact_grad_clip_by(g, 1e-3, norm, outs=other, bufs=copies)
+    with pytest.raises(ValueError):
+        gact.gact_grad_clip(g, 1e-3, outs=outs, bufs=in_place)
+    assert all(torch.equal(a, b) for a, b in zip(g, before)) and all((t == 0).all() for t in outs)
+    # the same memory by other names, and the list's beginning
+    same = [t.view(10, -1) for t in g]
+    assert torch.equal(gact.gact_grad_norm(same, bufs=in_place), norm) and torch.equal(gact.gact_grad_norm(g, bufs=copies), norm)
+    assert torch.equal(gact.gact_grad_norm(g[:2], bufs=in_place), gact.gact_grad_norm(g[:2]))
+    assert torch.equal(gact.gact_grad_clip(g, 1e-3, outs=outs, bufs=copies), norm)
+    # a tensor that has been given other memory
+    g[2].data = g[2].clone()
+    with pytest.raises(ValueError):
+        gact.gact_grad_norm(g, bufs=in_place)
+
+
+def test_a_table_keeps_its_buffers(gact):
+    """Memory of gradients that are let go is not handed to others while a table that lists it can still be used."""
+    g = grads((1 << 20,), ("f32",), 1)
+    bufs = gact.make_grad_bufs(g)
+    at = g[0].data_ptr()
+    del g
+    assert torch.zeros(1 << 20, device="cuda").data_ptr() != at
+    assert bufs[0].g == at

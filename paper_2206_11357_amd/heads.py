@@ -8,6 +8,7 @@ from __future__ import annotations
 from typing import Optional, Sequence
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import (GACT_BITS_UNCOMPRESSED, gact_head_norm_rotate, gact_head_norm_rotate_backward, make_head_context)
@@ -54,6 +55,13 @@ class _HeadNormRotate(torch.autograd.Function):
         return (*(g if n else None for g, n in zip(grads, need)), *(None,) * 10)
 
 
+def _refuse_tangents(*tensors: Optional[torch.Tensor]) -> None:
+    """The kernels pass no forward-mode derivatives on, and a result without one would stand for zero."""
+    if getattr(forward_ad, "_current_level", 0) >= 0 and any(
+            t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise NotImplementedError("head_norm_rotate has no forward-mode derivative")
+
+
 def head_norm_rotate(q: torch.Tensor, k: torch.Tensor, cos: Optional[torch.Tensor], sin: Optional[torch.Tensor],
                      wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None,
                      positions: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
@@ -62,7 +70,9 @@ def head_norm_rotate(q: torch.Tensor, k: torch.Tensor, cos: Optional[torch.Tenso
     """``gact_head_norm_rotate`` with gradients for q, k, wq and wk.  by_head: the results lie head by head
     ([..., heads, tokens, head_dim] in memory, of q's shape), as attention reads them.  bits: widths of the contexts of q
     and k, in groups of group_size with the noise of `seeds`; GACT_BITS_UNCOMPRESSED keeps the tensor itself through
-    autograd.  ``Controller.head_norm_rotate`` chooses them from its scheme."""
+    autograd.  ``Controller.head_norm_rotate`` chooses them from its scheme.  Reverse mode, once: forward-mode tangents and
+    second derivatives are refused."""
+    _refuse_tangents(q, k, wq, wk, cos, sin)
     if not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, wq, wk))):
         out = (_empty_by_head(q), _empty_by_head(k)) if by_head else None
         return gact_head_norm_rotate(q, k, cos, sin, wq, wk, positions, eps, interleaved, out=out)

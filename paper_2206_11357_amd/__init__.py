@@ -720,6 +720,14 @@ class HeadContext:
         rows = n // shape[-1] if n else 0
         self.blob = x.new_empty(packed + 2 * meta + 4 * rows, dtype=torch.uint8)
 
+    def filled(self, blob: torch.Tensor) -> "HeadContext":
+        """The same layout over a buffer that the forward pass has filled (and that was kept apart from it)."""
+        c = HeadContext.__new__(HeadContext)
+        c.bits, c.group_size, c.seed, c.shape, c.device, c.groups, c.off = \
+            self.bits, self.group_size, self.seed, self.shape, self.device, self.groups, self.off
+        c.blob = blob
+        return c
+
     @property
     def packed(self) -> torch.Tensor:
         return self.blob[:self.off[1]]

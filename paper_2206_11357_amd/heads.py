@@ -10,6 +10,7 @@ from typing import Optional, Sequence
 import torch
 from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
+from torch.multiprocessing.reductions import StorageWeakRef
 
 from . import (GACT_BITS_UNCOMPRESSED, gact_head_norm_rotate, gact_head_norm_rotate_backward, make_head_context)
 
@@ -24,6 +25,14 @@ def _consecutive(dy: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
     return dy if dy is None or dy.stride(-1) == 1 else dy.contiguous()
 
 
+def _held_by(storage: StorageWeakRef, x: torch.Tensor) -> bool:
+    """Whether x is still in that storage (a hook may have handed back a copy)."""
+    return not storage.expired() and storage.cdata == x.untyped_storage()._cdata
+
+
+_NONE = (None, None)
+
+
 class _HeadNormRotate(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, wq, wk, cos, sin, positions, eps, interleaved, by_head, bits, group_size, seeds, own):
@@ -32,26 +41,33 @@ class _HeadNormRotate(torch.autograd.Function):
                         for x, b, s in zip((q, k), bits, seeds))
         out = (_empty_by_head(q), _empty_by_head(k)) if by_head else None
         yq, yk = gact_head_norm_rotate(q, k, cos, sin, wq, wk, positions, eps, interleaved, out=out, context=context)
-        # What is not compressed goes through autograd (and whatever hooks are set), or, `own`, is kept as it is.
-        raw = tuple(x.detach() if b == GACT_BITS_UNCOMPRESSED else None for x, b in zip((q, k), bits))
-        ctx.kept = tuple((x, x._version) for x in raw if x is not None) if own else ()
-        ctx.raw = raw if own else None
-        saved = (q if bits[0] == GACT_BITS_UNCOMPRESSED else None, k if bits[1] == GACT_BITS_UNCOMPRESSED else None)
-        ctx.save_for_backward(*(saved if not own else (None, None)), wq, wk, cos, sin, positions)
+        # Kept as autograd keeps what it needs, so that it goes after the backward pass.  What is not compressed goes through
+        # whatever hooks are set or, `own`, past them: they leave alone what needs no gradient.  (The versions are for them, too:
+        # autograd looks at none where there are hooks.)
+        raw = [x if b == GACT_BITS_UNCOMPRESSED else None for x, b in zip((q, k), bits)]
+        if own:
+            raw = [x if x is None else x.detach() for x in raw]
+            ctx.versions = [None if x is None else (StorageWeakRef(x.untyped_storage()), x._version) for x in raw]
+        else:
+            ctx.versions = _NONE
+        ctx.save_for_backward(*raw, wq, wk, cos, sin, positions, *(c.blob for c in context))
+        for c in context:
+            c.blob = None
         ctx.context, ctx.interleaved = context, interleaved
         return yq, yk
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dyq, dyk):
-        q, k, wq, wk, cos, sin, positions = ctx.saved_tensors
-        for x, version in ctx.kept:
-            if x._version != version:
+        q, k, wq, wk, cos, sin, positions, *blobs = ctx.saved_tensors
+        for x, kept in zip((q, k), ctx.versions):
+            if kept is not None and _held_by(kept[0], x) and x._version != kept[1]:
                 raise RuntimeError("queries or keys kept for the backward pass were modified in place")
         need = ctx.needs_input_grad
         grads = gact_head_norm_rotate_backward(
-            _consecutive(dyq), _consecutive(dyk), cos, sin, wq, wk, positions, context=ctx.context,
-            x=ctx.raw if ctx.raw is not None else (q, k), interleaved=ctx.interleaved, weight_grads=need[2:4])
+            _consecutive(dyq), _consecutive(dyk), cos, sin, wq, wk, positions,
+            context=[c.filled(blob) for c, blob in zip(ctx.context, blobs)], x=(q, k), interleaved=ctx.interleaved,
+            weight_grads=need[2:4])
         return (*(g if n else None for g, n in zip(grads, need)), *(None,) * 10)
 
 

@@ -30,9 +30,6 @@ def _held_by(storage: StorageWeakRef, x: torch.Tensor) -> bool:
     return not storage.expired() and storage.cdata == x.untyped_storage()._cdata
 
 
-_NONE = (None, None)
-
-
 class _HeadNormRotate(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, wq, wk, cos, sin, positions, eps, interleaved, by_head, bits, group_size, seeds, own):
@@ -44,12 +41,13 @@ class _HeadNormRotate(torch.autograd.Function):
         # Kept as autograd keeps what it needs, so that it goes after the backward pass.  What is not compressed goes through
         # whatever hooks are set or, `own`, past them: they leave alone what needs no gradient.  (The versions are for them, too:
         # autograd looks at none where there are hooks.)
-        raw = [x if b == GACT_BITS_UNCOMPRESSED else None for x, b in zip((q, k), bits)]
-        if own:
-            raw = [x if x is None else x.detach() for x in raw]
-            ctx.versions = [None if x is None else (StorageWeakRef(x.untyped_storage()), x._version) for x in raw]
-        else:
-            ctx.versions = _NONE
+        raw, versions = [None, None], [None, None]
+        for j, (x, b) in enumerate(zip((q, k), bits)):
+            if b == GACT_BITS_UNCOMPRESSED:
+                raw[j] = x.detach() if own[j] else x
+                if own[j]:
+                    versions[j] = (StorageWeakRef(x.untyped_storage()), x._version)
+        ctx.versions = versions
         ctx.save_for_backward(*raw, wq, wk, cos, sin, positions, *(c.blob for c in context))
         for c in context:
             c.blob = None
@@ -82,7 +80,7 @@ def head_norm_rotate(q: torch.Tensor, k: torch.Tensor, cos: Optional[torch.Tenso
                      wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None,
                      positions: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
                      by_head: bool = False, bits: Sequence[int] = (GACT_BITS_UNCOMPRESSED, GACT_BITS_UNCOMPRESSED),
-                     group_size: int = 0, seeds: Sequence[int] = (0, 0), _own: bool = False):
+                     group_size: int = 0, seeds: Sequence[int] = (0, 0), _own: Sequence[bool] = (False, False)):
     """``gact_head_norm_rotate`` with gradients for q, k, wq and wk.  by_head: the results lie head by head
     ([..., heads, tokens, head_dim] in memory, of q's shape), as attention reads them.  bits: widths of the contexts of q
     and k, in groups of group_size with the noise of `seeds`; GACT_BITS_UNCOMPRESSED keeps the tensor itself through
@@ -93,4 +91,4 @@ def head_norm_rotate(q: torch.Tensor, k: torch.Tensor, cos: Optional[torch.Tenso
         out = (_empty_by_head(q), _empty_by_head(k)) if by_head else None
         return gact_head_norm_rotate(q, k, cos, sin, wq, wk, positions, eps, interleaved, out=out)
     return _HeadNormRotate.apply(q, k, wq, wk, cos, sin, positions, eps, interleaved, by_head, tuple(bits), group_size,
-                                 tuple(seeds), _own)
+                                 tuple(seeds), tuple(_own))

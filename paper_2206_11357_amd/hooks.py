@@ -299,23 +299,23 @@ class Controller:
         """``heads.head_norm_rotate`` whose context is part of the scheme: q and k before the norm are context tensors l
         like those of the hooks, with widths b_l, seeds r_l and a place in Alg. 1 and Eq. (ilp), but compressed by the
         forward kernel itself and read by the backward kernel as codes.  Their buffers stay on the device (they are
-        not swapped).  Heads that the controller's group size does not fit (``head_context_fits``), and tensors that the
-        hooks would not compress, are left to autograd, with or without hooks."""
-        bits, seeds, own = [GACT_BITS_UNCOMPRESSED] * 2, [0, 0], []
-        for j, x in enumerate((q, k)):
-            if (torch.is_grad_enabled() and x.is_cuda and x.requires_grad and x.numel() >= self.min_numel
-                    and x.dtype in (torch.float32, torch.bfloat16)
-                    and head_context_fits(self.group_size, x.shape[-1], x.shape[-2])):
-                own.append(j)
-        if len(own) < 2:                             # one launch with one kind of context, or none
-            return head_norm_rotate(q, k, cos, sin, wq, wk, positions, eps, interleaved, by_head)
-        for j in own:
-            index = len(self._handles)
-            self._handles.append(None)
-            self.numel.append((q, k)[j].numel())
-            bits[j], seeds[j] = self.bits_of(index), self.seed_of(index)
-        return head_norm_rotate(q, k, cos, sin, wq, wk, positions, eps, interleaved, by_head, bits, self.group_size, seeds,
-                                _own=True)
+        not swapped).  Of q and k, one that the controller's group size does not fit (``head_context_fits``) goes to the hooks as any
+        saved tensor does, copied first where it is a slice, which they do not take and which would keep the whole alive; one
+        that the hooks would not compress (size, type) is left to autograd."""
+        bits, seeds, own, x = [GACT_BITS_UNCOMPRESSED] * 2, [0, 0], [False] * 2, [q, k]
+        for j in range(2):
+            if not (torch.is_grad_enabled() and x[j].is_cuda and x[j].requires_grad and x[j].numel() >= self.min_numel
+                    and x[j].dtype in (torch.float32, torch.bfloat16)):
+                continue
+            own[j] = head_context_fits(self.group_size, x[j].shape[-1], x[j].shape[-2])
+            if own[j]:
+                index = len(self._handles)
+                self._handles.append(None)
+                self.numel.append(x[j].numel())
+                bits[j], seeds[j] = self.bits_of(index), self.seed_of(index)
+            else:
+                x[j] = x[j].contiguous()
+        return head_norm_rotate(*x, cos, sin, wq, wk, positions, eps, interleaved, by_head, bits, self.group_size, seeds, _own=own)
 
     def clip_grad_norm_(self, params: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float,
                         norm_type: float = 2.0) -> torch.Tensor:

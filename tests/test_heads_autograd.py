@@ -68,7 +68,7 @@ def test_contexts_go_with_the_backward_pass(monkeypatch, bits, own, hooked):
     def loss_of():
         projected = leaf * 2.0                          # what queries and keys are views of
         kept.append(StorageWeakRef(projected.untyped_storage()))
-        y = heads.head_norm_rotate(projected[:, :, :4], projected[:, :, 4:], t, t, bits=bits, group_size=32, _own=own)
+        y = heads.head_norm_rotate(projected[:, :, :4], projected[:, :, 4:], t, t, bits=bits, group_size=32, _own=(own, own))
         return y[0].sum() + y[1].sum()
     with torch.autograd.graph.saved_tensors_hooks(lambda x: x, lambda x: x) if hooked else contextlib.nullcontext():
         loss = loss_of()
@@ -92,7 +92,7 @@ def test_modified_queries_are_noticed_with_and_without_hooks(monkeypatch, hooked
         q, k = leaf * 1.0, leaf * 2.0
         q.add_(1.0)                                     # before: of no account
         with torch.autograd.graph.saved_tensors_hooks(lambda x: x, lambda x: x) if hooked else contextlib.nullcontext():
-            y = heads.head_norm_rotate(q, k, t, t, _own=True)
+            y = heads.head_norm_rotate(q, k, t, t, _own=(True, True))
         if modified:
             with torch.no_grad():
                 k.add_(1.0)
@@ -104,7 +104,52 @@ def test_modified_queries_are_noticed_with_and_without_hooks(monkeypatch, hooked
     q, k = leaf * 1.0, leaf * 2.0
     q.add_(1.0)
     with torch.autograd.graph.saved_tensors_hooks(lambda x: x.clone(), lambda x: x):
-        y = heads.head_norm_rotate(q, k, t, t, _own=True)
+        y = heads.head_norm_rotate(q, k, t, t, _own=(True, True))
     with torch.no_grad():
         q.add_(1.0)
     (y[0].sum() + y[1].sum()).backward()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16), ids=str)
+@pytest.mark.parametrize("Hq,Hk,D,G", [(16, 2, 64, 256), (2, 16, 64, 256), (4, 2, 80, 256)], ids=str)
+def test_each_of_queries_and_keys_is_compressed(gact, Hq, Hk, D, G, dtype):
+    """Slices of one projection under the controller, of which the group size fits one or none: the other is compressed by the
+    hooks, nothing keeps the projection, and both gradients are those of what the contexts hold."""
+    from paper_2206_11357_amd.hooks import Controller
+    B, S = 2, 32
+    g = torch.Generator("cuda").manual_seed(1)
+    leaf = torch.randn(B, S, Hq + Hk, D, device="cuda", generator=g).to(dtype).requires_grad_(True)
+    w = [(1 + 0.2 * torch.randn(D, device="cuda", generator=g)).requires_grad_(True) for _ in range(2)]
+    angle = torch.rand(S, D // 16 * 8, device="cuda", generator=g)
+    cos, sin = angle.cos(), angle.sin()
+    ctl = Controller(w, group_size=G, bits=4, seed=3, min_numel=256)
+    ctl.begin_iteration()
+    projected = leaf * 1.0
+    q, k = projected.detach()[:, :, :Hq].clone(), projected.detach()[:, :, Hq:].clone()
+    held = StorageWeakRef(projected.untyped_storage())
+    with ctl.hooks():
+        yq, yk = ctl.head_norm_rotate(projected[:, :, :Hq], projected[:, :, Hq:], cos, sin, *w, by_head=True)
+    own = [gact.head_context_fits(G, D, h) for h in (Hq, Hk)]
+    del projected
+    assert sum(own) < 2 and sorted(ctl.numel) == sorted((q.numel(), k.numel()))
+    assert [h is not None for h in ctl._handles] == ([False] * sum(own) + [True] * (2 - sum(own)))
+    dy = [torch.randn(y.shape, device="cuda", generator=g).to(dtype) for y in (yq, yk)]
+    index = [0, 1] if own[0] == own[1] or own[0] else [1, 0]       # what the forward kernel compresses is numbered first
+    seeds = [ctl.seed_of(i) for i in index]
+    ctl._flush()
+    assert held.expired()
+    grads = torch.autograd.grad((yq, yk), [leaf, *w], dy)
+    ctx, x = [], []
+    for t, s, o in zip((q, k), seeds, own):
+        ctx.append(gact.make_head_context(t, 4 if o else 32, G if o else 0, s))
+        x.append(None if o else gact.gact_decompress(*gact.gact_compress(t.view(-1), G, 4, s), t.numel(), G, 4, dtype).view(t.shape))
+    zq, zk = gact.gact_head_norm_rotate(q, k, cos, sin, *(t.detach() for t in w), context=ctx)
+    assert torch.equal(yq, zq) and torch.equal(yk, zk)
+    want = gact.gact_head_norm_rotate_backward(*dy, cos, sin, *(t.detach() for t in w), context=ctx, x=x)
+    assert torch.equal(grads[0], torch.cat(want[:2], 2)) and torch.equal(grads[1], want[2]) and torch.equal(grads[2], want[3])
+    # without gradients nothing is numbered, copied or kept
+    before = len(ctl._handles)
+    with torch.no_grad():
+        assert torch.equal(ctl.head_norm_rotate(leaf[:, :, :Hq], leaf[:, :, Hq:], cos, sin, *w)[0], zq)
+    assert len(ctl._handles) == before

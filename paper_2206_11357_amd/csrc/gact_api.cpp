@@ -503,8 +503,9 @@ int run_norm(const gact_grad_buf* bufs, int K, int kind, bool scale, bool given,
     const gact::NormTable* t = is_inline ? &table : nullptr;
     scale = scale && a.chunks != 0;
     const bool once = bytes >= (scale ? gact::kClipOnceBytes : gact::kNormOnceBytes);
-    a.blocks = std::min(a.chunks, once ? gact::kNormBlocks : gact::kNormFit);
-    a.clip_blocks = given || once ? std::min(a.chunks, gact::kClipBlocks) : a.blocks;
+    // By the list alone, whatever the call: they are the sum's order.
+    a.blocks = std::min(a.chunks, bytes >= gact::kClipOnceBytes ? gact::kNormBlocks : gact::kNormFit);
+    a.clip_blocks = std::min(a.chunks, given || once ? gact::kClipBlocks : gact::kNormFit);
     if (!given && gact_launch_grad_norm(t, &a, kind, once, !scale, stream) != 0) return GACT_E_HIP;
     if (scale && gact_launch_grad_clip(t, &a, kind, given, stream) != 0) return GACT_E_HIP;
     return GACT_OK;

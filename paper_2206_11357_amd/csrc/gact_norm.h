@@ -13,9 +13,11 @@ constexpr int kNormWaves = 8, kNormThreads = 64 * kNormWaves;
 constexpr int kNormPieces = 2;                    // of 16 bytes, per thread and chunk
 constexpr int64_t norm_chunk_elems(int dtype) { return kNormThreads * kNormPieces * (dtype == GACT_DT_F32 ? 4 : 8); }
 // Blocks of a norm's launch, each of which takes a run of neighbouring chunks and leaves one result: as many as the compute units
-// hold at a time (three of eight wavefronts, by their registers), twice as many for lists that do not stay in a cache.  Us, norm +
-// scaling behind it, or norm alone, 768 blocks | 1024 | 1536: 50 MB fp32 9.3 + 15.4 | 11.8 + 15.4, 202 MB 34.5 + 58.5 | 35.8 + 59.4;
-// 102 MB that need no scaling 17.5 + 4.4 | 17.9 + 5.8 | 17.5 + 7.5; 201 MB bf16 31.4 | 33.0 | 31.5, 608 MB 97 | 96 | 92.
+// hold at a time (three of eight wavefronts, by their registers), twice as many from kClipOnceBytes on.  Clipping and the norm alone
+// have the same number for a list, so that both add in one order.  Us, norm + scaling behind it, or norm alone, 768 blocks | 1024 |
+// 1536: 50 MB fp32 9.3 + 15.4 | 11.8 + 15.4, 202 MB 34.5 + 58.5 | 35.8 + 59.4; 102 MB that need no scaling 17.5 + 4.4 | 17.9 + 5.8 |
+// 17.5 + 7.5; 201 MB bf16 31.4 | 33.0 | 31.5, 608 MB 97 | 96 | 92.  Between, whole calls, 768 | 1536: clipping 270 MB 125 | 128,
+// 403 MB 187 | 200; norm alone 270 MB 42.5 | 43.6, 403 MB 62.4 | 64.4, bf16 43.5 | 43.9, 65.1 | 64.8.
 constexpr uint32_t kNormFit = 768, kNormBlocks = 1536;
 // Lists of this many bytes and more do not stay in the 256 MB cache from one launch to the next: a norm alone reads them as data
 // that nobody wants again, and clipping, which reads them twice, from the larger bound on.  Clipping has then kClipBlocks (each

@@ -287,3 +287,15 @@ def test_a_table_keeps_its_buffers(gact):
     del g
     assert torch.zeros(1 << 20, device="cuda").data_ptr() != at
     assert bufs[0].g == at
+
+
+@pytest.mark.parametrize("kinds", (("f32",), ("bf16",), ("f32", "bf16")), ids=str)
+@pytest.mark.parametrize("mb", (250, 270, 300, 400, 450, 470))
+def test_the_norm_is_the_same_in_every_call(gact, mb, kinds):
+    """Bit for bit, below, between and above the sizes at which the launches change: its order depends on the list alone."""
+    each = mb * 1_000_000 // sum(4 if t == "f32" else 2 for t in kinds)
+    g = grads((each + 1,) * len(kinds), kinds, mb, scale=1.0, odd=True)
+    norm = gact.gact_grad_norm(g)
+    assert abs(float(norm) - norm_of(g, 2)) <= 1e-11 * float(norm)
+    assert torch.equal(gact.gact_grad_clip(g, 1e9), norm)
+    assert torch.equal(gact.gact_grad_clip(g, 1.0, outs=[torch.empty_like(t) for t in g]), norm)

@@ -245,13 +245,15 @@ struct Angles {
             for (int i = 0; i < 4; ++i) { c[k + i] = cc[i]; s[k + i] = HALVES && !turn.second ? -ss[i] : ss[i]; }
         }
     }
-    // v turned by the angles (BACK: by their negatives)
+    // v turned by the angles (BACK: by their negatives); behind rot it stays, infinities too, which 0 times would make NaN.
+    // (A lane's partner is turned as it is.)
     template <bool BACK>
-    __device__ __forceinline__ void turn(float (&v)[8], int partner) const {
+    __device__ __forceinline__ void turn(float (&v)[8], const Turn<HALVES>& at) const {
+        if (!at.turned) return;
         if (HALVES) {
             float p[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) p[k] = lane_read(v[k], partner);
+            for (int k = 0; k < 8; ++k) p[k] = lane_read(v[k], at.partner);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = __builtin_fmaf(BACK ? -p[k] : p[k], s[k % N], v[k] * c[k % N]);
         } else {
@@ -473,7 +475,7 @@ __device__ __forceinline__ void heads_run(const HeadArgs& a, const HeadPart& p, 
                 ss = __builtin_fmaf(v[k], v[k], ss);
                 n[k] = v[k] * w[k];
             }
-            angles.template turn<false>(n, turn.partner);
+            angles.template turn<false>(n, turn);
             ss = add_over(ss, lanes);
             const float rstd = __builtin_amdgcn_rsqf(__builtin_fmaf(ss, a.inv_dim, a.eps));
 #pragma unroll
@@ -579,7 +581,7 @@ __device__ __forceinline__ void backward_run(const HeadArgs& a, const HeadPart& 
             widen8<DT>(in.dy, dn);
             if constexpr (BITS != 0) decompress8<BITS>(in.codes, in.mn, in.step, x);
             else widen8<DT>(in.x, x);
-            angles.template turn<true>(dn, turn.partner);
+            angles.template turn<true>(dn, turn);
             // r g and r mean(g x)
             float g[8];
 #pragma unroll

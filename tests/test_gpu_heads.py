@@ -417,3 +417,43 @@ def test_calls_whose_tensors_do_not_belong_together(gact):
         gact.gact_head_norm_rotate(*args, context=[gact.make_head_context(x, 4, 256, 1) for x in (q, k)])              # 2 * 64 < 256
     with pytest.raises(gact.GactError):
         gact.gact_head_norm_rotate(*args, eps=0.0)
+
+
+@pytest.mark.parametrize("interleaved", (False, True))
+@pytest.mark.parametrize("case", [(64, 0, "f32", 32), (64, 32, "bf16", 32), (64, 48, "f32", 4), (80, 16, "bf16", 2), (256, 64, "f32", 8),
+                                  (96, 96, "bf16", 32)], ids=str)
+def test_infinities_go_where_the_formula_has_them(gact, case, interleaved):
+    """In elements that are not rotated an infinite gradient reaches its own weight's gradient and, through the mean, its row,
+    not the element beside it; in rotated ones its pair.  The same for infinite inputs, of which the others' norm is 0."""
+    D, rot, dtype, bits = case
+    q, k, cos, sin, wq, wk, pos = inputs((1, 5, 2, 2, D, rot, dtype, "f32", interleaved), 1)
+    cos, sin = (cos.abs() + 0.1, sin.abs() + 0.1) if rot else (None, None)      # no turn by 0: 0 times infinity is NaN there
+    ctx = tuple(gact.make_head_context(x, bits, 0 if bits == 32 else 160 if D == 80 else 64, 3) for x in (q, k))
+    gact.gact_head_norm_rotate(q, k, cos, sin, wq, wk, pos, interleaved=interleaved, context=ctx)
+    f = Formula(q, wq, cos, sin, pos, interleaved)
+    held = f.x
+    if bits != 32:
+        held = gact.gact_decompress(ctx[0].packed, ctx[0].gmin, ctx[0].gscale, q.numel(), ctx[0].group_size, bits).view(q.shape).double()
+    for at in {0, rot // 2, max(rot - 1, 0), rot % D, D - 2, D - 1}:
+        dy = randn(90, *q.shape, dtype=q.dtype)
+        dy[0, 2, 1, at] = -math.inf
+        dx, _, dw, _ = gact.gact_head_norm_rotate_backward(dy, None, cos, sin, wq, wk, pos, context=ctx, x=(q, k), interleaved=interleaved)
+        dn, xr = f.turned(dy.double(), back=True), held * f.r
+        g = dn * f.w
+        want_w, want = (dn * xr).sum((0, 1, 2)), f.r * (g - xr * (g * xr).mean(-1, keepdim=True))
+        for got, ref in ((dw, want_w), (dx, want)):
+            assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.isinf(), ref.isinf()), at
+            inf = ref.isinf()
+            assert torch.equal(got[inf].double(), ref[inf]) and (~ref.isfinite()).any()
+        rest = want_w.isfinite()
+        assert rest.sum() == D - (1 if at >= rot else 2)
+        size = (f.turned(dy.double(), back=True, magnitude=True) * xr.abs()).sum((0, 1, 2))
+        assert ((dw.double() - want_w).abs() <= 301 * U * size)[rest].all()
+        x = q.clone()
+        x[0, 2, 1, at] = math.inf
+        y, _ = gact.gact_head_norm_rotate(x, None, cos, sin, wq, None, pos, interleaved=interleaved)
+        nan = torch.zeros(D, dtype=torch.bool, device="cuda")
+        nan[at] = True
+        if at < rot:
+            nan[at ^ 1 if interleaved else (at + rot // 2) % rot] = True
+        assert torch.equal(y[0, 2, 1].isnan(), nan) and (y[0, 2, 1][~nan] == 0).all()

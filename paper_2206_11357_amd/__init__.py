@@ -721,7 +721,12 @@ class HeadContext:
         self.blob = x.new_empty(packed + 2 * meta + 4 * rows, dtype=torch.uint8)
 
     def filled(self, blob: torch.Tensor) -> "HeadContext":
-        """The same layout over a buffer that the forward pass has filled (and that was kept apart from it)."""
+        """The same layout over a buffer that the forward pass has filled (and that was kept apart from it: what keeps it may
+        hand back another, made again with other widths)."""
+        rows = math.prod(self.shape[:-1])
+        if blob.dtype != torch.uint8 or blob.numel() != self.off[3] + 4 * rows or not blob.is_contiguous() \
+                or blob.get_device() != self.device:
+            raise ValueError("the buffer is not this context's")
         c = HeadContext.__new__(HeadContext)
         c.bits, c.group_size, c.seed, c.shape, c.device, c.groups, c.off = \
             self.bits, self.group_size, self.seed, self.shape, self.device, self.groups, self.off

@@ -315,7 +315,11 @@ class Controller:
                 bits[j], seeds[j] = self.bits_of(index), self.seed_of(index)
             else:
                 x[j] = x[j].contiguous()
-        return head_norm_rotate(*x, cos, sin, wq, wk, positions, eps, interleaved, by_head, bits, self.group_size, seeds, _own=own)
+        if own[0] == own[1] or q.shape[:-2] != k.shape[:-2] or q.dtype != k.dtype:      # (the last two are refused)
+            return head_norm_rotate(*x, cos, sin, wq, wk, positions, eps, interleaved, by_head, bits, self.group_size, seeds,
+                                    _own=all(own))
+        return tuple(head_norm_rotate(x[j], None, cos, sin, (wq, wk)[j], None, positions, eps, interleaved, by_head, (bits[j], 0),
+                                      self.group_size, (seeds[j], 0), _own=own[j])[0] for j in range(2))
 
     def clip_grad_norm_(self, params: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float,
                         norm_type: float = 2.0) -> torch.Tensor:

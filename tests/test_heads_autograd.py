@@ -68,7 +68,7 @@ def test_contexts_go_with_the_backward_pass(monkeypatch, bits, own, hooked):
     def loss_of():
         projected = leaf * 2.0                          # what queries and keys are views of
         kept.append(StorageWeakRef(projected.untyped_storage()))
-        y = heads.head_norm_rotate(projected[:, :, :4], projected[:, :, 4:], t, t, bits=bits, group_size=32, _own=(own, own))
+        y = heads.head_norm_rotate(projected[:, :, :4], projected[:, :, 4:], t, t, bits=bits, group_size=32, _own=own)
         return y[0].sum() + y[1].sum()
     with torch.autograd.graph.saved_tensors_hooks(lambda x: x, lambda x: x) if hooked else contextlib.nullcontext():
         loss = loss_of()
@@ -92,7 +92,7 @@ def test_modified_queries_are_noticed_with_and_without_hooks(monkeypatch, hooked
         q, k = leaf * 1.0, leaf * 2.0
         q.add_(1.0)                                     # before: of no account
         with torch.autograd.graph.saved_tensors_hooks(lambda x: x, lambda x: x) if hooked else contextlib.nullcontext():
-            y = heads.head_norm_rotate(q, k, t, t, _own=(True, True))
+            y = heads.head_norm_rotate(q, k, t, t, _own=True)
         if modified:
             with torch.no_grad():
                 k.add_(1.0)
@@ -100,14 +100,34 @@ def test_modified_queries_are_noticed_with_and_without_hooks(monkeypatch, hooked
                 (y[0].sum() + y[1].sum()).backward()
         else:
             (y[0].sum() + y[1].sum()).backward()
-    # hooks that keep a copy: what they give back is what was there
+    # also behind hooks that would keep copies: a scheme's contexts go past them
     q, k = leaf * 1.0, leaf * 2.0
-    q.add_(1.0)
     with torch.autograd.graph.saved_tensors_hooks(lambda x: x.clone(), lambda x: x):
-        y = heads.head_norm_rotate(q, k, t, t, _own=(True, True))
+        y = heads.head_norm_rotate(q, k, t, t, _own=True)
     with torch.no_grad():
         q.add_(1.0)
-    (y[0].sum() + y[1].sum()).backward()
+    with pytest.raises(RuntimeError):
+        (y[0].sum() + y[1].sum()).backward()
+
+
+def test_a_buffer_of_another_layout_is_refused(monkeypatch):
+    """A region that is computed again in the backward pass can come with other widths, and hooks can hand back anything: what
+    does not hold this context is not read by its layout."""
+    x = torch.zeros(1, 4, 2, 32)
+    c = gact.make_head_context(x, 4, 32, 1)
+    assert c.filled(c.blob.clone()).off == c.off
+    for bad in (gact.make_head_context(x, 2, 32, 1).blob, gact.make_head_context(x, 8, 32, 1).blob, gact.make_head_context(x).blob,
+                c.blob[:-1], c.blob.float(), torch.empty(2 * c.blob.numel(), dtype=torch.uint8)[::2], c.blob[:0]):
+        with pytest.raises(ValueError):
+            c.filled(bad)
+    assert gact.make_head_context(x[:0], 4, 32, 1).filled(gact.make_head_context(x[:0], 4, 32, 1).blob).blob.numel() == 0
+    # through autograd
+    monkeypatch.setattr(heads, "gact_head_norm_rotate", lambda q, k, *a, **kw: (torch.ones_like(q), torch.ones_like(k)))
+    q, t = torch.zeros(1, 4, 2, 32, requires_grad=True), torch.zeros(4, 16)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t[:-16] if t.dtype == torch.uint8 else t):
+        y = heads.head_norm_rotate(q, q, t, t, bits=(4, 4), group_size=32)
+    with pytest.raises(ValueError):
+        y[0].sum().backward()
 
 
 @pytest.mark.gpu
@@ -153,3 +173,30 @@ def test_each_of_queries_and_keys_is_compressed(gact, Hq, Hk, D, G, dtype):
     with torch.no_grad():
         assert torch.equal(ctl.head_norm_rotate(leaf[:, :, :Hq], leaf[:, :, Hq:], cos, sin, *w)[0], zq)
     assert len(ctl._handles) == before
+
+
+@pytest.mark.gpu
+def test_a_region_that_is_computed_twice(gact):
+    """Under activation checkpointing the backward pass numbers the contexts anew; widths and seeds are those of the forward
+    pass all the same, and so are the gradients."""
+    from torch.utils.checkpoint import checkpoint
+    from paper_2206_11357_amd.hooks import Controller
+    g = torch.Generator("cuda").manual_seed(1)
+    leaves = [torch.randn(2, 16, 4, 64, device="cuda", generator=g).requires_grad_(True) for _ in range(2)]
+    angle = torch.rand(16, 32, device="cuda", generator=g)
+    ctl = Controller(group_size=64, bits=4, seed=1, min_numel=16)
+
+    def layer(q, k):
+        q, k = ctl.head_norm_rotate(q * 1.0, k * 1.0, angle.cos(), angle.sin())
+        return q * k, k
+
+    def grads(run):
+        ctl.set_iteration(0)
+        ctl.begin_iteration()
+        q, k = run(*run(*leaves))
+        return torch.autograd.grad((q ** 2).sum() + (k ** 3).sum(), leaves)
+    for bits in ({}, {0: 8, 1: 2, 2: 1, 3: 32, 4: 1, 5: 4, 6: 2, 7: 8}):
+        ctl.bits = bits
+        want = grads(layer)
+        for a, b in zip(grads(lambda q, k: checkpoint(layer, q, k, use_reentrant=False)), want):
+            assert torch.equal(a, b)

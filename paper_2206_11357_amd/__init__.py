@@ -611,14 +611,14 @@ def make_grad_bufs(g: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tens
         raise ValueError("the tensors of a call lie on different devices")
     arr = _grad_table_type(len(g))()
     arr.g, arr.outs = g, outs
-    for b, a, o in zip(arr, g, outs):
+    arr.g_at = list(map(_address, g))
+    arr.outs_at = arr.g_at if outs is g else list(map(_address, outs))
+    for b, a, o, at, out_at in zip(arr, g, outs, arr.g_at, arr.outs_at):
         if not _dense(a):
             raise ValueError("gact needs contiguous tensors")
         if not _alike(o, a):
             raise ValueError("a buffer and its output differ in size, dtype or strides")
-        b.g, b.out, b.n, b.dtype = a.data_ptr(), o.data_ptr(), a.numel(), dtype_code(a.dtype)
-    arr.g_at = list(map(_address, g))
-    arr.outs_at = arr.g_at if outs is g else list(map(_address, outs))
+        b.g, b.out, b.n, b.dtype = at, out_at, a.numel(), dtype_code(a.dtype)
     return arr
 
 

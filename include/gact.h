@@ -294,9 +294,10 @@ int gact_compress_footprint_noalloc(const void *d_x, gact_dtype dtype, int64_t n
 /*
  * Global norm of a list of gradient buffers, and clipping by it.
  *     norm = sqrt(sum g^2)  (GACT_NORM_2)   or   max |g|  (GACT_NORM_INF), over all buffers together,
- *     out  = g * min(1, max_norm / (norm + 1e-6)),   rounded once to the buffer's type,
- * the squares added in binary64 in an order that depends on the list's sizes, types and alignments only, in every call.  A NaN among the
- * gradients gives a NaN norm and NaN outputs; an infinity gives an infinite norm and outputs 0 (NaN at its place).
+ *     out  = g * min(1, max_norm / (norm + 1e-6)),   from binary64 rounded to nearest, a bf16 result by way of binary32
+ *                                                    (off by half a step of bf16 and 2^-24 of the value, at most),
+ * the squares added in binary64 in an order that depends on the list's sizes, types and alignments only, the same in every call.  A
+ * NaN among the gradients gives a NaN norm and NaN outputs; an infinity gives an infinite norm and outputs 0 (NaN at its place).
  *   gact_grad_norm     d_norm receives the norm
  *   gact_grad_clip     the same, and the scaled gradients in two launches
  *   gact_grad_clip_by  scales by the norm in d_norm: one that several ranks have agreed on, or the square root

@@ -3,16 +3,17 @@
 //   norm = sqrt(sum g^2) or max |g| over all buffers,   out = g min(1, max_norm / (norm + 1e-6))
 //
 // Bound by HBM: the norm reads every element once, clipping reads and writes it once more, unless nothing has to be
-// scaled in place.  A launch is at most 1536 blocks, each with a run of neighbouring 16 KB chunks, so that a call
-// leaves at most 1536 results whatever its size.  That is few enough for every block of the scaling launch to add them
+// scaled in place.  The norm's launch is at most 1536 blocks (scaling has up to 8192), each with a run of neighbouring 16 KB
+// chunks, so that it leaves at most 1536 results whatever the list's size.  That is few enough for every block of the scaling launch to add them
 // up itself, in the same order: clipping is two launches, with no third one between them, no counter that would have
 // to start at zero and no block that waits for another, and can be captured into a graph as it is.  (A norm alone has a
 // second launch of one block.)  The squares are added in binary64: a sum of 10^9 of them in binary32 would lose what clipping
 // compares.
 //
 // Us and TB/s: norm of 101 M bf16 elements 31.4 (6.4), of 304 M at odd addresses 92 (6.6), of 302 M fp32 178 (6.8);
-// scaling 302 M fp32 behind it 434 (5.6), 101 M bf16 by a given norm 59 (6.8).  A large read reaches 6.8, a copy 5.0.  Lists of
-// less than some MB: 3.3 + 4.1, what two launches take.
+// scaling 302 M fp32 behind it 430 (5.6), 101 M bf16 by a given norm 59 (6.8).  A large read reaches 7.0; a copy what the cache lets
+// it, 6.8 for 200 MB, 5.7 for 400 MB, 5.3 for 1.2 GB, 5.0 for 4 GB, all fp32.  Lists of less than some MB: 3.3 + 4.1, what two
+// launches take.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

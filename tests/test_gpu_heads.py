@@ -457,3 +457,33 @@ def test_infinities_go_where_the_formula_has_them(gact, case, interleaved):
         if at < rot:
             nan[at ^ 1 if interleaved else (at + rot // 2) % rot] = True
         assert torch.equal(y[0, 2, 1].isnan(), nan) and (y[0, 2, 1][~nan] == 0).all()
+
+
+@pytest.mark.parametrize("expand", ((3, -1, -1, -1), (-1, 16, -1, -1), (-1, -1, 8, -1)), ids=str)
+@pytest.mark.parametrize("bits", (32, 4))
+def test_inputs_whose_rows_share_memory(gact, expand, bits):
+    """Queries, keys and gradients expanded over the batch, the tokens or the heads: read as if they were copies."""
+    B, S, H, D = 3, 16, 8, 64
+    cos, sin = tables(S, D)
+    w = [randn(5 + j, D, scale=0.3) + 1 for j in range(2)]
+    q, k = (randn(j, *(1 if e != -1 else n for e, n in zip(expand, (B, S, H, D))), dtype=torch.bfloat16).expand(B, S, H, D) for j in range(2))
+    dy = [randn(7 + j, *(1 if e != -1 else n for e, n in zip(expand, (B, S, H, D))), dtype=torch.bfloat16).expand(B, S, H, D) for j in range(2)]
+    got, want = [], []
+    for results, x, d in ((got, (q, k), dy), (want, [t.contiguous() for t in (q, k)], [t.contiguous() for t in dy])):
+        ctx = [gact.make_head_context(t, bits, 0 if bits == 32 else 64, 1 + j) for j, t in enumerate(x)]
+        results += gact.gact_head_norm_rotate(*x, cos, sin, *w, context=ctx)
+        results += gact.gact_head_norm_rotate_backward(*d, cos, sin, *w, context=ctx, x=x)
+        results += [c.packed for c in ctx]
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    with pytest.raises((gact.GactError, ValueError)):
+        gact.gact_head_norm_rotate(q, k, cos, sin, *w, out=(q, k))
+    if bits == 32:
+        leaf = q[tuple(slice(0, 1) if e != -1 else slice(None) for e in expand)].clone().requires_grad_(True)
+        from paper_2206_11357_amd import heads
+        y, _ = heads.head_norm_rotate(leaf.expand(B, S, H, D), k, cos, sin, *w)
+        y.backward(dy[0])
+        full = want[2].double().sum([i for i, e in enumerate(expand) if e != -1], keepdim=True)
+        size = want[2].double().abs().sum([i for i, e in enumerate(expand) if e != -1], keepdim=True)
+        # at most 16 rows added in binary32, rounded once
+        assert ((leaf.grad.double() - full).abs() <= 2.0 ** -8 * full.abs() * 1.001 + 16 * U * size).all()

@@ -17,9 +17,9 @@
 // in binary32: dn x^ r and the first term of dx are then linear in x^, so that the rounding noise leaves their
 // expectation where it is (Sec. 3.1 asks it of the compressor); from x^ itself r would be biased.
 //
-// Us and TB/s of what is read and written: 8192 tokens of 32 + 8 heads of 128, bf16, head by head 28.2 (5.9); with 4-bit
-// contexts, 32768 tokens 170 (4.5), backward 150 (5.2); 8192 tokens of 16 + 16 of 64, 21.6 (3.5) and 15.9 (4.8); fp32, 12608
-// of 16 + 16 of 64, 2 bits 44.7 (4.9) and 46.9 (4.7).  A copy reaches 6.8 where the cache holds its 200 MB, 5.7 for 400 MB, 5.0 for
+// Us and TB/s of what is read and written: 8192 tokens of 32 + 8 heads of 128, bf16, head by head 28.5 (5.9); with 4-bit
+// contexts, 32768 tokens 167 (4.6), backward 150 (5.2); 8192 tokens of 16 + 16 of 64, 21.6 (3.5) and 15.8 (4.9); fp32, 12608
+// of 16 + 16 of 64, 2 bits 44.4 (4.9) and 47.0 (4.7).  A copy reaches 6.8 where the cache holds its 200 MB, 5.7 for 400 MB, 5.0 for
 // 4 GB.  The compressing forward pass in bf16 is bound by its arithmetic, the noise and the rounding: without them 150 us of the 167.
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -428,6 +428,33 @@ int gact_head_norm_rotate_backward(const gact_heads *h_parts, int n_parts, const
                                    void *d_workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Weight gradient of a linear layer y = x W^T + b from the compressed context of its input, which is not decompressed
+ * to memory:
+ *     dW[n, k] = sum over t of dy[t, n] * x^[t, k],      db[n] = sum over t of dy[t, n],
+ * x^ being what gact_decompress gives of the context in dy's type (x laid out contiguously as [tokens, in_features];
+ * groups may pass from row to row).  Sums in binary32, over blocks and splits of the tokens in a fixed order, the same
+ * in every call of the same sizes and types; outputs rounded once.
+ *   d_dy         [tokens, out_features], its rows' elements consecutive, dy_stride elements from row to row (any value,
+ *                0 too: a gradient that all tokens share), aligned as its type
+ *   d_packed, d_gmin, d_gscale, group_size, bits   as gact_compress has left them
+ *   d_dw         out  [out_features, in_features], contiguous, of w_dtype
+ *   d_db         out  [out_features] of w_dtype, or NULL: not wanted.  Outputs overlap nothing.
+ *   d_workspace  device scratch, >= gact_linear_weight_grad_workspace_bytes(...) bytes of the same sizes (which may be 0),
+ *                16-byte aligned, in use until the enqueued kernels have run; calls that share one must not overlap in time.
+ * tokens == 0 writes zeros; out_features == 0 or in_features == 0 is GACT_OK and writes nothing but db.  Each size must be
+ * below 2^31, tokens * in_features below 2^35 and out_features * in_features below 2^38.  An infinity or NaN
+ * in a row of dy reaches that row's columns of dW (rows of x^ times it), in a group's minimum or step the elements of
+ * that group.  Can be captured into a HIP graph.
+ */
+size_t gact_linear_weight_grad_workspace_bytes(int64_t tokens, int64_t out_features, int64_t in_features,
+                                               gact_dtype dtype);
+
+int gact_linear_weight_grad(const void *d_dy, int64_t dy_stride, gact_dtype dtype, int64_t tokens, int64_t out_features,
+                            int64_t in_features, const void *d_packed, const float *d_gmin, const float *d_gscale,
+                            int group_size, int bits, void *d_dw, void *d_db, gact_dtype w_dtype, void *d_workspace,
+                            size_t workspace_bytes, void *stream);
+
+/*
  * Variance alert (host only): V(b) = sum_l c_l S(b_l) (Thm. 2) against the
  * gradient variance.  Writes V / grad_var to *h_ratio (may be NULL) and
  * returns 1 if it exceeds `threshold`, 0 if not, a negative code on error.

@@ -45,6 +45,7 @@ EXPORTS = (
     "gact_compress_footprint_workspace_bytes", "gact_compress_footprint_noalloc", "gact_copy_bounded",
     "gact_grad_norm_workspace_bytes", "gact_grad_norm", "gact_grad_clip", "gact_grad_clip_by",
     "gact_head_norm_rotate_workspace_bytes", "gact_head_norm_rotate", "gact_head_norm_rotate_backward",
+    "gact_linear_weight_grad_workspace_bytes", "gact_linear_weight_grad",
 )
 GACT_BITS_UNCOMPRESSED = 32
 
@@ -148,6 +149,10 @@ def _load() -> ctypes.CDLL:
     lib.gact_head_norm_rotate.restype = i32
     lib.gact_head_norm_rotate_backward.argtypes = [vp, i32, vp, vp, sz, vp]
     lib.gact_head_norm_rotate_backward.restype = i32
+    lib.gact_linear_weight_grad_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.gact_linear_weight_grad_workspace_bytes.restype = sz
+    lib.gact_linear_weight_grad.argtypes = [vp, i64, i32, i64, i64, i64, vp, vp, vp, i32, i32, vp, vp, i32, vp, sz, vp]
+    lib.gact_linear_weight_grad.restype = i32
     return lib
 
 
@@ -1021,3 +1026,76 @@ def _backward_part(dy, x, dx, w, dw, c: HeadContext, H: int) -> bytes:
         a_x, strides = x.data_ptr(), _head_strides(x)
     return _HEADS.pack(a_x, 0, dy.data_ptr(), dx.data_ptr(), 0 if w is None else w.data_ptr(), 0 if dw is None else dw.data_ptr(),
                        rstd, packed, gmin, gscale, *strides, 0, 0, 0, *_head_strides(dy), *_head_strides(dx), seed, H, bits)
+
+
+# ------------------------------------------- weight gradient of a linear layer
+@functools.lru_cache(maxsize=256)
+def gact_linear_weight_grad_workspace_bytes(tokens: int, out_features: int, in_features: int, dtype: torch.dtype) -> int:
+    return int(lib.gact_linear_weight_grad_workspace_bytes(tokens, out_features, in_features, dtype_code(dtype)))
+
+
+def _rows(x: torch.Tensor) -> Tuple[int, int]:
+    """(rows, elements from row to row) of [..., features] whose leading axes are one."""
+    shape, st = x.shape, x.stride()
+    if len(shape) < 2:
+        raise ValueError("gact needs [..., features]")
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError("a row's elements must be consecutive")
+    rows, stride = 1, None
+    for size, s in zip(reversed(shape[:-1]), reversed(st[:-1])):
+        if size != 1:
+            if stride is None:
+                stride = s
+            elif s != rows * stride:
+                raise ValueError("the rows must be evenly spaced")
+            rows *= size
+    return rows, shape[-1] if stride is None else stride
+
+
+def _weight_buffers(dy, dw, db, workspace, N: int, K: int, w_dtype, bias: bool, need: int):
+    if dw is None:
+        dw = dy.new_empty((N, K), dtype=w_dtype)
+    if bias and db is None:
+        db = dy.new_empty(N, dtype=w_dtype)
+    if workspace is None and need:
+        workspace = dy.new_empty(need, dtype=torch.uint8)
+    return dw, db, workspace
+
+
+def gact_linear_weight_grad(dy: torch.Tensor, packed: torch.Tensor, gmin: torch.Tensor, gscale: torch.Tensor, in_features: int,
+                            group_size: int, bits: int, w_dtype: Optional[torch.dtype] = None, bias: bool = False,
+                            dw: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None,
+                            workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dW, db) of a linear layer from dy, [..., out_features] with evenly spaced rows, and its input's context as
+    gact_compress has left it, read as codes.  w_dtype: of the gradients (dy's without); db is None unless `bias`."""
+    T, stride = _rows(dy)
+    N, K = dy.shape[-1], in_features
+    device = _same_device(dy, packed, gmin, gscale, dw, db, workspace)
+    dtype = dtype_code(dy.dtype)
+    if w_dtype is None:
+        w_dtype = dy.dtype if dw is None else dw.dtype
+    if K < 0 or gmin.dtype is not torch.float32 or gscale.dtype is not torch.float32 \
+            or not (packed.is_contiguous() and gmin.is_contiguous() and gscale.is_contiguous()):
+        raise ValueError("the context must be contiguous: packed codes, float32 minima and steps")
+    groups = -(-T * K // group_size) if group_size > 0 else 0
+    if packed.nbytes < (T * K * bits + 127 >> 7) * 16 or gmin.numel() < groups or gscale.numel() < groups:
+        raise ValueError("the context holds fewer elements than the layer's input has")
+    if dw is not None and (tuple(dw.shape) != (N, K) or dw.dtype is not w_dtype or not dw.is_contiguous()):
+        raise ValueError("dw must be contiguous, [out_features, in_features], of w_dtype")
+    if not bias:
+        db = None
+    elif db is not None and (db.numel() != N or db.dtype is not w_dtype or not db.is_contiguous()):
+        raise ValueError("db must be contiguous, one per output feature, of w_dtype")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    need = gact_linear_weight_grad_workspace_bytes(T, N, K, dy.dtype)
+    if stream is None:
+        dw, db, workspace = _weight_buffers(dy, dw, db, workspace, N, K, w_dtype, bias, need)
+    else:
+        with _allocating_for(stream, device):
+            dw, db, workspace = _weight_buffers(dy, dw, db, workspace, N, K, w_dtype, bias, need)
+    _enqueue(lib.gact_linear_weight_grad, "gact_linear_weight_grad", device, stream, dy.data_ptr(), stride, dtype, T, N, K,
+             packed.data_ptr(), gmin.data_ptr(), gscale.data_ptr(), group_size, bits, dw.data_ptr(),
+             None if db is None else db.data_ptr(), dtype_code(w_dtype),
+             *(workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0))
+    return dw, db

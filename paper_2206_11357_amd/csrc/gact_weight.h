@@ -1,0 +1,78 @@
+// Records of the weight gradient's kernels (gact_weight.hip), filled by its entry point.
+#ifndef GACT_WEIGHT_H
+#define GACT_WEIGHT_H
+
+#include <stdint.h>
+
+#include "gact_device.h"
+#include "gact_heads.h"
+
+namespace gact {
+
+// A block's tile of dW, n x k, and the tokens that it takes from memory at a time.
+struct WeightTile {
+    int n, k, tokens;
+};
+constexpr int kWeightThreads = 256;
+constexpr int kWeightTiles = 2;
+constexpr WeightTile weight_tile(int dtype, int which) {
+    return which == 0 ? WeightTile{256, 128, dtype == GACT_DT_F32 ? 16 : 32} : WeightTile{64, 64, dtype == GACT_DT_F32 ? 16 : 32};
+}
+
+struct WeightArgs {
+    const uint8_t* dy;
+    const uint8_t* packed;
+    const float*   gmin;
+    const float*   gscale;
+    void*          dw;
+    void*          db;                  // null: not wanted
+    float*         partial;             // [splits][N][K]; null with one split
+    float*         db_partial;          // [splits * db_every][N]; null: one block a tile of rows writes db
+    int64_t        dy_stride;           // elements from token to token
+    uint32_t       T, N, K;
+    uint64_t       last_word;           // of the packed string
+    uint32_t       last_group;
+    uint32_t       group;
+    Divisor        by_group;            // of an element's number / 32 by group / 32
+    uint32_t       tiles_n, tiles_k, splits;
+    uint32_t       chunks;              // of a split
+    uint32_t       db_every;            // a block adds every so many-th chunk to db
+    int32_t        w_f32;
+};
+
+inline uint64_t weight_up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+struct WeightPlan {
+    int which;
+    uint32_t tiles_n, tiles_k, chunks, splits, db_every;
+    bool db_apart;
+};
+inline WeightPlan plan_weight(uint64_t T, uint64_t N, uint64_t K, int dtype) {
+    WeightPlan p{};
+    p.which = N > 128 && K > 64 && T * N * K >= (uint64_t)1 << 28 ? 0 : 1;
+    const WeightTile tile = weight_tile(dtype, p.which);
+    p.tiles_n = (uint32_t)weight_up(N, (uint64_t)tile.n);
+    p.tiles_k = K ? (uint32_t)weight_up(K, (uint64_t)tile.k) : 1;      // (K = 0: db alone)
+    const uint64_t tiles = (uint64_t)p.tiles_n * p.tiles_k, chunks = weight_up(T, (uint64_t)tile.tokens);
+    uint64_t splits = tiles >= 256 ? 1 : 512 / tiles;
+    const uint64_t most = chunks / 8 ? chunks / 8 : 1;
+    if (splits > most) splits = most;
+    p.chunks = (uint32_t)weight_up(chunks, splits);
+    p.splits = p.chunks ? (uint32_t)weight_up(chunks, p.chunks) : 1;
+    if (p.splits == 0) p.splits = 1;
+    p.db_apart = p.splits > 1;
+    p.db_every = p.db_apart ? p.tiles_k : 1;
+    return p;
+}
+inline size_t weight_partial_bytes(const WeightPlan& p, uint64_t N, uint64_t K) {
+    return p.splits > 1 ? (size_t)((p.splits * N * K * sizeof(float) + 15) & ~(uint64_t)15) : 0;
+}
+inline size_t weight_workspace_bytes(const WeightPlan& p, uint64_t N, uint64_t K) {
+    return weight_partial_bytes(p, N, K) + (p.db_apart ? (size_t)p.splits * p.db_every * N * sizeof(float) : 0);
+}
+
+}  // namespace gact
+
+extern "C" int gact_launch_weight(const gact::WeightArgs* a, int which, int dtype, int bits, void* stream);
+
+#endif

@@ -1,0 +1,380 @@
+// Weight gradient of a linear layer from the compressed context of its input, for MI355X (gfx950).
+//
+//   dW[n, k] = sum over t of dy[t, n] x^[t, k],   db[n] = sum over t of dy[t, n],   x^ = code * step + minimum
+//
+// A matrix product whose right operand is decoded on its way into shared memory: codes are read from HBM, never x^.
+// Both operands have the summed axis outermost.  bf16: rows of tokens in shared memory as they come, read transposed
+// (ds_read_b64_tr_b16: four tokens of a column a lane), 32x32x16 products; fp32: 32x32x2 products, whose operands are a
+// row's elements as they lie.  A wavefront holds its part of dW in registers; the next tokens are on their way from
+// HBM meanwhile, and are decoded behind the products of the present ones.
+// The tokens are split over blocks where the tiles of dW are too few for the GPU; the splits' sums are added in a fixed
+// order by a second launch.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gact_codec.h"
+#include "gact_device.h"
+#include "gact_weight.h"
+
+namespace gact {
+
+typedef uint32_t w4 __attribute__((ext_vector_type(4)));
+typedef uint32_t w2 __attribute__((ext_vector_type(2)));
+typedef w4 w4_any2 __attribute__((aligned(2)));
+typedef w4 w4_any4 __attribute__((aligned(4)));
+typedef float wf4 __attribute__((ext_vector_type(4)));
+typedef float wf2 __attribute__((ext_vector_type(2)));
+typedef float wf16 __attribute__((ext_vector_type(16)));
+typedef short ws4 __attribute__((ext_vector_type(4)));
+typedef __bf16 wb8 __attribute__((ext_vector_type(8)));
+
+// ---------------------------------------------------------------- codes of x
+// Eight codes from element e on, and what they stand for.
+template <int BITS>
+struct Codes {
+    uint32_t lo, hi;
+    float mn[2], step[2];
+    uint32_t turn;                                     // the first of the eight that is of the next group; 8: none
+};
+template <int BITS, bool WHOLE>
+__device__ __forceinline__ Codes<BITS> load_x(const WeightArgs& a, uint64_t e) {
+    Codes<BITS> c;
+    const uint32_t g = divided((uint32_t)(e >> 5), a.by_group);
+    c.mn[0] = a.gmin[g];
+    c.step[0] = a.gscale[g];
+    c.hi = 0;
+    if (WHOLE) {                                       // e is a multiple of eight: whole bytes, one group
+        const uint8_t* p = a.packed + (e >> 3) * BITS;
+        if (BITS == 1) c.lo = *p;
+        if (BITS == 2) c.lo = *(const uint16_t*)p;
+        if (BITS == 4) c.lo = *(const uint32_t*)p;
+        if (BITS == 8) { const w2 w = *(const w2*)p; c.lo = w.x; c.hi = w.y; }
+        c.turn = 8;
+        c.mn[1] = c.mn[0];
+        c.step[1] = c.step[0];
+    } else {
+        const uint64_t end = (uint64_t)(g + 1) * a.group - e;
+        c.turn = end < 8 ? (uint32_t)end : 8u;
+        const uint32_t g1 = g < a.last_group ? g + 1 : g;
+        c.mn[1] = a.gmin[g1];
+        c.step[1] = a.gscale[g1];
+        const uint32_t* words = (const uint32_t*)a.packed;
+        const uint64_t bit = e * BITS;
+        const uint64_t i = bit >> 5, j = i < a.last_word ? i + 1 : i, l = j < a.last_word ? j + 1 : j;
+        const uint32_t s = (uint32_t)bit & 31u;
+        const uint32_t b = words[j];
+        c.lo = __builtin_amdgcn_alignbit(b, words[i], s);
+        if (BITS == 8) c.hi = __builtin_amdgcn_alignbit(words[l], b, s);
+    }
+    return c;
+}
+// their values in binary32, each operation rounded
+template <int BITS, bool WHOLE>
+__device__ __forceinline__ void decode_x(const Codes<BITS>& c, float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t word = BITS == 8 && j >= 4 ? c.hi : c.lo;
+        const uint32_t q = BITS == 8 ? word >> (8 * (j & 3)) & 0xFFu
+                         : BITS == 4 ? ((j & 1 ? word >> 4 : word) & 0x0F0F0F0Fu) >> (8 * (j >> 1)) & 0xFFu
+                         : word >> (j * BITS) & ((1u << BITS) - 1u);
+        const bool next = !WHOLE && (uint32_t)j >= c.turn;
+        const float t = (float)q * (next ? c.step[1] : c.step[0]);
+        x[j] = t + (next ? c.mn[1] : c.mn[0]);
+    }
+}
+
+// ------------------------------------------------------------------ the tiles
+template <int DT, int WHICH>
+struct Tiling {
+    static constexpr WeightTile tile = weight_tile(DT, WHICH);
+    static constexpr int BN = tile.n, BK = tile.k, BT = tile.tokens;
+    static constexpr int kSize = DT == GACT_DT_F32 ? 4 : 2;
+    static constexpr int kPiece = 16 / kSize;                       // elements of dy that a lane loads at a time
+    static constexpr int kRowPieces = BN / kPiece;
+    static constexpr int kPieces = BT * kRowPieces / kWeightThreads;
+    static constexpr int kRowBlocks = BK / 8;                       // blocks of eight elements of x
+    static constexpr int kBlocks = BT * kRowBlocks >= kWeightThreads ? BT * kRowBlocks / kWeightThreads : 1;
+    // Bytes from row to row in shared memory.  bf16: 64 more than a multiple of 256, so that the four rows of a
+    // transposed read lie in different banks.
+    static constexpr int kPad = DT == GACT_DT_F32 ? 0 : 64;
+    static constexpr int kRowN = BN * kSize + kPad, kRowK = BK * kSize + kPad;
+    static constexpr int kBufN = BT * kRowN, kBuf = kBufN + BT * kRowK;
+    static constexpr int TN = BN / 64, TK = BK / 64;                // 32 x 32 products of a wavefront, 2 x 2 of which share a tile
+    static_assert(kWeightThreads % kRowPieces == 0 && BT * kRowPieces % kWeightThreads == 0, "a thread stays in its column");
+};
+
+template <int DT, int BITS, int WHICH, bool WHOLE>
+__global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a) {
+    typedef Tiling<DT, WHICH> L;
+    constexpr int BN = L::BN, BK = L::BK, BT = L::BT, TN = L::TN, TK = L::TK;
+    __shared__ __align__(16) uint8_t lds[2][L::kBuf];
+    const uint32_t tid = threadIdx.x;
+    const int lane = (int)tid & 63, wave = (int)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
+
+    // Blocks of one XCD (every eighth) are neighbours in the order split, rows, columns: they share tokens in its L2.
+    const uint32_t total = gridDim.x, per = total >> 3, rest = total & 7u, xcd = blockIdx.x & 7u;
+    uint32_t b = xcd * per + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
+    const uint32_t tiles = a.tiles_n * a.tiles_k;
+    const uint32_t split = b / tiles;
+    b -= split * tiles;
+    const uint32_t tile_n = b / a.tiles_k, tile_k = b - tile_n * a.tiles_k;
+    const uint32_t n0 = tile_n * BN, k0 = tile_k * BK;
+    const uint32_t all = (a.T + BT - 1) / BT;
+    const uint32_t c0 = split * a.chunks, c1 = c0 + a.chunks < all ? c0 + a.chunks : all;
+
+    // ---- what a thread loads
+    const uint32_t pn = tid % L::kRowPieces, pt = tid / L::kRowPieces;
+    constexpr uint32_t kRows = kWeightThreads / L::kRowPieces;      // rows from piece to piece of a thread
+    const uint32_t n = n0 + pn * L::kPiece;
+    const uint32_t valid = n < a.N ? (a.N - n < (uint32_t)L::kPiece ? a.N - n : (uint32_t)L::kPiece) : 0;
+    const uint32_t bk = tid % L::kRowBlocks, bt = tid / L::kRowBlocks;
+    constexpr uint32_t kXRows = kWeightThreads / L::kRowBlocks;
+    const uint32_t k = k0 + bk * 8;
+    const bool x_thread = bt < (uint32_t)BT;
+
+    w4 dy[L::kPieces];
+    Codes<BITS> codes[L::kBlocks];
+    const auto fetch = [&](uint32_t chunk) {
+        const uint32_t t0 = chunk * BT;
+#pragma unroll
+        for (int q = 0; q < L::kPieces; ++q) {
+            const uint32_t t = t0 + pt + q * kRows;
+            w4 v = {0u, 0u, 0u, 0u};
+            if (t < a.T && valid != 0) {
+                const uint8_t* p = a.dy + ((int64_t)t * a.dy_stride + n) * L::kSize;
+                if (valid == (uint32_t)L::kPiece) {
+                    if (DT == GACT_DT_F32) v = *(const w4_any4*)p;
+                    else v = *(const w4_any2*)p;
+                } else {
+                    uint32_t h[8];
+#pragma unroll
+                    for (int j = 0; j < L::kPiece; ++j)
+                        h[j] = (uint32_t)j < valid ? (DT == GACT_DT_F32 ? ((const uint32_t*)p)[j] : ((const uint16_t*)p)[j]) : 0u;
+                    if (DT == GACT_DT_F32) v = w4{h[0], h[1], h[2], h[3]};
+                    else v = w4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4 % L::kPiece] | h[5 % L::kPiece] << 16,
+                                h[6 % L::kPiece] | h[7 % L::kPiece] << 16};
+                }
+            }
+            dy[q] = v;
+        }
+#pragma unroll
+        for (int q = 0; q < L::kBlocks; ++q) {
+            const uint32_t t = t0 + bt + q * kXRows;
+            codes[q] = Codes<BITS>{};
+            if (x_thread && t < a.T && k < a.K) codes[q] = load_x<BITS, WHOLE>(a, (uint64_t)t * a.K + k);
+        }
+    };
+    float sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+    const auto place = [&](uint8_t* buf, bool add) {
+#pragma unroll
+        for (int q = 0; q < L::kPieces; ++q) *(w4*)(buf + (pt + q * kRows) * L::kRowN + pn * 16) = dy[q];
+        if (add) {
+#pragma unroll
+            for (int q = 0; q < L::kPieces; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t v = dy[q][j];
+                    if (DT == GACT_DT_F32) sum[j] += __builtin_bit_cast(float, v);
+                    else {
+                        sum[2 * j] += __builtin_bit_cast(float, v << 16);
+                        sum[2 * j + 1] += __builtin_bit_cast(float, v & 0xFFFF0000u);
+                    }
+                }
+        }
+        if (x_thread) {
+#pragma unroll
+            for (int q = 0; q < L::kBlocks; ++q) {
+                float x[8];
+                decode_x<BITS, WHOLE>(codes[q], x);
+                uint8_t* p = buf + L::kBufN + (bt + q * kXRows) * L::kRowK + bk * (8 * L::kSize);
+                if (DT == GACT_DT_F32) {
+                    *(wf4*)p = wf4{x[0], x[1], x[2], x[3]};
+                    *(wf4*)(p + 16) = wf4{x[4], x[5], x[6], x[7]};
+                } else {
+                    *(w4*)p = w4{bf16_pair_rne(x[0], x[1]), bf16_pair_rne(x[2], x[3]), bf16_pair_rne(x[4], x[5]),
+                                 bf16_pair_rne(x[6], x[7])};
+                }
+            }
+        }
+    };
+
+    // ---- what a wavefront multiplies
+    const int wn = wave >> 1, wk = wave & 1;
+    wf16 acc[TN][TK];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TK; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    const auto multiply = [&](const uint8_t* buf) {
+        if constexpr (DT == GACT_DT_F32) {
+            // a lane's operands: TN (TK) neighbouring elements of row 2 s + lane / 32, one for each product
+            const uint8_t* pa = buf + (lane >> 5) * L::kRowN + (wn * 32 * TN + (lane & 31) * TN) * 4;
+            const uint8_t* pb = buf + L::kBufN + (lane >> 5) * L::kRowK + (wk * 32 * TK + (lane & 31) * TK) * 4;
+#pragma unroll
+            for (int s = 0; s < BT / 2; ++s) {
+                float x[TN], y[TK];
+                __builtin_memcpy(x, __builtin_assume_aligned(pa + 2 * s * L::kRowN, 4 * TN), 4 * TN);
+                __builtin_memcpy(y, __builtin_assume_aligned(pb + 2 * s * L::kRowK, 4 * TK), 4 * TK);
+#pragma unroll
+                for (int i = 0; i < TN; ++i)
+#pragma unroll
+                    for (int j = 0; j < TK; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[j], acc[i][j], 0, 0, 0);
+            }
+        } else {
+            // 16 lanes read 4 rows of 16 elements, of which each gets a column
+            const int row = 8 * (lane >> 5) + ((lane & 15) >> 2), col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+            const uint8_t* pa = buf + row * L::kRowN + (wn * 32 * TN + col) * 2;
+            const uint8_t* pb = buf + L::kBufN + row * L::kRowK + (wk * 32 * TK + col) * 2;
+            const auto column = [](const uint8_t* p, int stride) {
+                typedef __attribute__((address_space(3))) ws4* lds_ptr;
+                union { ws4 h[2]; wb8 v; } u;
+                u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+                u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * stride));
+                return u.v;
+            };
+#pragma unroll
+            for (int s = 0; s < BT / 16; ++s) {
+                wb8 x[TN], y[TK];
+#pragma unroll
+                for (int j = 0; j < TK; ++j) y[j] = column(pb + 16 * s * L::kRowK + 64 * j, L::kRowK);
+#pragma unroll
+                for (int i = 0; i < TN; ++i) x[i] = column(pa + 16 * s * L::kRowN + 64 * i, L::kRowN);
+#pragma unroll
+                for (int i = 0; i < TN; ++i)
+#pragma unroll
+                    for (int j = 0; j < TK; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
+            }
+        }
+    };
+
+    const bool with_db = a.db != nullptr && (a.db_partial || tile_k == 0);
+    const auto adds = [&](uint32_t chunk) { return with_db && chunk % a.db_every == (a.db_partial ? tile_k : 0); };
+    if (c0 < c1) {
+        fetch(c0);
+        place(lds[0], adds(c0));
+        __syncthreads();
+        for (uint32_t c = c0; c < c1; ++c) {
+            const uint32_t now = (c - c0) & 1u;
+            const bool more = c + 1 < c1;
+            if (more) fetch(c + 1);
+            multiply(lds[now]);
+            if (more) place(lds[now ^ 1u], adds(c + 1));
+            __syncthreads();
+        }
+    }
+
+    // ---- out: element r of a product is row (r & 3) + 8 (r >> 2) + 4 (lane / 32), column lane % 32
+    const bool whole = a.partial == nullptr;
+    float* part = whole ? nullptr : a.partial + (size_t)split * a.N * a.K;
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
+            const uint32_t on = n0 + (uint32_t)(wn * 32 * TN + (DT == GACT_DT_F32 ? row * TN + i : i * 32 + row));
+            if (on >= a.N) continue;
+#pragma unroll
+            for (int j = 0; j < TK; ++j) {
+                const uint32_t ok = k0 + (uint32_t)(wk * 32 * TK + (DT == GACT_DT_F32 ? (lane & 31) * TK + j : j * 32 + (lane & 31)));
+                if (ok >= a.K) continue;
+                const size_t o = (size_t)on * a.K + ok;
+                if (!whole) part[o] = acc[i][j][r];
+                else if (a.w_f32) ((float*)a.dw)[o] = acc[i][j][r];
+                else ((uint16_t*)a.dw)[o] = (uint16_t)bf16_pair_rne(acc[i][j][r], 0.0f);
+            }
+        }
+
+    if (!with_db) return;
+    // db of the tile's rows: over the threads of a column, in their order
+    float* col = (float*)lds[0];
+#pragma unroll
+    for (int j = 0; j < L::kPiece; ++j) col[pt * BN + pn * L::kPiece + j] = sum[j];
+    __syncthreads();
+    for (uint32_t i = tid; i < (uint32_t)BN; i += kWeightThreads) {
+        if (n0 + i >= a.N) continue;
+        float s = 0.0f;
+        for (uint32_t r = 0; r < kRows; ++r) s += col[r * BN + i];
+        if (a.db_partial) a.db_partial[((size_t)split * a.db_every + tile_k) * a.N + n0 + i] = s;
+        else if (a.w_f32) ((float*)a.db)[n0 + i] = s;
+        else ((uint16_t*)a.db)[n0 + i] = (uint16_t)bf16_pair_rne(s, 0.0f);
+    }
+}
+
+// dW and db from the splits' sums, added in their order: a thread four neighbouring elements of dW, or one of db.
+constexpr int kJoinThreads = 256;
+__device__ __forceinline__ void put_weight(void* p, int f32, size_t i, float v) {
+    if (f32) ((float*)p)[i] = v;
+    else ((uint16_t*)p)[i] = (uint16_t)bf16_pair_rne(v, 0.0f);
+}
+__global__ __launch_bounds__(kJoinThreads) void weight_join_kernel(WeightArgs a, uint32_t dw_blocks) {
+    const size_t n = (size_t)a.N * a.K;
+    if (blockIdx.x < dw_blocks) {
+        const size_t i = ((size_t)blockIdx.x * kJoinThreads + threadIdx.x) * 4;
+        if (i >= n) return;
+        if (n % 4 == 0) {
+            wf4 s = *(const wf4*)(a.partial + i);
+            for (uint32_t k = 1; k < a.splits; ++k) {
+                const wf4 v = *(const wf4*)(a.partial + k * n + i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[j] += v[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) put_weight(a.dw, a.w_f32, i + j, s[j]);
+        } else {
+            for (size_t e = i; e < i + 4 && e < n; ++e) {
+                float s = a.partial[e];
+                for (uint32_t k = 1; k < a.splits; ++k) s += a.partial[k * n + e];
+                put_weight(a.dw, a.w_f32, e, s);
+            }
+        }
+    } else {
+        const uint32_t i = (blockIdx.x - dw_blocks) * kJoinThreads + threadIdx.x;
+        if (i >= a.N) return;
+        float s = 0.0f;
+        for (uint32_t k = 0; k < a.splits * a.db_every; ++k) s += a.db_partial[(size_t)k * a.N + i];
+        put_weight(a.db, a.w_f32, i, s);
+    }
+}
+
+// ------------------------------------------------------------- host launchers
+template <int DT, int BITS, int WHICH>
+static void launch_tile(const WeightArgs& a, hipStream_t s) {
+    const dim3 grid(a.tiles_n * a.tiles_k * a.splits), block(kWeightThreads);
+    if (a.K % 8 == 0) hipLaunchKernelGGL((weight_kernel<DT, BITS, WHICH, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((weight_kernel<DT, BITS, WHICH, false>), grid, block, 0, s, a);
+}
+template <int DT, int BITS>
+static void launch_bits(const WeightArgs& a, int which, hipStream_t s) {
+    if (which == 0) launch_tile<DT, BITS, 0>(a, s);
+    else launch_tile<DT, BITS, 1>(a, s);
+}
+template <int DT>
+static void launch_type(const WeightArgs& a, int which, int bits, hipStream_t s) {
+    switch (bits) {
+        case 1: launch_bits<DT, 1>(a, which, s); break;
+        case 2: launch_bits<DT, 2>(a, which, s); break;
+        case 4: launch_bits<DT, 4>(a, which, s); break;
+        default: launch_bits<DT, 8>(a, which, s); break;
+    }
+}
+
+}  // namespace gact
+
+extern "C" int gact_launch_weight(const gact::WeightArgs* a, int which, int dtype, int bits, void* stream) {
+    const hipStream_t s = (hipStream_t)stream;
+    if (dtype == GACT_DT_F32) gact::launch_type<GACT_DT_F32>(*a, which, bits, s);
+    else gact::launch_type<GACT_DT_BF16>(*a, which, bits, s);
+    if (hipGetLastError() != hipSuccess) return -1;
+    if (a->splits > 1) {
+        const uint64_t n = (uint64_t)a->N * a->K, each = 4 * gact::kJoinThreads;
+        const uint32_t dw_blocks = (uint32_t)((n + each - 1) / each);
+        const uint32_t db_blocks = a->db ? (a->N + gact::kJoinThreads - 1) / gact::kJoinThreads : 0;
+        hipLaunchKernelGGL(gact::weight_join_kernel, dim3(dw_blocks + db_blocks), dim3(gact::kJoinThreads), 0, s, *a, dw_blocks);
+        if (hipGetLastError() != hipSuccess) return -1;
+    }
+    return 0;
+}

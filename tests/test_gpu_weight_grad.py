@@ -1,0 +1,173 @@
+"""Weight gradient of a linear layer from the codes of its input, against the same sums in binary64 over what
+gact_decompress gives of the context."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2206_11357_amd as gact
+
+pytestmark = pytest.mark.gpu
+
+EPS = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}       # half a step, relative
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def inputs(T, N, K, G, bits, dtype, seed=0, wide=0):
+    gen = torch.Generator().manual_seed(1000 * seed + T + 31 * N + 7 * K)
+    x = (torch.randn(T, K, generator=gen) * torch.exp(0.5 * torch.randn(K, generator=gen)) + 0.3).to(dtype).cuda()
+    dy = (torch.randn(T, N + wide, generator=gen) * 0.1).to(dtype).cuda()[:, wide:]
+    packed, gmin, gscale = gact.gact_compress(x, G, bits, 11 + seed)
+    return dy, packed, gmin, gscale
+
+
+def reference(dy, context, K, G, bits):
+    """dW, db in binary64, and the sums of the terms' sizes."""
+    T, N = dy.shape
+    x = gact.gact_decompress(*context, T * K, G, bits, dtype=dy.dtype).view(T, K).cpu().double()
+    d = dy.cpu().double()
+    return d.t() @ x, d.sum(0), d.abs().t() @ x.abs(), d.abs().sum(0)
+
+
+def close(got, want, size, terms):
+    """Off by a rounding of the sum's type and, in binary32, a rounding for each product and each addition of T terms in
+    whatever order; a step inside a matrix product may cut instead of rounding: 2^-23 of the terms' sizes each."""
+    got = got.cpu()
+    bound = EPS[got.dtype] * want.abs() + (terms + 2) * 2.0 ** -23 * size * (1 + EPS[got.dtype]) + 2.0 ** -126
+    off = (got.double() - want).abs() - bound
+    assert torch.isfinite(got).all()
+    assert off.max() <= 0, "off by %g more than the roundings, at %s" % (off.max(), np.unravel_index(int(off.argmax()), want.shape))
+
+
+def check(T, N, K, G, bits, dtype, w_dtype=torch.float32, bias=True, seed=0, wide=0):
+    dy, *context = inputs(T, N, K, G, bits, dtype, seed, wide)
+    dw, db = gact.gact_linear_weight_grad(dy, *context, K, G, bits, w_dtype=w_dtype, bias=bias)
+    want, want_b, size, size_b = reference(dy, context, K, G, bits)
+    assert dw.shape == (N, K) and dw.dtype == w_dtype
+    close(dw, want, size, T)
+    if bias:
+        close(db, want_b, size_b, T)
+    else:
+        assert db is None
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 31, 33, 64, 257])
+def test_tokens(T, dtype):
+    check(T, 40, 72, 32, 4, DTYPES[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K", [(1, 1), (1, 8), (3, 5), (7, 200), (47, 200), (64, 64), (65, 65), (63, 129), (200, 7), (300, 33), (1, 1000)])
+def test_odd_sizes(N, K, dtype):
+    check(130, N, K, 96, 2, DTYPES[dtype], wide=N % 5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bits", [1, 2, 4, 8])
+@pytest.mark.parametrize("G", [32, 96, 256, 1024])
+@pytest.mark.parametrize("K", [104, 111])
+def test_codes(K, G, bits, dtype):
+    check(77, 72, K, G, bits, DTYPES[dtype])
+
+
+# large tiles, one and several splits, edges of tiles
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("w_dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,K", [(4096, 256, 256), (3001, 300, 392), (2500, 513, 333), (700, 2304, 768)])
+def test_large_tiles(T, N, K, w_dtype, dtype):
+    check(T, N, K, 128, 4, DTYPES[dtype], DTYPES[w_dtype], bias=K != 392, wide=8 * (N % 2))
+
+
+def test_rows_at_odd_addresses():
+    dy, *context = inputs(300, 129, 64, 32, 8, torch.bfloat16, wide=3)
+    assert dy.data_ptr() % 4 == 2
+    check(300, 129, 64, 32, 8, torch.bfloat16, wide=3)
+
+
+@pytest.mark.parametrize("T,N,K", [(5, 70, 40), (3000, 260, 264)])
+def test_a_gradient_that_all_tokens_share(T, N, K):
+    _, *context = inputs(T, N, K, 64, 4, torch.float32)
+    dy = torch.randn(N, device="cuda").expand(T, N)
+    dw, db = gact.gact_linear_weight_grad(dy, *context, K, 64, 4, bias=True)
+    want, want_b, size, size_b = reference(dy, context, K, 64, 4)
+    close(dw, want, size, T)
+    close(db, want_b, size_b, T)
+
+
+def test_axes_in_front_are_one():
+    dy, *context = inputs(60, 48, 40, 32, 4, torch.float32)
+    two, _ = gact.gact_linear_weight_grad(dy, *context, 40, 32, 4)
+    three, _ = gact.gact_linear_weight_grad(dy.view(3, 20, 48), *context, 40, 32, 4)
+    assert torch.equal(two, three)
+
+
+def test_no_tokens_and_no_features():
+    e = torch.empty(0, device="cuda")
+    u = torch.empty(0, dtype=torch.uint8, device="cuda")
+    dw, db = gact.gact_linear_weight_grad(torch.empty(0, 5, device="cuda"), u, e, e, 7, 32, 4, bias=True)
+    assert torch.equal(dw, torch.zeros(5, 7, device="cuda")) and torch.equal(db, torch.zeros(5, device="cuda"))
+    dy = torch.randn(9, 5, device="cuda")
+    dw, db = gact.gact_linear_weight_grad(dy, u, e, e, 0, 32, 4, bias=True)
+    assert dw.shape == (5, 0)
+    close(db, dy.cpu().double().sum(0), dy.cpu().double().abs().sum(0), 9)
+
+
+def test_what_lies_behind_the_outputs_stays():
+    T, N, K = 2100, 257, 136
+    dy, *context = inputs(T, N, K, 32, 4, torch.bfloat16)
+    for dtype in (torch.float32, torch.bfloat16):
+        room = torch.full((N * K + 64,), 7.0, dtype=dtype, device="cuda")
+        rowb = torch.full((N + 64,), 7.0, dtype=dtype, device="cuda")
+        need = gact.gact_linear_weight_grad_workspace_bytes(T, N, K, torch.bfloat16)
+        ws = torch.full((need + 64,), 77, dtype=torch.uint8, device="cuda")
+        gact.gact_linear_weight_grad(dy, *context, K, 32, 4, w_dtype=dtype, bias=True, dw=room[:N * K].view(N, K), db=rowb[:N],
+                                     workspace=ws[:need])
+        assert (room[N * K:] == 7).all() and (rowb[N:] == 7).all() and (ws[need:] == 77).all()
+
+
+def test_not_a_number_stays_in_its_row():
+    T, N, K = 200, 70, 64
+    dy, *context = inputs(T, N, K, 32, 4, torch.bfloat16)
+    clean, _ = gact.gact_linear_weight_grad(dy, *context, K, 32, 4)
+    dy[50, 3] = float("nan")
+    dy[60, 9] = float("inf")
+    dw, db = gact.gact_linear_weight_grad(dy, *context, K, 32, 4, bias=True)
+    rows = torch.ones(N, dtype=torch.bool, device="cuda")
+    rows[[3, 9]] = False
+    assert torch.isnan(dw[3]).all() and not torch.isfinite(dw[9]).any()
+    assert torch.equal(dw[rows], clean[rows]) and torch.isnan(db[3]) and torch.isinf(db[9])
+
+
+def test_same_sums_in_every_call():
+    dy, *context = inputs(5000, 260, 264, 64, 2, torch.bfloat16)
+    first = gact.gact_linear_weight_grad(dy, *context, 264, 64, 2, bias=True)
+    for _ in range(5):
+        again = gact.gact_linear_weight_grad(dy, *context, 264, 64, 2, bias=True)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_captured_and_on_another_stream():
+    T, N, K = 5000, 260, 264
+    dy, *context = inputs(T, N, K, 64, 4, torch.bfloat16)
+    dw, db = torch.empty(N, K, device="cuda"), torch.empty(N, device="cuda")
+    ws = torch.empty(gact.gact_linear_weight_grad_workspace_bytes(T, N, K, torch.bfloat16), dtype=torch.uint8, device="cuda")
+    call = lambda: gact.gact_linear_weight_grad(dy, *context, K, 64, 4, bias=True, dw=dw, db=db, workspace=ws)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(3):
+        dy.copy_(torch.randn(T, N, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want, want_b, size, size_b = reference(dy, context, K, 64, 4)
+        close(dw, want, size, T)
+        close(db, want_b, size_b, T)
+        eager = gact.gact_linear_weight_grad(dy, *context, K, 64, 4, w_dtype=torch.float32, bias=True)
+        assert torch.equal(eager[0], dw) and torch.equal(eager[1], db)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = gact.gact_linear_weight_grad(dy, *context, K, 64, 4, w_dtype=torch.float32, bias=True, stream=side)
+    side.synchronize()
+    assert torch.equal(other[0], dw) and torch.equal(other[1], db)

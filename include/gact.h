@@ -428,6 +428,77 @@ int gact_head_norm_rotate_backward(const gact_heads *h_parts, int n_parts, const
                                    void *d_workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Group normalisation with an activation over a channels-last map, [batch, pixels, channels] with a pixel's channels
+ * consecutive and every other stride its own, whose context (x) can leave the same pass compressed, and the gradients,
+ * taken from the compressed context without decompressing it to memory.  The channels lie in `groups` groups of
+ * D = channels / groups; over the M = pixels * D elements of a group of a sample
+ *     m = mean x,   r = 1 / sqrt(mean (x - m)^2 + eps),   n = (x - m) * r,   z = n * w + b,   y = act(z),
+ * act(z) = z (GACT_ACT_NONE) or z / (1 + exp(-z)) (GACT_ACT_SILU).  Backward, n from the forward pass's m and r,
+ *     dz = dy * act'(z),  g = dz * w,  dx = r * (g - mean g - n * mean(g * n)),  dw = sum of dz * n,  db = sum of dz.
+ * Arithmetic in binary32, sums over threads' parts in binary32 and from there on in binary64, all in an order that depends
+ * on the sizes only; outputs rounded once.  Samples reach each other in dw and db only.
+ *
+ * Context.  With bits in {1, 2, 4, 8} the forward pass writes what gact_compress gives for x laid out contiguously with
+ * the same group_size, bits and seed, byte for byte, and the backward pass uses codes * step + minimum (in
+ * binary32, not rounded to x's type) for x.  m and r are not taken from these: the forward pass leaves them in mean and
+ * rstd.  With GACT_BITS_UNCOMPRESSED nothing is compressed and the backward pass reads x.
+ *
+ *   forward    reads x; writes y, mean and rstd (batch * groups floats each; both NULL: not wanted, only with bits ==
+ *              GACT_BITS_UNCOMPRESSED) and, compressing, packed (16-byte aligned), gmin and gscale.  y may be x itself with x's
+ *              strides.
+ *   backward   reads dy, mean, rstd and packed, gmin, gscale (compressed) or x; writes dx and, where they are not NULL, dw
+ *              and db.  dx may be dy itself with dy's strides.
+ *   Nothing else may overlap an output.  GACT_E_ARG for what pointers and strides show of it: a buffer given twice, in place
+ *   with other strides, an output's pixels that share memory.
+ *   w, b       weights and shifts of w_dtype, one a channel; NULL: ones, zeros (dw, db must be NULL then)
+ *   strides    in elements: sample, pixel
+ *   channels   a multiple of 8 and of groups;  group_size of a context: 32, 64, 128, 256 or 512 (GACT_E_GROUP otherwise:
+ *              gact_compress takes such a tensor)
+ *   batch * pixels * channels must be below 2^34, batch * pixels below 2^31, batch * channels below 2^30.
+ *   d_workspace  device scratch, >= gact_group_norm_workspace_bytes(...) of the same sizes (of both passes), 16-byte
+ *              aligned, in use until the enqueued kernels have run; calls that share one must not overlap in time.
+ * An empty tensor (batch or pixels 0) is GACT_OK; its dw and db are 0.  Both calls can be captured into a HIP graph.
+ */
+typedef enum { GACT_ACT_NONE = 0, GACT_ACT_SILU = 1 } gact_activation;
+
+typedef struct {
+    const void *x;
+    void       *y;
+    const void *dy;
+    void       *dx;
+    const void *w;
+    const void *b;
+    void       *dw;
+    void       *db;
+    float      *mean;
+    float      *rstd;
+    void       *packed;
+    float      *gmin;
+    float      *gscale;
+    int64_t     x_stride[2];
+    int64_t     y_stride[2];
+    int64_t     dy_stride[2];
+    int64_t     dx_stride[2];
+    int64_t     batch;
+    int64_t     pixels;
+    uint64_t    seed;
+    int32_t     channels;
+    int32_t     groups;
+    int32_t     act;         /* gact_activation */
+    int32_t     dtype;       /* gact_dtype of x, y, dy, dx */
+    int32_t     w_dtype;     /* gact_dtype of w, b, dw, db */
+    int32_t     bits;
+    int32_t     group_size;  /* of the context */
+    float       eps;         /* a normal number > 0; forward only */
+} gact_channel_norm;
+
+size_t gact_group_norm_workspace_bytes(int64_t batch, int64_t pixels, int channels, int groups);
+
+int gact_group_norm(const gact_channel_norm *h_norm, void *d_workspace, size_t workspace_bytes, void *stream);
+
+int gact_group_norm_backward(const gact_channel_norm *h_norm, void *d_workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Weight gradient of a linear layer y = x W^T + b from the compressed context of its input, which is not decompressed
  * to memory:
  *     dW[n, k] = sum over t of dy[t, n] * x^[t, k],      db[n] = sum over t of dy[t, n],

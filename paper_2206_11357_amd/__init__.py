@@ -35,6 +35,8 @@ GACT_E_SCRATCH = -7
 GACT_NOALLOC_SCRATCH_BYTES = 2 << 20
 GACT_NORM_2 = 0
 GACT_NORM_INF = 1
+GACT_ACT_NONE = 0
+GACT_ACT_SILU = 1
 
 EXPORTS = (
     "gact_num_groups", "gact_packed_bytes", "gact_error_string", "gact_compress",
@@ -45,6 +47,7 @@ EXPORTS = (
     "gact_compress_footprint_workspace_bytes", "gact_compress_footprint_noalloc", "gact_copy_bounded",
     "gact_grad_norm_workspace_bytes", "gact_grad_norm", "gact_grad_clip", "gact_grad_clip_by",
     "gact_head_norm_rotate_workspace_bytes", "gact_head_norm_rotate", "gact_head_norm_rotate_backward",
+    "gact_group_norm_workspace_bytes", "gact_group_norm", "gact_group_norm_backward",
     "gact_linear_weight_grad_workspace_bytes", "gact_linear_weight_grad",
 )
 GACT_BITS_UNCOMPRESSED = 32
@@ -87,6 +90,9 @@ _HEADS = struct.Struct("10P12qQ2i")
 # gact_rotation: batch, tokens; cos, sin, positions; n_positions; head_dim, rot_dim, interleaved, dtype, w_dtype,
 # group_size; eps, reserved.
 _ROTATION = struct.Struct("2q3Pq6ifi")
+# gact_channel_norm: x, y, dy, dx, w, b, dw, db, mean, rstd, packed, gmin, gscale; strides of x, y, dy, dx; batch, pixels;
+# seed; channels, groups, act, dtype, w_dtype, bits, group_size; eps.
+_CHANNEL_NORM = struct.Struct("13P10qQ7if")
 
 
 def _load() -> ctypes.CDLL:
@@ -149,6 +155,12 @@ def _load() -> ctypes.CDLL:
     lib.gact_head_norm_rotate.restype = i32
     lib.gact_head_norm_rotate_backward.argtypes = [vp, i32, vp, vp, sz, vp]
     lib.gact_head_norm_rotate_backward.restype = i32
+    lib.gact_group_norm_workspace_bytes.argtypes = [i64, i64, i32, i32]
+    lib.gact_group_norm_workspace_bytes.restype = sz
+    lib.gact_group_norm.argtypes = [vp, vp, sz, vp]
+    lib.gact_group_norm.restype = i32
+    lib.gact_group_norm_backward.argtypes = [vp, vp, sz, vp]
+    lib.gact_group_norm_backward.restype = i32
     lib.gact_linear_weight_grad_workspace_bytes.argtypes = [i64, i64, i64, i32]
     lib.gact_linear_weight_grad_workspace_bytes.restype = sz
     lib.gact_linear_weight_grad.argtypes = [vp, i64, i32, i64, i64, i64, vp, vp, vp, i32, i32, vp, vp, i32, vp, sz, vp]
@@ -1099,3 +1111,235 @@ def gact_linear_weight_grad(dy: torch.Tensor, packed: torch.Tensor, gmin: torch.
              None if db is None else db.data_ptr(), dtype_code(w_dtype),
              *(workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0))
     return dw, db
+
+
+# ---------------------------------------------- group norm with an activation
+_ACTIVATIONS = {"none": GACT_ACT_NONE, "silu": GACT_ACT_SILU}
+
+
+def _map_strides(x: torch.Tensor) -> Tuple[int, int, int, int, int]:
+    """(batch, pixels, channels, elements from sample to sample, from pixel to pixel) of [batch, ..., channels] whose axes in
+    between are one."""
+    shape, st = x.shape, x.stride()
+    if len(shape) < 3:
+        raise ValueError("gact needs [batch, ..., channels]")
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError("a pixel's channels must be consecutive")
+    if len(shape) == 3:
+        return shape[0], shape[1], shape[2], st[0], st[1]
+    pixels, stride = 1, shape[-1]
+    for size, s in zip(reversed(shape[1:-1]), reversed(st[1:-1])):
+        if size != 1:
+            if pixels == 1:
+                stride = s
+            elif s != pixels * stride:
+                raise ValueError("the pixels must be evenly spaced")
+            pixels *= size
+    return shape[0], pixels, shape[-1], st[0], stride
+
+
+class GroupNormContext:
+    """What the forward pass keeps of x for its gradient, in one buffer: mean and rstd, float32 [batch, groups], and, where bits
+    is not GACT_BITS_UNCOMPRESSED, packed, gmin and gscale as gact_compress lays them out."""
+    __slots__ = ("bits", "group_size", "seed", "shape", "groups", "device", "blob", "off")
+
+    def __init__(self, x: torch.Tensor, groups: int, bits: int, group_size: int, seed: int):
+        self.bits, self.group_size, self.seed, self.groups = bits, group_size, seed & (2**64 - 1), groups
+        self.shape, self.device = x.shape, x.get_device()
+        packed = meta = 0
+        if bits != GACT_BITS_UNCOMPRESSED:
+            n = x.numel()
+            packed = (n * bits + 127 >> 7) * 16
+            meta = ((-(-n // group_size) if group_size > 0 else 0) + 3 >> 2) * 16
+        each = (4 * self.shape[0] * max(groups, 0) + 15 >> 4) * 16
+        self.off = (0, packed, packed + meta, packed + 2 * meta, packed + 2 * meta + each)   # of packed, gmin, gscale, mean, rstd
+        self.blob = x.new_empty(self.off[4] + each, dtype=torch.uint8)
+
+    def filled(self, blob: torch.Tensor) -> "GroupNormContext":
+        """The same layout over a buffer that the forward pass has filled."""
+        if blob.dtype != torch.uint8 or blob.numel() != 2 * self.off[4] - self.off[3] or not blob.is_contiguous() \
+                or blob.get_device() != self.device:
+            raise ValueError("the buffer is not this context's")
+        c = GroupNormContext.__new__(GroupNormContext)
+        for name in GroupNormContext.__slots__:
+            if name != "blob":
+                setattr(c, name, getattr(self, name))
+        c.blob = blob
+        return c
+
+    def _floats(self, k: int, count: int) -> torch.Tensor:
+        return self.blob[self.off[k]:self.off[k] + 4 * count].view(torch.float32)
+
+    def _context_groups(self) -> int:
+        return -(-math.prod(self.shape) // self.group_size) if self.bits != GACT_BITS_UNCOMPRESSED else 0
+
+    @property
+    def packed(self) -> torch.Tensor:
+        return self.blob[:self.off[1]]
+
+    @property
+    def gmin(self) -> torch.Tensor:
+        return self._floats(1, self._context_groups())
+
+    @property
+    def gscale(self) -> torch.Tensor:
+        return self._floats(2, self._context_groups())
+
+    @property
+    def mean(self) -> torch.Tensor:
+        return self._floats(3, self.shape[0] * self.groups).view(self.shape[0], self.groups)
+
+    @property
+    def rstd(self) -> torch.Tensor:
+        return self._floats(4, self.shape[0] * self.groups).view(self.shape[0], self.groups)
+
+    def addresses(self) -> tuple:
+        """Addresses of mean, rstd, packed, gmin, gscale."""
+        a, off = self.blob.data_ptr(), self.off
+        if self.bits == GACT_BITS_UNCOMPRESSED:
+            return a + off[3], a + off[4], 0, 0, 0
+        return a + off[3], a + off[4], a, a + off[1], a + off[2]
+
+
+def make_group_norm_context(x: torch.Tensor, groups: int, bits: int = GACT_BITS_UNCOMPRESSED, group_size: int = 0, seed: int = 0,
+                            stream=None) -> GroupNormContext:
+    """Buffers for the context of x, [batch, ..., channels]."""
+    if stream is None:
+        return GroupNormContext(x, groups, bits, group_size, seed)
+    with _allocating_for(stream, x.get_device()):
+        return GroupNormContext(x, groups, bits, group_size, seed)
+
+
+def group_norm_context_fits(group_size: int, channels: int) -> bool:
+    """Whether the forward pass can compress the context of maps of so many channels in groups of group_size (gact.h)."""
+    return group_size in (32, 64, 128, 256, 512) and channels % 8 == 0
+
+
+@functools.lru_cache(maxsize=256)
+def gact_group_norm_workspace_bytes(batch: int, pixels: int, channels: int, groups: int) -> int:
+    return int(lib.gact_group_norm_workspace_bytes(batch, pixels, channels, groups))
+
+
+def _channel_weights(w, b, C: int):
+    """The one type of those that are given; None if none is."""
+    dtype = None
+    for v in (w, b):
+        if v is not None:
+            if v.numel() != C or not v.is_contiguous():
+                raise ValueError("weights and shifts must be contiguous, one per channel")
+            if dtype is None:
+                dtype = v.dtype
+            elif v.dtype is not dtype:
+                raise ValueError("weights and shifts must have one type")
+    return GACT_F32 if dtype is None else dtype_code(dtype)
+
+
+def _activation(act: str) -> int:
+    try:
+        return _ACTIVATIONS[act]
+    except KeyError:
+        raise ValueError("the activation must be one of %s, got %r" % (", ".join(_ACTIVATIONS), act)) from None
+
+
+def _norm_context(c: GroupNormContext, x: torch.Tensor, device: int, groups: int) -> None:
+    if c.shape != x.shape or c.device != device or c.groups != groups:
+        raise ValueError("the context was made for another shape, device or number of groups")
+
+
+def _norm_workspace(x: torch.Tensor, need: int, workspace: Optional[torch.Tensor]):
+    if workspace is None:
+        return x.new_empty(need, dtype=torch.uint8) if need else None
+    if not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return workspace
+
+
+def _norm_forward_record(x, groups, w, b, eps, act, context, out, workspace):
+    """(device, record) of a forward call into `out`."""
+    B, P, C, sample, pixel = _map_strides(x)
+    device = _same_device(x, out, w, b, workspace)
+    ys, yp = sample, pixel
+    if out is not x:
+        _check_like(out, x)
+        _, _, _, ys, yp = _map_strides(out)
+    a, bits, G, seed = (0, 0, 0, 0, 0), GACT_BITS_UNCOMPRESSED, 0, 0
+    if context is not None:
+        _norm_context(context, x, device, groups)
+        a, bits, G, seed = context.addresses(), context.bits, context.group_size, context.seed
+    return device, _CHANNEL_NORM.pack(
+        x.data_ptr(), out.data_ptr(), 0, 0, 0 if w is None else w.data_ptr(), 0 if b is None else b.data_ptr(), 0, 0, *a, sample, pixel,
+        ys, yp, 0, 0, 0, 0, B, P, seed, C, groups, _activation(act), dtype_code(x.dtype), _channel_weights(w, b, C), bits, G, eps)
+
+
+def gact_group_norm(x: torch.Tensor, groups: int, w: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,
+                    eps: float = 1e-5, act: str = "none", context: Optional[GroupNormContext] = None,
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Group norm of a channels-last map x, [batch, ..., channels] with evenly spaced pixels (an NCHW tensor in torch's
+    channels_last format is one after permute(0, 2, 3, 1)), with weights, shifts and an activation, "none" or "silu"; returns
+    y.  context: a GroupNormContext that the pass fills."""
+    need = gact_group_norm_workspace_bytes(*_map_strides(x)[:3], groups)
+    if out is None or workspace is None:
+        if stream is None:
+            out = x.new_empty(x.shape) if out is None else out
+            workspace = _norm_workspace(x, need, workspace)
+        else:
+            with _allocating_for(stream, x.get_device()):
+                out = x.new_empty(x.shape) if out is None else out
+                workspace = _norm_workspace(x, need, workspace)
+    device, record = _norm_forward_record(x, groups, w, b, eps, act, context, out, workspace)
+    _enqueue(lib.gact_group_norm, "gact_group_norm", device, stream, record,
+             *(workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0))
+    return out
+
+
+def prepare_group_norm(x: torch.Tensor, groups: int, w=None, b=None, eps: float = 1e-5, act: str = "none", *, out: torch.Tensor,
+                       context: Optional[GroupNormContext] = None, workspace: Optional[torch.Tensor] = None) -> PreparedCall:
+    """gact_group_norm(...) into `out`, as a PreparedCall, which keeps its workspace."""
+    workspace = _norm_workspace(x, gact_group_norm_workspace_bytes(*_map_strides(x)[:3], groups), workspace)
+    _, record = _norm_forward_record(x, groups, w, b, eps, act, context, out, workspace)
+    vp = ctypes.c_void_p
+    keep = ctypes.create_string_buffer(record, len(record))
+    args = (vp(ctypes.addressof(keep)), vp(workspace.data_ptr() if workspace is not None else 0),
+            ctypes.c_size_t(workspace.nbytes if workspace is not None else 0))
+    return PreparedCall(lib.gact_group_norm, "gact_group_norm", args, (keep, x, w, b, out, context, workspace))
+
+
+def _norm_gradients(dy, w, b, out, weight_grads, workspace, need: int):
+    dx = dy.new_empty(dy.shape) if out is None else out
+    dw = w.new_empty(w.shape) if w is not None and weight_grads[0] else None
+    db = b.new_empty(b.shape) if b is not None and weight_grads[1] else None
+    return dx, dw, db, _norm_workspace(dy, need, workspace)
+
+
+def gact_group_norm_backward(dy: torch.Tensor, groups: int, w: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,
+                             act: str = "none", *, context: GroupNormContext, x: Optional[torch.Tensor] = None,
+                             out: Optional[torch.Tensor] = None, weight_grads=(True, True),
+                             workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dw, db) of gact_group_norm from dy (strides as x's may be) and the context that it has filled; x where this is not
+    compressed.  None for weights that there are none of or whose gradient is not wanted."""
+    B, P, C, sample, pixel = _map_strides(dy)
+    device = _same_device(dy, w, b, x, out, workspace)
+    _norm_context(context, dy, device, groups)
+    need = gact_group_norm_workspace_bytes(B, P, C, groups)
+    if stream is None:
+        dx, dw, db, workspace = _norm_gradients(dy, w, b, out, weight_grads, workspace, need)
+    else:
+        with _allocating_for(stream, device):
+            dx, dw, db, workspace = _norm_gradients(dy, w, b, out, weight_grads, workspace, need)
+    _check_like(dx, dy)
+    a_x = xs = xp = 0
+    if context.bits == GACT_BITS_UNCOMPRESSED:
+        if x is None:
+            raise ValueError("the context is not compressed: x is needed")
+        _check_like(x, dy)
+        a_x = x.data_ptr()
+        _, _, _, xs, xp = _map_strides(x)
+    _, _, _, ds, dp = _map_strides(dx)
+    record = _CHANNEL_NORM.pack(
+        a_x, 0, dy.data_ptr(), dx.data_ptr(), 0 if w is None else w.data_ptr(), 0 if b is None else b.data_ptr(),
+        0 if dw is None else dw.data_ptr(), 0 if db is None else db.data_ptr(), *context.addresses(), xs, xp, 0, 0, sample, pixel,
+        ds, dp, B, P, context.seed, C, groups, _activation(act), dtype_code(dy.dtype), _channel_weights(w, b, C), context.bits,
+        context.group_size, 0.0)
+    _enqueue(lib.gact_group_norm_backward, "gact_group_norm_backward", device, stream, record,
+             *(workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0))
+    return dx, dw, db

@@ -1,0 +1,98 @@
+// Records of the group norm's kernels (gact_group_norm.hip), filled by their entry points.
+#ifndef GACT_GROUP_NORM_H
+#define GACT_GROUP_NORM_H
+
+#include <stdint.h>
+
+#include "gact_device.h"
+#include "gact_heads.h"
+
+namespace gact {
+
+constexpr int kGnThreads = 256;
+
+// [sample, pixel, channel], channels consecutive, the strides of the others in elements.
+struct GnTensor {
+    void*   p;
+    int64_t sample, pixel;
+};
+
+// Work goes by blocks of eight channels.  Kernels that add over pixels: a thread stays in its column, one such block, a
+// workgroup takes `rows` pixels of `cols` columns at a time, of one sample and one chunk of its pixels.
+struct GnArgs {
+    GnTensor x, y, dy, dx;
+    const void* w;                      // null: ones
+    const void* b;                      // null: zeros
+    void*       dw;                     // null: not wanted
+    void*       db;
+    float*      mean;                   // [samples][H]
+    float*      rstd;
+    uint8_t*    packed;
+    float*      gmin;
+    float*      gscale;
+    float*      partial;                // of each sample, chunk and channel (or column): two floats
+    float*      sums;                   // backward: of each sample and channel: sum of dz, sum of dz n
+    float*      means;                  // backward: of each sample and group: mean g, mean g n
+    uint32_t    B, P, C, H, D;
+    uint32_t    C8, cols, rows, slabs;  // columns of a workgroup; cols * slabs >= C8
+    uint32_t    chunks, per_chunk;      // pixels of a chunk
+    uint32_t    blocks8;                // B P C / 8
+    uint32_t    period, passes;         // a pass is 64 blocks; lanes come back to their channels after `period` passes
+    uint32_t    stride_passes;
+    uint32_t    dx_blocks;
+    Divisor     by_c8, by_p, by_d, by_cols;
+    uint32_t    seed_lo, seed_hi;
+    uint32_t    block_shift;            // log2 of a context group's blocks of eight
+    float       eps;
+    int32_t     w_f32;
+};
+
+inline uint32_t gn_up(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
+
+// Whether a block of eight channels lies in one group of the norm.
+inline bool gn_uniform(const GnArgs& a) { return a.D % 8 == 0; }
+
+constexpr uint32_t kGnBlocks = 2048;    // of a launch that adds over pixels, about
+
+inline void plan_group_norm(GnArgs* a) {
+    a->C8 = a->C / 8;
+    a->slabs = gn_up(a->C8, kGnThreads);
+    a->cols = gn_up(a->C8, a->slabs);
+    a->rows = (uint32_t)kGnThreads / a->cols;
+    a->by_c8 = divisor(a->C8);
+    a->by_p = divisor(a->P);
+    a->by_d = divisor(a->D);
+    a->by_cols = divisor(a->cols);
+    a->blocks8 = a->B * a->P * a->C8;
+    // chunks of eight pixels a thread at least
+    const uint64_t want = kGnBlocks / ((uint64_t)a->B * a->slabs) ? kGnBlocks / ((uint64_t)a->B * a->slabs) : 1;
+    const uint64_t most = gn_up(a->P, (uint64_t)a->rows * 8);
+    const uint64_t chunks = want < most ? want : most;
+    a->per_chunk = gn_up(a->P, chunks);
+    a->chunks = gn_up(a->P, a->per_chunk);
+    uint32_t g = a->C8, h = 64;
+    while (h) { const uint32_t t = g % h; g = h; h = t; }            // greatest common divisor
+    a->period = a->C8 / g;
+    a->passes = gn_up(a->blocks8, 64);
+    uint32_t waves = a->passes / 4 ? a->passes / 4 : 1;
+    if (waves > 16384) waves = 16384;
+    a->stride_passes = gn_up(waves, a->period) * a->period;
+}
+inline size_t gn_align(size_t v) { return (v + 15) & ~(size_t)15; }
+// Workspace: partial sums; forward: mean and rstd where the caller keeps none; backward: sums, means.
+inline size_t gn_partial_bytes(const GnArgs& a) {
+    return gn_align((size_t)a.B * a.chunks * a.C * 2 * sizeof(float));
+}
+inline size_t gn_forward_bytes(const GnArgs& a) { return gn_partial_bytes(a) + 2 * gn_align((size_t)a.B * a.H * sizeof(float)); }
+inline size_t gn_backward_bytes(const GnArgs& a) {
+    return gn_partial_bytes(a) + gn_align((size_t)a.B * a.C * 2 * sizeof(float)) + gn_align((size_t)a.B * a.H * 2 * sizeof(float));
+}
+
+}  // namespace gact
+
+// bits: 0 without a context; act: 0 none, 1 silu
+extern "C" int gact_launch_group_norm(const gact::GnArgs* a, int dtype, int bits, int act, void* stream);
+extern "C" int gact_launch_group_norm_backward(const gact::GnArgs* a, int dtype, int bits, int act, void* stream);
+extern "C" int gact_launch_group_norm_zero(const gact::GnArgs* a, void* stream);       // dw and db of nothing
+
+#endif

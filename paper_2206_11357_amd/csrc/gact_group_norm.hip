@@ -1,0 +1,513 @@
+// Group normalisation with an activation over channels-last maps, its compressed context and its gradients, for MI355X (gfx950).
+//
+//   over a group's M = P D elements of a sample:  m = mean x,  r = 1 / sqrt(mean (x - m)^2 + eps)
+//   n = (x - m) r,  z = n w + b,  y = act(z)
+//   dz = dy act'(z),  g = dz w,  dx = r (g - mean g - n mean(g n)),  dw = sum dz n,  db = sum dz
+//
+// Eight consecutive channels a lane: one block of the compressor's noise generator and `bits` whole bytes of its string, so that
+// the pass that writes y leaves the compressed context of x from the registers that hold x, and the backward passes take x
+// from the codes.  m and r are kept from the forward pass in binary32.
+// Forward: statistics (x read once), then y and the context (x read again, from the cache where it holds it).  A thread of the
+// first pass takes several pixels at a time: their mean, their squared distances from it, and both are merged with what it has
+// (T. Chan, G. Golub, R. LeVeque 1979), so that nothing cancels.  Backward: sums of dz and dz n over the pixels for each
+// channel and sample, from which the groups' means and dw, db follow; then dx.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gact_block8.h"
+#include "gact_codec.h"
+#include "gact_device.h"
+#include "gact_group_norm.h"
+
+namespace gact {
+
+// ----------------------------------------------------------------- activation
+// exp(-z).  The exponent's rounding, z times 2^-24 of the result, is taken back: fp32 results keep their last bits.
+template <int DT>
+__device__ __forceinline__ float exp_neg(float z) {
+    constexpr float kLog2e = 0x1.715476p+0f, kLog2eLow = 0x1.4ae0cp-26f;        // their sum: log2 e
+    const float e = __builtin_amdgcn_exp2f(-z * kLog2e);
+    if (DT == GACT_DT_BF16) return e;
+    const float c = __builtin_amdgcn_fmed3f(z, -150.0f, 150.0f);
+    const float low = __builtin_fmaf(-c, kLog2eLow, __builtin_fmaf(-c, kLog2e, c * kLog2e));
+    return e * __builtin_fmaf(low, 0x1.62e43p-1f, 1.0f);
+}
+template <int DT>
+__device__ __forceinline__ float inverse(float v) {
+    return DT == GACT_DT_BF16 ? __builtin_amdgcn_rcpf(v) : 1.0f / v;
+}
+template <int DT, bool SILU>
+__device__ __forceinline__ float activate(float z) {
+    return SILU ? z * inverse<DT>(1.0f + exp_neg<DT>(z)) : z;
+}
+// act'(z)
+template <int DT>
+__device__ __forceinline__ float silu_slope(float z) {
+    const float p = inverse<DT>(1.0f + exp_neg<DT>(z));
+    return p * __builtin_fmaf(z, 1.0f - p, 1.0f);
+}
+
+// ------------------------------------------------------------------- channels
+// What belongs to a lane's eight channels: weights; and of their groups, which are one where D is a multiple of eight.
+__device__ __forceinline__ void load_channels(const void* p, int f32, float without, uint32_t c, float (&v)[8]) {
+    if (!p) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = without;
+    } else if (f32) widen8<GACT_DT_F32>(load8<GACT_DT_F32>((const uint8_t*)p, c * 4u), v);
+    else widen8<GACT_DT_BF16>(load8<GACT_DT_BF16>((const uint8_t*)p, c * 2u), v);
+}
+template <bool UNI>
+struct OfGroups {
+    static constexpr int N = UNI ? 1 : 8;
+    float v[N];
+    // of the groups of channels c .. c + 7 of a sample, whose values `p` holds, `step` floats apart
+    __device__ __forceinline__ void load(const GnArgs& a, const float* p, int step, uint32_t c) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = p[(size_t)divided(c + (uint32_t)k, a.by_d) * step];
+    }
+    __device__ __forceinline__ float operator[](int k) const { return v[UNI ? 0 : k]; }
+};
+// A workgroup's place in a pass over pixels.
+struct Column {
+    uint32_t sample, chunk, p0, p1, c8, row;
+    bool     holds;
+    __device__ __forceinline__ Column(const GnArgs& a, uint32_t block) {
+        const uint32_t slab = block % a.slabs;
+        block /= a.slabs;
+        sample = block / a.chunks;
+        chunk = block - sample * a.chunks;
+        p0 = chunk * a.per_chunk;
+        p1 = p0 + a.per_chunk < a.P ? p0 + a.per_chunk : a.P;
+        row = divided(threadIdx.x, a.by_cols);
+        const uint32_t col = threadIdx.x - row * a.cols;
+        c8 = slab * a.cols + col;
+        holds = row < a.rows && c8 < a.C8;
+    }
+    __device__ __forceinline__ size_t partial(const GnArgs& a) const { return ((size_t)sample * a.chunks + chunk) * a.C8 + c8; }
+};
+
+// ------------------------------------------------------------------ statistics
+// Number, mean and squared distances from it of a thread's elements, for each group (a column's, or a channel's).
+template <bool UNI>
+struct Moments {
+    static constexpr int N = UNI ? 1 : 8;
+    float n, mean[N], m2[N];
+    __device__ __forceinline__ void merge(float other, const float (&om)[N], const float (&o2)[N]) {
+        const float all = n + other;
+        const float f = all > 0.0f ? other / all : 0.0f;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float d = om[k] - mean[k];
+            mean[k] = __builtin_fmaf(d, f, mean[k]);
+            m2[k] += __builtin_fmaf(d * d, f * n, o2[k]);
+        }
+        n = all;
+    }
+};
+template <int DT, bool UNI>
+__global__ __launch_bounds__(kGnThreads) void gn_stats_kernel(GnArgs a) {
+    constexpr int N = UNI ? 1 : 8, U = DT == GACT_DT_F32 ? 4 : 8;
+    __shared__ float lds[kGnThreads][2 * N + 1];
+    const Column at(a, blockIdx.x);
+    Moments<UNI> s = {};
+    const uint8_t* x = (const uint8_t*)a.x.p;
+    const int64_t first = (int64_t)at.sample * a.x.sample + (int64_t)at.c8 * 8;
+    for (uint32_t p = at.p0 + at.row; at.holds && p < at.p1; p += U * a.rows) {
+        Raw<DT> raw[U];
+        float on[U], count = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t q = p + (uint32_t)u * a.rows;
+            on[u] = q < at.p1 ? 1.0f : 0.0f;
+            count += on[u];
+            raw[u] = load8<DT>(x, (first + (int64_t)(q < at.p1 ? q : p) * a.x.pixel) * kSize<DT>);
+        }
+        float mean[N], m2[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) mean[k] = m2[k] = 0.0f;
+        const float all = UNI ? 8.0f * count : count, inv = 1.0f / all;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[8];
+            widen8<DT>(raw[u], v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) if (on[u] != 0.0f) mean[UNI ? 0 : k] += v[k];
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) mean[k] *= inv;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[8];
+            widen8<DT>(raw[u], v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float d = v[k] - mean[UNI ? 0 : k];
+                if (on[u] != 0.0f) m2[UNI ? 0 : k] = __builtin_fmaf(d, d, m2[UNI ? 0 : k]);
+            }
+        }
+        s.merge(all, mean, m2);
+    }
+    // over the rows of a column, halves at a time
+    float* mine = lds[threadIdx.x];
+    mine[0] = s.n;
+#pragma unroll
+    for (int k = 0; k < N; ++k) { mine[1 + k] = s.mean[k]; mine[1 + N + k] = s.m2[k]; }
+    for (uint32_t left = a.rows; left > 1;) {
+        const uint32_t half = (left + 1) >> 1;
+        __syncthreads();
+        if (at.holds && at.row + half < left) {
+            const float* o = lds[threadIdx.x + half * a.cols];
+            float om[N], o2[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) { om[k] = o[1 + k]; o2[k] = o[1 + N + k]; }
+            s.merge(o[0], om, o2);
+            mine[0] = s.n;
+#pragma unroll
+            for (int k = 0; k < N; ++k) { mine[1 + k] = s.mean[k]; mine[1 + N + k] = s.m2[k]; }
+        }
+        left = half;
+    }
+    if (!at.holds || at.row != 0) return;
+    float* out = a.partial + at.partial(a) * (2 * N);
+#pragma unroll
+    for (int k = 0; k < N; ++k) { out[2 * k] = s.mean[k]; out[2 * k + 1] = s.m2[k]; }
+}
+
+// Sum over the wavefront, in all lanes.
+__device__ __forceinline__ double over_wave(double v) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m);
+    return v;
+}
+__device__ __forceinline__ uint32_t gn_wave() { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+// m and r of a sample's group, a wavefront each, from its columns' (channels') in all chunks, in binary64.
+template <bool UNI>
+__global__ __launch_bounds__(kGnThreads) void gn_finish_kernel(GnArgs a) {
+    const uint32_t i = blockIdx.x * (kGnThreads / 64) + gn_wave();
+    if (i >= a.B * a.H) return;
+    const uint32_t sample = i / a.H, h = i - sample * a.H, lane = threadIdx.x & 63u;
+    const uint32_t each = UNI ? a.D / 8 : a.D, row = UNI ? a.C8 : a.C, items = each * a.chunks;
+    const float* p = a.partial + ((size_t)sample * a.chunks * row + (size_t)h * each) * 2;
+    const double per = UNI ? 8.0 : 1.0, last = per * (a.P - (a.chunks - 1) * a.per_chunk), all = per * a.per_chunk;
+    double mean = 0.0, m2 = 0.0;
+    for (uint32_t k = lane; k < items; k += 64) {
+        const uint32_t chunk = k / each;
+        mean += (chunk + 1 == a.chunks ? last : all) * (double)p[((size_t)chunk * row + (k - chunk * each)) * 2];
+    }
+    mean = over_wave(mean) / ((double)a.P * a.D);
+    for (uint32_t k = lane; k < items; k += 64) {
+        const uint32_t chunk = k / each;
+        const float* v = p + ((size_t)chunk * row + (k - chunk * each)) * 2;
+        const double d = (double)v[0] - mean;
+        m2 += (double)v[1] + (chunk + 1 == a.chunks ? last : all) * d * d;
+    }
+    m2 = over_wave(m2) / ((double)a.P * a.D);
+    if (lane != 0) return;
+    a.mean[i] = (float)mean;
+    a.rstd[i] = (float)(1.0 / sqrt(m2 + (double)a.eps));
+}
+
+// ------------------------------------------------------------------ y, context
+template <int DT, int BITS, bool UNI, bool SILU>
+__global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
+    const uint32_t lane = threadIdx.x & 63u;
+    uint32_t pass = blockIdx.x * (kGnThreads / 64) + gn_wave();
+    if (BITS != 0 && pass == 0) {                      // the packed string ends at a multiple of 16 bytes, zeros behind the last code
+        const uint64_t bytes = (uint64_t)a.blocks8 * BITS;
+        if (lane < (uint32_t)(0u - bytes & 15u)) a.packed[bytes + lane] = 0;
+    }
+    if (pass >= a.stride_passes || pass >= a.passes) return;
+    uint32_t e = pass * 64u + lane;                    // the lane's block of eight
+    uint32_t q = divided(e, a.by_c8);                  // its pixel, of all samples'
+    const uint32_t c = (e - q * a.C8) * 8u;
+    const uint32_t e_step = a.stride_passes * 64u, q_step = e_step / a.C8;
+    float w[8], b[8];
+    load_channels(a.w, a.w_f32, 1.0f, c, w);
+    load_channels(a.b, a.w_f32, 0.0f, c, b);
+    uint32_t sample = ~0u;
+    OfGroups<UNI> m, r;
+    for (;; ) {
+        const bool active = e < a.blocks8;
+        if (!active) q = a.B * a.P - 1;
+        const uint32_t s = divided(q, a.by_p), p = q - s * a.P;
+        const int64_t at = (int64_t)s * a.x.sample + (int64_t)p * a.x.pixel + c;
+        const Raw<DT> raw = load8<DT>((const uint8_t*)a.x.p, at * kSize<DT>);
+        if (s != sample) {
+            m.load(a, a.mean + (size_t)s * a.H, 1, c);
+            r.load(a, a.rstd + (size_t)s * a.H, 1, c);
+            sample = s;
+        }
+        float v[8], y[8];
+        widen8<DT>(raw, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] = activate<DT, SILU>(__builtin_fmaf((v[k] - m[k]) * r[k], w[k], b[k]));
+        if (active)
+            store8<DT>((uint8_t*)a.y.p, ((int64_t)s * a.y.sample + (int64_t)p * a.y.pixel + c) * kSize<DT>, y);
+        if constexpr (BITS != 0) {
+            float mn, step;
+            const uint64_t codes = compress8<BITS>(v, active, 1 << a.block_shift, (uint64_t)pass * 64u, lane, a.seed_lo, a.seed_hi, mn, step);
+            if (active) {
+                store_codes<BITS>(a.packed + (uint64_t)e * BITS, codes);
+                if ((lane & ((1u << a.block_shift) - 1u)) == 0) {
+                    a.gmin[e >> a.block_shift] = mn;
+                    a.gscale[e >> a.block_shift] = step;
+                }
+            }
+        }
+        if (a.passes - pass <= a.stride_passes) return;
+        pass += a.stride_passes;
+        e += e_step;
+        q += q_step;
+    }
+}
+
+// ------------------------------------------------------------------- gradients
+// dy and x of a block of eight: from its codes or as they are.
+template <int DT, int BITS>
+struct GnInput {
+    Raw<DT> dy, x;
+    uint64_t codes;
+    float mn, step;
+    __device__ __forceinline__ void load(const GnArgs& a, uint32_t sample, uint32_t p, uint32_t c8) {
+        dy = load8<DT>((const uint8_t*)a.dy.p, ((int64_t)sample * a.dy.sample + (int64_t)p * a.dy.pixel + (int64_t)c8 * 8) * kSize<DT>);
+        if constexpr (BITS != 0) {
+            const uint32_t e = (sample * a.P + p) * a.C8 + c8;
+            codes = load_codes<BITS>(a.packed + (uint64_t)e * BITS);
+            mn = a.gmin[e >> a.block_shift];
+            step = a.gscale[e >> a.block_shift];
+        } else {
+            x = load8<DT>((const uint8_t*)a.x.p, ((int64_t)sample * a.x.sample + (int64_t)p * a.x.pixel + (int64_t)c8 * 8) * kSize<DT>);
+        }
+    }
+    // n and dz
+    template <bool UNI, bool SILU>
+    __device__ __forceinline__ void take(const OfGroups<UNI>& m, const OfGroups<UNI>& r, const float (&w)[8], const float (&b)[8],
+                                         float (&n)[8], float (&dz)[8]) const {
+        widen8<DT>(dy, dz);
+        if constexpr (BITS != 0) decompress8<BITS>(codes, mn, step, n);
+        else widen8<DT>(x, n);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            n[k] = (n[k] - m[k]) * r[k];
+            if (SILU) dz[k] *= silu_slope<DT>(__builtin_fmaf(n[k], w[k], b[k]));
+        }
+    }
+};
+
+template <int DT, int BITS, bool UNI, bool SILU>
+__global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnArgs a) {
+    constexpr int U = 2;
+    __shared__ float lds[kGnThreads * 17];             // 16 values a thread, and one to shift the banks
+    const Column at(a, blockIdx.x);
+    const uint32_t c = at.c8 * 8u;
+    float s0[8], s1[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s0[k] = s1[k] = 0.0f;
+    if (at.holds) {
+        float w[8], b[8];
+        load_channels(a.w, a.w_f32, 1.0f, c, w);
+        load_channels(a.b, a.w_f32, 0.0f, c, b);
+        OfGroups<UNI> m, r;
+        m.load(a, a.mean + (size_t)at.sample * a.H, 1, c);
+        r.load(a, a.rstd + (size_t)at.sample * a.H, 1, c);
+        for (uint32_t p = at.p0 + at.row; p < at.p1; p += U * a.rows) {
+            GnInput<DT, BITS> in[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t q = p + (uint32_t)u * a.rows;
+                in[u].load(a, at.sample, q < at.p1 ? q : p, at.c8);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (u > 0 && p + (uint32_t)u * a.rows >= at.p1) break;
+                float n[8], dz[8];
+                in[u].template take<UNI, SILU>(m, r, w, b, n, dz);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    s0[k] += dz[k];
+                    s1[k] = __builtin_fmaf(dz[k], n[k], s1[k]);
+                }
+            }
+        }
+    }
+    float* mine = lds + threadIdx.x * 17;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { mine[k] = s0[k]; mine[8 + k] = s1[k]; }
+    for (uint32_t left = a.rows; left > 1;) {
+        const uint32_t half = (left + 1) >> 1;
+        __syncthreads();
+        if (at.holds && at.row + half < left) {
+            const float* o = mine + half * a.cols * 17;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) mine[k] += o[k];
+        }
+        left = half;
+    }
+    if (!at.holds || at.row != 0) return;
+    float* out = a.partial + at.partial(a) * 16;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { out[2 * k] = mine[k]; out[2 * k + 1] = mine[8 + k]; }
+}
+
+// Of a sample's group, a wavefront each: the channels' sums over the chunks, and the means of g and g n, in binary64.
+__global__ __launch_bounds__(kGnThreads) void gn_means_kernel(GnArgs a) {
+    const uint32_t i = blockIdx.x * (kGnThreads / 64) + gn_wave();
+    if (i >= a.B * a.H) return;
+    const uint32_t sample = i / a.H, h = i - sample * a.H, lane = threadIdx.x & 63u;
+    // lanes: D channels (64 of them at a time), and as many parts of the chunks as fit
+    const uint32_t wide = a.D < 64u ? a.D : 64u, parts = 64u / wide, part = lane / wide, d0 = lane - part * wide;
+    double m1 = 0.0, m2 = 0.0;
+    for (uint32_t d = 0; d < a.D; d += 64u) {
+        const uint32_t c = h * a.D + d + d0;
+        const bool holds = part < parts && d + d0 < a.D;
+        double s0 = 0.0, s1 = 0.0;
+        if (holds) {
+            const float* p = a.partial + ((size_t)sample * a.chunks * a.C + c) * 2;
+            for (uint32_t k = part; k < a.chunks; k += parts) {
+                s0 += (double)p[(size_t)k * a.C * 2];
+                s1 += (double)p[(size_t)k * a.C * 2 + 1];
+            }
+        }
+        // over the parts, in their order
+        double t0 = 0.0, t1 = 0.0;
+        for (uint32_t k = 0; k < parts; ++k) {
+            t0 += __shfl(s0, (int)(d0 + k * wide));
+            t1 += __shfl(s1, (int)(d0 + k * wide));
+        }
+        if (!holds || part != 0) continue;
+        float* out = a.sums + ((size_t)sample * a.C + c) * 2;
+        out[0] = (float)t0;
+        out[1] = (float)t1;
+        double w = 1.0;
+        if (a.w) w = a.w_f32 ? (double)((const float*)a.w)[c]
+                             : (double)__builtin_bit_cast(float, (uint32_t)((const uint16_t*)a.w)[c] << 16);
+        m1 += w * t0;
+        m2 += w * t1;
+    }
+    m1 = over_wave(m1) / ((double)a.P * a.D);
+    m2 = over_wave(m2) / ((double)a.P * a.D);
+    if (lane != 0) return;
+    a.means[2 * i] = (float)m1;
+    a.means[2 * i + 1] = (float)m2;
+}
+
+// dw and db of 32 channels: over the samples, eight parts of them, in binary64 and in a fixed order.
+__device__ __forceinline__ void gn_weights(const GnArgs& a, uint32_t block, double (&lds)[2][kGnThreads]) {
+    const uint32_t part = threadIdx.x >> 5, c = block * 32u + (threadIdx.x & 31u);
+    double s0 = 0.0, s1 = 0.0;
+    if (c < a.C)
+        for (uint32_t s = part; s < a.B; s += kGnThreads / 32) {
+            const float* p = a.sums + ((size_t)s * a.C + c) * 2;
+            s0 += (double)p[0];
+            s1 += (double)p[1];
+        }
+    lds[0][threadIdx.x] = s0;
+    lds[1][threadIdx.x] = s1;
+    __syncthreads();
+    if (part != 0 || c >= a.C) return;
+    for (uint32_t k = 1; k < kGnThreads / 32; ++k) {
+        s0 += lds[0][threadIdx.x + 32 * k];
+        s1 += lds[1][threadIdx.x + 32 * k];
+    }
+    const auto put = [&](void* p, double v) {
+        if (!p) return;
+        if (a.w_f32) ((float*)p)[c] = (float)v;
+        else ((uint16_t*)p)[c] = (uint16_t)bf16_pair_rne((float)v, 0.0f);
+    };
+    put(a.dw, s1);
+    put(a.db, s0);
+}
+
+template <int DT, int BITS, bool UNI, bool SILU>
+__global__ __launch_bounds__(kGnThreads) void gn_dx_kernel(GnArgs a) {
+    __shared__ double lds[2][kGnThreads];
+    if (blockIdx.x >= a.dx_blocks) {
+        gn_weights(a, blockIdx.x - a.dx_blocks, lds);
+        return;
+    }
+    const Column at(a, blockIdx.x);
+    if (!at.holds) return;
+    const uint32_t c = at.c8 * 8u;
+    float w[8], b[8];
+    load_channels(a.w, a.w_f32, 1.0f, c, w);
+    load_channels(a.b, a.w_f32, 0.0f, c, b);
+    OfGroups<UNI> m, r, m1, m2;
+    const size_t group = (size_t)at.sample * a.H;
+    m.load(a, a.mean + group, 1, c);
+    r.load(a, a.rstd + group, 1, c);
+    m1.load(a, a.means + 2 * group, 2, c);
+    m2.load(a, a.means + 2 * group + 1, 2, c);
+    for (uint32_t p = at.p0 + at.row; p < at.p1; p += a.rows) {
+        GnInput<DT, BITS> in;
+        in.load(a, at.sample, p, at.c8);
+        float n[8], dz[8];
+        in.template take<UNI, SILU>(m, r, w, b, n, dz);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dz[k] = r[k] * __builtin_fmaf(-n[k], m2[k], __builtin_fmaf(dz[k], w[k], -m1[k]));
+        store8<DT>((uint8_t*)a.dx.p, ((int64_t)at.sample * a.dx.sample + (int64_t)p * a.dx.pixel + c) * kSize<DT>, dz);
+    }
+}
+
+__global__ __launch_bounds__(kGnThreads) void gn_zero_kernel(GnArgs a) {
+    const uint32_t c = blockIdx.x * kGnThreads + threadIdx.x;
+    if (c >= a.C) return;
+    for (void* p : {a.dw, a.db}) {
+        if (!p) continue;
+        if (a.w_f32) ((float*)p)[c] = 0.0f;
+        else ((uint16_t*)p)[c] = 0;
+    }
+}
+
+// ------------------------------------------------------------- host launchers
+template <int DT, int BITS, bool UNI, bool SILU>
+static int gn_launch(bool backward, const GnArgs& a, hipStream_t s) {
+    const uint32_t slots = a.B * a.chunks * a.slabs, groups = (a.B * a.H + 3) / 4;
+    if (!backward) {
+        hipLaunchKernelGGL((gn_stats_kernel<DT, UNI>), dim3(slots), dim3(kGnThreads), 0, s, a);
+        hipLaunchKernelGGL((gn_finish_kernel<UNI>), dim3(groups), dim3(kGnThreads), 0, s, a);
+        const uint32_t waves = a.stride_passes < a.passes ? a.stride_passes : a.passes;
+        hipLaunchKernelGGL((gn_apply_kernel<DT, BITS, UNI, SILU>), dim3((waves + 3) / 4), dim3(kGnThreads), 0, s, a);
+    } else {
+        GnArgs d = a;
+        d.dx_blocks = slots;
+        hipLaunchKernelGGL((gn_sums_kernel<DT, BITS, UNI, SILU>), dim3(slots), dim3(kGnThreads), 0, s, a);
+        hipLaunchKernelGGL(gn_means_kernel, dim3(groups), dim3(kGnThreads), 0, s, a);
+        const uint32_t extra = a.dw || a.db ? (a.C + 31) / 32 : 0;
+        hipLaunchKernelGGL((gn_dx_kernel<DT, BITS, UNI, SILU>), dim3(slots + extra), dim3(kGnThreads), 0, s, d);
+    }
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+template <int DT, int BITS>
+static int gn_launch_form(bool backward, const GnArgs& a, int act, hipStream_t s) {
+    if (gn_uniform(a)) return act ? gn_launch<DT, BITS, true, true>(backward, a, s) : gn_launch<DT, BITS, true, false>(backward, a, s);
+    return act ? gn_launch<DT, BITS, false, true>(backward, a, s) : gn_launch<DT, BITS, false, false>(backward, a, s);
+}
+template <int DT>
+static int gn_launch_bits(bool backward, const GnArgs& a, int bits, int act, hipStream_t s) {
+    switch (bits) {
+        case 0: return gn_launch_form<DT, 0>(backward, a, act, s);
+        case 1: return gn_launch_form<DT, 1>(backward, a, act, s);
+        case 2: return gn_launch_form<DT, 2>(backward, a, act, s);
+        case 4: return gn_launch_form<DT, 4>(backward, a, act, s);
+        default: return gn_launch_form<DT, 8>(backward, a, act, s);
+    }
+}
+static int gn_launch_any(bool backward, const GnArgs& a, int dtype, int bits, int act, hipStream_t s) {
+    return dtype == GACT_DT_F32 ? gn_launch_bits<GACT_DT_F32>(backward, a, bits, act, s)
+                                : gn_launch_bits<GACT_DT_BF16>(backward, a, bits, act, s);
+}
+
+}  // namespace gact
+
+extern "C" int gact_launch_group_norm(const gact::GnArgs* a, int dtype, int bits, int act, void* stream) {
+    return gact::gn_launch_any(false, *a, dtype, bits, act, (hipStream_t)stream);
+}
+extern "C" int gact_launch_group_norm_backward(const gact::GnArgs* a, int dtype, int bits, int act, void* stream) {
+    return gact::gn_launch_any(true, *a, dtype, bits, act, (hipStream_t)stream);
+}
+extern "C" int gact_launch_group_norm_zero(const gact::GnArgs* a, void* stream) {
+    hipLaunchKernelGGL(gact::gn_zero_kernel, dim3((a->C + gact::kGnThreads - 1) / gact::kGnThreads), dim3(gact::kGnThreads), 0,
+                       (hipStream_t)stream, *a);
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+}

@@ -1,9 +1,12 @@
 // Entry points of layers whose context is read as codes (include/gact.h): argument checks and launch plans.  The kernels
-// are in gact_weight.hip.
+// are in gact_weight.hip and gact_group_norm.hip.
 #include <hip/hip_runtime.h>
+
+#include <cmath>
 
 #include "gact.h"
 #include "gact_device.h"
+#include "gact_group_norm.h"
 #include "gact_weight.h"
 
 namespace {
@@ -21,9 +24,154 @@ bool weight_sizes_ok(int64_t T, int64_t N, int64_t K) {
     return (uint64_t)T * (uint64_t)K < 1ull << 35 && (uint64_t)N * (uint64_t)K < 1ull << 38;
 }
 
+// -------------------------------------------------------------------- group norm
+bool norm_sizes_ok(int64_t B, int64_t P, int C, int H) {
+    if (B < 0 || P < 0 || B > kMost || P > kMost || C < 8 || C % 8 != 0 || C > 1 << 20 || H < 1 || C % H != 0) return false;
+    return (uint64_t)B * (uint64_t)P <= (uint64_t)kMost && (uint64_t)B * (uint64_t)C < 1ull << 30 &&
+           (uint64_t)B * (uint64_t)P * (uint64_t)C < 1ull << 34;
+}
+void norm_sizes(int64_t B, int64_t P, int C, int H, gact::GnArgs* a) {
+    a->B = (uint32_t)B;
+    a->P = (uint32_t)P;
+    a->C = (uint32_t)C;
+    a->H = (uint32_t)H;
+    a->D = (uint32_t)(C / H);
+    gact::plan_group_norm(a);
+}
+
+// Whether two pixels of a tensor can share memory: unless, in the order of their sizes, each stride passes what lies below it.
+bool pixels_overlap(const int64_t (&stride)[2], const gact_channel_norm* h) {
+    const auto size = [](int64_t v) { return v < 0 ? 0 - (uint64_t)v : (uint64_t)v; };
+    uint64_t s[2] = {size(stride[0]), size(stride[1])}, n[2] = {(uint64_t)h->batch, (uint64_t)h->pixels};
+    const int low = s[0] < s[1] ? 0 : 1;
+    uint64_t extent = (uint64_t)h->channels;
+    for (const int k : {low, 1 - low}) {
+        if (n[k] < 2) continue;
+        if (s[k] < extent || s[k] >= (uint64_t)1 << 48) return true;               // (behind that products would wrap)
+        extent += s[k] * (n[k] - 1);
+    }
+    return false;
+}
+bool same_strides(const int64_t (&a)[2], const int64_t (&b)[2], const gact_channel_norm* h) {
+    return (a[0] == b[0] || h->batch < 2) && (a[1] == b[1] || h->pixels < 2);
+}
+// Whether an output is another of the call's buffers, as far as pointers and strides show it.
+bool norm_overlaps(const gact_channel_norm* h, bool backward, bool compressed) {
+    const void* out = backward ? h->dx : h->y;
+    const void* in = backward ? h->dy : h->x;
+    const auto& out_stride = backward ? h->dx_stride : h->y_stride;
+    const auto& in_stride = backward ? h->dy_stride : h->x_stride;
+    if (pixels_overlap(out_stride, h)) return true;
+    if (out == in && !same_strides(out_stride, in_stride, h)) return true;
+    const void* others[] = {h->w, h->b, h->mean, h->rstd, compressed ? h->packed : nullptr, compressed ? (const void*)h->gmin : nullptr,
+                            compressed ? (const void*)h->gscale : nullptr, backward ? h->dw : nullptr, backward ? h->db : nullptr,
+                            backward && !compressed ? h->x : nullptr};
+    for (const void* p : others) if (p && p == out) return true;
+    if (backward) {
+        for (const void* p : {(const void*)h->dw, (const void*)h->db})
+            if (p && (p == h->w || p == h->b || p == h->mean || p == h->rstd || p == h->dy)) return true;
+        return h->dw && h->dw == h->db;
+    }
+    return (h->mean && h->mean == h->rstd) || (compressed && (h->packed == h->gmin || h->packed == h->gscale || h->gmin == h->gscale));
+}
+
+// Checks a call; fills *a and *bits (0 without a context).
+int stage_norm(const gact_channel_norm* h, bool backward, void* ws, size_t ws_bytes, gact::GnArgs* a, int* bits) {
+    if (!h) return GACT_E_ARG;
+    if (h->bits != GACT_BITS_UNCOMPRESSED && !bits_ok(h->bits)) return GACT_E_BITS;
+    *bits = h->bits == GACT_BITS_UNCOMPRESSED ? 0 : h->bits;
+    if (!dtype_ok(h->dtype) || !dtype_ok(h->w_dtype) || (h->act != GACT_ACT_NONE && h->act != GACT_ACT_SILU)) return GACT_E_ARG;
+    if (!norm_sizes_ok(h->batch, h->pixels, h->channels, h->groups)) return GACT_E_ARG;
+    if (!backward && !(std::isnormal(h->eps) && h->eps > 0.0f)) return GACT_E_ARG;
+    const int G = h->group_size;
+    if (*bits != 0 && (G < 32 || G > 512 || (G & (G - 1)) != 0)) return GACT_E_GROUP;
+    const size_t size = size_of(h->dtype), w_size = size_of(h->w_dtype);
+    if (!aligned(h->w, w_size) || !aligned(h->b, w_size)) return GACT_E_ARG;
+    if (backward && ((h->dw && (!h->w || !aligned(h->dw, w_size))) || (h->db && (!h->b || !aligned(h->db, w_size))))) return GACT_E_ARG;
+    const bool empty = h->batch == 0 || h->pixels == 0;
+    if (!empty) {
+        const void* in = backward ? h->dy : h->x;
+        const void* out = backward ? h->dx : h->y;
+        if (!in || !out || !aligned(in, size) || !aligned(out, size) || !aligned(h->mean, 4) || !aligned(h->rstd, 4)) return GACT_E_ARG;
+        if (!h->mean != !h->rstd || (!h->mean && (backward || *bits != 0))) return GACT_E_ARG;
+        if (backward && *bits == 0 && (!h->x || !aligned(h->x, size))) return GACT_E_ARG;
+        if (*bits != 0 && (!h->packed || !h->gmin || !h->gscale || !aligned(h->packed, 16) || !aligned(h->gmin, 4) ||
+                           !aligned(h->gscale, 4)))
+            return GACT_E_ARG;
+        if (norm_overlaps(h, backward, *bits != 0)) return GACT_E_ARG;
+    }
+    const auto tensor = [](const void* p, const int64_t (&stride)[2]) {
+        return gact::GnTensor{const_cast<void*>(p), stride[0], stride[1]};
+    };
+    a->x = tensor(h->x, h->x_stride);
+    a->y = tensor(h->y, h->y_stride);
+    a->dy = tensor(h->dy, h->dy_stride);
+    a->dx = tensor(h->dx, h->dx_stride);
+    a->w = h->w;
+    a->b = h->b;
+    a->dw = h->dw;
+    a->db = h->db;
+    a->mean = h->mean;
+    a->rstd = h->rstd;
+    a->packed = (uint8_t*)h->packed;
+    a->gmin = h->gmin;
+    a->gscale = h->gscale;
+    a->seed_lo = (uint32_t)h->seed;
+    a->seed_hi = (uint32_t)(h->seed >> 32);
+    a->eps = h->eps;
+    a->w_f32 = h->w_dtype == GACT_F32;
+    if (empty) {
+        a->C = (uint32_t)h->channels;
+        return GACT_OK;
+    }
+    if (*bits != 0) while ((8 << a->block_shift) < G) ++a->block_shift;
+    norm_sizes(h->batch, h->pixels, h->channels, h->groups, a);
+    if (!gact::launchable((uint64_t)a->B * a->chunks * a->slabs + a->C, gact::kGnThreads)) return GACT_E_ARG;
+    uint8_t* at = (uint8_t*)ws;
+    const size_t need = backward ? gact::gn_backward_bytes(*a) : gact::gn_forward_bytes(*a);
+    if (!at || !aligned(at, 16) || ws_bytes < need) return GACT_E_ARG;
+    a->partial = (float*)at;
+    at += gact::gn_partial_bytes(*a);
+    if (backward) {
+        a->sums = (float*)at;
+        a->means = (float*)(at + gact::gn_align((size_t)a->B * a->C * 2 * sizeof(float)));
+    } else if (!a->mean) {
+        a->mean = (float*)at;
+        a->rstd = (float*)(at + gact::gn_align((size_t)a->B * a->H * sizeof(float)));
+    }
+    return GACT_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t gact_group_norm_workspace_bytes(int64_t batch, int64_t pixels, int channels, int groups) {
+    if (!norm_sizes_ok(batch, pixels, channels, groups) || batch == 0 || pixels == 0) return 0;
+    gact::GnArgs a{};
+    norm_sizes(batch, pixels, channels, groups, &a);
+    const size_t f = gact::gn_forward_bytes(a), b = gact::gn_backward_bytes(a);
+    return f > b ? f : b;
+}
+
+int gact_group_norm(const gact_channel_norm* h_norm, void* d_workspace, size_t workspace_bytes, void* stream) {
+    gact::GnArgs a{};
+    int bits = 0;
+    if (const int rc = stage_norm(h_norm, false, d_workspace, workspace_bytes, &a, &bits)) return rc;
+    if (a.B == 0) return GACT_OK;
+    return gact_launch_group_norm(&a, h_norm->dtype, bits, h_norm->act, stream) == 0 ? GACT_OK : GACT_E_HIP;
+}
+
+int gact_group_norm_backward(const gact_channel_norm* h_norm, void* d_workspace, size_t workspace_bytes, void* stream) {
+    gact::GnArgs a{};
+    int bits = 0;
+    if (const int rc = stage_norm(h_norm, true, d_workspace, workspace_bytes, &a, &bits)) return rc;
+    if (a.B == 0) {                                     // nothing to add: the sums are zero
+        if (!a.dw && !a.db) return GACT_OK;
+        return gact_launch_group_norm_zero(&a, stream) == 0 ? GACT_OK : GACT_E_HIP;
+    }
+    return gact_launch_group_norm_backward(&a, h_norm->dtype, bits, h_norm->act, stream) == 0 ? GACT_OK : GACT_E_HIP;
+}
 
 size_t gact_linear_weight_grad_workspace_bytes(int64_t tokens, int64_t out_features, int64_t in_features, gact_dtype dtype) {
     if (!weight_sizes_ok(tokens, out_features, in_features) || !dtype_ok((int)dtype)) return 0;

@@ -224,6 +224,10 @@ int gact_linear_weight_grad(const void* d_dy, int64_t dy_stride, gact_dtype dtyp
     a.splits = plan.splits;
     a.chunks = plan.chunks;
     a.db_every = plan.db_every;
+    const uint32_t BT = (uint32_t)gact::weight_tile((int)dtype, plan.which).tokens;
+    a.dy_chunk = BT * (uint32_t)dy_stride * (uint32_t)size_of(dtype);
+    a.code_chunk = BT * a.K / 8 * (uint32_t)bits;
+    a.group_chunk = BT * a.K / a.group * 4;
     a.w_f32 = w_dtype == GACT_F32;
     return gact_launch_weight(&a, plan.which, (int)dtype, bits, stream) == 0 ? GACT_OK : GACT_E_HIP;
 }

@@ -37,8 +37,24 @@ struct WeightArgs {
     uint32_t       tiles_n, tiles_k, splits;
     uint32_t       chunks;              // of a split
     uint32_t       db_every;            // a block adds every so many-th chunk to db
+    uint32_t       dy_chunk, code_chunk, group_chunk;   // bytes from chunk to chunk (kEven)
     int32_t        w_f32;
 };
+
+// How a launch loads.
+//   kOdd    anything: elements of x in blocks of eight whose codes begin inside bytes and may pass from group to group
+//   kWhole  in_features a multiple of eight: whole bytes, one group a block
+//   kEven   and out_features of what a lane loads, a chunk's tokens of whole groups, and a split within 2^31 bytes of each of its
+//           tensors: offsets are counted on by the wavefront, and what lies behind the end reads as zero
+enum { kOdd, kWhole, kEven };
+inline int weight_mode(const WeightArgs& a, int dtype, int bits, int which) {
+    if (a.K % 8 != 0) return kOdd;
+    const uint64_t size = dtype == GACT_DT_F32 ? 4 : 2, BT = (uint64_t)weight_tile(dtype, which).tokens;
+    if (a.N % (16 / size) != 0 || BT * a.K % a.group != 0 || a.dy_stride < (int64_t)a.N || a.T == 0) return kWhole;
+    const uint64_t tokens = ((uint64_t)a.chunks + 1) * BT, most = 1ull << 31;       // and the chunk behind the last
+    if ((uint64_t)a.dy_stride >= most || tokens * (uint64_t)a.dy_stride * size >= most || tokens * a.K * 4 >= most) return kWhole;
+    return kEven;
+}
 
 inline uint64_t weight_up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
@@ -70,6 +86,9 @@ inline size_t weight_partial_bytes(const WeightPlan& p, uint64_t N, uint64_t K) 
 inline size_t weight_workspace_bytes(const WeightPlan& p, uint64_t N, uint64_t K) {
     return weight_partial_bytes(p, N, K) + (p.db_apart ? (size_t)p.splits * p.db_every * N * sizeof(float) : 0);
 }
+
+// Parts that a workgroup of the second launch divides the splits into.
+inline int join_parts(uint32_t splits) { return splits >= 64 ? 16 : splits >= 12 ? 4 : 1; }
 
 }  // namespace gact
 

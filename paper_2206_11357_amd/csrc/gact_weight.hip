@@ -83,6 +83,28 @@ __device__ __forceinline__ void decode_x(const Codes<BITS>& c, float (&x)[8]) {
     }
 }
 
+// ---------------------------------------------------------------- buffer loads
+// From a buffer of so many bytes, at an offset of the lane's and one of the wavefront's; zeros behind the end.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_of(const void* p, uint64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(uint32_t)bytes, 0x00027000);
+}
+__device__ __forceinline__ uint32_t buffer_word(Buffer b, uint32_t lane, uint32_t wave) {
+    return __builtin_amdgcn_raw_buffer_load_b32(b, lane, wave, 0);
+}
+template <int BITS>
+__device__ __forceinline__ void buffer_codes(Buffer b, uint32_t lane, uint32_t wave, Codes<BITS>& c) {
+    c.hi = 0;
+    if (BITS == 1) c.lo = __builtin_amdgcn_raw_buffer_load_b8(b, lane, wave, 0);
+    if (BITS == 2) c.lo = __builtin_amdgcn_raw_buffer_load_b16(b, lane, wave, 0);
+    if (BITS == 4) c.lo = buffer_word(b, lane, wave);
+    if (BITS == 8) {
+        const w2 w = __builtin_bit_cast(w2, __builtin_amdgcn_raw_buffer_load_b64(b, lane, wave, 0));
+        c.lo = w.x;
+        c.hi = w.y;
+    }
+}
+
 // ------------------------------------------------------------------ the tiles
 template <int DT, int WHICH>
 struct Tiling {
@@ -103,9 +125,13 @@ struct Tiling {
     static_assert(kWeightThreads % kRowPieces == 0 && BT * kRowPieces % kWeightThreads == 0, "a thread stays in its column");
 };
 
-template <int DT, int BITS, int WHICH, bool WHOLE>
+// bytes of a buffer: all that a split reaches lies below 2^31 (weight_mode)
+__device__ __forceinline__ uint64_t within(uint64_t bytes) { return bytes < 0x80000000ull ? bytes : 0x80000000ull; }
+
+template <int DT, int BITS, int WHICH, int MODE>
 __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a) {
     typedef Tiling<DT, WHICH> L;
+    constexpr bool WHOLE = MODE != kOdd;
     constexpr int BN = L::BN, BK = L::BK, BT = L::BT, TN = L::TN, TK = L::TK;
     __shared__ __align__(16) uint8_t lds[2][L::kBuf];
     const uint32_t tid = threadIdx.x;
@@ -134,7 +160,40 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
 
     w4 dy[L::kPieces];
     Codes<BITS> codes[L::kBlocks];
+    // kEven: a split's rows, codes, minima and steps as buffers from its first token on; a lane's offsets in them stay, the
+    // wavefront's go on from chunk to chunk.  What lies behind the last token reads as zero.
+    Buffer in_dy, in_codes, in_mn, in_step;
+    uint32_t dy_at[L::kPieces], code_at[L::kBlocks], group_at[L::kBlocks];
+    if constexpr (MODE == kEven) {
+        const uint64_t t0 = (uint64_t)c0 * BT, tokens = a.T - t0;
+        in_dy = buffer_of(a.dy + t0 * a.dy_stride * L::kSize, within(((tokens - 1) * a.dy_stride + a.N) * L::kSize));
+        in_codes = buffer_of(a.packed + t0 * a.K / 8 * BITS, within(tokens * a.K / 8 * BITS));
+        const uint64_t g0 = t0 * a.K / a.group, groups = (uint64_t)a.last_group + 1 - g0;
+        in_mn = buffer_of(a.gmin + g0, within(groups * 4));
+        in_step = buffer_of(a.gscale + g0, within(groups * 4));
+#pragma unroll
+        for (int q = 0; q < L::kPieces; ++q) dy_at[q] = ((pt + q * kRows) * (uint32_t)a.dy_stride + n) * L::kSize;
+#pragma unroll
+        for (int q = 0; q < L::kBlocks; ++q) {
+            const uint32_t e = (bt + q * kXRows) * a.K + k;
+            code_at[q] = e / 8 * BITS;
+            group_at[q] = divided(e >> 5, a.by_group) * 4;
+        }
+    }
     const auto fetch = [&](uint32_t chunk) {
+        if constexpr (MODE == kEven) {
+            const uint32_t i = chunk - c0;
+#pragma unroll
+            for (int q = 0; q < L::kPieces; ++q)
+                dy[q] = __builtin_bit_cast(w4, __builtin_amdgcn_raw_buffer_load_b128(in_dy, dy_at[q], i * a.dy_chunk, 0));
+#pragma unroll
+            for (int q = 0; q < L::kBlocks; ++q) {
+                buffer_codes<BITS>(in_codes, code_at[q], i * a.code_chunk, codes[q]);
+                codes[q].mn[0] = __builtin_bit_cast(float, buffer_word(in_mn, group_at[q], i * a.group_chunk));
+                codes[q].step[0] = __builtin_bit_cast(float, buffer_word(in_step, group_at[q], i * a.group_chunk));
+            }
+            return;
+        }
         const uint32_t t0 = chunk * BT;
 #pragma unroll
         for (int q = 0; q < L::kPieces; ++q) {
@@ -304,48 +363,62 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
     }
 }
 
-// dW and db from the splits' sums, added in their order: a thread four neighbouring elements of dW, or one of db.
+// dW and db from the splits' sums.  A workgroup takes 1024 / PARTS neighbouring elements of dW, four a thread, and each
+// PARTS-th of the splits goes to one of its PARTS parts, whose sums are added in their order; the workgroups behind them add db
+// likewise, a thread an element.  Many splits are those of a small dW, whose elements alone would not fill the GPU.
 constexpr int kJoinThreads = 256;
 __device__ __forceinline__ void put_weight(void* p, int f32, size_t i, float v) {
     if (f32) ((float*)p)[i] = v;
     else ((uint16_t*)p)[i] = (uint16_t)bf16_pair_rne(v, 0.0f);
 }
+template <int PARTS>
 __global__ __launch_bounds__(kJoinThreads) void weight_join_kernel(WeightArgs a, uint32_t dw_blocks) {
-    const size_t n = (size_t)a.N * a.K;
-    if (blockIdx.x < dw_blocks) {
-        const size_t i = ((size_t)blockIdx.x * kJoinThreads + threadIdx.x) * 4;
-        if (i >= n) return;
+    constexpr uint32_t kEach = kJoinThreads / PARTS;
+    __shared__ wf4 lds[PARTS][kEach];
+    const uint32_t part = threadIdx.x / kEach, j = threadIdx.x % kEach;
+    const bool of_db = blockIdx.x >= dw_blocks;
+    const size_t n = of_db ? a.N : (size_t)a.N * a.K;
+    const size_t i = ((size_t)(of_db ? blockIdx.x - dw_blocks : blockIdx.x) * kEach + j) * 4;
+    const float* from = of_db ? a.db_partial : a.partial;
+    const uint32_t terms = of_db ? a.splits * a.db_every : a.splits;
+    wf4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (i < n) {
         if (n % 4 == 0) {
-            wf4 s = *(const wf4*)(a.partial + i);
-            for (uint32_t k = 1; k < a.splits; ++k) {
-                const wf4 v = *(const wf4*)(a.partial + k * n + i);
+#pragma unroll 8
+            for (uint32_t k = part; k < terms; k += PARTS) {
+                const wf4 v = *(const wf4*)(from + k * n + i);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[j] += v[j];
+                for (int c = 0; c < 4; ++c) s[c] += v[c];
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) put_weight(a.dw, a.w_f32, i + j, s[j]);
         } else {
-            for (size_t e = i; e < i + 4 && e < n; ++e) {
-                float s = a.partial[e];
-                for (uint32_t k = 1; k < a.splits; ++k) s += a.partial[k * n + e];
-                put_weight(a.dw, a.w_f32, e, s);
-            }
+            for (uint32_t k = part; k < terms; k += PARTS)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) s[c] += i + c < n ? from[k * n + i + c] : 0.0f;
         }
-    } else {
-        const uint32_t i = (blockIdx.x - dw_blocks) * kJoinThreads + threadIdx.x;
-        if (i >= a.N) return;
-        float s = 0.0f;
-        for (uint32_t k = 0; k < a.splits * a.db_every; ++k) s += a.db_partial[(size_t)k * a.N + i];
-        put_weight(a.db, a.w_f32, i, s);
     }
+    if (PARTS > 1) {
+        lds[part][j] = s;
+        __syncthreads();
+        if (part != 0) return;
+#pragma unroll
+        for (int k = 1; k < PARTS; ++k)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[c] += lds[k][j][c];
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (i + c < n) put_weight(of_db ? a.db : a.dw, a.w_f32, i + c, s[c]);
 }
 
 // ------------------------------------------------------------- host launchers
 template <int DT, int BITS, int WHICH>
 static void launch_tile(const WeightArgs& a, hipStream_t s) {
     const dim3 grid(a.tiles_n * a.tiles_k * a.splits), block(kWeightThreads);
-    if (a.K % 8 == 0) hipLaunchKernelGGL((weight_kernel<DT, BITS, WHICH, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((weight_kernel<DT, BITS, WHICH, false>), grid, block, 0, s, a);
+    switch (weight_mode(a, DT, BITS, WHICH)) {
+        case kEven: hipLaunchKernelGGL((weight_kernel<DT, BITS, WHICH, kEven>), grid, block, 0, s, a); break;
+        case kWhole: hipLaunchKernelGGL((weight_kernel<DT, BITS, WHICH, kWhole>), grid, block, 0, s, a); break;
+        default: hipLaunchKernelGGL((weight_kernel<DT, BITS, WHICH, kOdd>), grid, block, 0, s, a); break;
+    }
 }
 template <int DT, int BITS>
 static void launch_bits(const WeightArgs& a, int which, hipStream_t s) {
@@ -370,10 +443,16 @@ extern "C" int gact_launch_weight(const gact::WeightArgs* a, int which, int dtyp
     else gact::launch_type<GACT_DT_BF16>(*a, which, bits, s);
     if (hipGetLastError() != hipSuccess) return -1;
     if (a->splits > 1) {
-        const uint64_t n = (uint64_t)a->N * a->K, each = 4 * gact::kJoinThreads;
+        const int parts = gact::join_parts(a->splits);
+        const uint64_t n = (uint64_t)a->N * a->K, each = 4 * gact::kJoinThreads / parts;
         const uint32_t dw_blocks = (uint32_t)((n + each - 1) / each);
-        const uint32_t db_blocks = a->db ? (a->N + gact::kJoinThreads - 1) / gact::kJoinThreads : 0;
-        hipLaunchKernelGGL(gact::weight_join_kernel, dim3(dw_blocks + db_blocks), dim3(gact::kJoinThreads), 0, s, *a, dw_blocks);
+        const uint32_t db_blocks = a->db ? (uint32_t)((a->N + each - 1) / each) : 0;
+        const dim3 grid(dw_blocks + db_blocks), block(gact::kJoinThreads);
+        switch (parts) {
+            case 1: hipLaunchKernelGGL(gact::weight_join_kernel<1>, grid, block, 0, s, *a, dw_blocks); break;
+            case 4: hipLaunchKernelGGL(gact::weight_join_kernel<4>, grid, block, 0, s, *a, dw_blocks); break;
+            default: hipLaunchKernelGGL(gact::weight_join_kernel<16>, grid, block, 0, s, *a, dw_blocks); break;
+        }
         if (hipGetLastError() != hipSuccess) return -1;
     }
     return 0;

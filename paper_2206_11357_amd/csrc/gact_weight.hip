@@ -71,11 +71,15 @@ __device__ __forceinline__ Codes<BITS> load_x(const WeightArgs& a, uint64_t e) {
 // their values in binary32, each operation rounded
 template <int BITS, bool WHOLE>
 __device__ __forceinline__ void decode_x(const Codes<BITS>& c, float (&x)[8]) {
+    // 4 bits: every other nibble of a word, so that its bytes convert in place (an empty statement keeps the compiler from
+    // taking each nibble out by itself)
+    uint32_t even = c.lo & 0x0F0F0F0Fu, odd = c.lo >> 4 & 0x0F0F0F0Fu;
+    if (BITS == 4) asm("" : "+v"(even), "+v"(odd));
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const uint32_t word = BITS == 8 && j >= 4 ? c.hi : c.lo;
         const uint32_t q = BITS == 8 ? word >> (8 * (j & 3)) & 0xFFu
-                         : BITS == 4 ? ((j & 1 ? word >> 4 : word) & 0x0F0F0F0Fu) >> (8 * (j >> 1)) & 0xFFu
+                         : BITS == 4 ? (j & 1 ? odd : even) >> (8 * (j >> 1)) & 0xFFu
                          : word >> (j * BITS) & ((1u << BITS) - 1u);
         const bool next = !WHOLE && (uint32_t)j >= c.turn;
         const float t = (float)q * (next ? c.step[1] : c.step[0]);
@@ -226,22 +230,22 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
     float sum[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
-    const auto place = [&](uint8_t* buf, bool add) {
+    const auto add_db = [&] {
+#pragma unroll
+        for (int q = 0; q < L::kPieces; ++q)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t v = dy[q][j];
+                if (DT == GACT_DT_F32) sum[j] += __builtin_bit_cast(float, v);
+                else {
+                    sum[2 * j] += __builtin_bit_cast(float, v << 16);
+                    sum[2 * j + 1] += __builtin_bit_cast(float, v & 0xFFFF0000u);
+                }
+            }
+    };
+    const auto place = [&](uint8_t* buf) {
 #pragma unroll
         for (int q = 0; q < L::kPieces; ++q) *(w4*)(buf + (pt + q * kRows) * L::kRowN + pn * 16) = dy[q];
-        if (add) {
-#pragma unroll
-            for (int q = 0; q < L::kPieces; ++q)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t v = dy[q][j];
-                    if (DT == GACT_DT_F32) sum[j] += __builtin_bit_cast(float, v);
-                    else {
-                        sum[2 * j] += __builtin_bit_cast(float, v << 16);
-                        sum[2 * j + 1] += __builtin_bit_cast(float, v & 0xFFFF0000u);
-                    }
-                }
-        }
         if (x_thread) {
 #pragma unroll
             for (int q = 0; q < L::kBlocks; ++q) {
@@ -314,14 +318,19 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
     const auto adds = [&](uint32_t chunk) { return with_db && chunk % a.db_every == (a.db_partial ? tile_k : 0); };
     if (c0 < c1) {
         fetch(c0);
-        place(lds[0], adds(c0));
+        if (adds(c0)) add_db();
+        place(lds[0]);
+        if (c0 + 1 < c1) fetch(c0 + 1);
         __syncthreads();
         for (uint32_t c = c0; c < c1; ++c) {
+            // a chunk is multiplied while the next one is decoded and the one behind it is on its way
             const uint32_t now = (c - c0) & 1u;
-            const bool more = c + 1 < c1;
-            if (more) fetch(c + 1);
+            if (c + 1 < c1) {
+                if (adds(c + 1)) add_db();
+                place(lds[now ^ 1u]);
+                if (c + 2 < c1) fetch(c + 2);
+            }
             multiply(lds[now]);
-            if (more) place(lds[now ^ 1u], adds(c + 1));
             __syncthreads();
         }
     }

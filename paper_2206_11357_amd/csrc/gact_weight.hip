@@ -68,23 +68,25 @@ __device__ __forceinline__ Codes<BITS> load_x(const WeightArgs& a, uint64_t e) {
     }
     return c;
 }
-// their values in binary32, each operation rounded
+// 4 bits: every other nibble of a word, so that its bytes convert in place (an empty statement keeps the compiler from
+// taking each nibble out by itself).
+template <int BITS>
+__device__ __forceinline__ void part_codes(Codes<BITS>& c) {
+    if (BITS != 4) return;
+    c.hi = c.lo >> 4 & 0x0F0F0F0Fu;
+    c.lo &= 0x0F0F0F0Fu;
+    asm("" : "+v"(c.lo), "+v"(c.hi));
+}
+// Value j of them in binary32, each operation rounded.
 template <int BITS, bool WHOLE>
-__device__ __forceinline__ void decode_x(const Codes<BITS>& c, float (&x)[8]) {
-    // 4 bits: every other nibble of a word, so that its bytes convert in place (an empty statement keeps the compiler from
-    // taking each nibble out by itself)
-    uint32_t even = c.lo & 0x0F0F0F0Fu, odd = c.lo >> 4 & 0x0F0F0F0Fu;
-    if (BITS == 4) asm("" : "+v"(even), "+v"(odd));
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t word = BITS == 8 && j >= 4 ? c.hi : c.lo;
-        const uint32_t q = BITS == 8 ? word >> (8 * (j & 3)) & 0xFFu
-                         : BITS == 4 ? (j & 1 ? odd : even) >> (8 * (j >> 1)) & 0xFFu
-                         : word >> (j * BITS) & ((1u << BITS) - 1u);
-        const bool next = !WHOLE && (uint32_t)j >= c.turn;
-        const float t = (float)q * (next ? c.step[1] : c.step[0]);
-        x[j] = t + (next ? c.mn[1] : c.mn[0]);
-    }
+__device__ __forceinline__ float value_of(const Codes<BITS>& c, int j) {
+    const uint32_t word = BITS == 8 ? (j >= 4 ? c.hi : c.lo) : BITS == 4 && (j & 1) != 0 ? c.hi : c.lo;
+    const uint32_t q = BITS == 8 ? word >> (8 * (j & 3)) & 0xFFu
+                     : BITS == 4 ? word >> (8 * (j >> 1)) & 0xFFu
+                     : word >> (j * BITS) & ((1u << BITS) - 1u);
+    const bool next = !WHOLE && (uint32_t)j >= c.turn;
+    const float t = (float)q * (next ? c.step[1] : c.step[0]);
+    return t + (next ? c.mn[1] : c.mn[0]);
 }
 
 // ---------------------------------------------------------------- buffer loads
@@ -110,6 +112,14 @@ __device__ __forceinline__ void buffer_codes(Buffer b, uint32_t lane, uint32_t w
 }
 
 // ------------------------------------------------------------------ the tiles
+template <int DT>
+struct Operand {
+    typedef wb8 type;
+};
+template <>
+struct Operand<GACT_DT_F32> {
+    typedef float type;
+};
 template <int DT, int WHICH>
 struct Tiling {
     static constexpr WeightTile tile = weight_tile(DT, WHICH);
@@ -160,7 +170,7 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
     const uint32_t bk = tid % L::kRowBlocks, bt = tid / L::kRowBlocks;
     constexpr uint32_t kXRows = kWeightThreads / L::kRowBlocks;
     const uint32_t k = k0 + bk * 8;
-    const bool x_thread = bt < (uint32_t)BT;
+    const bool x_thread = BT * L::kRowBlocks >= kWeightThreads || bt < (uint32_t)BT;
 
     w4 dy[L::kPieces];
     Codes<BITS> codes[L::kBlocks];
@@ -184,18 +194,23 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
             group_at[q] = divided(e >> 5, a.by_group) * 4;
         }
     }
+    const auto fetch_dy = [&](uint32_t chunk, int q) {
+        dy[q] = __builtin_bit_cast(w4, __builtin_amdgcn_raw_buffer_load_b128(in_dy, dy_at[q], (chunk - c0) * a.dy_chunk, 0));
+    };
+    const auto fetch_x = [&](uint32_t chunk) {
+        const uint32_t i = chunk - c0;
+#pragma unroll
+        for (int q = 0; q < L::kBlocks; ++q) {
+            buffer_codes<BITS>(in_codes, code_at[q], i * a.code_chunk, codes[q]);
+            codes[q].mn[0] = __builtin_bit_cast(float, buffer_word(in_mn, group_at[q], i * a.group_chunk));
+            codes[q].step[0] = __builtin_bit_cast(float, buffer_word(in_step, group_at[q], i * a.group_chunk));
+        }
+    };
     const auto fetch = [&](uint32_t chunk) {
         if constexpr (MODE == kEven) {
-            const uint32_t i = chunk - c0;
 #pragma unroll
-            for (int q = 0; q < L::kPieces; ++q)
-                dy[q] = __builtin_bit_cast(w4, __builtin_amdgcn_raw_buffer_load_b128(in_dy, dy_at[q], i * a.dy_chunk, 0));
-#pragma unroll
-            for (int q = 0; q < L::kBlocks; ++q) {
-                buffer_codes<BITS>(in_codes, code_at[q], i * a.code_chunk, codes[q]);
-                codes[q].mn[0] = __builtin_bit_cast(float, buffer_word(in_mn, group_at[q], i * a.group_chunk));
-                codes[q].step[0] = __builtin_bit_cast(float, buffer_word(in_step, group_at[q], i * a.group_chunk));
-            }
+            for (int q = 0; q < L::kPieces; ++q) fetch_dy(chunk, q);
+            fetch_x(chunk);
             return;
         }
         const uint32_t t0 = chunk * BT;
@@ -243,23 +258,27 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
                 }
             }
     };
+    const auto place_dy = [&](uint8_t* buf, int q) { *(w4*)(buf + (pt + q * kRows) * L::kRowN + pn * 16) = dy[q]; };
+    const auto place_x = [&](uint8_t* buf, int q, const float (&x)[8]) {
+        uint8_t* p = buf + L::kBufN + (bt + q * kXRows) * L::kRowK + bk * (8 * L::kSize);
+        if (DT == GACT_DT_F32) {
+            *(wf4*)p = wf4{x[0], x[1], x[2], x[3]};
+            *(wf4*)(p + 16) = wf4{x[4], x[5], x[6], x[7]};
+        } else {
+            *(w4*)p = w4{bf16_pair_rne(x[0], x[1]), bf16_pair_rne(x[2], x[3]), bf16_pair_rne(x[4], x[5]), bf16_pair_rne(x[6], x[7])};
+        }
+    };
     const auto place = [&](uint8_t* buf) {
 #pragma unroll
-        for (int q = 0; q < L::kPieces; ++q) *(w4*)(buf + (pt + q * kRows) * L::kRowN + pn * 16) = dy[q];
-        if (x_thread) {
+        for (int q = 0; q < L::kPieces; ++q) place_dy(buf, q);
+        if (!x_thread) return;
 #pragma unroll
-            for (int q = 0; q < L::kBlocks; ++q) {
-                float x[8];
-                decode_x<BITS, WHOLE>(codes[q], x);
-                uint8_t* p = buf + L::kBufN + (bt + q * kXRows) * L::kRowK + bk * (8 * L::kSize);
-                if (DT == GACT_DT_F32) {
-                    *(wf4*)p = wf4{x[0], x[1], x[2], x[3]};
-                    *(wf4*)(p + 16) = wf4{x[4], x[5], x[6], x[7]};
-                } else {
-                    *(w4*)p = w4{bf16_pair_rne(x[0], x[1]), bf16_pair_rne(x[2], x[3]), bf16_pair_rne(x[4], x[5]),
-                                 bf16_pair_rne(x[6], x[7])};
-                }
-            }
+        for (int q = 0; q < L::kBlocks; ++q) {
+            float x[8];
+            part_codes<BITS>(codes[q]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = value_of<BITS, WHOLE>(codes[q], j);
+            place_x(buf, q, x);
         }
     };
 
@@ -272,46 +291,91 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
         for (int j = 0; j < TK; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-    const auto multiply = [&](const uint8_t* buf) {
+    // Operands of step s of a chunk in registers: part i of the rows, part j of the columns, of a 32 x 32 product each.
+    //   bf16  a step is 16 tokens; 16 lanes read 4 rows of 16 elements, of which each gets a column
+    //   fp32  a step is two tokens; a lane's operands are TN (TK) neighbouring elements of row 2 s + lane / 32
+    typedef typename Operand<DT>::type Op;
+    constexpr int kSteps = BT / (DT == GACT_DT_F32 ? 2 : 16);
+    const uint32_t op_row = DT == GACT_DT_F32 ? (uint32_t)(lane >> 5) : (uint32_t)(8 * (lane >> 5) + ((lane & 15) >> 2));
+    const int col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    const uint32_t op_n = op_row * L::kRowN + (DT == GACT_DT_F32 ? (wn * 32 * TN + (lane & 31) * TN) * 4 : (wn * 32 * TN + col) * 2);
+    const uint32_t op_k = L::kBufN + op_row * L::kRowK + (DT == GACT_DT_F32 ? (wk * 32 * TK + (lane & 31) * TK) * 4 : (wk * 32 * TK + col) * 2);
+    const auto columns = [](const uint8_t* p, int stride) {
+        typedef __attribute__((address_space(3))) ws4* lds_ptr;
+        union { ws4 h[2]; Op v; } u;
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * stride));
+        return u.v;
+    };
+    const auto read_n = [&](const uint8_t* buf, int s, int i, Op (&x)[TN]) {
         if constexpr (DT == GACT_DT_F32) {
-            // a lane's operands: TN (TK) neighbouring elements of row 2 s + lane / 32, one for each product
-            const uint8_t* pa = buf + (lane >> 5) * L::kRowN + (wn * 32 * TN + (lane & 31) * TN) * 4;
-            const uint8_t* pb = buf + L::kBufN + (lane >> 5) * L::kRowK + (wk * 32 * TK + (lane & 31) * TK) * 4;
-#pragma unroll
-            for (int s = 0; s < BT / 2; ++s) {
-                float x[TN], y[TK];
-                __builtin_memcpy(x, __builtin_assume_aligned(pa + 2 * s * L::kRowN, 4 * TN), 4 * TN);
-                __builtin_memcpy(y, __builtin_assume_aligned(pb + 2 * s * L::kRowK, 4 * TK), 4 * TK);
-#pragma unroll
-                for (int i = 0; i < TN; ++i)
-#pragma unroll
-                    for (int j = 0; j < TK; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[j], acc[i][j], 0, 0, 0);
-            }
+            if (i == 0) __builtin_memcpy(x, __builtin_assume_aligned(buf + op_n + 2 * s * L::kRowN, 4 * TN), 4 * TN);
         } else {
-            // 16 lanes read 4 rows of 16 elements, of which each gets a column
-            const int row = 8 * (lane >> 5) + ((lane & 15) >> 2), col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-            const uint8_t* pa = buf + row * L::kRowN + (wn * 32 * TN + col) * 2;
-            const uint8_t* pb = buf + L::kBufN + row * L::kRowK + (wk * 32 * TK + col) * 2;
-            const auto column = [](const uint8_t* p, int stride) {
-                typedef __attribute__((address_space(3))) ws4* lds_ptr;
-                union { ws4 h[2]; wb8 v; } u;
-                u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
-                u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * stride));
-                return u.v;
-            };
-#pragma unroll
-            for (int s = 0; s < BT / 16; ++s) {
-                wb8 x[TN], y[TK];
-#pragma unroll
-                for (int j = 0; j < TK; ++j) y[j] = column(pb + 16 * s * L::kRowK + 64 * j, L::kRowK);
-#pragma unroll
-                for (int i = 0; i < TN; ++i) x[i] = column(pa + 16 * s * L::kRowN + 64 * i, L::kRowN);
-#pragma unroll
-                for (int i = 0; i < TN; ++i)
-#pragma unroll
-                    for (int j = 0; j < TK; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
-            }
+            x[i] = columns(buf + op_n + 16 * s * L::kRowN + 64 * i, L::kRowN);
         }
+    };
+    const auto read_k = [&](const uint8_t* buf, int s, Op (&y)[TK]) {
+        if constexpr (DT == GACT_DT_F32) {
+            __builtin_memcpy(y, __builtin_assume_aligned(buf + op_k + 2 * s * L::kRowK, 4 * TK), 4 * TK);
+        } else {
+#pragma unroll
+            for (int j = 0; j < TK; ++j) y[j] = columns(buf + op_k + 16 * s * L::kRowK + 64 * j, L::kRowK);
+        }
+    };
+    const auto product = [&](int i, const Op (&x)[TN], const Op (&y)[TK]) {
+#pragma unroll
+        for (int j = 0; j < TK; ++j) {
+            if constexpr (DT == GACT_DT_F32) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[j], acc[i][j], 0, 0, 0);
+            else acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
+        }
+    };
+    const auto multiply = [&](const uint8_t* buf) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            Op x[TN], y[TK];
+            read_k(buf, s, y);
+#pragma unroll
+            for (int i = 0; i < TN; ++i) read_n(buf, s, i, x);
+#pragma unroll
+            for (int i = 0; i < TN; ++i) product(i, x, y);
+        }
+    };
+    // Chunk c is multiplied while chunk c + 1 is decoded and c + 2 fetched, a little of each behind every row of products, in this
+    // order: two wavefronts of a SIMD that do one after the other fall into step and leave the matrix unit idle together.
+    // Without a question, also behind the split's last chunk, where nothing is read outside the buffers and nothing uses what is
+    // placed.
+    const auto flow = [&](const uint8_t* buf, uint8_t* other, uint32_t c) {
+        constexpr int kSlots = kSteps * TN, kValues = 8 * L::kBlocks;
+        Op x[2][TN], y[2][TK];
+        float v[L::kBlocks][8];
+        read_k(buf, 0, y[0]);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) read_n(buf, 0, i, x[0]);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int i = 0; i < TN; ++i) {
+                const int slot = s * TN + i;
+                product(i, x[s & 1], y[s & 1]);
+                if (s + 1 < kSteps) {
+                    if (i == 0) read_k(buf, s + 1, y[(s + 1) & 1]);
+                    read_n(buf, s + 1, i, x[(s + 1) & 1]);
+                }
+#pragma unroll
+                for (int e = slot * kValues / kSlots; e < (slot + 1) * kValues / kSlots; ++e) {
+                    if (e % 8 == 0) part_codes<BITS>(codes[e / 8]);
+                    v[e / 8][e % 8] = value_of<BITS, WHOLE>(codes[e / 8], e % 8);
+                    if (e % 8 == 7) place_x(other, e / 8, v[e / 8]);
+                }
+                // dy in the first half, its loads in the second
+#pragma unroll
+                for (int q = 0; q < L::kPieces; ++q) {
+                    if (slot == q * kSlots / (2 * L::kPieces)) place_dy(other, q);
+                    if (slot == kSlots / 2 + q * kSlots / (2 * L::kPieces)) fetch_dy(c + 2, q);
+                }
+                if (slot == kSlots - 1) fetch_x(c + 2);
+                __builtin_amdgcn_sched_barrier(0);
+            }
     };
 
     const bool with_db = a.db != nullptr && (a.db_partial || tile_k == 0);
@@ -322,15 +386,20 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
         place(lds[0]);
         if (c0 + 1 < c1) fetch(c0 + 1);
         __syncthreads();
+        // A chunk is multiplied while the next one is decoded and the one behind it is on its way.
         for (uint32_t c = c0; c < c1; ++c) {
-            // a chunk is multiplied while the next one is decoded and the one behind it is on its way
             const uint32_t now = (c - c0) & 1u;
-            if (c + 1 < c1) {
-                if (adds(c + 1)) add_db();
-                place(lds[now ^ 1u]);
-                if (c + 2 < c1) fetch(c + 2);
+            if constexpr (MODE == kEven && WHICH == 0) {
+                if (c + 1 < c1 && adds(c + 1)) add_db();
+                flow(lds[now], lds[now ^ 1u], c);
+            } else {
+                if (c + 1 < c1) {
+                    if (adds(c + 1)) add_db();
+                    place(lds[now ^ 1u]);
+                    if (c + 2 < c1) fetch(c + 2);
+                }
+                multiply(lds[now]);
             }
-            multiply(lds[now]);
             __syncthreads();
         }
     }
@@ -358,14 +427,14 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
 
     if (!with_db) return;
     // db of the tile's rows: over the threads of a column, in their order
-    float* col = (float*)lds[0];
+    float* sums = (float*)lds[0];
 #pragma unroll
-    for (int j = 0; j < L::kPiece; ++j) col[pt * BN + pn * L::kPiece + j] = sum[j];
+    for (int j = 0; j < L::kPiece; ++j) sums[pt * BN + pn * L::kPiece + j] = sum[j];
     __syncthreads();
     for (uint32_t i = tid; i < (uint32_t)BN; i += kWeightThreads) {
         if (n0 + i >= a.N) continue;
         float s = 0.0f;
-        for (uint32_t r = 0; r < kRows; ++r) s += col[r * BN + i];
+        for (uint32_t r = 0; r < kRows; ++r) s += sums[r * BN + i];
         if (a.db_partial) a.db_partial[((size_t)split * a.db_every + tile_k) * a.N + n0 + i] = s;
         else if (a.w_f32) ((float*)a.db)[n0 + i] = s;
         else ((uint16_t*)a.db)[n0 + i] = (uint16_t)bf16_pair_rne(s, 0.0f);

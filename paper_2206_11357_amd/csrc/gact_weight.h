@@ -51,7 +51,7 @@ inline int weight_mode(const WeightArgs& a, int dtype, int bits, int which) {
     if (a.K % 8 != 0) return kOdd;
     const uint64_t size = dtype == GACT_DT_F32 ? 4 : 2, BT = (uint64_t)weight_tile(dtype, which).tokens;
     if (a.N % (16 / size) != 0 || BT * a.K % a.group != 0 || a.dy_stride < (int64_t)a.N || a.T == 0) return kWhole;
-    const uint64_t tokens = ((uint64_t)a.chunks + 2) * BT, most = 1ull << 31;       // and two chunks behind the last
+    const uint64_t tokens = ((uint64_t)a.chunks + 4) * BT, most = 1ull << 31;       // and what is fetched behind the last
     if ((uint64_t)a.dy_stride >= most || tokens * (uint64_t)a.dy_stride * size >= most || tokens * a.K * 4 >= most) return kWhole;
     return kEven;
 }

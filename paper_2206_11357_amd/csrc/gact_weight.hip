@@ -77,16 +77,19 @@ __device__ __forceinline__ void part_codes(Codes<BITS>& c) {
     c.lo &= 0x0F0F0F0Fu;
     asm("" : "+v"(c.lo), "+v"(c.hi));
 }
-// Value j of them in binary32, each operation rounded.
-template <int BITS, bool WHOLE>
+// Value j of them in binary32.  fp32: the product is rounded before the sum, as gact_decompress does it; bf16: once, in one
+// instruction, in front of the rounding to bf16.
+template <int DT, int BITS, bool WHOLE>
 __device__ __forceinline__ float value_of(const Codes<BITS>& c, int j) {
     const uint32_t word = BITS == 8 ? (j >= 4 ? c.hi : c.lo) : BITS == 4 && (j & 1) != 0 ? c.hi : c.lo;
     const uint32_t q = BITS == 8 ? word >> (8 * (j & 3)) & 0xFFu
                      : BITS == 4 ? word >> (8 * (j >> 1)) & 0xFFu
                      : word >> (j * BITS) & ((1u << BITS) - 1u);
     const bool next = !WHOLE && (uint32_t)j >= c.turn;
-    const float t = (float)q * (next ? c.step[1] : c.step[0]);
-    return t + (next ? c.mn[1] : c.mn[0]);
+    const float step = next ? c.step[1] : c.step[0], mn = next ? c.mn[1] : c.mn[0];
+    if (DT == GACT_DT_BF16) return __builtin_fmaf((float)q, step, mn);
+    const float t = (float)q * step;
+    return t + mn;
 }
 
 // ---------------------------------------------------------------- buffer loads
@@ -197,20 +200,18 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
     const auto fetch_dy = [&](uint32_t chunk, int q) {
         dy[q] = __builtin_bit_cast(w4, __builtin_amdgcn_raw_buffer_load_b128(in_dy, dy_at[q], (chunk - c0) * a.dy_chunk, 0));
     };
-    const auto fetch_x = [&](uint32_t chunk) {
+    const auto fetch_x = [&](uint32_t chunk, int q) {
         const uint32_t i = chunk - c0;
-#pragma unroll
-        for (int q = 0; q < L::kBlocks; ++q) {
-            buffer_codes<BITS>(in_codes, code_at[q], i * a.code_chunk, codes[q]);
-            codes[q].mn[0] = __builtin_bit_cast(float, buffer_word(in_mn, group_at[q], i * a.group_chunk));
-            codes[q].step[0] = __builtin_bit_cast(float, buffer_word(in_step, group_at[q], i * a.group_chunk));
-        }
+        buffer_codes<BITS>(in_codes, code_at[q], i * a.code_chunk, codes[q]);
+        codes[q].mn[0] = __builtin_bit_cast(float, buffer_word(in_mn, group_at[q], i * a.group_chunk));
+        codes[q].step[0] = __builtin_bit_cast(float, buffer_word(in_step, group_at[q], i * a.group_chunk));
     };
     const auto fetch = [&](uint32_t chunk) {
         if constexpr (MODE == kEven) {
 #pragma unroll
             for (int q = 0; q < L::kPieces; ++q) fetch_dy(chunk, q);
-            fetch_x(chunk);
+#pragma unroll
+            for (int q = 0; q < L::kBlocks; ++q) fetch_x(chunk, q);
             return;
         }
         const uint32_t t0 = chunk * BT;
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
             float x[8];
             part_codes<BITS>(codes[q]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = value_of<BITS, WHOLE>(codes[q], j);
+            for (int j = 0; j < 8; ++j) x[j] = value_of<DT, BITS, WHOLE>(codes[q], j);
             place_x(buf, q, x);
         }
     };
@@ -340,67 +341,102 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
             for (int i = 0; i < TN; ++i) product(i, x, y);
         }
     };
-    // Chunk c is multiplied while chunk c + 1 is decoded and c + 2 fetched, a little of each behind every row of products, in this
-    // order: two wavefronts of a SIMD that do one after the other fall into step and leave the matrix unit idle together.
+    // Large tiles: chunk c is multiplied while chunk c + 1 is placed, the first of its blocks decoded a step ahead, and c + 2
+    // fetched, a little of each behind every row of products, in this order: two wavefronts of a SIMD that do one after the other
+    // fall into step and leave the matrix unit idle together.  A step's operands are read during the step before it, so that
+    // all of a chunk's have been read by the beginning of its last step; there the one barrier of a chunk stands: behind it chunk
+    // c + 1 is whole, and the place of chunk c is free.
     // Without a question, also behind the split's last chunk, where nothing is read outside the buffers and nothing uses what is
     // placed.
-    const auto flow = [&](const uint8_t* buf, uint8_t* other, uint32_t c) {
-        constexpr int kSlots = kSteps * TN, kValues = 8 * L::kBlocks;
-        Op x[2][TN], y[2][TK];
-        float v[L::kBlocks][8];
+    constexpr int kEarly = kSteps == 2 ? L::kBlocks / 2 : 0;
+    Op x[2][TN], y[2][TK];
+    float v[L::kBlocks][8];
+    const auto decode = [&](uint32_t next, int e) {
+        const int q = e / 8;
+        if (e % 8 == 0) part_codes<BITS>(codes[q]);
+        v[q][e % 8] = value_of<DT, BITS, WHOLE>(codes[q], e % 8);
+        if (e % 8 == 7) fetch_x(next, q);
+    };
+    const auto read_all = [&](const uint8_t* buf) {
         read_k(buf, 0, y[0]);
 #pragma unroll
         for (int i = 0; i < TN; ++i) read_n(buf, 0, i, x[0]);
+    };
+    const auto flow = [&](const uint8_t* buf, uint8_t* other, uint32_t c) {
+        constexpr int kSlots = (kSteps - 1) * TN, kValues = 8 * (L::kBlocks - kEarly);
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
+        for (int s = 0; s + 1 < kSteps; ++s)
 #pragma unroll
             for (int i = 0; i < TN; ++i) {
                 const int slot = s * TN + i;
                 product(i, x[s & 1], y[s & 1]);
-                if (s + 1 < kSteps) {
-                    if (i == 0) read_k(buf, s + 1, y[(s + 1) & 1]);
-                    read_n(buf, s + 1, i, x[(s + 1) & 1]);
-                }
+                if (i == 0) read_k(buf, s + 1, y[(s + 1) & 1]);
+                read_n(buf, s + 1, i, x[(s + 1) & 1]);
+#pragma unroll
+                for (int q = 0; q < kEarly; ++q)
+                    if (slot == q) place_x(other, q, v[q]);
 #pragma unroll
                 for (int e = slot * kValues / kSlots; e < (slot + 1) * kValues / kSlots; ++e) {
-                    if (e % 8 == 0) part_codes<BITS>(codes[e / 8]);
-                    v[e / 8][e % 8] = value_of<BITS, WHOLE>(codes[e / 8], e % 8);
-                    if (e % 8 == 7) place_x(other, e / 8, v[e / 8]);
+                    decode(c + 2, 8 * kEarly + e);
+                    if (e % 8 == 7) place_x(other, kEarly + e / 8, v[kEarly + e / 8]);
                 }
-                // dy in the first half, its loads in the second
 #pragma unroll
-                for (int q = 0; q < L::kPieces; ++q) {
-                    if (slot == q * kSlots / (2 * L::kPieces)) place_dy(other, q);
-                    if (slot == kSlots / 2 + q * kSlots / (2 * L::kPieces)) fetch_dy(c + 2, q);
-                }
-                if (slot == kSlots - 1) fetch_x(c + 2);
+                for (int q = 0; q < L::kPieces; ++q)
+                    if (slot == q * kSlots / L::kPieces) {
+                        place_dy(other, q);
+                        fetch_dy(c + 2, q);
+                    }
                 __builtin_amdgcn_sched_barrier(0);
             }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            product(i, x[(kSteps - 1) & 1], y[(kSteps - 1) & 1]);
+            if (i == 0) read_k(other, 0, y[0]);
+            read_n(other, 0, i, x[0]);
+#pragma unroll
+            for (int e = i * 8 * kEarly / TN; e < (i + 1) * 8 * kEarly / TN; ++e) decode(c + 3, e);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
 
     const bool with_db = a.db != nullptr && (a.db_partial || tile_k == 0);
-    const auto adds = [&](uint32_t chunk) { return with_db && chunk % a.db_every == (a.db_partial ? tile_k : 0); };
+    // the next chunk that this block adds to db
+    uint32_t db_next = with_db && a.db_partial ? c0 + (tile_k + a.db_every - c0 % a.db_every) % a.db_every : with_db ? c0 : ~0u;
+    const auto adds = [&](uint32_t chunk) {
+        if (chunk != db_next) return false;
+        db_next += a.db_every;
+        return true;
+    };
     if (c0 < c1) {
         fetch(c0);
         if (adds(c0)) add_db();
         place(lds[0]);
-        if (c0 + 1 < c1) fetch(c0 + 1);
-        __syncthreads();
-        // A chunk is multiplied while the next one is decoded and the one behind it is on its way.
-        for (uint32_t c = c0; c < c1; ++c) {
-            const uint32_t now = (c - c0) & 1u;
-            if constexpr (MODE == kEven && WHICH == 0) {
+        if constexpr (MODE == kEven && WHICH == 0) {
+            fetch(c0 + 1);
+            __syncthreads();
+            read_all(lds[0]);
+#pragma unroll
+            for (int e = 0; e < 8 * kEarly; ++e) decode(c0 + 2, e);
+            for (uint32_t c = c0; c < c1; ++c) {
+                const uint32_t now = (c - c0) & 1u;
                 if (c + 1 < c1 && adds(c + 1)) add_db();
                 flow(lds[now], lds[now ^ 1u], c);
-            } else {
+            }
+            __syncthreads();
+        } else {
+            if (c0 + 1 < c1) fetch(c0 + 1);
+            __syncthreads();
+            for (uint32_t c = c0; c < c1; ++c) {
+                const uint32_t now = (c - c0) & 1u;
                 if (c + 1 < c1) {
                     if (adds(c + 1)) add_db();
                     place(lds[now ^ 1u]);
                     if (c + 2 < c1) fetch(c + 2);
                 }
                 multiply(lds[now]);
+                __syncthreads();
             }
-            __syncthreads();
         }
     }
 

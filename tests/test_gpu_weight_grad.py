@@ -1,5 +1,5 @@
-"""Weight gradient of a linear layer from the codes of its input, against the same sums in binary64 over what
-gact_decompress gives of the context."""
+"""Weight gradient of a linear layer from the codes of its input, against the same sums in binary64 over what the codes
+stand for."""
 import numpy as np
 import pytest
 import torch
@@ -23,7 +23,14 @@ def inputs(T, N, K, G, bits, dtype, seed=0, wide=0):
 def reference(dy, context, K, G, bits):
     """dW, db in binary64, and the sums of the terms' sizes."""
     T, N = dy.shape
-    x = gact.gact_decompress(*context, T * K, G, bits, dtype=dy.dtype).view(T, K).cpu().double()
+    if dy.dtype == torch.float32:
+        x = gact.gact_decompress(*context, T * K, G, bits).view(T, K).cpu().double()
+    else:
+        packed, gmin, gscale = (t.cpu() for t in context)
+        at = torch.arange(T * K)
+        q = (packed[at * bits // 8].long() >> (at * bits % 8)) & (2 ** bits - 1)
+        # the product has 32 bits at most; the sum is rounded to binary32 once (it fits 53 bits here), then to bf16
+        x = (q.double() * gscale[at // G].double() + gmin[at // G].double()).float().bfloat16().double().view(T, K)
     d = dy.cpu().double()
     return d.t() @ x, d.sum(0), d.abs().t() @ x.abs(), d.abs().sum(0)
 

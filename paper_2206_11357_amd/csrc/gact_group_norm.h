@@ -45,6 +45,10 @@ struct GnArgs {
     uint32_t    block_shift;            // log2 of a context group's blocks of eight
     float       eps;
     int32_t     w_f32;
+    // Kernels that hold their maps in registers: a workgroup takes the whole of a sample's next few units, a unit being a group of
+    // the norm, or a column where a group is part of one.  A unit's columns are lanes 0 .. unit_cols - 1 of 2^unit_shift.
+    uint32_t    units, unit_cols, unit_shift, slab_shift, col_shift;       // slab_shift: log2 of a slab's units; col_shift: of its lanes
+    uint32_t    unit_slabs, norm_blocks;
 };
 
 inline uint32_t gn_up(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
@@ -78,6 +82,36 @@ inline void plan_group_norm(GnArgs* a) {
     if (waves > 16384) waves = 16384;
     a->stride_passes = gn_up(waves, a->period) * a->period;
 }
+// Workgroups that hold `threads` x `blocks` blocks of eight.
+struct GnWhole {
+    uint32_t threads, blocks;
+};
+constexpr GnWhole kGnWhole[2] = {{256, 4}, {1024, 8}};
+// Whether a sample's group fits the registers of a workgroup: which of them it is (0: of none, 1, 2), and how it is laid out.
+inline int plan_whole(GnArgs* a, int dtype) {
+    uint32_t cols = a->D / 8;
+    if (a->D % 8 != 0) {
+        if (8 % a->D != 0) return 0;
+        cols = 1;
+    }
+    a->unit_cols = cols;
+    a->units = a->C8 / cols;
+    a->unit_shift = 0;
+    while ((1u << a->unit_shift) < cols) ++a->unit_shift;
+    if (a->unit_shift > 6) return 0;
+    // whole cache lines of a pixel, if they fit
+    const uint32_t size = dtype == GACT_DT_F32 ? 4 : 2;
+    uint32_t shift = 0;
+    while ((cols << shift) * 8 * size < 128 && (1u << shift) < a->units && a->unit_shift + shift < 6) ++shift;
+    const auto fits = [&](const GnWhole& w) { return (uint64_t)a->P << (a->unit_shift + shift) <= (uint64_t)w.threads * w.blocks; };
+    while (!fits(kGnWhole[1]) && shift > 0) --shift;
+    if (!fits(kGnWhole[1])) return 0;
+    a->slab_shift = shift;
+    a->col_shift = a->unit_shift + shift;
+    a->unit_slabs = gn_up(a->units, 1u << shift);
+    a->norm_blocks = a->B * a->unit_slabs;
+    return fits(kGnWhole[0]) ? 1 : 2;
+}
 inline size_t gn_align(size_t v) { return (v + 15) & ~(size_t)15; }
 // Workspace: partial sums; forward: mean and rstd where the caller keeps none; backward: sums, means.
 inline size_t gn_partial_bytes(const GnArgs& a) {
@@ -91,8 +125,9 @@ inline size_t gn_backward_bytes(const GnArgs& a) {
 }  // namespace gact
 
 // bits: 0 without a context; act: 0 none, 1 silu
-extern "C" int gact_launch_group_norm(const gact::GnArgs* a, int dtype, int bits, int act, void* stream);
-extern "C" int gact_launch_group_norm_backward(const gact::GnArgs* a, int dtype, int bits, int act, void* stream);
+// whole: what plan_whole gave
+extern "C" int gact_launch_group_norm(const gact::GnArgs* a, int dtype, int bits, int act, int whole, void* stream);
+extern "C" int gact_launch_group_norm_backward(const gact::GnArgs* a, int dtype, int bits, int act, int whole, void* stream);
 extern "C" int gact_launch_group_norm_zero(const gact::GnArgs* a, void* stream);       // dw and db of nothing
 
 #endif

@@ -21,6 +21,8 @@
 
 namespace gact {
 
+typedef float hf2 __attribute__((ext_vector_type(2)));
+
 // ----------------------------------------------------------------- activation
 // exp(-z).  The exponent's rounding, z times 2^-24 of the result, is taken back: fp32 results keep their last bits.
 template <int DT>
@@ -181,42 +183,81 @@ __device__ __forceinline__ double over_wave(double v) {
 }
 __device__ __forceinline__ uint32_t gn_wave() { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 
-// m and r of a sample's group, a wavefront each, from its columns' (channels') in all chunks, in binary64.
+// Sum over the workgroup, in all threads, of two values.
+__device__ __forceinline__ void over_block(double& u, double& v, double (&lds)[2][kGnThreads / 64]) {
+    u = over_wave(u);
+    v = over_wave(v);
+    if ((threadIdx.x & 63u) == 0) {
+        lds[0][threadIdx.x >> 6] = u;
+        lds[1][threadIdx.x >> 6] = v;
+    }
+    __syncthreads();
+    u = v = 0.0;
+#pragma unroll
+    for (int k = 0; k < kGnThreads / 64; ++k) {
+        u += lds[0][k];
+        v += lds[1][k];
+    }
+    __syncthreads();
+}
+
+// m and r of a sample's group, a workgroup each, from its columns' (channels') in all chunks, in binary64.
 template <bool UNI>
 __global__ __launch_bounds__(kGnThreads) void gn_finish_kernel(GnArgs a) {
-    const uint32_t i = blockIdx.x * (kGnThreads / 64) + gn_wave();
-    if (i >= a.B * a.H) return;
-    const uint32_t sample = i / a.H, h = i - sample * a.H, lane = threadIdx.x & 63u;
+    __shared__ double lds[2][kGnThreads / 64];
+    const uint32_t i = blockIdx.x, sample = i / a.H, h = i - sample * a.H;
     const uint32_t each = UNI ? a.D / 8 : a.D, row = UNI ? a.C8 : a.C, items = each * a.chunks;
     const float* p = a.partial + ((size_t)sample * a.chunks * row + (size_t)h * each) * 2;
     const double per = UNI ? 8.0 : 1.0, last = per * (a.P - (a.chunks - 1) * a.per_chunk), all = per * a.per_chunk;
-    double mean = 0.0, m2 = 0.0;
-    for (uint32_t k = lane; k < items; k += 64) {
+    double mean = 0.0, m2 = 0.0, none = 0.0;
+#pragma unroll 4
+    for (uint32_t k = threadIdx.x; k < items; k += kGnThreads) {
         const uint32_t chunk = k / each;
         mean += (chunk + 1 == a.chunks ? last : all) * (double)p[((size_t)chunk * row + (k - chunk * each)) * 2];
     }
-    mean = over_wave(mean) / ((double)a.P * a.D);
-    for (uint32_t k = lane; k < items; k += 64) {
+    over_block(mean, none, lds);
+    mean /= (double)a.P * a.D;
+#pragma unroll 4
+    for (uint32_t k = threadIdx.x; k < items; k += kGnThreads) {
         const uint32_t chunk = k / each;
         const float* v = p + ((size_t)chunk * row + (k - chunk * each)) * 2;
         const double d = (double)v[0] - mean;
         m2 += (double)v[1] + (chunk + 1 == a.chunks ? last : all) * d * d;
     }
-    m2 = over_wave(m2) / ((double)a.P * a.D);
-    if (lane != 0) return;
+    over_block(m2, none, lds);
+    m2 /= (double)a.P * a.D;
+    if (threadIdx.x != 0) return;
     a.mean[i] = (float)mean;
     a.rstd[i] = (float)(1.0 / sqrt(m2 + (double)a.eps));
 }
 
 // ------------------------------------------------------------------ y, context
+// Leaves the context of a pass, 64 blocks of eight that follow each other in x laid out contiguously.
+template <int BITS>
+__device__ __forceinline__ void gn_compress_pass(const GnArgs& a, uint32_t pass, uint32_t lane, bool active, const float (&v)[8]) {
+    const uint32_t e = pass * 64u + lane;
+    float mn, step;
+    const uint64_t codes = compress8<BITS>(v, active, 1 << a.block_shift, (uint64_t)pass * 64u, lane, a.seed_lo, a.seed_hi, mn, step);
+    if (!active) return;
+    store_codes<BITS>(a.packed + (uint64_t)e * BITS, codes);
+    if ((lane & ((1u << a.block_shift) - 1u)) == 0) {
+        a.gmin[e >> a.block_shift] = mn;
+        a.gscale[e >> a.block_shift] = step;
+    }
+}
+// The packed string ends at a multiple of 16 bytes, zeros behind the last code.
+template <int BITS>
+__device__ __forceinline__ void gn_zero_pad(const GnArgs& a, uint32_t lane) {
+    const uint64_t bytes = (uint64_t)a.blocks8 * BITS;
+    if (lane < (uint32_t)(0u - bytes & 15u)) a.packed[bytes + lane] = 0;
+}
+
 template <int DT, int BITS, bool UNI, bool SILU>
 __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
     const uint32_t lane = threadIdx.x & 63u;
     uint32_t pass = blockIdx.x * (kGnThreads / 64) + gn_wave();
-    if (BITS != 0 && pass == 0) {                      // the packed string ends at a multiple of 16 bytes, zeros behind the last code
-        const uint64_t bytes = (uint64_t)a.blocks8 * BITS;
-        if (lane < (uint32_t)(0u - bytes & 15u)) a.packed[bytes + lane] = 0;
-    }
+    if constexpr (BITS != 0)
+        if (pass == 0) gn_zero_pad<BITS>(a, lane);
     if (pass >= a.stride_passes || pass >= a.passes) return;
     uint32_t e = pass * 64u + lane;                    // the lane's block of eight
     uint32_t q = divided(e, a.by_c8);                  // its pixel, of all samples'
@@ -244,17 +285,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
         for (int k = 0; k < 8; ++k) y[k] = activate<DT, SILU>(__builtin_fmaf((v[k] - m[k]) * r[k], w[k], b[k]));
         if (active)
             store8<DT>((uint8_t*)a.y.p, ((int64_t)s * a.y.sample + (int64_t)p * a.y.pixel + c) * kSize<DT>, y);
-        if constexpr (BITS != 0) {
-            float mn, step;
-            const uint64_t codes = compress8<BITS>(v, active, 1 << a.block_shift, (uint64_t)pass * 64u, lane, a.seed_lo, a.seed_hi, mn, step);
-            if (active) {
-                store_codes<BITS>(a.packed + (uint64_t)e * BITS, codes);
-                if ((lane & ((1u << a.block_shift) - 1u)) == 0) {
-                    a.gmin[e >> a.block_shift] = mn;
-                    a.gscale[e >> a.block_shift] = step;
-                }
-            }
-        }
+        if constexpr (BITS != 0) gn_compress_pass<BITS>(a, pass, lane, active, v);
         if (a.passes - pass <= a.stride_passes) return;
         pass += a.stride_passes;
         e += e_step;
@@ -294,6 +325,17 @@ struct GnInput {
         }
     }
 };
+
+// x of a block of eight in binary32.
+template <int DT, int BITS>
+__device__ __forceinline__ void gn_load_x(const GnArgs& a, uint32_t sample, uint32_t p, uint32_t c8, float (&x)[8]) {
+    if constexpr (BITS != 0) {
+        const uint32_t e = (sample * a.P + p) * a.C8 + c8;
+        decompress8<BITS>(load_codes<BITS>(a.packed + (uint64_t)e * BITS), a.gmin[e >> a.block_shift], a.gscale[e >> a.block_shift], x);
+    } else {
+        widen8<DT>(load8<DT>((const uint8_t*)a.x.p, ((int64_t)sample * a.x.sample + (int64_t)p * a.x.pixel + (int64_t)c8 * 8) * kSize<DT>), x);
+    }
+}
 
 template <int DT, int BITS, bool UNI, bool SILU>
 __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnArgs a) {
@@ -350,46 +392,52 @@ __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnArgs a) {
     for (int k = 0; k < 8; ++k) { out[2 * k] = mine[k]; out[2 * k + 1] = mine[8 + k]; }
 }
 
-// Of a sample's group, a wavefront each: the channels' sums over the chunks, and the means of g and g n, in binary64.
+// Of a sample's group, a workgroup each: the channels' sums over the chunks, and the means of g and g n, in binary64.
 __global__ __launch_bounds__(kGnThreads) void gn_means_kernel(GnArgs a) {
-    const uint32_t i = blockIdx.x * (kGnThreads / 64) + gn_wave();
-    if (i >= a.B * a.H) return;
-    const uint32_t sample = i / a.H, h = i - sample * a.H, lane = threadIdx.x & 63u;
-    // lanes: D channels (64 of them at a time), and as many parts of the chunks as fit
-    const uint32_t wide = a.D < 64u ? a.D : 64u, parts = 64u / wide, part = lane / wide, d0 = lane - part * wide;
+    __shared__ double lds[2][kGnThreads];
+    __shared__ double of_block[2][kGnThreads / 64];
+    const uint32_t i = blockIdx.x, sample = i / a.H, h = i - sample * a.H;
+    // threads: D channels (all threads' at a time), and as many parts of the chunks as fit
+    const uint32_t wide = a.D < (uint32_t)kGnThreads ? a.D : (uint32_t)kGnThreads, parts = kGnThreads / wide;
+    const uint32_t part = threadIdx.x / wide, d0 = threadIdx.x - part * wide;
     double m1 = 0.0, m2 = 0.0;
-    for (uint32_t d = 0; d < a.D; d += 64u) {
+    for (uint32_t d = 0; d < a.D; d += wide) {
         const uint32_t c = h * a.D + d + d0;
         const bool holds = part < parts && d + d0 < a.D;
         double s0 = 0.0, s1 = 0.0;
         if (holds) {
             const float* p = a.partial + ((size_t)sample * a.chunks * a.C + c) * 2;
+#pragma unroll 4
             for (uint32_t k = part; k < a.chunks; k += parts) {
-                s0 += (double)p[(size_t)k * a.C * 2];
-                s1 += (double)p[(size_t)k * a.C * 2 + 1];
+                const hf2 v = *(const hf2*)(p + (size_t)k * a.C * 2);
+                s0 += (double)v.x;
+                s1 += (double)v.y;
             }
         }
         // over the parts, in their order
-        double t0 = 0.0, t1 = 0.0;
-        for (uint32_t k = 0; k < parts; ++k) {
-            t0 += __shfl(s0, (int)(d0 + k * wide));
-            t1 += __shfl(s1, (int)(d0 + k * wide));
+        lds[0][threadIdx.x] = s0;
+        lds[1][threadIdx.x] = s1;
+        __syncthreads();
+        if (holds && part == 0) {
+            for (uint32_t k = 1; k < parts; ++k) {
+                s0 += lds[0][d0 + k * wide];
+                s1 += lds[1][d0 + k * wide];
+            }
+            float* out = a.sums + ((size_t)sample * a.C + c) * 2;
+            out[0] = (float)s0;
+            out[1] = (float)s1;
+            double w = 1.0;
+            if (a.w) w = a.w_f32 ? (double)((const float*)a.w)[c]
+                                 : (double)__builtin_bit_cast(float, (uint32_t)((const uint16_t*)a.w)[c] << 16);
+            m1 += w * s0;
+            m2 += w * s1;
         }
-        if (!holds || part != 0) continue;
-        float* out = a.sums + ((size_t)sample * a.C + c) * 2;
-        out[0] = (float)t0;
-        out[1] = (float)t1;
-        double w = 1.0;
-        if (a.w) w = a.w_f32 ? (double)((const float*)a.w)[c]
-                             : (double)__builtin_bit_cast(float, (uint32_t)((const uint16_t*)a.w)[c] << 16);
-        m1 += w * t0;
-        m2 += w * t1;
+        __syncthreads();
     }
-    m1 = over_wave(m1) / ((double)a.P * a.D);
-    m2 = over_wave(m2) / ((double)a.P * a.D);
-    if (lane != 0) return;
-    a.means[2 * i] = (float)m1;
-    a.means[2 * i + 1] = (float)m2;
+    over_block(m1, m2, of_block);
+    if (threadIdx.x != 0) return;
+    a.means[2 * i] = (float)(m1 / ((double)a.P * a.D));
+    a.means[2 * i + 1] = (float)(m2 / ((double)a.P * a.D));
 }
 
 // dw and db of 32 channels: over the samples, eight parts of them, in binary64 and in a fixed order.
@@ -449,6 +497,293 @@ __global__ __launch_bounds__(kGnThreads) void gn_dx_kernel(GnArgs a) {
     }
 }
 
+// ------------------------------------------------------- maps held in registers
+// A lane's place among the units that a workgroup holds.
+struct WholePlace {
+    uint32_t sample, col, row, rows, c8, unit;
+    int      wave, lane;
+    bool     holds;
+    __device__ __forceinline__ WholePlace(const GnArgs& a, uint32_t threads) {
+        // slabs of a cache line go to one XCD (every eighth workgroup): neighbours in this order
+        const uint32_t per = a.norm_blocks >> 3, rest = a.norm_blocks & 7u, xcd = blockIdx.x & 7u;
+        const uint32_t block = xcd * per + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
+        lane = (int)(threadIdx.x & 63u);
+        wave = (int)gn_wave();
+        sample = block / a.unit_slabs;
+        col = threadIdx.x & ((1u << a.col_shift) - 1u);
+        row = threadIdx.x >> a.col_shift;
+        rows = threads >> a.col_shift;
+        unit = ((block - sample * a.unit_slabs) << a.slab_shift) + (col >> a.unit_shift);
+        const uint32_t cu = col & ((1u << a.unit_shift) - 1u);
+        holds = unit < a.units && cu < a.unit_cols;
+        c8 = unit * a.unit_cols + cu;
+    }
+};
+// Sum of v over a slab's rows, for each of the lane's values; UNI: over its unit's columns too.  In all lanes.
+template <int NT, int N, bool UNI>
+__device__ __forceinline__ void over_rows(const GnArgs& a, const WholePlace& at, float (&lds)[NT / 64][64 * N], float (&v)[N]) {
+    const int cols = 1 << a.col_shift, unit = UNI ? 1 << a.unit_shift : 1;
+    for (int m = 1; m < 64; m <<= 1) {
+        if (m >= unit && m < cols) continue;
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], m);
+    }
+    if (at.lane < cols) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) lds[at.wave][at.lane * N + k] = v[k];
+    }
+    __syncthreads();
+    const int c = at.lane & (cols - 1);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) s += lds[w][c * N + k];
+        v[k] = s;
+    }
+}
+// Sums of the groups that parts of a column are, from those of its channels.
+__device__ __forceinline__ void within_column(const GnArgs& a, float (&v)[8]) {
+    if (a.D >= 2) {
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) v[k] = v[k + 1] = v[k] + v[k + 1];
+    }
+    if (a.D >= 4) {
+#pragma unroll
+        for (int k = 0; k < 8; k += 4) v[k] = v[k + 1] = v[k + 2] = v[k + 3] = v[k] + v[k + 2];
+    }
+}
+
+// Context of x by workgroups of their own, behind those that hold the maps.
+template <int DT, int BITS, int NT>
+__device__ __forceinline__ void gn_compress_blocks(const GnArgs& a) {
+    const uint32_t lane = threadIdx.x & 63u, stride = (gridDim.x - a.norm_blocks) * (NT / 64);
+    uint32_t pass = (blockIdx.x - a.norm_blocks) * (NT / 64) + gn_wave();
+    if (pass == 0) gn_zero_pad<BITS>(a, lane);
+    for (; pass < a.passes; pass += stride) {
+        const uint32_t e = pass * 64u + lane;
+        const bool active = e < a.blocks8;
+        const uint32_t i = active ? e : a.blocks8 - 1, q = divided(i, a.by_c8), s = divided(q, a.by_p);
+        const int64_t at = (int64_t)s * a.x.sample + (int64_t)(q - s * a.P) * a.x.pixel + (int64_t)(i - q * a.C8) * 8;
+        float v[8];
+        widen8<DT>(load8<DT>((const uint8_t*)a.x.p, at * kSize<DT>), v);
+        gn_compress_pass<BITS>(a, pass, lane, active, v);
+    }
+}
+
+// One launch forward: x is read once for y; once more for a context, whose groups do not keep to the norm's.
+template <int DT, bool UNI, bool SILU, int WHICH>
+__global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_kernel(GnArgs a, int bits) {
+    constexpr int NT = (int)kGnWhole[WHICH].threads, R = (int)kGnWhole[WHICH].blocks, N = UNI ? 1 : 8;
+    __shared__ float lds[2][NT / 64][64 * N];
+    if (blockIdx.x >= a.norm_blocks) {
+        switch (bits) {
+            case 1: gn_compress_blocks<DT, 1, NT>(a); break;
+            case 2: gn_compress_blocks<DT, 2, NT>(a); break;
+            case 4: gn_compress_blocks<DT, 4, NT>(a); break;
+            default: gn_compress_blocks<DT, 8, NT>(a); break;
+        }
+        return;
+    }
+    const WholePlace at(a, NT);
+    const uint32_t c = at.c8 * 8u;
+    const int64_t in = (int64_t)at.sample * a.x.sample + c;
+    Raw<DT> raw[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const uint32_t p = at.row + (uint32_t)i * at.rows;
+        raw[i] = Raw<DT>{};
+        if (at.holds && p < a.P) raw[i] = load8<DT>((const uint8_t*)a.x.p, (in + (int64_t)p * a.x.pixel) * kSize<DT>);
+    }
+    const float inv = 1.0f / ((float)a.P * (float)a.D);
+    float m[N], r[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) m[k] = r[k] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        float v[8];
+        widen8<DT>(raw[i], v);
+        if (UNI) m[0] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        else
+#pragma unroll
+            for (int k = 0; k < 8; ++k) m[k % N] += v[k];
+    }
+    over_rows<NT, N, UNI>(a, at, lds[0], m);
+    if constexpr (!UNI) within_column(a, m);
+#pragma unroll
+    for (int k = 0; k < N; ++k) m[k] *= inv;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if (at.row + (uint32_t)i * at.rows >= a.P) continue;
+        float v[8], s[8];
+        widen8<DT>(raw[i], v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float d = v[k] - m[k % N];
+            s[k] = d * d;
+        }
+        if (UNI) r[0] += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+        else
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k % N] += s[k];
+    }
+    if (!at.holds)
+#pragma unroll
+        for (int k = 0; k < N; ++k) r[k] = 0.0f;
+    over_rows<NT, N, UNI>(a, at, lds[1], r);
+    if constexpr (!UNI) within_column(a, r);
+#pragma unroll
+    for (int k = 0; k < N; ++k) r[k] = 1.0f / __builtin_sqrtf(__builtin_fmaf(r[k], inv, a.eps));
+    if (!at.holds) return;
+    if (a.mean && at.row == 0) {
+        const uint32_t first = at.sample * a.H;
+        if (UNI) {
+            if ((at.col & ((1u << a.unit_shift) - 1u)) == 0) {
+                a.mean[first + at.unit] = m[0];
+                a.rstd[first + at.unit] = r[0];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k % a.D == 0) {
+                    a.mean[first + (c + (uint32_t)k) / a.D] = m[k % N];
+                    a.rstd[first + (c + (uint32_t)k) / a.D] = r[k % N];
+                }
+        }
+    }
+    float w[8], b[8];
+    load_channels(a.w, a.w_f32, 1.0f, c, w);
+    load_channels(a.b, a.w_f32, 0.0f, c, b);
+    const int64_t out = (int64_t)at.sample * a.y.sample + c;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const uint32_t p = at.row + (uint32_t)i * at.rows;
+        if (p >= a.P) break;
+        float v[8];
+        widen8<DT>(raw[i], v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = activate<DT, SILU>(__builtin_fmaf((v[k] - m[k % N]) * r[k % N], w[k], b[k]));
+        store8<DT>((uint8_t*)a.y.p, (out + (int64_t)p * a.y.pixel) * kSize<DT>, v);
+    }
+}
+
+// One launch backward for dx: dy is read once, dz stays in registers; x, mostly codes, is read again for dx.
+template <int DT, int BITS, bool UNI, bool SILU, int WHICH>
+__global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_backward_kernel(GnArgs a) {
+    constexpr int NT = (int)kGnWhole[WHICH].threads, R = (int)kGnWhole[WHICH].blocks;
+    __shared__ float lds[NT / 64][64 * 16];
+    __shared__ float total[64 * 16];
+    __shared__ float of_column[64][2];
+    const WholePlace at(a, NT);
+    const uint32_t c = at.c8 * 8u;
+    const int cols = 1 << a.col_shift;
+    float w[8], b[8], dz[R][8], s[16];
+    OfGroups<UNI> m, r;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s[k] = 0.0f;
+    if (at.holds) {
+        load_channels(a.w, a.w_f32, 1.0f, c, w);
+        load_channels(a.b, a.w_f32, 0.0f, c, b);
+        m.load(a, a.mean + (size_t)at.sample * a.H, 1, c);
+        r.load(a, a.rstd + (size_t)at.sample * a.H, 1, c);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const uint32_t p = at.row + (uint32_t)i * at.rows;
+            if (p >= a.P) break;
+            GnInput<DT, BITS> in;
+            in.load(a, at.sample, p, at.c8);
+            float n[8];
+            in.template take<UNI, SILU>(m, r, w, b, n, dz[i]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                s[k] += dz[i][k];
+                s[8 + k] = __builtin_fmaf(dz[i][k], n[k], s[8 + k]);
+            }
+        }
+    }
+    for (int mask = cols; mask < 64; mask <<= 1)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s[k] += __shfl_xor(s[k], mask);
+    if (at.lane < cols) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) lds[at.wave][at.lane * 16 + k] = s[k];
+    }
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < cols * 16; i += NT) {
+        float v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NT / 64; ++k) v += lds[k][i];
+        total[i] = v;
+    }
+    __syncthreads();
+    float m1[UNI ? 1 : 8], m2[UNI ? 1 : 8];
+    const float inv = 1.0f / ((float)a.P * (float)a.D);
+    if constexpr (UNI) {
+        if ((int)threadIdx.x < cols) {
+            float t0 = 0.0f, t1 = 0.0f;
+            if (at.holds) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    t0 = __builtin_fmaf(w[k], total[threadIdx.x * 16 + k], t0);
+                    t1 = __builtin_fmaf(w[k], total[threadIdx.x * 16 + 8 + k], t1);
+                }
+            }
+            of_column[threadIdx.x][0] = t0;
+            of_column[threadIdx.x][1] = t1;
+        }
+        __syncthreads();
+        const uint32_t first = at.col & ~((1u << a.unit_shift) - 1u);
+        m1[0] = m2[0] = 0.0f;
+        for (uint32_t k = 0; k < a.unit_cols; ++k) {
+            m1[0] += of_column[first + k][0];
+            m2[0] += of_column[first + k][1];
+        }
+        m1[0] *= inv;
+        m2[0] *= inv;
+    } else {
+        if (!at.holds) return;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            m1[k % (UNI ? 1 : 8)] = w[k] * total[at.col * 16 + k];
+            m2[k % (UNI ? 1 : 8)] = w[k] * total[at.col * 16 + 8 + k];
+        }
+        within_column(a, m1);
+        within_column(a, m2);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            m1[k % (UNI ? 1 : 8)] *= inv;
+            m2[k % (UNI ? 1 : 8)] *= inv;
+        }
+    }
+    if (!at.holds) return;
+    if ((a.dw || a.db) && at.row == 0) {
+        float* out = a.sums + ((size_t)at.sample * a.C + c) * 2;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            out[2 * k] = total[at.col * 16 + k];
+            out[2 * k + 1] = total[at.col * 16 + 8 + k];
+        }
+    }
+    const int64_t out = (int64_t)at.sample * a.dx.sample + c;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const uint32_t p = at.row + (uint32_t)i * at.rows;
+        if (p >= a.P) break;
+        float n[8];
+        gn_load_x<DT, BITS>(a, at.sample, p, at.c8, n);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            n[k] = (n[k] - m[k]) * r[k];
+            dz[i][k] = r[k] * __builtin_fmaf(-n[k], m2[k % (UNI ? 1 : 8)], __builtin_fmaf(dz[i][k], w[k], -m1[k % (UNI ? 1 : 8)]));
+        }
+        store8<DT>((uint8_t*)a.dx.p, (out + (int64_t)p * a.dx.pixel) * kSize<DT>, dz[i]);
+    }
+}
+__global__ __launch_bounds__(kGnThreads) void gn_weights_kernel(GnArgs a) {
+    __shared__ double lds[2][kGnThreads];
+    gn_weights(a, blockIdx.x, lds);
+}
+
 __global__ __launch_bounds__(kGnThreads) void gn_zero_kernel(GnArgs a) {
     const uint32_t c = blockIdx.x * kGnThreads + threadIdx.x;
     if (c >= a.C) return;
@@ -460,51 +795,76 @@ __global__ __launch_bounds__(kGnThreads) void gn_zero_kernel(GnArgs a) {
 }
 
 // ------------------------------------------------------------- host launchers
+// Passes over memory, for maps of any size.
 template <int DT, int BITS, bool UNI, bool SILU>
-static int gn_launch(bool backward, const GnArgs& a, hipStream_t s) {
-    const uint32_t slots = a.B * a.chunks * a.slabs, groups = (a.B * a.H + 3) / 4;
+static void gn_launch(bool backward, const GnArgs& a, hipStream_t s) {
+    const uint32_t slots = a.B * a.chunks * a.slabs;
     if (!backward) {
         hipLaunchKernelGGL((gn_stats_kernel<DT, UNI>), dim3(slots), dim3(kGnThreads), 0, s, a);
-        hipLaunchKernelGGL((gn_finish_kernel<UNI>), dim3(groups), dim3(kGnThreads), 0, s, a);
+        hipLaunchKernelGGL((gn_finish_kernel<UNI>), dim3(a.B * a.H), dim3(kGnThreads), 0, s, a);
         const uint32_t waves = a.stride_passes < a.passes ? a.stride_passes : a.passes;
         hipLaunchKernelGGL((gn_apply_kernel<DT, BITS, UNI, SILU>), dim3((waves + 3) / 4), dim3(kGnThreads), 0, s, a);
     } else {
         GnArgs d = a;
         d.dx_blocks = slots;
         hipLaunchKernelGGL((gn_sums_kernel<DT, BITS, UNI, SILU>), dim3(slots), dim3(kGnThreads), 0, s, a);
-        hipLaunchKernelGGL(gn_means_kernel, dim3(groups), dim3(kGnThreads), 0, s, a);
+        hipLaunchKernelGGL(gn_means_kernel, dim3(a.B * a.H), dim3(kGnThreads), 0, s, a);
         const uint32_t extra = a.dw || a.db ? (a.C + 31) / 32 : 0;
         hipLaunchKernelGGL((gn_dx_kernel<DT, BITS, UNI, SILU>), dim3(slots + extra), dim3(kGnThreads), 0, s, d);
     }
-    return hipGetLastError() == hipSuccess ? 0 : -1;
 }
-template <int DT, int BITS>
-static int gn_launch_form(bool backward, const GnArgs& a, int act, hipStream_t s) {
-    if (gn_uniform(a)) return act ? gn_launch<DT, BITS, true, true>(backward, a, s) : gn_launch<DT, BITS, true, false>(backward, a, s);
-    return act ? gn_launch<DT, BITS, false, true>(backward, a, s) : gn_launch<DT, BITS, false, false>(backward, a, s);
-}
-template <int DT>
-static int gn_launch_bits(bool backward, const GnArgs& a, int bits, int act, hipStream_t s) {
-    switch (bits) {
-        case 0: return gn_launch_form<DT, 0>(backward, a, act, s);
-        case 1: return gn_launch_form<DT, 1>(backward, a, act, s);
-        case 2: return gn_launch_form<DT, 2>(backward, a, act, s);
-        case 4: return gn_launch_form<DT, 4>(backward, a, act, s);
-        default: return gn_launch_form<DT, 8>(backward, a, act, s);
+template <int DT, int BITS, bool UNI, bool SILU, int WHICH>
+static void gn_launch_whole(bool backward, const GnArgs& a, hipStream_t s) {
+    constexpr uint32_t NT = kGnWhole[WHICH].threads;
+    if (!backward) {
+        // two passes a wavefront of those that compress
+        const uint32_t extra = BITS ? gn_up(a.passes, NT / 64 * 2) : 0;
+        const dim3 grid(a.norm_blocks + (extra < 4096 ? extra : 4096));
+        hipLaunchKernelGGL((gn_whole_kernel<DT, UNI, SILU, WHICH>), grid, dim3(NT), 0, s, a, BITS);
+    } else {
+        hipLaunchKernelGGL((gn_whole_backward_kernel<DT, BITS, UNI, SILU, WHICH>), dim3(a.norm_blocks), dim3(NT), 0, s, a);
+        if (a.dw || a.db) hipLaunchKernelGGL(gn_weights_kernel, dim3((a.C + 31) / 32), dim3(kGnThreads), 0, s, a);
     }
 }
-static int gn_launch_any(bool backward, const GnArgs& a, int dtype, int bits, int act, hipStream_t s) {
-    return dtype == GACT_DT_F32 ? gn_launch_bits<GACT_DT_F32>(backward, a, bits, act, s)
-                                : gn_launch_bits<GACT_DT_BF16>(backward, a, bits, act, s);
+template <int DT, int BITS, bool UNI, bool SILU>
+static void gn_launch_sized(bool backward, const GnArgs& a, int whole, hipStream_t s) {
+    if (whole == 0) gn_launch<DT, BITS, UNI, SILU>(backward, a, s);
+    else if (whole == 1) gn_launch_whole<DT, BITS, UNI, SILU, 0>(backward, a, s);
+    else gn_launch_whole<DT, BITS, UNI, SILU, 1>(backward, a, s);
+}
+template <int DT, int BITS>
+static void gn_launch_form(bool backward, const GnArgs& a, int act, int whole, hipStream_t s) {
+    if (gn_uniform(a)) {
+        if (act) gn_launch_sized<DT, BITS, true, true>(backward, a, whole, s);
+        else gn_launch_sized<DT, BITS, true, false>(backward, a, whole, s);
+    } else {
+        if (act) gn_launch_sized<DT, BITS, false, true>(backward, a, whole, s);
+        else gn_launch_sized<DT, BITS, false, false>(backward, a, whole, s);
+    }
+}
+template <int DT>
+static void gn_launch_bits(bool backward, const GnArgs& a, int bits, int act, int whole, hipStream_t s) {
+    switch (bits) {
+        case 0: gn_launch_form<DT, 0>(backward, a, act, whole, s); break;
+        case 1: gn_launch_form<DT, 1>(backward, a, act, whole, s); break;
+        case 2: gn_launch_form<DT, 2>(backward, a, act, whole, s); break;
+        case 4: gn_launch_form<DT, 4>(backward, a, act, whole, s); break;
+        default: gn_launch_form<DT, 8>(backward, a, act, whole, s); break;
+    }
+}
+static int gn_launch_any(bool backward, const GnArgs& a, int dtype, int bits, int act, int whole, hipStream_t s) {
+    if (dtype == GACT_DT_F32) gn_launch_bits<GACT_DT_F32>(backward, a, bits, act, whole, s);
+    else gn_launch_bits<GACT_DT_BF16>(backward, a, bits, act, whole, s);
+    return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 }  // namespace gact
 
-extern "C" int gact_launch_group_norm(const gact::GnArgs* a, int dtype, int bits, int act, void* stream) {
-    return gact::gn_launch_any(false, *a, dtype, bits, act, (hipStream_t)stream);
+extern "C" int gact_launch_group_norm(const gact::GnArgs* a, int dtype, int bits, int act, int whole, void* stream) {
+    return gact::gn_launch_any(false, *a, dtype, bits, act, whole, (hipStream_t)stream);
 }
-extern "C" int gact_launch_group_norm_backward(const gact::GnArgs* a, int dtype, int bits, int act, void* stream) {
-    return gact::gn_launch_any(true, *a, dtype, bits, act, (hipStream_t)stream);
+extern "C" int gact_launch_group_norm_backward(const gact::GnArgs* a, int dtype, int bits, int act, int whole, void* stream) {
+    return gact::gn_launch_any(true, *a, dtype, bits, act, whole, (hipStream_t)stream);
 }
 extern "C" int gact_launch_group_norm_zero(const gact::GnArgs* a, void* stream) {
     hipLaunchKernelGGL(gact::gn_zero_kernel, dim3((a->C + gact::kGnThreads - 1) / gact::kGnThreads), dim3(gact::kGnThreads), 0,

@@ -126,7 +126,7 @@ int stage_norm(const gact_channel_norm* h, bool backward, void* ws, size_t ws_by
     }
     if (*bits != 0) while ((8 << a->block_shift) < G) ++a->block_shift;
     norm_sizes(h->batch, h->pixels, h->channels, h->groups, a);
-    if (!gact::launchable((uint64_t)a->B * a->chunks * a->slabs + a->C, gact::kGnThreads)) return GACT_E_ARG;
+    if (!gact::launchable((uint64_t)a->B * (a->chunks * a->slabs + a->C8) + a->C, gact::kGnThreads)) return GACT_E_ARG;
     uint8_t* at = (uint8_t*)ws;
     const size_t need = backward ? gact::gn_backward_bytes(*a) : gact::gn_forward_bytes(*a);
     if (!at || !aligned(at, 16) || ws_bytes < need) return GACT_E_ARG;
@@ -159,7 +159,9 @@ int gact_group_norm(const gact_channel_norm* h_norm, void* d_workspace, size_t w
     int bits = 0;
     if (const int rc = stage_norm(h_norm, false, d_workspace, workspace_bytes, &a, &bits)) return rc;
     if (a.B == 0) return GACT_OK;
-    return gact_launch_group_norm(&a, h_norm->dtype, bits, h_norm->act, stream) == 0 ? GACT_OK : GACT_E_HIP;
+    // in place, the pass that compresses has to be the one that writes
+    const int whole = bits != 0 && h_norm->x == h_norm->y ? 0 : gact::plan_whole(&a, h_norm->dtype);
+    return gact_launch_group_norm(&a, h_norm->dtype, bits, h_norm->act, whole, stream) == 0 ? GACT_OK : GACT_E_HIP;
 }
 
 int gact_group_norm_backward(const gact_channel_norm* h_norm, void* d_workspace, size_t workspace_bytes, void* stream) {
@@ -170,7 +172,8 @@ int gact_group_norm_backward(const gact_channel_norm* h_norm, void* d_workspace,
         if (!a.dw && !a.db) return GACT_OK;
         return gact_launch_group_norm_zero(&a, stream) == 0 ? GACT_OK : GACT_E_HIP;
     }
-    return gact_launch_group_norm_backward(&a, h_norm->dtype, bits, h_norm->act, stream) == 0 ? GACT_OK : GACT_E_HIP;
+    const int whole = gact::plan_whole(&a, h_norm->dtype);
+    return gact_launch_group_norm_backward(&a, h_norm->dtype, bits, h_norm->act, whole, stream) == 0 ? GACT_OK : GACT_E_HIP;
 }
 
 size_t gact_linear_weight_grad_workspace_bytes(int64_t tokens, int64_t out_features, int64_t in_features, gact_dtype dtype) {

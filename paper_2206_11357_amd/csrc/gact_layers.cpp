@@ -199,7 +199,7 @@ int gact_linear_weight_grad(const void* d_dy, int64_t dy_stride, gact_dtype dtyp
         return GACT_E_ARG;
     const gact::WeightPlan plan = gact::plan_weight(T, N, K, (int)dtype);
     const uint64_t blocks = (uint64_t)plan.tiles_n * plan.tiles_k * plan.splits;
-    if (!gact::launchable(blocks, gact::kWeightThreads)) return GACT_E_ARG;
+    if (!gact::launchable(blocks, (uint32_t)gact::weight_tile((int)dtype, plan.which).threads)) return GACT_E_ARG;
     const size_t need = gact::weight_workspace_bytes(plan, N, K);
     if (need > 0 && (!d_workspace || !aligned(d_workspace, 16) || workspace_bytes < need)) return GACT_E_ARG;
     gact::WeightArgs a{};

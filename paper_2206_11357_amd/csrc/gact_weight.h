@@ -9,14 +9,14 @@
 
 namespace gact {
 
-// A block's tile of dW, n x k, and the tokens that it takes from memory at a time.
+// A block's tile of dW, n x k, the tokens that it takes from memory at a time, and its threads.  Four wavefronts share a tile; where
+// there are eight, two teams of four take half of the tokens each, and their sums are added in shared memory: half as many
+// splits fill the GPU as with blocks of four.
 struct WeightTile {
-    int n, k, tokens;
+    int n, k, tokens, threads;
 };
-constexpr int kWeightThreads = 256;
-constexpr int kWeightTiles = 2;
 constexpr WeightTile weight_tile(int dtype, int which) {
-    return which == 0 ? WeightTile{256, 128, dtype == GACT_DT_F32 ? 16 : 32} : WeightTile{64, 64, dtype == GACT_DT_F32 ? 16 : 32};
+    return which == 0 ? WeightTile{256, 128, dtype == GACT_DT_F32 ? 32 : 64, 512} : WeightTile{64, 64, dtype == GACT_DT_F32 ? 16 : 32, 256};
 }
 
 struct WeightArgs {
@@ -70,8 +70,9 @@ inline WeightPlan plan_weight(uint64_t T, uint64_t N, uint64_t K, int dtype) {
     p.tiles_n = (uint32_t)weight_up(N, (uint64_t)tile.n);
     p.tiles_k = K ? (uint32_t)weight_up(K, (uint64_t)tile.k) : 1;      // (K = 0: db alone)
     const uint64_t tiles = (uint64_t)p.tiles_n * p.tiles_k, chunks = weight_up(T, (uint64_t)tile.tokens);
-    uint64_t splits = tiles >= 256 ? 1 : 512 / tiles;
-    const uint64_t most = chunks / 8 ? chunks / 8 : 1;
+    const uint64_t fill = p.which == 0 ? 256 : 512;
+    uint64_t splits = tiles >= fill ? 1 : fill / tiles;
+    const uint64_t most = chunks / 4 ? chunks / 4 : 1;
     if (splits > most) splits = most;
     p.chunks = (uint32_t)weight_up(chunks, splits);
     p.splits = p.chunks ? (uint32_t)weight_up(chunks, p.chunks) : 1;

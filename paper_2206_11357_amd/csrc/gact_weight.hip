@@ -126,27 +126,27 @@ struct Operand<GACT_DT_F32> {
 template <int DT, int WHICH>
 struct Tiling {
     static constexpr WeightTile tile = weight_tile(DT, WHICH);
-    static constexpr int BN = tile.n, BK = tile.k, BT = tile.tokens;
+    static constexpr int BN = tile.n, BK = tile.k, BT = tile.tokens, kThreads = tile.threads, kTeams = kThreads / 256;
     static constexpr int kSize = DT == GACT_DT_F32 ? 4 : 2;
     static constexpr int kPiece = 16 / kSize;                       // elements of dy that a lane loads at a time
     static constexpr int kRowPieces = BN / kPiece;
-    static constexpr int kPieces = BT * kRowPieces / kWeightThreads;
+    static constexpr int kPieces = BT * kRowPieces / kThreads;
     static constexpr int kRowBlocks = BK / 8;                       // blocks of eight elements of x
-    static constexpr int kBlocks = BT * kRowBlocks >= kWeightThreads ? BT * kRowBlocks / kWeightThreads : 1;
+    static constexpr int kBlocks = BT * kRowBlocks >= kThreads ? BT * kRowBlocks / kThreads : 1;
     // Bytes from row to row in shared memory.  bf16: 64 more than a multiple of 256, so that the four rows of a
     // transposed read lie in different banks.
     static constexpr int kPad = DT == GACT_DT_F32 ? 0 : 64;
     static constexpr int kRowN = BN * kSize + kPad, kRowK = BK * kSize + kPad;
     static constexpr int kBufN = BT * kRowN, kBuf = kBufN + BT * kRowK;
     static constexpr int TN = BN / 64, TK = BK / 64;                // 32 x 32 products of a wavefront, 2 x 2 of which share a tile
-    static_assert(kWeightThreads % kRowPieces == 0 && BT * kRowPieces % kWeightThreads == 0, "a thread stays in its column");
+    static_assert(kThreads % kRowPieces == 0 && BT * kRowPieces % kThreads == 0, "a thread stays in its column");
 };
 
 // bytes of a buffer: all that a split reaches lies below 2^31 (weight_mode)
 __device__ __forceinline__ uint64_t within(uint64_t bytes) { return bytes < 0x80000000ull ? bytes : 0x80000000ull; }
 
 template <int DT, int BITS, int WHICH, int MODE>
-__global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a) {
+__global__ __launch_bounds__(weight_tile(DT, WHICH).threads, 2) void weight_kernel(WeightArgs a) {
     typedef Tiling<DT, WHICH> L;
     constexpr bool WHOLE = MODE != kOdd;
     constexpr int BN = L::BN, BK = L::BK, BT = L::BT, TN = L::TN, TK = L::TK;
@@ -167,13 +167,13 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
 
     // ---- what a thread loads
     const uint32_t pn = tid % L::kRowPieces, pt = tid / L::kRowPieces;
-    constexpr uint32_t kRows = kWeightThreads / L::kRowPieces;      // rows from piece to piece of a thread
+    constexpr uint32_t kRows = L::kThreads / L::kRowPieces;      // rows from piece to piece of a thread
     const uint32_t n = n0 + pn * L::kPiece;
     const uint32_t valid = n < a.N ? (a.N - n < (uint32_t)L::kPiece ? a.N - n : (uint32_t)L::kPiece) : 0;
     const uint32_t bk = tid % L::kRowBlocks, bt = tid / L::kRowBlocks;
-    constexpr uint32_t kXRows = kWeightThreads / L::kRowBlocks;
+    constexpr uint32_t kXRows = L::kThreads / L::kRowBlocks;
     const uint32_t k = k0 + bk * 8;
-    const bool x_thread = BT * L::kRowBlocks >= kWeightThreads || bt < (uint32_t)BT;
+    const bool x_thread = BT * L::kRowBlocks >= L::kThreads || bt < (uint32_t)BT;
 
     w4 dy[L::kPieces];
     Codes<BITS> codes[L::kBlocks];
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
     };
 
     // ---- what a wavefront multiplies
-    const int wn = wave >> 1, wk = wave & 1;
+    const int team = wave >> 2, wn = wave >> 1 & 1, wk = wave & 1;
     wf16 acc[TN][TK];
 #pragma unroll
     for (int i = 0; i < TN; ++i)
@@ -296,8 +296,8 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
     //   bf16  a step is 16 tokens; 16 lanes read 4 rows of 16 elements, of which each gets a column
     //   fp32  a step is two tokens; a lane's operands are TN (TK) neighbouring elements of row 2 s + lane / 32
     typedef typename Operand<DT>::type Op;
-    constexpr int kSteps = BT / (DT == GACT_DT_F32 ? 2 : 16);
-    const uint32_t op_row = DT == GACT_DT_F32 ? (uint32_t)(lane >> 5) : (uint32_t)(8 * (lane >> 5) + ((lane & 15) >> 2));
+    constexpr int kSteps = BT / L::kTeams / (DT == GACT_DT_F32 ? 2 : 16);      // of a team
+    const uint32_t op_row = (uint32_t)(team * (BT / L::kTeams) + (DT == GACT_DT_F32 ? lane >> 5 : 8 * (lane >> 5) + ((lane & 15) >> 2)));
     const int col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
     const uint32_t op_n = op_row * L::kRowN + (DT == GACT_DT_F32 ? (wn * 32 * TN + (lane & 31) * TN) * 4 : (wn * 32 * TN + col) * 2);
     const uint32_t op_k = L::kBufN + op_row * L::kRowK + (DT == GACT_DT_F32 ? (wk * 32 * TK + (lane & 31) * TK) * 4 : (wk * 32 * TK + col) * 2);
@@ -440,7 +440,34 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
         }
     }
 
+    // ---- the teams' sums: half of the second one's registers at a time, through shared memory
+    if constexpr (L::kTeams == 2) {
+        static_assert(TN % 2 == 0 && TN / 2 * TK * 16 * 256 * 4 <= 2 * L::kBuf, "room");
+        float* room = (float*)lds[0] + (tid & 255u);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            __syncthreads();
+#pragma unroll
+            for (int i = half * TN / 2; i < (half + 1) * TN / 2; ++i)
+#pragma unroll
+                for (int j = 0; j < TK; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (team == 1) room[(((i - half * TN / 2) * TK + j) * 16 + r) * 256] = acc[i][j][r];
+            __syncthreads();
+#pragma unroll
+            for (int i = half * TN / 2; i < (half + 1) * TN / 2; ++i)
+#pragma unroll
+                for (int j = 0; j < TK; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (team == 0) acc[i][j][r] += room[(((i - half * TN / 2) * TK + j) * 16 + r) * 256];
+        }
+        __syncthreads();
+    }
+
     // ---- out: element r of a product is row (r & 3) + 8 (r >> 2) + 4 (lane / 32), column lane % 32
+    if (L::kTeams == 1 || team == 0) {
     const bool whole = a.partial == nullptr;
     float* part = whole ? nullptr : a.partial + (size_t)split * a.N * a.K;
 #pragma unroll
@@ -461,13 +488,15 @@ __global__ __launch_bounds__(kWeightThreads, 2) void weight_kernel(WeightArgs a)
             }
         }
 
+    }
+
     if (!with_db) return;
     // db of the tile's rows: over the threads of a column, in their order
     float* sums = (float*)lds[0];
 #pragma unroll
     for (int j = 0; j < L::kPiece; ++j) sums[pt * BN + pn * L::kPiece + j] = sum[j];
     __syncthreads();
-    for (uint32_t i = tid; i < (uint32_t)BN; i += kWeightThreads) {
+    for (uint32_t i = tid; i < (uint32_t)BN; i += L::kThreads) {
         if (n0 + i >= a.N) continue;
         float s = 0.0f;
         for (uint32_t r = 0; r < kRows; ++r) s += sums[r * BN + i];
@@ -527,7 +556,7 @@ __global__ __launch_bounds__(kJoinThreads) void weight_join_kernel(WeightArgs a,
 // ------------------------------------------------------------- host launchers
 template <int DT, int BITS, int WHICH>
 static void launch_tile(const WeightArgs& a, hipStream_t s) {
-    const dim3 grid(a.tiles_n * a.tiles_k * a.splits), block(kWeightThreads);
+    const dim3 grid(a.tiles_n * a.tiles_k * a.splits), block(weight_tile(DT, WHICH).threads);
     switch (weight_mode(a, DT, BITS, WHICH)) {
         case kEven: hipLaunchKernelGGL((weight_kernel<DT, BITS, WHICH, kEven>), grid, block, 0, s, a); break;
         case kWhole: hipLaunchKernelGGL((weight_kernel<DT, BITS, WHICH, kWhole>), grid, block, 0, s, a); break;

@@ -455,8 +455,8 @@ int gact_head_norm_rotate_backward(const gact_heads *h_parts, int n_parts, const
  *   channels   a multiple of 8 and of groups;  group_size of a context: 32, 64, 128, 256 or 512 (GACT_E_GROUP otherwise:
  *              gact_compress takes such a tensor)
  *   batch * pixels * channels must be below 2^34, batch * pixels below 2^31, batch * channels below 2^30.
- *   d_workspace  device scratch, >= gact_group_norm_workspace_bytes(...) of the same sizes (of both passes), 16-byte
- *              aligned, in use until the enqueued kernels have run; calls that share one must not overlap in time.
+ *   d_workspace  device scratch, >= gact_group_norm_workspace_bytes(...) of the same sizes, dtype and pass (which may be 0),
+ *              16-byte aligned, in use until the enqueued kernels have run; calls that share one must not overlap in time.
  * An empty tensor (batch or pixels 0) is GACT_OK; its dw and db are 0.  Both calls can be captured into a HIP graph.
  */
 typedef enum { GACT_ACT_NONE = 0, GACT_ACT_SILU = 1 } gact_activation;
@@ -492,7 +492,8 @@ typedef struct {
     float       eps;         /* a normal number > 0; forward only */
 } gact_channel_norm;
 
-size_t gact_group_norm_workspace_bytes(int64_t batch, int64_t pixels, int channels, int groups);
+size_t gact_group_norm_workspace_bytes(int64_t batch, int64_t pixels, int channels, int groups, gact_dtype dtype,
+                                       int backward);
 
 int gact_group_norm(const gact_channel_norm *h_norm, void *d_workspace, size_t workspace_bytes, void *stream);
 
@@ -505,11 +506,11 @@ int gact_group_norm_backward(const gact_channel_norm *h_norm, void *d_workspace,
  * x^ = code * step + minimum of the context (x laid out contiguously as [tokens, in_features]; groups may pass from row to
  * row), rounded to dy's type: in fp32 what gact_decompress gives, in bf16 the product is not rounded before the sum.  Sums in binary32, over blocks and splits of the tokens in a fixed order, the same
  * in every call of the same sizes and types; outputs rounded once.
- *   d_dy         [tokens, out_features], its rows' elements consecutive, dy_stride elements from row to row (any value,
+ *   dy           [tokens, out_features] of dtype, its rows' elements consecutive, dy_stride elements from row to row (any value,
  *                0 too: a gradient that all tokens share), aligned as its type
- *   d_packed, d_gmin, d_gscale, group_size, bits   as gact_compress has left them
- *   d_dw         out  [out_features, in_features], contiguous, of w_dtype
- *   d_db         out  [out_features] of w_dtype, or NULL: not wanted.  Outputs overlap nothing.
+ *   packed, gmin, gscale, group_size, bits   as gact_compress has left them
+ *   dw           out  [out_features, in_features], contiguous, of w_dtype
+ *   db           out  [out_features] of w_dtype, or NULL: not wanted.  Outputs overlap nothing.
  *   d_workspace  device scratch, >= gact_linear_weight_grad_workspace_bytes(...) bytes of the same sizes (which may be 0),
  *                16-byte aligned, in use until the enqueued kernels have run; calls that share one must not overlap in time.
  * tokens == 0 writes zeros; out_features == 0 or in_features == 0 is GACT_OK and writes nothing but db.  Each size must be
@@ -517,13 +518,27 @@ int gact_group_norm_backward(const gact_channel_norm *h_norm, void *d_workspace,
  * in a row of dy reaches that row's columns of dW (rows of x^ times it), in a group's minimum or step the elements of
  * that group.  Can be captured into a HIP graph.
  */
+typedef struct {
+    const void  *dy;
+    const void  *packed;
+    const float *gmin;
+    const float *gscale;
+    void        *dw;
+    void        *db;
+    int64_t      dy_stride;
+    int64_t      tokens;
+    int64_t      out_features;
+    int64_t      in_features;
+    int32_t      dtype;       /* gact_dtype of dy */
+    int32_t      w_dtype;     /* gact_dtype of dw, db */
+    int32_t      group_size;
+    int32_t      bits;
+} gact_linear_grad;
+
 size_t gact_linear_weight_grad_workspace_bytes(int64_t tokens, int64_t out_features, int64_t in_features,
                                                gact_dtype dtype);
 
-int gact_linear_weight_grad(const void *d_dy, int64_t dy_stride, gact_dtype dtype, int64_t tokens, int64_t out_features,
-                            int64_t in_features, const void *d_packed, const float *d_gmin, const float *d_gscale,
-                            int group_size, int bits, void *d_dw, void *d_db, gact_dtype w_dtype, void *d_workspace,
-                            size_t workspace_bytes, void *stream);
+int gact_linear_weight_grad(const gact_linear_grad *h_grad, void *d_workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Variance alert (host only): V(b) = sum_l c_l S(b_l) (Thm. 2) against the

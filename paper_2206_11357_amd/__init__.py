@@ -93,6 +93,8 @@ _ROTATION = struct.Struct("2q3Pq6ifi")
 # gact_channel_norm: x, y, dy, dx, w, b, dw, db, mean, rstd, packed, gmin, gscale; strides of x, y, dy, dx; batch, pixels;
 # seed; channels, groups, act, dtype, w_dtype, bits, group_size; eps.
 _CHANNEL_NORM = struct.Struct("13P10qQ7if")
+# gact_linear_grad: dy, packed, gmin, gscale, dw, db; dy_stride, tokens, out_features, in_features; dtype, w_dtype, group_size, bits.
+_LINEAR_GRAD = struct.Struct("6P4q4i")
 
 
 def _load() -> ctypes.CDLL:
@@ -155,7 +157,7 @@ def _load() -> ctypes.CDLL:
     lib.gact_head_norm_rotate.restype = i32
     lib.gact_head_norm_rotate_backward.argtypes = [vp, i32, vp, vp, sz, vp]
     lib.gact_head_norm_rotate_backward.restype = i32
-    lib.gact_group_norm_workspace_bytes.argtypes = [i64, i64, i32, i32]
+    lib.gact_group_norm_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
     lib.gact_group_norm_workspace_bytes.restype = sz
     lib.gact_group_norm.argtypes = [vp, vp, sz, vp]
     lib.gact_group_norm.restype = i32
@@ -163,7 +165,7 @@ def _load() -> ctypes.CDLL:
     lib.gact_group_norm_backward.restype = i32
     lib.gact_linear_weight_grad_workspace_bytes.argtypes = [i64, i64, i64, i32]
     lib.gact_linear_weight_grad_workspace_bytes.restype = sz
-    lib.gact_linear_weight_grad.argtypes = [vp, i64, i32, i64, i64, i64, vp, vp, vp, i32, i32, vp, vp, i32, vp, sz, vp]
+    lib.gact_linear_weight_grad.argtypes = [vp, vp, sz, vp]
     lib.gact_linear_weight_grad.restype = i32
     return lib
 
@@ -1053,6 +1055,8 @@ def _rows(x: torch.Tensor) -> Tuple[int, int]:
         raise ValueError("gact needs [..., features]")
     if st[-1] != 1 and shape[-1] > 1:
         raise ValueError("a row's elements must be consecutive")
+    if len(shape) == 2:
+        return shape[0], st[0]
     rows, stride = 1, None
     for size, s in zip(reversed(shape[:-1]), reversed(st[:-1])):
         if size != 1:
@@ -1083,7 +1087,6 @@ def gact_linear_weight_grad(dy: torch.Tensor, packed: torch.Tensor, gmin: torch.
     T, stride = _rows(dy)
     N, K = dy.shape[-1], in_features
     device = _same_device(dy, packed, gmin, gscale, dw, db, workspace)
-    dtype = dtype_code(dy.dtype)
     if w_dtype is None:
         w_dtype = dy.dtype if dw is None else dw.dtype
     if K < 0 or gmin.dtype is not torch.float32 or gscale.dtype is not torch.float32 \
@@ -1106,10 +1109,13 @@ def gact_linear_weight_grad(dy: torch.Tensor, packed: torch.Tensor, gmin: torch.
     else:
         with _allocating_for(stream, device):
             dw, db, workspace = _weight_buffers(dy, dw, db, workspace, N, K, w_dtype, bias, need)
-    _enqueue(lib.gact_linear_weight_grad, "gact_linear_weight_grad", device, stream, dy.data_ptr(), stride, dtype, T, N, K,
-             packed.data_ptr(), gmin.data_ptr(), gscale.data_ptr(), group_size, bits, dw.data_ptr(),
-             None if db is None else db.data_ptr(), dtype_code(w_dtype),
-             *(workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0))
+    record = _LINEAR_GRAD.pack(dy.data_ptr(), packed.data_ptr(), gmin.data_ptr(), gscale.data_ptr(), dw.data_ptr(),
+                               0 if db is None else db.data_ptr(), stride, T, N, K, dtype_code(dy.dtype), dtype_code(w_dtype),
+                               group_size, bits)
+    if workspace is None:
+        _enqueue(lib.gact_linear_weight_grad, "gact_linear_weight_grad", device, stream, record, None, 0)
+    else:
+        _enqueue(lib.gact_linear_weight_grad, "gact_linear_weight_grad", device, stream, record, workspace.data_ptr(), workspace.nbytes)
     return dw, db
 
 
@@ -1216,8 +1222,8 @@ def group_norm_context_fits(group_size: int, channels: int) -> bool:
 
 
 @functools.lru_cache(maxsize=256)
-def gact_group_norm_workspace_bytes(batch: int, pixels: int, channels: int, groups: int) -> int:
-    return int(lib.gact_group_norm_workspace_bytes(batch, pixels, channels, groups))
+def gact_group_norm_workspace_bytes(batch: int, pixels: int, channels: int, groups: int, dtype: torch.dtype, backward: bool = False) -> int:
+    return int(lib.gact_group_norm_workspace_bytes(batch, pixels, channels, groups, dtype_code(dtype), backward))
 
 
 def _channel_weights(w, b, C: int):
@@ -1254,10 +1260,9 @@ def _norm_workspace(x: torch.Tensor, need: int, workspace: Optional[torch.Tensor
     return workspace
 
 
-def _norm_forward_record(x, groups, w, b, eps, act, context, out, workspace):
-    """(device, record) of a forward call into `out`."""
-    B, P, C, sample, pixel = _map_strides(x)
-    device = _same_device(x, out, w, b, workspace)
+def _norm_forward_record(x, strides, groups, w, b, eps, act, context, out, device: int) -> bytes:
+    """gact_channel_norm of a forward call into `out`; strides: _map_strides(x)."""
+    B, P, C, sample, pixel = strides
     ys, yp = sample, pixel
     if out is not x:
         _check_like(out, x)
@@ -1266,7 +1271,7 @@ def _norm_forward_record(x, groups, w, b, eps, act, context, out, workspace):
     if context is not None:
         _norm_context(context, x, device, groups)
         a, bits, G, seed = context.addresses(), context.bits, context.group_size, context.seed
-    return device, _CHANNEL_NORM.pack(
+    return _CHANNEL_NORM.pack(
         x.data_ptr(), out.data_ptr(), 0, 0, 0 if w is None else w.data_ptr(), 0 if b is None else b.data_ptr(), 0, 0, *a, sample, pixel,
         ys, yp, 0, 0, 0, 0, B, P, seed, C, groups, _activation(act), dtype_code(x.dtype), _channel_weights(w, b, C), bits, G, eps)
 
@@ -1277,26 +1282,31 @@ def gact_group_norm(x: torch.Tensor, groups: int, w: Optional[torch.Tensor] = No
     """Group norm of a channels-last map x, [batch, ..., channels] with evenly spaced pixels (an NCHW tensor in torch's
     channels_last format is one after permute(0, 2, 3, 1)), with weights, shifts and an activation, "none" or "silu"; returns
     y.  context: a GroupNormContext that the pass fills."""
-    need = gact_group_norm_workspace_bytes(*_map_strides(x)[:3], groups)
-    if out is None or workspace is None:
-        if stream is None:
+    strides = _map_strides(x)
+    device = _same_device(x, out, w, b, workspace)
+    need = gact_group_norm_workspace_bytes(*strides[:3], groups, x.dtype)
+    if stream is None:
+        out = x.new_empty(x.shape) if out is None else out
+        workspace = _norm_workspace(x, need, workspace)
+    else:
+        with _allocating_for(stream, device):
             out = x.new_empty(x.shape) if out is None else out
             workspace = _norm_workspace(x, need, workspace)
-        else:
-            with _allocating_for(stream, x.get_device()):
-                out = x.new_empty(x.shape) if out is None else out
-                workspace = _norm_workspace(x, need, workspace)
-    device, record = _norm_forward_record(x, groups, w, b, eps, act, context, out, workspace)
-    _enqueue(lib.gact_group_norm, "gact_group_norm", device, stream, record,
-             *(workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0))
+    record = _norm_forward_record(x, strides, groups, w, b, eps, act, context, out, device)
+    if workspace is None:
+        _enqueue(lib.gact_group_norm, "gact_group_norm", device, stream, record, None, 0)
+    else:
+        _enqueue(lib.gact_group_norm, "gact_group_norm", device, stream, record, workspace.data_ptr(), workspace.nbytes)
     return out
 
 
 def prepare_group_norm(x: torch.Tensor, groups: int, w=None, b=None, eps: float = 1e-5, act: str = "none", *, out: torch.Tensor,
                        context: Optional[GroupNormContext] = None, workspace: Optional[torch.Tensor] = None) -> PreparedCall:
     """gact_group_norm(...) into `out`, as a PreparedCall, which keeps its workspace."""
-    workspace = _norm_workspace(x, gact_group_norm_workspace_bytes(*_map_strides(x)[:3], groups), workspace)
-    _, record = _norm_forward_record(x, groups, w, b, eps, act, context, out, workspace)
+    strides = _map_strides(x)
+    device = _same_device(x, out, w, b, workspace)
+    workspace = _norm_workspace(x, gact_group_norm_workspace_bytes(*strides[:3], groups, x.dtype), workspace)
+    record = _norm_forward_record(x, strides, groups, w, b, eps, act, context, out, device)
     vp = ctypes.c_void_p
     keep = ctypes.create_string_buffer(record, len(record))
     args = (vp(ctypes.addressof(keep)), vp(workspace.data_ptr() if workspace is not None else 0),
@@ -1320,7 +1330,7 @@ def gact_group_norm_backward(dy: torch.Tensor, groups: int, w: Optional[torch.Te
     B, P, C, sample, pixel = _map_strides(dy)
     device = _same_device(dy, w, b, x, out, workspace)
     _norm_context(context, dy, device, groups)
-    need = gact_group_norm_workspace_bytes(B, P, C, groups)
+    need = gact_group_norm_workspace_bytes(B, P, C, groups, dy.dtype, True)
     if stream is None:
         dx, dw, db, workspace = _norm_gradients(dy, w, b, out, weight_grads, workspace, need)
     else:
@@ -1340,6 +1350,8 @@ def gact_group_norm_backward(dy: torch.Tensor, groups: int, w: Optional[torch.Te
         0 if dw is None else dw.data_ptr(), 0 if db is None else db.data_ptr(), *context.addresses(), xs, xp, 0, 0, sample, pixel,
         ds, dp, B, P, context.seed, C, groups, _activation(act), dtype_code(dy.dtype), _channel_weights(w, b, C), context.bits,
         context.group_size, 0.0)
-    _enqueue(lib.gact_group_norm_backward, "gact_group_norm_backward", device, stream, record,
-             *(workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0))
+    if workspace is None:
+        _enqueue(lib.gact_group_norm_backward, "gact_group_norm_backward", device, stream, record, None, 0)
+    else:
+        _enqueue(lib.gact_group_norm_backward, "gact_group_norm_backward", device, stream, record, workspace.data_ptr(), workspace.nbytes)
     return dx, dw, db

@@ -86,8 +86,9 @@ inline void plan_group_norm(GnArgs* a) {
 struct GnWhole {
     uint32_t threads, blocks;
 };
-constexpr GnWhole kGnWhole[2] = {{256, 4}, {1024, 8}};
-// Whether a sample's group fits the registers of a workgroup: which of them it is (0: of none, 1, 2), and how it is laid out.
+constexpr int kGnWholes = 3;
+constexpr GnWhole kGnWhole[kGnWholes] = {{256, 4}, {512, 8}, {1024, 8}};
+// Whether a sample's group fits the registers of a workgroup: which of them it is (0: of none, 1 ..), and how it is laid out.
 inline int plan_whole(GnArgs* a, int dtype) {
     uint32_t cols = a->D / 8;
     if (a->D % 8 != 0) {
@@ -99,27 +100,34 @@ inline int plan_whole(GnArgs* a, int dtype) {
     a->unit_shift = 0;
     while ((1u << a->unit_shift) < cols) ++a->unit_shift;
     if (a->unit_shift > 6) return 0;
-    // whole cache lines of a pixel, if they fit
+    // 64 bytes of a pixel at least, if they fit.  Us, step of 32 x 1024 x 512 bf16, 4 bits, forward + backward, by bytes: 32 29.1 + 27.8,
+    // 64 26.2 + 22.6, 128 (twice the threads) 29.7 + 21.9; of 64 x 3136 x 256 fp32, 2 bits 32 162 + 170, 64 (the most) 136 + 131.
     const uint32_t size = dtype == GACT_DT_F32 ? 4 : 2;
     uint32_t shift = 0;
-    while ((cols << shift) * 8 * size < 128 && (1u << shift) < a->units && a->unit_shift + shift < 6) ++shift;
+    while ((cols << shift) * 8 * size < 64 && (1u << shift) < a->units && a->unit_shift + shift < 6) ++shift;
     const auto fits = [&](const GnWhole& w) { return (uint64_t)a->P << (a->unit_shift + shift) <= (uint64_t)w.threads * w.blocks; };
-    while (!fits(kGnWhole[1]) && shift > 0) --shift;
-    if (!fits(kGnWhole[1])) return 0;
+    while (!fits(kGnWhole[kGnWholes - 1]) && shift > 0) --shift;
+    if (!fits(kGnWhole[kGnWholes - 1])) return 0;
     a->slab_shift = shift;
     a->col_shift = a->unit_shift + shift;
     a->unit_slabs = gn_up(a->units, 1u << shift);
     a->norm_blocks = a->B * a->unit_slabs;
-    return fits(kGnWhole[0]) ? 1 : 2;
+    for (int k = 0; k < kGnWholes; ++k) if (fits(kGnWhole[k])) return k + 1;
+    return 0;
 }
 inline size_t gn_align(size_t v) { return (v + 15) & ~(size_t)15; }
-// Workspace: partial sums; forward: mean and rstd where the caller keeps none; backward: sums, means.
+// Workspace: partial sums; forward: mean and rstd where the caller keeps none; backward: sums, means.  Maps held in registers:
+// sums alone.
 inline size_t gn_partial_bytes(const GnArgs& a) {
     return gn_align((size_t)a.B * a.chunks * a.C * 2 * sizeof(float));
 }
-inline size_t gn_forward_bytes(const GnArgs& a) { return gn_partial_bytes(a) + 2 * gn_align((size_t)a.B * a.H * sizeof(float)); }
-inline size_t gn_backward_bytes(const GnArgs& a) {
-    return gn_partial_bytes(a) + gn_align((size_t)a.B * a.C * 2 * sizeof(float)) + gn_align((size_t)a.B * a.H * 2 * sizeof(float));
+inline size_t gn_sums_bytes(const GnArgs& a) { return gn_align((size_t)a.B * a.C * 2 * sizeof(float)); }
+inline size_t gn_forward_bytes(const GnArgs& a, int whole) {
+    return whole ? 0 : gn_partial_bytes(a) + 2 * gn_align((size_t)a.B * a.H * sizeof(float));
+}
+inline size_t gn_backward_bytes(const GnArgs& a, int whole) {
+    if (whole) return a.B > 1 ? gn_sums_bytes(a) : 0;
+    return gn_partial_bytes(a) + gn_sums_bytes(a) + gn_align((size_t)a.B * a.H * 2 * sizeof(float));
 }
 
 }  // namespace gact

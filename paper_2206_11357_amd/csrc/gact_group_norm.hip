@@ -209,23 +209,22 @@ __global__ __launch_bounds__(kGnThreads) void gn_finish_kernel(GnArgs a) {
     const uint32_t each = UNI ? a.D / 8 : a.D, row = UNI ? a.C8 : a.C, items = each * a.chunks;
     const float* p = a.partial + ((size_t)sample * a.chunks * row + (size_t)h * each) * 2;
     const double per = UNI ? 8.0 : 1.0, last = per * (a.P - (a.chunks - 1) * a.per_chunk), all = per * a.per_chunk;
-    double mean = 0.0, m2 = 0.0, none = 0.0;
+    // distances from the first part's mean, so that their squares cancel nothing
+    const double from = (double)p[0], whole = (double)a.P * a.D;
+    double off = 0.0, m2 = 0.0;
 #pragma unroll 4
     for (uint32_t k = threadIdx.x; k < items; k += kGnThreads) {
         const uint32_t chunk = k / each;
-        mean += (chunk + 1 == a.chunks ? last : all) * (double)p[((size_t)chunk * row + (k - chunk * each)) * 2];
+        const hf2 v = *(const hf2*)(p + ((size_t)chunk * row + (k - chunk * each)) * 2);
+        const double n = chunk + 1 == a.chunks ? last : all, d = (double)v.x - from;
+        off += n * d;
+        m2 += (double)v.y + n * d * d;
     }
-    over_block(mean, none, lds);
-    mean /= (double)a.P * a.D;
-#pragma unroll 4
-    for (uint32_t k = threadIdx.x; k < items; k += kGnThreads) {
-        const uint32_t chunk = k / each;
-        const float* v = p + ((size_t)chunk * row + (k - chunk * each)) * 2;
-        const double d = (double)v[0] - mean;
-        m2 += (double)v[1] + (chunk + 1 == a.chunks ? last : all) * d * d;
-    }
-    over_block(m2, none, lds);
-    m2 /= (double)a.P * a.D;
+    over_block(off, m2, lds);
+    off /= whole;
+    const double mean = from + off;
+    m2 = m2 / whole - off * off;
+    m2 = m2 > 0.0 || m2 != m2 ? m2 : 0.0;
     if (threadIdx.x != 0) return;
     a.mean[i] = (float)mean;
     a.rstd[i] = (float)(1.0 / sqrt(m2 + (double)a.eps));
@@ -263,11 +262,11 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
     uint32_t q = divided(e, a.by_c8);                  // its pixel, of all samples'
     const uint32_t c = (e - q * a.C8) * 8u;
     const uint32_t e_step = a.stride_passes * 64u, q_step = e_step / a.C8;
-    float w[8], b[8];
+    float w[8], b[8], rw[8];
     load_channels(a.w, a.w_f32, 1.0f, c, w);
     load_channels(a.b, a.w_f32, 0.0f, c, b);
     uint32_t sample = ~0u;
-    OfGroups<UNI> m, r;
+    OfGroups<UNI> m;
     for (;; ) {
         const bool active = e < a.blocks8;
         if (!active) q = a.B * a.P - 1;
@@ -276,13 +275,16 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
         const Raw<DT> raw = load8<DT>((const uint8_t*)a.x.p, at * kSize<DT>);
         if (s != sample) {
             m.load(a, a.mean + (size_t)s * a.H, 1, c);
+            OfGroups<UNI> r;
             r.load(a, a.rstd + (size_t)s * a.H, 1, c);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) rw[k] = r[k] * w[k];
             sample = s;
         }
         float v[8], y[8];
         widen8<DT>(raw, v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = activate<DT, SILU>(__builtin_fmaf((v[k] - m[k]) * r[k], w[k], b[k]));
+        for (int k = 0; k < 8; ++k) y[k] = activate<DT, SILU>(__builtin_fmaf(v[k] - m[k], rw[k], b[k]));
         if (active)
             store8<DT>((uint8_t*)a.y.p, ((int64_t)s * a.y.sample + (int64_t)p * a.y.pixel + c) * kSize<DT>, y);
         if constexpr (BITS != 0) gn_compress_pass<BITS>(a, pass, lane, active, v);
@@ -440,6 +442,12 @@ __global__ __launch_bounds__(kGnThreads) void gn_means_kernel(GnArgs a) {
     a.means[2 * i + 1] = (float)(m2 / ((double)a.P * a.D));
 }
 
+// into dw or db, if it is wanted
+__device__ __forceinline__ void gn_put(const GnArgs& a, void* p, uint32_t c, float v) {
+    if (!p) return;
+    if (a.w_f32) ((float*)p)[c] = v;
+    else ((uint16_t*)p)[c] = (uint16_t)bf16_pair_rne(v, 0.0f);
+}
 // dw and db of 32 channels: over the samples, eight parts of them, in binary64 and in a fixed order.
 __device__ __forceinline__ void gn_weights(const GnArgs& a, uint32_t block, double (&lds)[2][kGnThreads]) {
     const uint32_t part = threadIdx.x >> 5, c = block * 32u + (threadIdx.x & 31u);
@@ -458,13 +466,8 @@ __device__ __forceinline__ void gn_weights(const GnArgs& a, uint32_t block, doub
         s0 += lds[0][threadIdx.x + 32 * k];
         s1 += lds[1][threadIdx.x + 32 * k];
     }
-    const auto put = [&](void* p, double v) {
-        if (!p) return;
-        if (a.w_f32) ((float*)p)[c] = (float)v;
-        else ((uint16_t*)p)[c] = (uint16_t)bf16_pair_rne((float)v, 0.0f);
-    };
-    put(a.dw, s1);
-    put(a.db, s0);
+    gn_put(a, a.dw, c, (float)s1);
+    gn_put(a, a.db, c, (float)s0);
 }
 
 template <int DT, int BITS, bool UNI, bool SILU>
@@ -656,13 +659,15 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_kernel(GnArg
     load_channels(a.b, a.w_f32, 0.0f, c, b);
     const int64_t out = (int64_t)at.sample * a.y.sample + c;
 #pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] *= r[k % N];
+#pragma unroll
     for (int i = 0; i < R; ++i) {
         const uint32_t p = at.row + (uint32_t)i * at.rows;
         if (p >= a.P) break;
         float v[8];
         widen8<DT>(raw[i], v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = activate<DT, SILU>(__builtin_fmaf((v[k] - m[k % N]) * r[k % N], w[k], b[k]));
+        for (int k = 0; k < 8; ++k) v[k] = activate<DT, SILU>(__builtin_fmaf(v[k] - m[k % N], w[k], b[k]));
         store8<DT>((uint8_t*)a.y.p, (out + (int64_t)p * a.y.pixel) * kSize<DT>, v);
     }
 }
@@ -757,11 +762,15 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_backward_ker
     }
     if (!at.holds) return;
     if ((a.dw || a.db) && at.row == 0) {
-        float* out = a.sums + ((size_t)at.sample * a.C + c) * 2;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            out[2 * k] = total[at.col * 16 + k];
-            out[2 * k + 1] = total[at.col * 16 + 8 + k];
+            const float db = total[at.col * 16 + k], dw = total[at.col * 16 + 8 + k];
+            if (a.B == 1) {
+                gn_put(a, a.dw, c + (uint32_t)k, dw);
+                gn_put(a, a.db, c + (uint32_t)k, db);
+            } else {
+                *(hf2*)(a.sums + ((size_t)at.sample * a.C + c + (uint32_t)k) * 2) = hf2{db, dw};
+            }
         }
     }
     const int64_t out = (int64_t)at.sample * a.dx.sample + c;
@@ -818,19 +827,26 @@ static void gn_launch_whole(bool backward, const GnArgs& a, hipStream_t s) {
     constexpr uint32_t NT = kGnWhole[WHICH].threads;
     if (!backward) {
         // two passes a wavefront of those that compress
-        const uint32_t extra = BITS ? gn_up(a.passes, NT / 64 * 2) : 0;
-        const dim3 grid(a.norm_blocks + (extra < 4096 ? extra : 4096));
-        hipLaunchKernelGGL((gn_whole_kernel<DT, UNI, SILU, WHICH>), grid, dim3(NT), 0, s, a, BITS);
+        uint32_t extra = BITS ? gn_up(a.passes, NT / 64 * 2) : 0;
+        if (extra > 4096) extra = 4096;
+        if (BITS && a.x.p == a.y.p) {                  // in place: x is compressed before it is overwritten
+            GnArgs x = a;
+            x.norm_blocks = 0;
+            hipLaunchKernelGGL((gn_whole_kernel<DT, UNI, SILU, WHICH>), dim3(extra), dim3(NT), 0, s, x, BITS);
+            extra = 0;
+        }
+        hipLaunchKernelGGL((gn_whole_kernel<DT, UNI, SILU, WHICH>), dim3(a.norm_blocks + extra), dim3(NT), 0, s, a, BITS);
     } else {
         hipLaunchKernelGGL((gn_whole_backward_kernel<DT, BITS, UNI, SILU, WHICH>), dim3(a.norm_blocks), dim3(NT), 0, s, a);
-        if (a.dw || a.db) hipLaunchKernelGGL(gn_weights_kernel, dim3((a.C + 31) / 32), dim3(kGnThreads), 0, s, a);
+        if (a.B > 1 && (a.dw || a.db)) hipLaunchKernelGGL(gn_weights_kernel, dim3((a.C + 31) / 32), dim3(kGnThreads), 0, s, a);
     }
 }
 template <int DT, int BITS, bool UNI, bool SILU>
 static void gn_launch_sized(bool backward, const GnArgs& a, int whole, hipStream_t s) {
     if (whole == 0) gn_launch<DT, BITS, UNI, SILU>(backward, a, s);
     else if (whole == 1) gn_launch_whole<DT, BITS, UNI, SILU, 0>(backward, a, s);
-    else gn_launch_whole<DT, BITS, UNI, SILU, 1>(backward, a, s);
+    else if (whole == 2) gn_launch_whole<DT, BITS, UNI, SILU, 1>(backward, a, s);
+    else gn_launch_whole<DT, BITS, UNI, SILU, 2>(backward, a, s);
 }
 template <int DT, int BITS>
 static void gn_launch_form(bool backward, const GnArgs& a, int act, int whole, hipStream_t s) {

@@ -75,8 +75,8 @@ bool norm_overlaps(const gact_channel_norm* h, bool backward, bool compressed) {
     return (h->mean && h->mean == h->rstd) || (compressed && (h->packed == h->gmin || h->packed == h->gscale || h->gmin == h->gscale));
 }
 
-// Checks a call; fills *a and *bits (0 without a context).
-int stage_norm(const gact_channel_norm* h, bool backward, void* ws, size_t ws_bytes, gact::GnArgs* a, int* bits) {
+// Checks a call; fills *a, *bits (0 without a context) and *whole (plan_whole).
+int stage_norm(const gact_channel_norm* h, bool backward, void* ws, size_t ws_bytes, gact::GnArgs* a, int* bits, int* whole) {
     if (!h) return GACT_E_ARG;
     if (h->bits != GACT_BITS_UNCOMPRESSED && !bits_ok(h->bits)) return GACT_E_BITS;
     *bits = h->bits == GACT_BITS_UNCOMPRESSED ? 0 : h->bits;
@@ -127,14 +127,19 @@ int stage_norm(const gact_channel_norm* h, bool backward, void* ws, size_t ws_by
     if (*bits != 0) while ((8 << a->block_shift) < G) ++a->block_shift;
     norm_sizes(h->batch, h->pixels, h->channels, h->groups, a);
     if (!gact::launchable((uint64_t)a->B * (a->chunks * a->slabs + a->C8) + a->C, gact::kGnThreads)) return GACT_E_ARG;
+    *whole = gact::plan_whole(a, h->dtype);
     uint8_t* at = (uint8_t*)ws;
-    const size_t need = backward ? gact::gn_backward_bytes(*a) : gact::gn_forward_bytes(*a);
-    if (!at || !aligned(at, 16) || ws_bytes < need) return GACT_E_ARG;
+    const size_t need = backward ? gact::gn_backward_bytes(*a, *whole) : gact::gn_forward_bytes(*a, *whole);
+    if (need > 0 && (!at || !aligned(at, 16) || ws_bytes < need)) return GACT_E_ARG;
+    if (*whole) {
+        a->sums = (float*)at;
+        return GACT_OK;
+    }
     a->partial = (float*)at;
     at += gact::gn_partial_bytes(*a);
     if (backward) {
         a->sums = (float*)at;
-        a->means = (float*)(at + gact::gn_align((size_t)a->B * a->C * 2 * sizeof(float)));
+        a->means = (float*)(at + gact::gn_sums_bytes(*a));
     } else if (!a->mean) {
         a->mean = (float*)at;
         a->rstd = (float*)(at + gact::gn_align((size_t)a->B * a->H * sizeof(float)));
@@ -146,33 +151,30 @@ int stage_norm(const gact_channel_norm* h, bool backward, void* ws, size_t ws_by
 
 extern "C" {
 
-size_t gact_group_norm_workspace_bytes(int64_t batch, int64_t pixels, int channels, int groups) {
-    if (!norm_sizes_ok(batch, pixels, channels, groups) || batch == 0 || pixels == 0) return 0;
+size_t gact_group_norm_workspace_bytes(int64_t batch, int64_t pixels, int channels, int groups, gact_dtype dtype, int backward) {
+    if (!norm_sizes_ok(batch, pixels, channels, groups) || !dtype_ok((int)dtype) || batch == 0 || pixels == 0) return 0;
     gact::GnArgs a{};
     norm_sizes(batch, pixels, channels, groups, &a);
-    const size_t f = gact::gn_forward_bytes(a), b = gact::gn_backward_bytes(a);
-    return f > b ? f : b;
+    const int whole = gact::plan_whole(&a, (int)dtype);
+    return backward ? gact::gn_backward_bytes(a, whole) : gact::gn_forward_bytes(a, whole);
 }
 
 int gact_group_norm(const gact_channel_norm* h_norm, void* d_workspace, size_t workspace_bytes, void* stream) {
     gact::GnArgs a{};
-    int bits = 0;
-    if (const int rc = stage_norm(h_norm, false, d_workspace, workspace_bytes, &a, &bits)) return rc;
+    int bits = 0, whole = 0;
+    if (const int rc = stage_norm(h_norm, false, d_workspace, workspace_bytes, &a, &bits, &whole)) return rc;
     if (a.B == 0) return GACT_OK;
-    // in place, the pass that compresses has to be the one that writes
-    const int whole = bits != 0 && h_norm->x == h_norm->y ? 0 : gact::plan_whole(&a, h_norm->dtype);
     return gact_launch_group_norm(&a, h_norm->dtype, bits, h_norm->act, whole, stream) == 0 ? GACT_OK : GACT_E_HIP;
 }
 
 int gact_group_norm_backward(const gact_channel_norm* h_norm, void* d_workspace, size_t workspace_bytes, void* stream) {
     gact::GnArgs a{};
-    int bits = 0;
-    if (const int rc = stage_norm(h_norm, true, d_workspace, workspace_bytes, &a, &bits)) return rc;
+    int bits = 0, whole = 0;
+    if (const int rc = stage_norm(h_norm, true, d_workspace, workspace_bytes, &a, &bits, &whole)) return rc;
     if (a.B == 0) {                                     // nothing to add: the sums are zero
         if (!a.dw && !a.db) return GACT_OK;
         return gact_launch_group_norm_zero(&a, stream) == 0 ? GACT_OK : GACT_E_HIP;
     }
-    const int whole = gact::plan_whole(&a, h_norm->dtype);
     return gact_launch_group_norm_backward(&a, h_norm->dtype, bits, h_norm->act, whole, stream) == 0 ? GACT_OK : GACT_E_HIP;
 }
 
@@ -183,56 +185,56 @@ size_t gact_linear_weight_grad_workspace_bytes(int64_t tokens, int64_t out_featu
     return gact::weight_workspace_bytes(gact::plan_weight(T, N, K, (int)dtype), N, K);
 }
 
-int gact_linear_weight_grad(const void* d_dy, int64_t dy_stride, gact_dtype dtype, int64_t tokens, int64_t out_features,
-                            int64_t in_features, const void* d_packed, const float* d_gmin, const float* d_gscale,
-                            int group_size, int bits, void* d_dw, void* d_db, gact_dtype w_dtype, void* d_workspace,
-                            size_t workspace_bytes, void* stream) {
-    if (!bits_ok(bits)) return GACT_E_BITS;
-    if (!group_ok(group_size)) return GACT_E_GROUP;
-    if (!dtype_ok((int)dtype) || !dtype_ok((int)w_dtype) || !weight_sizes_ok(tokens, out_features, in_features)) return GACT_E_ARG;
-    const uint64_t T = (uint64_t)tokens, N = (uint64_t)out_features, K = (uint64_t)in_features;
-    if (N == 0 || (K == 0 && !d_db)) return GACT_OK;
-    const size_t w_size = size_of(w_dtype);
-    if (!aligned(d_db, w_size) || (K > 0 && (!d_dw || !aligned(d_dw, w_size) || d_dw == d_db))) return GACT_E_ARG;
-    if (T > 0 && (!d_dy || !aligned(d_dy, size_of(dtype)))) return GACT_E_ARG;
-    if (T * K > 0 && (!d_packed || !d_gmin || !d_gscale || !aligned(d_packed, 16) || !aligned(d_gmin, 4) || !aligned(d_gscale, 4)))
+int gact_linear_weight_grad(const gact_linear_grad* h_grad, void* d_workspace, size_t workspace_bytes, void* stream) {
+    if (!h_grad) return GACT_E_ARG;
+    const gact_linear_grad& h = *h_grad;
+    if (!bits_ok(h.bits)) return GACT_E_BITS;
+    if (!group_ok(h.group_size)) return GACT_E_GROUP;
+    if (!dtype_ok(h.dtype) || !dtype_ok(h.w_dtype) || !weight_sizes_ok(h.tokens, h.out_features, h.in_features)) return GACT_E_ARG;
+    const uint64_t T = (uint64_t)h.tokens, N = (uint64_t)h.out_features, K = (uint64_t)h.in_features;
+    if (N == 0 || (K == 0 && !h.db)) return GACT_OK;
+    const size_t w_size = size_of(h.w_dtype);
+    if (!aligned(h.db, w_size) || (K > 0 && (!h.dw || !aligned(h.dw, w_size) || h.dw == h.db))) return GACT_E_ARG;
+    if (T > 0 && (!h.dy || !aligned(h.dy, size_of(h.dtype)) || h.dy == h.dw || h.dy == h.db)) return GACT_E_ARG;
+    if (T * K > 0 && (!h.packed || !h.gmin || !h.gscale || !aligned(h.packed, 16) || !aligned(h.gmin, 4) || !aligned(h.gscale, 4)))
         return GACT_E_ARG;
-    const gact::WeightPlan plan = gact::plan_weight(T, N, K, (int)dtype);
+    const gact::WeightPlan plan = gact::plan_weight(T, N, K, h.dtype);
+    const gact::WeightTile tile = gact::weight_tile(h.dtype, plan.which);
     const uint64_t blocks = (uint64_t)plan.tiles_n * plan.tiles_k * plan.splits;
-    if (!gact::launchable(blocks, (uint32_t)gact::weight_tile((int)dtype, plan.which).threads)) return GACT_E_ARG;
+    if (!gact::launchable(blocks, (uint32_t)tile.threads)) return GACT_E_ARG;
     const size_t need = gact::weight_workspace_bytes(plan, N, K);
     if (need > 0 && (!d_workspace || !aligned(d_workspace, 16) || workspace_bytes < need)) return GACT_E_ARG;
     gact::WeightArgs a{};
-    a.dy = (const uint8_t*)d_dy;
-    a.packed = (const uint8_t*)d_packed;
-    a.gmin = d_gmin;
-    a.gscale = d_gscale;
-    a.dw = d_dw;
-    a.db = d_db;
+    a.dy = (const uint8_t*)h.dy;
+    a.packed = (const uint8_t*)h.packed;
+    a.gmin = h.gmin;
+    a.gscale = h.gscale;
+    a.dw = h.dw;
+    a.db = h.db;
     if (plan.splits > 1) {
         a.partial = (float*)d_workspace;
         a.db_partial = (float*)((uint8_t*)d_workspace + gact::weight_partial_bytes(plan, N, K));
     }
-    a.dy_stride = dy_stride;
+    a.dy_stride = h.dy_stride;
     a.T = (uint32_t)T;
     a.N = (uint32_t)N;
     a.K = (uint32_t)K;
-    const uint64_t words = (T * K * (uint64_t)bits + 127) / 128 * 4;
+    const uint64_t words = (T * K * (uint64_t)h.bits + 127) / 128 * 4;
     a.last_word = words ? words - 1 : 0;
-    a.last_group = T * K ? (uint32_t)((T * K - 1) / (uint64_t)group_size) : 0;
-    a.group = (uint32_t)group_size;
-    a.by_group = gact::divisor((uint32_t)group_size / 32);
+    a.last_group = T * K ? (uint32_t)((T * K - 1) / (uint64_t)h.group_size) : 0;
+    a.group = (uint32_t)h.group_size;
+    a.by_group = gact::divisor((uint32_t)h.group_size / 32);
     a.tiles_n = plan.tiles_n;
     a.tiles_k = plan.tiles_k;
     a.splits = plan.splits;
     a.chunks = plan.chunks;
     a.db_every = plan.db_every;
-    const uint32_t BT = (uint32_t)gact::weight_tile((int)dtype, plan.which).tokens;
-    a.dy_chunk = BT * (uint32_t)dy_stride * (uint32_t)size_of(dtype);
-    a.code_chunk = BT * a.K / 8 * (uint32_t)bits;
+    const uint32_t BT = (uint32_t)tile.tokens;
+    a.dy_chunk = BT * (uint32_t)h.dy_stride * (uint32_t)size_of(h.dtype);
+    a.code_chunk = BT * a.K / 8 * (uint32_t)h.bits;
     a.group_chunk = BT * a.K / a.group * 4;
-    a.w_f32 = w_dtype == GACT_F32;
-    return gact_launch_weight(&a, plan.which, (int)dtype, bits, stream) == 0 ? GACT_OK : GACT_E_HIP;
+    a.w_f32 = h.w_dtype == GACT_F32;
+    return gact_launch_weight(&a, plan.which, h.dtype, h.bits, stream) == 0 ? GACT_OK : GACT_E_HIP;
 }
 
 }  // extern "C"

@@ -213,7 +213,7 @@ def test_what_lies_behind_the_buffers_stays():
     x, dy, w, b = inputs(B, P, C, torch.bfloat16, torch.float32)
     room = torch.full((B * P * C + 256,), 7.0, dtype=torch.bfloat16, device="cuda")
     gapped = torch.full((B, P, C + 24), 7.0, dtype=torch.bfloat16, device="cuda")
-    need = gact.gact_group_norm_workspace_bytes(B, P, C, H)
+    need = max(gact.gact_group_norm_workspace_bytes(B, P, C, H, x.dtype, back) for back in (False, True))
     ws = torch.full((need + 256,), 77, dtype=torch.uint8, device="cuda")
     context = gact.make_group_norm_context(x, H, 2, 32, 1)
     size = context.blob.numel()
@@ -231,7 +231,8 @@ def test_captured_repeated_and_on_another_stream():
     x, dy, w, b = inputs(B, P, C, torch.bfloat16, torch.float32)
     y, dx = torch.empty_like(x), torch.empty_like(x)
     context = gact.make_group_norm_context(x, H, 4, 64, 9)
-    ws = torch.empty(gact.gact_group_norm_workspace_bytes(B, P, C, H), dtype=torch.uint8, device="cuda")
+    need = max(gact.gact_group_norm_workspace_bytes(B, P, C, H, x.dtype, back) for back in (False, True))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
 
     def step():
         gact.gact_group_norm(x, H, w, b, 1e-5, "silu", context=context, out=y, workspace=ws)

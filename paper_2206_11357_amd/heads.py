@@ -63,11 +63,11 @@ class _HeadNormRotate(torch.autograd.Function):
         return (*(g if n else None for g, n in zip(grads, need)), *(None,) * 10)
 
 
-def _refuse_tangents(*tensors: Optional[torch.Tensor]) -> None:
+def _refuse_tangents(*tensors: Optional[torch.Tensor], of: str = "head_norm_rotate") -> None:
     """The kernels pass no forward-mode derivatives on, and a result without one would stand for zero."""
     if getattr(forward_ad, "_current_level", 0) >= 0 and any(
             t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
-        raise NotImplementedError("head_norm_rotate has no forward-mode derivative")
+        raise NotImplementedError("%s has no forward-mode derivative" % of)
 
 
 def head_norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], cos: Optional[torch.Tensor], sin: Optional[torch.Tensor],

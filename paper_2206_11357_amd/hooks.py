@@ -26,7 +26,8 @@ from torch.multiprocessing.reductions import StorageWeakRef
 from . import (GACT_BITS_UNCOMPRESSED, GACT_OK, GactError, TensorDesc, dtype_code, gact_allocate_bits_levels,
                gact_copy_bounded, gact_grad_clip, head_context_fits,
                gact_multi_workspace_bytes, gact_num_groups, gact_packed_bytes, gact_sensitivity, lib)
-from .heads import head_norm_rotate
+from . import group_norm_context_fits, layers
+from .heads import _itself, head_norm_rotate
 
 _MASK64 = (1 << 64) - 1
 _MAX_BATCH = 64            # a launch table of at most 64 tensors travels in the kernel arguments
@@ -320,6 +321,44 @@ class Controller:
                                     _own=all(own))
         return tuple(head_norm_rotate(x[j], None, cos, sin, (wq, wk)[j], None, positions, eps, interleaved, by_head, (bits[j], 0),
                                       self.group_size, (seeds[j], 0), _own=own[j])[0] for j in range(2))
+
+    def _takes(self, x: torch.Tensor) -> bool:
+        """Whether x, of any strides, is a context tensor that the scheme compresses."""
+        return (torch.is_grad_enabled() and x.is_cuda and x.requires_grad and x.numel() >= self.min_numel
+                and x.dtype in (torch.float32, torch.bfloat16))
+
+    def _number(self, x: torch.Tensor):
+        """Makes x the scheme's next context tensor; its width and seed."""
+        index = len(self._handles)
+        self._handles.append(None)
+        self.numel.append(x.numel())
+        return self.bits_of(index), self.seed_of(index)
+
+    def linear(self, x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """``layers.linear`` whose context is part of the scheme: x is a context tensor l like those of the hooks, with width b_l,
+        seed r_l and a place in Alg. 1 and Eq. (ilp), but read by the weight gradient's kernel as codes.  Its buffers stay on
+        the device (they are not swapped), and an x that several layers share is compressed for each.  An x that the
+        hooks would not compress (size, type, no gradient), or a weight without a gradient, is left to autograd."""
+        if not (self._takes(x) and weight.requires_grad) or x.dim() < 2 or torch.is_autocast_enabled("cuda"):
+            return torch.nn.functional.linear(x, weight, bias)
+        bits, seed = self._number(x)
+        if bits == GACT_BITS_UNCOMPRESSED:
+            with torch.autograd.graph.saved_tensors_hooks(_itself, _itself):      # numbered already
+                return torch.nn.functional.linear(x, weight, bias)
+        return layers.linear(x, weight, bias, bits, self.group_size, seed, _own=True)
+
+    def group_norm(self, x: torch.Tensor, groups: int, w: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,
+                   eps: float = 1e-5, act: str = "none") -> torch.Tensor:
+        """``layers.group_norm`` whose context is part of the scheme: x is a context tensor l like those of the hooks, but
+        compressed by the forward call and read by the backward kernels as codes; its buffers stay on the device.  Where the
+        controller's group size does not fit (``group_norm_context_fits``) x goes to the hooks as any saved tensor does,
+        copied first where it is a slice; one that the hooks would not compress (size, type) is left to autograd."""
+        if not self._takes(x):
+            return layers.group_norm(x, groups, w, b, eps, act)
+        if not group_norm_context_fits(self.group_size, x.shape[-1]):
+            return layers.group_norm(x.contiguous(), groups, w, b, eps, act)
+        bits, seed = self._number(x)
+        return layers.group_norm(x, groups, w, b, eps, act, bits, self.group_size, seed, _own=True)
 
     def clip_grad_norm_(self, params: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float,
                         norm_type: float = 2.0) -> torch.Tensor:

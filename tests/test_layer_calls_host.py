@@ -1,0 +1,222 @@
+"""What the calls of layers with compressed contexts refuse, before anything is launched, and the sizes of their workspaces (CPU)."""
+import ctypes
+
+import pytest
+import torch
+from torch.autograd import forward_ad
+
+import paper_2206_11357_amd as gact
+from paper_2206_11357_amd import layers
+
+LIB = gact.lib
+RAW = gact.GACT_BITS_UNCOMPRESSED
+
+
+@pytest.fixture(scope="module")
+def room():
+    """Addresses that are valid to name, 16-byte aligned, 1 KB apart; nothing is read from them."""
+    buf = (ctypes.c_char * (64 << 10))()
+    first = (ctypes.addressof(buf) + 1023) // 1024 * 1024
+    yield [first + 1024 * k for k in range(60)], buf
+
+
+def linear_record(room, **over):
+    p, _ = room
+    a = dict(dy=p[0], packed=p[1], gmin=p[2], gscale=p[3], dw=p[4], db=p[5], stride=16, T=8, N=16, K=32, dtype=0, w_dtype=0, G=32, bits=4)
+    a.update(over)
+    return gact._LINEAR_GRAD.pack(*a.values())
+
+
+@pytest.mark.parametrize("over,want", [
+    (dict(bits=3), gact.GACT_E_BITS), (dict(bits=32), gact.GACT_E_BITS), (dict(G=48), gact.GACT_E_GROUP), (dict(G=0), gact.GACT_E_GROUP),
+    (dict(G=2048), gact.GACT_E_GROUP), (dict(dtype=2), gact.GACT_E_ARG), (dict(w_dtype=-1), gact.GACT_E_ARG), (dict(T=-1), gact.GACT_E_ARG),
+    (dict(N=-1), gact.GACT_E_ARG), (dict(K=1 << 31), gact.GACT_E_ARG), (dict(T=1 << 30, K=32), gact.GACT_E_ARG),
+    (dict(N=1 << 30, K=1 << 8), gact.GACT_E_ARG), (dict(dy=0), gact.GACT_E_ARG), (dict(packed=0), gact.GACT_E_ARG),
+    (dict(gmin=0), gact.GACT_E_ARG), (dict(gscale=0), gact.GACT_E_ARG), (dict(dw=0), gact.GACT_E_ARG)])
+def test_linear_refusals(room, over, want):
+    assert LIB.gact_linear_weight_grad(linear_record(room, **over), None, 0, None) == want
+
+
+@pytest.mark.parametrize("name,off", [("dy", 2), ("packed", 8), ("gmin", 2), ("gscale", 1), ("dw", 2), ("db", 3)])
+def test_linear_misaligned(room, name, off):
+    at = dict(dy=0, packed=1, gmin=2, gscale=3, dw=4, db=5)[name]
+    assert LIB.gact_linear_weight_grad(linear_record(room, **{name: room[0][at] + off}), None, 0, None) == gact.GACT_E_ARG
+
+
+def test_linear_outputs_apart(room):
+    p, _ = room
+    for over in (dict(db=p[4]), dict(dw=p[0]), dict(db=p[0])):
+        assert LIB.gact_linear_weight_grad(linear_record(room, **over), None, 0, None) == gact.GACT_E_ARG
+    assert LIB.gact_linear_weight_grad(None, None, 0, None) == gact.GACT_E_ARG
+
+
+def test_linear_workspace(room):
+    need = gact.gact_linear_weight_grad_workspace_bytes(100000, 256, 256, torch.float32)
+    assert need >= 2 * 256 * 256 * 4
+    record = linear_record(room, T=100000, N=256, K=256, stride=256)
+    p, _ = room
+    for ws, size in ((None, need), (p[10], need - 1), (p[10] + 8, need)):
+        assert LIB.gact_linear_weight_grad(record, ws, size, None) == gact.GACT_E_ARG
+    assert gact.gact_linear_weight_grad_workspace_bytes(1, 64, 64, torch.bfloat16) == 0
+    for bad in ((-1, 8, 8), (8, -1, 8), (8, 8, 1 << 31), (1 << 30, 8, 64)):
+        assert LIB.gact_linear_weight_grad_workspace_bytes(*bad, 0) == 0
+    # whatever the sizes, the splits' sums stay within a few times the GPU's accumulators
+    for T in (1, 63, 64, 4096, 1 << 20, 1 << 27):
+        for N in (1, 64, 300, 4096):
+            for K in (1, 64, 250):
+                for dtype in (0, 1):
+                    assert LIB.gact_linear_weight_grad_workspace_bytes(T, N, K, dtype) <= 96 << 20
+
+
+def test_nothing_to_do(room):
+    assert LIB.gact_linear_weight_grad(linear_record(room, N=0, dw=0, dy=0), None, 0, None) == gact.GACT_OK
+    assert LIB.gact_linear_weight_grad(linear_record(room, K=0, dw=0, db=0), None, 0, None) == gact.GACT_OK
+    assert LIB.gact_group_norm(norm_record(room, B=0, x=0, y=0), None, 0, None) == gact.GACT_OK
+    assert LIB.gact_group_norm_backward(norm_record(room, P=0, dy=0, dx=0, dw=0, db=0), None, 0, None) == gact.GACT_OK
+
+
+def norm_record(room, **over):
+    p, _ = room
+    names = ("x", "y", "dy", "dx", "w", "b", "dw", "db", "mean", "rstd", "packed", "gmin", "gscale")
+    a = {n: p[k] for k, n in enumerate(names)}
+    a.update(strides=(64 * 9, 64) * 4, B=2, P=9, seed=1, C=64, H=8, act=1, dtype=0, w_dtype=0, bits=4, G=64, eps=1e-5)
+    a.update(over)
+    strides = a.pop("strides")
+    v = list(a.values())
+    return gact._CHANNEL_NORM.pack(*v[:13], *strides, *v[13:])
+
+
+NORM = [(dict(bits=3), gact.GACT_E_BITS), (dict(G=96), gact.GACT_E_GROUP), (dict(G=1024), gact.GACT_E_GROUP), (dict(G=16), gact.GACT_E_GROUP),
+        (dict(dtype=5), gact.GACT_E_ARG), (dict(w_dtype=2), gact.GACT_E_ARG), (dict(act=2), gact.GACT_E_ARG), (dict(act=-1), gact.GACT_E_ARG),
+        (dict(B=-1), gact.GACT_E_ARG), (dict(P=-1), gact.GACT_E_ARG), (dict(C=60), gact.GACT_E_ARG), (dict(C=0), gact.GACT_E_ARG),
+        (dict(H=0), gact.GACT_E_ARG), (dict(H=7), gact.GACT_E_ARG), (dict(H=128), gact.GACT_E_ARG), (dict(C=(1 << 20) + 8), gact.GACT_E_ARG),
+        (dict(B=1 << 20, P=1 << 11), gact.GACT_E_ARG), (dict(B=1 << 16, P=1 << 14), gact.GACT_E_ARG), (dict(B=1 << 25), gact.GACT_E_ARG),
+        (dict(mean=0), gact.GACT_E_ARG), (dict(rstd=0), gact.GACT_E_ARG), (dict(mean=0, rstd=0), gact.GACT_E_ARG),
+        (dict(packed=0), gact.GACT_E_ARG), (dict(gmin=0), gact.GACT_E_ARG), (dict(gscale=0), gact.GACT_E_ARG)]
+
+
+@pytest.mark.parametrize("over,want", NORM)
+def test_norm_refusals(room, over, want):
+    assert LIB.gact_group_norm(norm_record(room, **over), room[0][20], 1 << 10, None) == want
+    assert LIB.gact_group_norm_backward(norm_record(room, **over), room[0][20], 1 << 10, None) == want
+
+
+@pytest.mark.parametrize("over", [dict(x=0), dict(y=0), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")),
+                                  dict(eps=1e-42)])
+def test_forward_refusals(room, over):
+    assert LIB.gact_group_norm(norm_record(room, **over), room[0][20], 1 << 10, None) == gact.GACT_E_ARG
+
+
+@pytest.mark.parametrize("over", [dict(dy=0), dict(dx=0), dict(w=0), dict(b=0), dict(bits=RAW, x=0)])
+def test_backward_refusals(room, over):
+    assert LIB.gact_group_norm_backward(norm_record(room, **over), room[0][20], 1 << 10, None) == gact.GACT_E_ARG
+
+
+@pytest.mark.parametrize("name", ["x", "y", "dy", "dx", "w", "b", "dw", "db", "mean", "rstd", "packed", "gmin", "gscale"])
+def test_norm_misaligned(room, name):
+    at = ("x", "y", "dy", "dx", "w", "b", "dw", "db", "mean", "rstd", "packed", "gmin", "gscale").index(name)
+    record = norm_record(room, **{name: room[0][at] + 2}, bits=RAW if name == "x" else 4)
+    backward = name in ("dy", "dx", "dw", "db")
+    call = LIB.gact_group_norm_backward if backward else LIB.gact_group_norm
+    assert call(record, room[0][20], 1 << 10, None) == gact.GACT_E_ARG
+
+
+def test_norm_outputs_apart(room):
+    p, _ = room
+    inside = (64 * 9, 64)
+    other = (64 * 9, 64, 64 * 10, 64, 64 * 9, 64, 64 * 10, 64)
+    for over in (dict(y=p[4]), dict(y=p[8]), dict(y=p[10]), dict(mean=p[9]), dict(packed=p[11]), dict(gmin=p[12]),
+                 dict(y=p[0], strides=other), dict(strides=inside + (64, 32) + inside + (64, 32)),
+                 dict(strides=inside + (64 * 4, 64) + inside * 2), dict(strides=inside + (0, 64) + inside * 2)):
+        assert LIB.gact_group_norm(norm_record(room, **over), p[20], 1 << 10, None) == gact.GACT_E_ARG, over
+    for over in (dict(dx=p[4]), dict(dx=p[6]), dict(dx=p[10]), dict(dw=p[7]), dict(dw=p[4]), dict(db=p[2]), dict(bits=RAW, dx=p[0]),
+                 dict(dx=p[2], strides=other), dict(strides=inside * 3 + (64 * 9, 63))):
+        assert LIB.gact_group_norm_backward(norm_record(room, **over), p[20], 1 << 10, None) == gact.GACT_E_ARG, over
+
+
+def test_norm_workspace(room):
+    p, _ = room
+    size = lambda *a, back=0, dtype=0: LIB.gact_group_norm_workspace_bytes(*a, dtype, back)
+    assert size(1, 64, 512, 32) == 0 and size(1, 64, 512, 32, back=1) == 0       # held in registers
+    assert size(3, 64, 512, 32, back=1) == 3 * 512 * 8
+    need = size(1, 1 << 18, 128, 32)
+    assert need >= 8 * 32
+    for bad in ((-1, 8, 8, 1), (1, 8, 12, 1), (1, 8, 16, 3), (1 << 16, 1 << 15, 8, 1), (1, 8, 8, 0)):
+        assert size(*bad) == 0
+    record = norm_record(room, B=1, P=1 << 18, C=128, H=32, strides=(128 << 18, 128) * 4)
+    for ws, n in ((None, need), (p[20], need - 1), (p[20] + 4, need)):
+        assert LIB.gact_group_norm(record, ws, n, None) == gact.GACT_E_ARG
+    assert LIB.gact_group_norm(None, None, 0, None) == gact.GACT_E_ARG
+    assert LIB.gact_group_norm_backward(None, None, 0, None) == gact.GACT_E_ARG
+
+
+# ---------------------------------------------------------------- the binding
+def test_shapes_that_the_binding_takes():
+    assert gact._rows(torch.empty(6, 8)) == (6, 8)
+    assert gact._rows(torch.empty(2, 3, 8)) == (6, 8)
+    assert gact._rows(torch.empty(2, 3, 16)[..., 8:]) == (6, 16)
+    assert gact._rows(torch.empty(8).expand(5, 8)) == (5, 0)
+    assert gact._rows(torch.empty(1, 1, 8)) == (1, 8)
+    assert gact._map_strides(torch.empty(2, 3, 4, 8)) == (2, 12, 8, 96, 8)
+    assert gact._map_strides(torch.empty(2, 8, 3, 4).to(memory_format=torch.channels_last).permute(0, 2, 3, 1)) == (2, 12, 8, 96, 8)
+    assert gact._map_strides(torch.empty(2, 3, 4, 16)[..., :8]) == (2, 12, 8, 192, 16)
+    for bad in (torch.empty(8), torch.empty(8, 6).t(), torch.empty(4, 3, 8)[:, :2]):
+        with pytest.raises(ValueError):
+            gact._rows(bad)
+    for bad in (torch.empty(8, 8), torch.empty(2, 8, 3).transpose(1, 2), torch.empty(2, 5, 4, 8)[:, :, :3]):
+        with pytest.raises(ValueError):
+            gact._map_strides(bad)
+
+
+def test_binding_refuses_host_memory_and_wrong_types():
+    x = torch.zeros(2, 9, 64)
+    with pytest.raises(ValueError):
+        gact.gact_group_norm(x, 8)
+    u, f = torch.zeros(64, dtype=torch.uint8), torch.zeros(8)
+    with pytest.raises(ValueError):
+        gact.gact_linear_weight_grad(torch.zeros(4, 8), u, f, f, 8, 32, 4)
+    with pytest.raises(ValueError):
+        gact._activation("relu")
+    with pytest.raises(ValueError):
+        gact._channel_weights(torch.ones(8), torch.ones(8).bfloat16(), 8)
+    with pytest.raises(ValueError):
+        gact._channel_weights(torch.ones(7), None, 8)
+    c = gact.make_group_norm_context(x, 8, 4, 64)
+    with pytest.raises(ValueError):
+        gact._norm_context(c, torch.zeros(2, 9, 32), -1, 8)
+    with pytest.raises(ValueError):
+        gact._norm_context(c, x, -1, 4)
+    with pytest.raises(ValueError):
+        c.filled(torch.zeros(3, dtype=torch.uint8))
+    assert c.filled(c.blob).addresses() == c.addresses()
+    assert c.packed.numel() == gact.gact_packed_bytes(x.numel(), 4) and c.gmin.numel() == c.gscale.numel() == 18
+    assert c.mean.shape == c.rstd.shape == (2, 8)
+
+
+def test_context_fits():
+    assert gact.group_norm_context_fits(256, 64) and not gact.group_norm_context_fits(96, 64)
+    assert not gact.group_norm_context_fits(1024, 64) and not gact.group_norm_context_fits(64, 60)
+
+
+# ------------------------------------------------------------------ autograd
+@pytest.mark.parametrize("which", range(3))
+def test_forward_mode_tangents_are_refused(monkeypatch, which):
+    """A result without a tangent would mean that the derivative is zero.  (Nothing is launched.)"""
+    monkeypatch.setattr(layers, "gact_group_norm", lambda x, *a, **k: x.detach().clone())
+    for call, args in ((lambda x, w, b: layers.group_norm(x, 2, w, b), [torch.zeros(2, 3, 8), torch.ones(8), torch.zeros(8)]),
+                       (lambda x, w, b: layers.linear(x, w, b, 4, 32), [torch.zeros(2, 8), torch.ones(4, 8).requires_grad_(), torch.zeros(4)])):
+        with forward_ad.dual_level():
+            args[which] = forward_ad.make_dual(args[which], torch.ones_like(args[which]))
+            with pytest.raises(NotImplementedError):
+                call(*args)
+
+
+def test_linear_without_a_context_is_torchs():
+    x, w = torch.randn(3, 8, requires_grad=True), torch.randn(4, 8, requires_grad=True)
+    assert torch.equal(layers.linear(x, w), torch.nn.functional.linear(x, w))
+    with torch.no_grad():
+        assert torch.equal(layers.linear(x, w, bits=4, group_size=32), torch.nn.functional.linear(x, w))
+    with pytest.raises(ValueError):
+        layers.linear(x, w.bfloat16(), bits=4, group_size=32)
+    with pytest.raises(ValueError):
+        layers.linear(x[0], w, bits=4, group_size=32)

@@ -503,8 +503,8 @@ int gact_group_norm_backward(const gact_channel_norm *h_norm, void *d_workspace,
  * Weight gradient of a linear layer y = x W^T + b from the compressed context of its input, which is not decompressed
  * to memory:
  *     dW[n, k] = sum over t of dy[t, n] * x^[t, k],      db[n] = sum over t of dy[t, n],
- * x^ = code * step + minimum of the context (x laid out contiguously as [tokens, in_features]; groups may pass from row to
- * row), rounded to dy's type: in fp32 what gact_decompress gives, in bf16 the product is not rounded before the sum.  Sums in binary32, over blocks and splits of the tokens in a fixed order, the same
+ * x^ being what gact_decompress gives of the context in dy's type (x laid out contiguously as [tokens, in_features];
+ * groups may pass from row to row).  Sums in binary32, over blocks and splits of the tokens in a fixed order, the same
  * in every call of the same sizes and types; outputs rounded once.
  *   dy           [tokens, out_features] of dtype, its rows' elements consecutive, dy_stride elements from row to row (any value,
  *                0 too: a gradient that all tokens share), aligned as its type

@@ -77,9 +77,9 @@ __device__ __forceinline__ void part_codes(Codes<BITS>& c) {
     c.lo &= 0x0F0F0F0Fu;
     asm("" : "+v"(c.lo), "+v"(c.hi));
 }
-// Value j of them in binary32.  fp32: the product is rounded before the sum, as gact_decompress does it; bf16: once, in one
-// instruction, in front of the rounding to bf16.
-template <int DT, int BITS, bool WHOLE>
+// Value j of them in binary32, as gact_decompress has it: the product is rounded before the sum.  (In one instruction, a few bf16
+// values in a million come out a step apart: 1.5e-5 of a dW of 12608 tokens, 8 bits, where 1.8e-7 is its own sums'.)
+template <int BITS, bool WHOLE>
 __device__ __forceinline__ float value_of(const Codes<BITS>& c, int j) {
     const uint32_t word = BITS == 8 ? (j >= 4 ? c.hi : c.lo) : BITS == 4 && (j & 1) != 0 ? c.hi : c.lo;
     const uint32_t q = BITS == 8 ? word >> (8 * (j & 3)) & 0xFFu
@@ -87,7 +87,6 @@ __device__ __forceinline__ float value_of(const Codes<BITS>& c, int j) {
                      : word >> (j * BITS) & ((1u << BITS) - 1u);
     const bool next = !WHOLE && (uint32_t)j >= c.turn;
     const float step = next ? c.step[1] : c.step[0], mn = next ? c.mn[1] : c.mn[0];
-    if (DT == GACT_DT_BF16) return __builtin_fmaf((float)q, step, mn);
     const float t = (float)q * step;
     return t + mn;
 }
@@ -278,7 +277,7 @@ __global__ __launch_bounds__(weight_tile(DT, WHICH).threads, 2) void weight_kern
             float x[8];
             part_codes<BITS>(codes[q]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = value_of<DT, BITS, WHOLE>(codes[q], j);
+            for (int j = 0; j < 8; ++j) x[j] = value_of<BITS, WHOLE>(codes[q], j);
             place_x(buf, q, x);
         }
     };
@@ -354,7 +353,7 @@ __global__ __launch_bounds__(weight_tile(DT, WHICH).threads, 2) void weight_kern
     const auto decode = [&](uint32_t next, int e) {
         const int q = e / 8;
         if (e % 8 == 0) part_codes<BITS>(codes[q]);
-        v[q][e % 8] = value_of<DT, BITS, WHOLE>(codes[q], e % 8);
+        v[q][e % 8] = value_of<BITS, WHOLE>(codes[q], e % 8);
         if (e % 8 == 7) fetch_x(next, q);
     };
     const auto read_all = [&](const uint8_t* buf) {

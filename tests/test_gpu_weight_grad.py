@@ -1,5 +1,5 @@
-"""Weight gradient of a linear layer from the codes of its input, against the same sums in binary64 over what the codes
-stand for."""
+"""Weight gradient of a linear layer from the codes of its input, against the same sums in binary64 over what
+gact_decompress gives of the context."""
 import numpy as np
 import pytest
 import torch
@@ -23,14 +23,7 @@ def inputs(T, N, K, G, bits, dtype, seed=0, wide=0):
 def reference(dy, context, K, G, bits):
     """dW, db in binary64, and the sums of the terms' sizes."""
     T, N = dy.shape
-    if dy.dtype == torch.float32:
-        x = gact.gact_decompress(*context, T * K, G, bits).view(T, K).cpu().double()
-    else:
-        packed, gmin, gscale = (t.cpu() for t in context)
-        at = torch.arange(T * K)
-        q = (packed[at * bits // 8].long() >> (at * bits % 8)) & (2 ** bits - 1)
-        # the product has 32 bits at most; the sum is rounded to binary32 once (it fits 53 bits here), then to bf16
-        x = (q.double() * gscale[at // G].double() + gmin[at // G].double()).float().bfloat16().double().view(T, K)
+    x = gact.gact_decompress(*context, T * K, G, bits, dtype=dy.dtype).view(T, K).cpu().double()
     d = dy.cpu().double()
     return d.t() @ x, d.sum(0), d.abs().t() @ x.abs(), d.abs().sum(0)
 
@@ -83,6 +76,17 @@ def test_codes(K, G, bits, dtype):
 @pytest.mark.parametrize("T,N,K", [(4096, 256, 256), (3001, 300, 392), (2500, 513, 333), (700, 2304, 768)])
 def test_large_tiles(T, N, K, w_dtype, dtype):
     check(T, N, K, 128, 4, DTYPES[dtype], DTYPES[w_dtype], bias=K != 392, wide=8 * (N % 2))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bits", [1, 2, 4, 8])
+@pytest.mark.parametrize("N,K,G", [(8, 2048, 64), (264, 8192, 96), (264, 8192, 256)])
+def test_values_are_those_of_the_decompressor(N, K, G, bits, dtype):
+    """Every token's row of dy picks one row of dW: the products are x^ itself, with nothing to round."""
+    dy, *context = inputs(N, N, K, G, bits, DTYPES[dtype])
+    dw, _ = gact.gact_linear_weight_grad(torch.eye(N, dtype=DTYPES[dtype], device="cuda"), *context, K, G, bits, w_dtype=torch.float32)
+    x = gact.gact_decompress(*context, N * K, G, bits, dtype=DTYPES[dtype]).view(N, K)
+    assert torch.equal(dw, x.float())
 
 
 def test_rows_at_odd_addresses():

@@ -89,7 +89,7 @@ inline size_t weight_workspace_bytes(const WeightPlan& p, uint64_t N, uint64_t K
 }
 
 // Parts that a workgroup of the second launch divides the splits into.
-inline int join_parts(uint32_t splits) { return splits >= 64 ? 16 : splits >= 12 ? 4 : 1; }
+inline int join_parts(uint32_t splits) { return splits >= 64 ? 16 : splits >= 4 ? 4 : 1; }
 
 }  // namespace gact
 

@@ -12,6 +12,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "gact_codec.h"
 #include "gact_device.h"
 #include "gact_weight.h"
@@ -439,56 +441,66 @@ __global__ __launch_bounds__(weight_tile(DT, WHICH).threads, 2) void weight_kern
         }
     }
 
-    // ---- the teams' sums: half of the second one's registers at a time, through shared memory
+    // ---- the teams' sums: each team hands half of its products to the other through shared memory, a row of products at a time, and
+    // is left with the other half's sums
+    constexpr int kMine = TN / L::kTeams;                           // rows of products that a wavefront writes
+    const int first = L::kTeams == 2 ? team * kMine : 0;
     if constexpr (L::kTeams == 2) {
-        static_assert(TN % 2 == 0 && TN / 2 * TK * 16 * 256 * 4 <= 2 * L::kBuf, "room");
+        static_assert(TN % 2 == 0 && 2 * TK * 16 * 256 * 4 <= 2 * L::kBuf, "room");
         float* room = (float*)lds[0] + (tid & 255u);
+        constexpr int kHalf = TK * 16 * 256;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int i = 0; i < kMine; ++i) {
             __syncthreads();
 #pragma unroll
-            for (int i = half * TN / 2; i < (half + 1) * TN / 2; ++i)
+            for (int j = 0; j < TK; ++j)
 #pragma unroll
-                for (int j = 0; j < TK; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (team == 1) room[(((i - half * TN / 2) * TK + j) * 16 + r) * 256] = acc[i][j][r];
+                for (int r = 0; r < 16; ++r) {
+                    if (team == 0) room[(j * 16 + r) * 256] = acc[kMine + i][j][r];
+                    else room[kHalf + (j * 16 + r) * 256] = acc[i][j][r];
+                }
             __syncthreads();
 #pragma unroll
-            for (int i = half * TN / 2; i < (half + 1) * TN / 2; ++i)
+            for (int j = 0; j < TK; ++j)
 #pragma unroll
-                for (int j = 0; j < TK; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (team == 0) acc[i][j][r] += room[(((i - half * TN / 2) * TK + j) * 16 + r) * 256];
+                for (int r = 0; r < 16; ++r) {
+                    // the first team's first, for both
+                    if (team == 0) acc[i][j][r] = acc[i][j][r] + room[kHalf + (j * 16 + r) * 256];
+                    else acc[i][j][r] = room[(j * 16 + r) * 256] + acc[kMine + i][j][r];
+                }
         }
-        __syncthreads();
     }
 
     // ---- out: element r of a product is row (r & 3) + 8 (r >> 2) + 4 (lane / 32), column lane % 32
-    if (L::kTeams == 1 || team == 0) {
-    const bool whole = a.partial == nullptr;
-    float* part = whole ? nullptr : a.partial + (size_t)split * a.N * a.K;
+    const bool whole = a.partial == nullptr, inside = n0 + BN <= a.N && k0 + BK <= a.K;
+    const int low = lane >> 5, at_k = lane & 31;
+    // of a lane: row, column, and their elements; of row r of products i: what all lanes add to them
+    const uint32_t lane_n = n0 + (uint32_t)(wn * 32 * TN + (DT == GACT_DT_F32 ? 4 * low * TN + first : first * 32 + 4 * low));
+    const uint32_t lane_k = k0 + (uint32_t)(wk * 32 * TK + (DT == GACT_DT_F32 ? at_k * TK : at_k));
+    const auto put = [&](auto* to) {
+        typedef typename std::remove_pointer<decltype(to)>::type Out;
+        to += (size_t)lane_n * a.K + lane_k;
 #pragma unroll
-    for (int i = 0; i < TN; ++i)
+        for (int i = 0; i < kMine; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
-            const uint32_t on = n0 + (uint32_t)(wn * 32 * TN + (DT == GACT_DT_F32 ? row * TN + i : i * 32 + row));
-            if (on >= a.N) continue;
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t row = (uint32_t)((r & 3) + 8 * (r >> 2)), n = DT == GACT_DT_F32 ? row * TN + i : i * 32 + row;
+                if (!inside && lane_n + n >= a.N) continue;
+                Out* p = to + (size_t)n * a.K;
 #pragma unroll
-            for (int j = 0; j < TK; ++j) {
-                const uint32_t ok = k0 + (uint32_t)(wk * 32 * TK + (DT == GACT_DT_F32 ? (lane & 31) * TK + j : j * 32 + (lane & 31)));
-                if (ok >= a.K) continue;
-                const size_t o = (size_t)on * a.K + ok;
-                if (!whole) part[o] = acc[i][j][r];
-                else if (a.w_f32) ((float*)a.dw)[o] = acc[i][j][r];
-                else ((uint16_t*)a.dw)[o] = (uint16_t)bf16_pair_rne(acc[i][j][r], 0.0f);
+                for (int j = 0; j < TK; ++j) {
+                    const uint32_t k = DT == GACT_DT_F32 ? j : j * 32;
+                    if (!inside && lane_k + k >= a.K) continue;
+                    if constexpr (sizeof(Out) == 4) p[k] = acc[i][j][r];
+                    else p[k] = (Out)bf16_pair_rne(acc[i][j][r], 0.0f);
+                }
             }
-        }
+    };
+    if (!whole) put(a.partial + (size_t)split * a.N * a.K);
+    else if (a.w_f32) put((float*)a.dw);
+    else put((uint16_t*)a.dw);
 
-    }
-
+    if (L::kTeams == 2) __syncthreads();
     if (!with_db) return;
     // db of the tile's rows: over the threads of a column, in their order
     float* sums = (float*)lds[0];

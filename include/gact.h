@@ -440,7 +440,7 @@ int gact_head_norm_rotate_backward(const gact_heads *h_parts, int n_parts, const
  *
  * Context.  With bits in {1, 2, 4, 8} the forward pass writes what gact_compress gives for x laid out contiguously with
  * the same group_size, bits and seed, byte for byte, and the backward pass uses codes * step + minimum (in
- * binary32, not rounded to x's type) for x.  m and r are not taken from these: the forward pass leaves them in mean and
+ * binary32, not rounded to x's type) for x in n.  m and r are not taken from these: the forward pass leaves them in mean and
  * rstd.  With GACT_BITS_UNCOMPRESSED nothing is compressed and the backward pass reads x.
  *
  *   forward    reads x; writes y, mean and rstd (batch * groups floats each; both NULL: not wanted, only with bits ==

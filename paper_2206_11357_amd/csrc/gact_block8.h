@@ -180,17 +180,25 @@ __device__ __forceinline__ uint64_t load_codes(const uint8_t* p) {
     return *(const uint64_t*)p;
 }
 
-// x of eight elements from their codes.
+// Eight codes as numbers.
 template <int BITS>
-__device__ __forceinline__ void decompress8(uint64_t codes, float mn, float step, float (&x)[8]) {
+__device__ __forceinline__ void codes_of(uint64_t codes, float (&q)[8]) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         // a nibble of every byte of a word, so that the bytes convert in place
         const uint32_t word = BITS == 8 && k >= 4 ? (uint32_t)(codes >> 32) : (uint32_t)codes;
-        const uint32_t q = BITS == 8 ? word >> (8 * (k & 3)) & 0xFFu
-                         : BITS == 4 ? ((k & 1 ? word >> 4 : word) & 0x0F0F0F0Fu) >> (8 * (k >> 1)) & 0xFFu
-                         : word >> (k * BITS) & ((1u << BITS) - 1u);
-        const float t = (float)q * step;
+        q[k] = (float)(BITS == 8 ? word >> (8 * (k & 3)) & 0xFFu
+                     : BITS == 4 ? ((k & 1 ? word >> 4 : word) & 0x0F0F0F0Fu) >> (8 * (k >> 1)) & 0xFFu
+                     : word >> (k * BITS) & ((1u << BITS) - 1u));
+    }
+}
+// x of eight elements from their codes.
+template <int BITS>
+__device__ __forceinline__ void decompress8(uint64_t codes, float mn, float step, float (&x)[8]) {
+    codes_of<BITS>(codes, x);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float t = x[k] * step;
         x[k] = t + mn;
     }
 }

@@ -72,7 +72,10 @@ inline void plan_group_norm(GnArgs* a) {
     const uint64_t want = kGnBlocks / ((uint64_t)a->B * a->slabs) ? kGnBlocks / ((uint64_t)a->B * a->slabs) : 1;
     const uint64_t most = gn_up(a->P, (uint64_t)a->rows * 8);
     const uint64_t chunks = want < most ? want : most;
+    // whole batches of the pixels that a thread takes at a time, if a chunk has several
+    const uint32_t batch = a->rows * 4;
     a->per_chunk = gn_up(a->P, chunks);
+    if (a->per_chunk > 2 * batch) a->per_chunk = gn_up(a->per_chunk, batch) * batch;
     a->chunks = gn_up(a->P, a->per_chunk);
     uint32_t g = a->C8, h = 64;
     while (h) { const uint32_t t = g % h; g = h; h = t; }            // greatest common divisor

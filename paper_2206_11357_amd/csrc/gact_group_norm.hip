@@ -296,6 +296,23 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnArgs a) {
 }
 
 // ------------------------------------------------------------------- gradients
+// n = (code step + minimum - m) r of a block of eight: where m and r are one, code (step r) + (minimum - m) r, an operation a
+// value instead of four.
+template <int BITS, bool UNI>
+__device__ __forceinline__ void gn_normal(uint64_t codes, float mn, float step, const OfGroups<UNI>& m, const OfGroups<UNI>& r,
+                                          float (&n)[8]) {
+    if constexpr (UNI) {
+        const float scale = step * r[0], shift = (mn - m[0]) * r[0];
+        float q[8];
+        codes_of<BITS>(codes, q);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) n[k] = __builtin_fmaf(q[k], scale, shift);
+    } else {
+        decompress8<BITS>(codes, mn, step, n);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) n[k] = (n[k] - m[k]) * r[k];
+    }
+}
 // dy and x of a block of eight: from its codes or as they are.
 template <int DT, int BITS>
 struct GnInput {
@@ -318,24 +335,30 @@ struct GnInput {
     __device__ __forceinline__ void take(const OfGroups<UNI>& m, const OfGroups<UNI>& r, const float (&w)[8], const float (&b)[8],
                                          float (&n)[8], float (&dz)[8]) const {
         widen8<DT>(dy, dz);
-        if constexpr (BITS != 0) decompress8<BITS>(codes, mn, step, n);
-        else widen8<DT>(x, n);
+        if constexpr (BITS != 0) {
+            gn_normal<BITS, UNI>(codes, mn, step, m, r, n);
+        } else {
+            widen8<DT>(x, n);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            n[k] = (n[k] - m[k]) * r[k];
-            if (SILU) dz[k] *= silu_slope<DT>(__builtin_fmaf(n[k], w[k], b[k]));
+            for (int k = 0; k < 8; ++k) n[k] = (n[k] - m[k]) * r[k];
         }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (SILU) dz[k] *= silu_slope<DT>(__builtin_fmaf(n[k], w[k], b[k]));
     }
 };
 
-// x of a block of eight in binary32.
-template <int DT, int BITS>
-__device__ __forceinline__ void gn_load_x(const GnArgs& a, uint32_t sample, uint32_t p, uint32_t c8, float (&x)[8]) {
+// n of a block of eight.
+template <int DT, int BITS, bool UNI>
+__device__ __forceinline__ void gn_load_n(const GnArgs& a, uint32_t sample, uint32_t p, uint32_t c8, const OfGroups<UNI>& m,
+                                          const OfGroups<UNI>& r, float (&n)[8]) {
     if constexpr (BITS != 0) {
         const uint32_t e = (sample * a.P + p) * a.C8 + c8;
-        decompress8<BITS>(load_codes<BITS>(a.packed + (uint64_t)e * BITS), a.gmin[e >> a.block_shift], a.gscale[e >> a.block_shift], x);
+        gn_normal<BITS, UNI>(load_codes<BITS>(a.packed + (uint64_t)e * BITS), a.gmin[e >> a.block_shift], a.gscale[e >> a.block_shift], m, r, n);
     } else {
-        widen8<DT>(load8<DT>((const uint8_t*)a.x.p, ((int64_t)sample * a.x.sample + (int64_t)p * a.x.pixel + (int64_t)c8 * 8) * kSize<DT>), x);
+        widen8<DT>(load8<DT>((const uint8_t*)a.x.p, ((int64_t)sample * a.x.sample + (int64_t)p * a.x.pixel + (int64_t)c8 * 8) * kSize<DT>), n);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) n[k] = (n[k] - m[k]) * r[k];
     }
 }
 
@@ -779,10 +802,9 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_backward_ker
         const uint32_t p = at.row + (uint32_t)i * at.rows;
         if (p >= a.P) break;
         float n[8];
-        gn_load_x<DT, BITS>(a, at.sample, p, at.c8, n);
+        gn_load_n<DT, BITS, UNI>(a, at.sample, p, at.c8, m, r, n);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            n[k] = (n[k] - m[k]) * r[k];
             dz[i][k] = r[k] * __builtin_fmaf(-n[k], m2[k % (UNI ? 1 : 8)], __builtin_fmaf(dz[i][k], w[k], -m1[k % (UNI ? 1 : 8)]));
         }
         store8<DT>((uint8_t*)a.dx.p, (out + (int64_t)p * a.dx.pixel) * kSize<DT>, dz[i]);

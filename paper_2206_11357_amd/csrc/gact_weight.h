@@ -10,13 +10,15 @@
 namespace gact {
 
 // A block's tile of dW, n x k, the tokens that it takes from memory at a time, and its threads.  Four wavefronts share a tile; where
-// there are eight, two teams of four take half of the tokens each, and their sums are added in shared memory: half as many
-// splits fill the GPU as with blocks of four.
+// there are more, each team of four takes its part of the tokens, and the teams' sums are added in shared memory.
+enum { kWeightLarge, kWeightSmall, kWeightLong, kWeightForms };
 struct WeightTile {
     int n, k, tokens, threads;
 };
 constexpr WeightTile weight_tile(int dtype, int which) {
-    return which == 0 ? WeightTile{256, 128, dtype == GACT_DT_F32 ? 32 : 64, 512} : WeightTile{64, 64, dtype == GACT_DT_F32 ? 16 : 32, 256};
+    const int team = dtype == GACT_DT_F32 ? 16 : 32;                // tokens of a team
+    return which == kWeightLarge ? WeightTile{256, 128, 2 * team, 512}
+         : which == kWeightSmall ? WeightTile{64, 64, team, 256} : WeightTile{64, 64, 4 * team, 1024};
 }
 
 struct WeightArgs {
@@ -65,14 +67,16 @@ struct WeightPlan {
 };
 inline WeightPlan plan_weight(uint64_t T, uint64_t N, uint64_t K, int dtype) {
     WeightPlan p{};
-    p.which = N > 128 && K > 64 && T * N * K >= (uint64_t)1 << 28 ? 0 : 1;
+    const uint64_t small = weight_up(N, 64) * (K ? weight_up(K, 64) : 1);
+    p.which = N > 128 && K > 64 && T * N * K >= (uint64_t)1 << 28 ? kWeightLarge : small >= 256 || T <= 64 ? kWeightSmall : kWeightLong;
     const WeightTile tile = weight_tile(dtype, p.which);
     p.tiles_n = (uint32_t)weight_up(N, (uint64_t)tile.n);
     p.tiles_k = K ? (uint32_t)weight_up(K, (uint64_t)tile.k) : 1;      // (K = 0: db alone)
     const uint64_t tiles = (uint64_t)p.tiles_n * p.tiles_k, chunks = weight_up(T, (uint64_t)tile.tokens);
-    const uint64_t fill = p.which == 0 ? 256 : 512;
+    const uint64_t fill = p.which == kWeightSmall ? 512 : 256;
     uint64_t splits = tiles >= fill ? 1 : fill / tiles;
-    const uint64_t most = chunks / 4 ? chunks / 4 : 1;
+    // a second launch costs as much as a few chunks
+    const uint64_t most = chunks <= 12 ? 1 : chunks / 4;
     if (splits > most) splits = most;
     p.chunks = (uint32_t)weight_up(chunks, splits);
     p.splits = p.chunks ? (uint32_t)weight_up(chunks, p.chunks) : 1;

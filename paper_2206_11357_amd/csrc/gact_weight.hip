@@ -147,7 +147,7 @@ struct Tiling {
 __device__ __forceinline__ uint64_t within(uint64_t bytes) { return bytes < 0x80000000ull ? bytes : 0x80000000ull; }
 
 template <int DT, int BITS, int WHICH, int MODE>
-__global__ __launch_bounds__(weight_tile(DT, WHICH).threads, 2) void weight_kernel(WeightArgs a) {
+__global__ __launch_bounds__(weight_tile(DT, WHICH).threads, weight_tile(DT, WHICH).threads == 1024 ? 4 : 2) void weight_kernel(WeightArgs a) {
     typedef Tiling<DT, WHICH> L;
     constexpr bool WHOLE = MODE != kOdd;
     constexpr int BN = L::BN, BK = L::BK, BT = L::BT, TN = L::TN, TK = L::TK;
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(weight_tile(DT, WHICH).threads, 2) void weight_kern
         fetch(c0);
         if (adds(c0)) add_db();
         place(lds[0]);
-        if constexpr (MODE == kEven && WHICH == 0) {
+        if constexpr (MODE == kEven && WHICH == kWeightLarge) {
             fetch(c0 + 1);
             __syncthreads();
             read_all(lds[0]);
@@ -441,14 +441,14 @@ __global__ __launch_bounds__(weight_tile(DT, WHICH).threads, 2) void weight_kern
         }
     }
 
-    // ---- the teams' sums: each team hands half of its products to the other through shared memory, a row of products at a time, and
-    // is left with the other half's sums
-    constexpr int kMine = TN / L::kTeams;                           // rows of products that a wavefront writes
+    // ---- the teams' sums, through shared memory.  Two teams: each hands half of its products to the other, a row of products at a
+    // time, and is left with the other half's sums; more: the first adds them all.
+    constexpr int kMine = L::kTeams == 2 ? TN / 2 : TN;             // rows of products that a wavefront writes
     const int first = L::kTeams == 2 ? team * kMine : 0;
+    float* room = (float*)lds[0] + (tid & 255u);
+    constexpr int kRow = TK * 16 * 256;
     if constexpr (L::kTeams == 2) {
-        static_assert(TN % 2 == 0 && 2 * TK * 16 * 256 * 4 <= 2 * L::kBuf, "room");
-        float* room = (float*)lds[0] + (tid & 255u);
-        constexpr int kHalf = TK * 16 * 256;
+        static_assert(TN % 2 == 0 && 2 * kRow * 4 <= 2 * L::kBuf, "room");
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             __syncthreads();
@@ -457,7 +457,7 @@ __global__ __launch_bounds__(weight_tile(DT, WHICH).threads, 2) void weight_kern
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     if (team == 0) room[(j * 16 + r) * 256] = acc[kMine + i][j][r];
-                    else room[kHalf + (j * 16 + r) * 256] = acc[i][j][r];
+                    else room[kRow + (j * 16 + r) * 256] = acc[i][j][r];
                 }
             __syncthreads();
 #pragma unroll
@@ -465,9 +465,26 @@ __global__ __launch_bounds__(weight_tile(DT, WHICH).threads, 2) void weight_kern
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     // the first team's first, for both
-                    if (team == 0) acc[i][j][r] = acc[i][j][r] + room[kHalf + (j * 16 + r) * 256];
+                    if (team == 0) acc[i][j][r] = acc[i][j][r] + room[kRow + (j * 16 + r) * 256];
                     else acc[i][j][r] = room[(j * 16 + r) * 256] + acc[kMine + i][j][r];
                 }
+        }
+    } else if constexpr (L::kTeams > 2) {
+        static_assert(TN == 1 && (L::kTeams - 1) * kRow * 4 <= 2 * L::kBuf, "room");
+        if (team > 0) {
+#pragma unroll
+            for (int j = 0; j < TK; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) room[(team - 1) * kRow + (j * 16 + r) * 256] = acc[0][j][r];
+        }
+        __syncthreads();
+        if (team == 0) {
+#pragma unroll
+            for (int t = 0; t < L::kTeams - 1; ++t)
+#pragma unroll
+                for (int j = 0; j < TK; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[0][j][r] += room[t * kRow + (j * 16 + r) * 256];
         }
     }
 
@@ -496,11 +513,13 @@ __global__ __launch_bounds__(weight_tile(DT, WHICH).threads, 2) void weight_kern
                 }
             }
     };
-    if (!whole) put(a.partial + (size_t)split * a.N * a.K);
-    else if (a.w_f32) put((float*)a.dw);
-    else put((uint16_t*)a.dw);
+    if (L::kTeams <= 2 || team == 0) {
+        if (!whole) put(a.partial + (size_t)split * a.N * a.K);
+        else if (a.w_f32) put((float*)a.dw);
+        else put((uint16_t*)a.dw);
+    }
 
-    if (L::kTeams == 2) __syncthreads();
+    if (L::kTeams > 1) __syncthreads();
     if (!with_db) return;
     // db of the tile's rows: over the threads of a column, in their order
     float* sums = (float*)lds[0];
@@ -576,8 +595,11 @@ static void launch_tile(const WeightArgs& a, hipStream_t s) {
 }
 template <int DT, int BITS>
 static void launch_bits(const WeightArgs& a, int which, hipStream_t s) {
-    if (which == 0) launch_tile<DT, BITS, 0>(a, s);
-    else launch_tile<DT, BITS, 1>(a, s);
+    switch (which) {
+        case kWeightLarge: launch_tile<DT, BITS, kWeightLarge>(a, s); break;
+        case kWeightSmall: launch_tile<DT, BITS, kWeightSmall>(a, s); break;
+        default: launch_tile<DT, BITS, kWeightLong>(a, s); break;
+    }
 }
 template <int DT>
 static void launch_type(const WeightArgs& a, int which, int bits, hipStream_t s) {

@@ -182,3 +182,12 @@ def test_captured_and_on_another_stream():
     other = gact.gact_linear_weight_grad(dy, *context, K, 64, 4, w_dtype=torch.float32, bias=True, stream=side)
     side.synchronize()
     assert torch.equal(other[0], dw) and torch.equal(other[1], db)
+
+
+# every form at its borders: tokens of one block's teams, of few and many chunks, of splits
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [63, 64, 65, 127, 129, 767, 769, 1535, 1537, 6000])
+@pytest.mark.parametrize("N,K", [(20, 24), (130, 70)])
+def test_forms_of_small_tiles(N, K, T, dtype):
+    check(T, N, K, 32, 4, DTYPES[dtype])
+    check(T, N + 1, K + 1, 32, 1, DTYPES[dtype], DTYPES["bf16"], bias=False)

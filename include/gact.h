@@ -513,8 +513,9 @@ int gact_group_norm_backward(const gact_channel_norm *h_norm, void *d_workspace,
  *   db           out  [out_features] of w_dtype, or NULL: not wanted.  Outputs overlap nothing.
  *   d_workspace  device scratch, >= gact_linear_weight_grad_workspace_bytes(...) bytes of the same sizes (which may be 0),
  *                16-byte aligned, in use until the enqueued kernels have run; calls that share one must not overlap in time.
- * tokens == 0 writes zeros; out_features == 0 or in_features == 0 is GACT_OK and writes nothing but db.  Each size must be
- * below 2^31, tokens * in_features below 2^35 and out_features * in_features below 2^38.  An infinity or NaN
+ * tokens == 0 writes zeros; out_features == 0 or in_features == 0 is GACT_OK and writes nothing but db.  tokens and
+ * out_features must be below 2^31, in_features below 2^22, tokens * in_features below 2^34, out_features * in_features
+ * below 2^38.  An infinity or NaN
  * in a row of dy reaches that row's columns of dW (rows of x^ times it), in a group's minimum or step the elements of
  * that group.  Can be captured into a HIP graph.
  */

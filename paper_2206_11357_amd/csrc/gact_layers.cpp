@@ -20,8 +20,8 @@ size_t size_of(int dt) { return dt == GACT_F32 ? 4 : 2; }
 constexpr int64_t kMost = 0x7FFFFFFFll;
 
 bool weight_sizes_ok(int64_t T, int64_t N, int64_t K) {
-    if (T < 0 || N < 0 || K < 0 || T > kMost || N > kMost || K > kMost) return false;
-    return (uint64_t)T * (uint64_t)K < 1ull << 35 && (uint64_t)N * (uint64_t)K < 1ull << 38;
+    if (T < 0 || N < 0 || K < 0 || T > kMost || N > kMost || K >= 1 << 22) return false;
+    return (uint64_t)T * (uint64_t)K < 1ull << 34 && (uint64_t)N * (uint64_t)K < 1ull << 38;
 }
 
 // -------------------------------------------------------------------- group norm
@@ -199,7 +199,7 @@ int gact_linear_weight_grad(const gact_linear_grad* h_grad, void* d_workspace, s
     if (T * K > 0 && (!h.packed || !h.gmin || !h.gscale || !aligned(h.packed, 16) || !aligned(h.gmin, 4) || !aligned(h.gscale, 4)))
         return GACT_E_ARG;
     const gact::WeightPlan plan = gact::plan_weight(T, N, K, h.dtype);
-    const gact::WeightTile tile = gact::weight_tile(h.dtype, plan.which);
+    const gact::WeightTile tile = gact::weight_tile(h.dtype, plan.form);
     const uint64_t blocks = (uint64_t)plan.tiles_n * plan.tiles_k * plan.splits;
     if (!gact::launchable(blocks, (uint32_t)tile.threads)) return GACT_E_ARG;
     const size_t need = gact::weight_workspace_bytes(plan, N, K);
@@ -234,7 +234,7 @@ int gact_linear_weight_grad(const gact_linear_grad* h_grad, void* d_workspace, s
     a.code_chunk = BT * a.K / 8 * (uint32_t)h.bits;
     a.group_chunk = BT * a.K / a.group * 4;
     a.w_f32 = h.w_dtype == GACT_F32;
-    return gact_launch_weight(&a, plan.which, h.dtype, h.bits, stream) == 0 ? GACT_OK : GACT_E_HIP;
+    return gact_launch_weight(&a, plan.form, h.dtype, h.bits, stream) == 0 ? GACT_OK : GACT_E_HIP;
 }
 
 }  // extern "C"

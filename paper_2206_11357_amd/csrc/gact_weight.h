@@ -72,9 +72,14 @@ struct WeightPlan {
 inline WeightPlan plan_weight(uint64_t T, uint64_t N, uint64_t K, int dtype) {
     WeightPlan p{};
     const uint64_t small = weight_up(N, 64) * (K ? weight_up(K, 64) : 1);
+    // Us, large | small | long tiles, 4 bits, by tokens x out x in features:
+    //   bf16   1024 x 1024 x 1024 25.3 | 16.0 | 8.8    4096 x 1024 x 1024 32.7 | 28.6 | 19.9    8192 x 1024 x 1024 36.6 | 45.5 | 35.9
+    //          512 x 4096 x 1024 18.7 | 12.9 | 22.5    2048 x 4096 x 1024 39.8 | 35.4 | 43.6    12608 x 1024 x 1024 44.6 | 65.2 | 52.9
+    //   fp32   1024 x 1024 x 1024 50.2 | 32.8 | 22.8   4096 x 1024 x 1024 86.5 | 96.0 | 76.1    8192 x 1024 x 1024 142 | 181 | 147
+    //          512 x 4096 x 1024 58.2 | 42.7 | 50.8    50000 x 1000 x 100 119 | 166 | 140       128 x 4096 x 1024 27.2 | 15.7 | 24.4
     p.form = N <= 32 ? kWeightWide : K <= 32 ? kWeightTall
-           : N > 128 && K > 64 && T * N * K >= (uint64_t)1 << 28 ? kWeightLarge
-           : small >= 256 || T <= 64 ? kWeightSmall : kWeightLong;
+           : N > 128 && K > 64 && T * N * K >= 9ull << 29 ? kWeightLarge
+           : small > 256 || T <= 64 ? kWeightSmall : kWeightLong;
     const WeightTile tile = weight_tile(dtype, p.form);
     p.tiles_n = (uint32_t)weight_up(N, (uint64_t)tile.n);
     p.tiles_k = K ? (uint32_t)weight_up(K, (uint64_t)tile.k) : 1;      // (K = 0: db alone)

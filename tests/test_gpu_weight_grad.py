@@ -191,3 +191,24 @@ def test_captured_and_on_another_stream():
 def test_forms_of_small_tiles(N, K, T, dtype):
     check(T, N, K, 32, 4, DTYPES[dtype])
     check(T, N + 1, K + 1, 32, 1, DTYPES[dtype], DTYPES["bf16"], bias=False)
+
+
+def on_gpu(dy, context, K, G, bits, dw, db):
+    """close() for sizes whose reference a CPU takes long for: products of the GPU's own in binary64."""
+    T = dy.shape[0]
+    x, d = gact.gact_decompress(*context, T * K, G, bits, dtype=dy.dtype).view(T, K).double(), dy.double()
+    close(dw, (d.t() @ x).cpu(), (d.abs().t() @ x.abs()).cpu(), T)
+    if db is not None:
+        close(db, d.sum(0).cpu(), d.abs().sum(0).cpu(), T)
+
+
+# the form of the largest products: whole tiles and edges, one split and several, every kind of address and group
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,K,G,bits,wide", [(19000, 512, 512, 256, 4, 0), (19001, 510, 520, 96, 2, 0), (33333, 300, 501, 64, 1, 0),
+                                               (40009, 257, 490, 1024, 8, 3), (700, 4100, 1704, 128, 4, 0), (9001, 1031, 648, 32, 8, 1)])
+def test_largest_products(T, N, K, G, bits, wide, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    x = (torch.randn(T, K, generator=gen, device="cuda") + 0.3).to(DTYPES[dtype])
+    dy = (torch.randn(T, N + wide, generator=gen, device="cuda") * 0.1).to(DTYPES[dtype])[:, wide:]
+    context = gact.gact_compress(x, G, bits, 7)
+    on_gpu(dy, context, K, G, bits, *gact.gact_linear_weight_grad(dy, *context, K, G, bits, w_dtype=torch.float32, bias=True))

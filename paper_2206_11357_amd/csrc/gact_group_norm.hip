@@ -526,10 +526,10 @@ __global__ __launch_bounds__(kGnThreads) void gn_dx_kernel(GnArgs a) {
 // ------------------------------------------------------- maps held in registers
 // A lane's place among the units that a workgroup holds.
 struct WholePlace {
-    uint32_t sample, col, row, rows, c8, unit;
+    uint32_t sample, col, row, rows, c8, unit, threads;
     int      wave, lane;
     bool     holds;
-    __device__ __forceinline__ WholePlace(const GnArgs& a, uint32_t threads) {
+    __device__ __forceinline__ WholePlace(const GnArgs& a, uint32_t n_threads) : threads(n_threads) {
         // slabs of a cache line go to one XCD (every eighth workgroup): neighbours in this order
         const uint32_t per = a.norm_blocks >> 3, rest = a.norm_blocks & 7u, xcd = blockIdx.x & 7u;
         const uint32_t block = xcd * per + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
@@ -568,15 +568,40 @@ __device__ __forceinline__ void over_rows(const GnArgs& a, const WholePlace& at,
         v[k] = s;
     }
 }
-// Sums of the groups that parts of a column are, from those of its channels.
-__device__ __forceinline__ void within_column(const GnArgs& a, float (&v)[8]) {
-    if (a.D >= 2) {
+// Room for the sums of groups that are no whole columns: of the slab's channels, and of its groups.
+template <int N>
+struct GroupRoom {
+    float of_channel[N][64 * 8], of_group[N][64 * 8];
+};
+template <>
+struct GroupRoom<0> {};
+// Sums of the groups of the lane's eight channels, from sums of the channels, which the lanes of row 0 hold: for each of N values.
+template <int N>
+__device__ __forceinline__ void over_groups(const GnArgs& a, const WholePlace& at, GroupRoom<N>& room, float (&v)[N][8]) {
+    if (at.row == 0) {
 #pragma unroll
-        for (int k = 0; k < 8; k += 2) v[k] = v[k + 1] = v[k] + v[k + 1];
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) room.of_channel[i][at.col * 8 + k] = v[i][k];
     }
-    if (a.D >= 4) {
+    __syncthreads();
+    const uint32_t each = a.unit_cols * 8 / a.D;                        // groups of a unit
+    for (uint32_t t = threadIdx.x; t < each << a.slab_shift; t += at.threads) {
+        const uint32_t unit = t / each, first = (unit << a.unit_shift) * 8 + (t - unit * each) * a.D;
 #pragma unroll
-        for (int k = 0; k < 8; k += 4) v[k] = v[k + 1] = v[k + 2] = v[k + 3] = v[k] + v[k + 2];
+        for (int i = 0; i < N; ++i) {
+            float s = 0.0f;
+            for (uint32_t d = 0; d < a.D; ++d) s += room.of_channel[i][first + d];
+            room.of_group[i][t] = s;
+        }
+    }
+    __syncthreads();
+    const uint32_t unit = at.col >> a.unit_shift, cu = at.col & ((1u << a.unit_shift) - 1u);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t t = unit * each + divided(cu * 8 + (uint32_t)k, a.by_d);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i][k] = room.of_group[i][t < 512u ? t : 511u];        // (lanes that hold nothing)
     }
 }
 
@@ -602,6 +627,7 @@ template <int DT, bool UNI, bool SILU, int WHICH>
 __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_kernel(GnArgs a, int bits) {
     constexpr int NT = (int)kGnWhole[WHICH].threads, R = (int)kGnWhole[WHICH].blocks, N = UNI ? 1 : 8;
     __shared__ float lds[2][NT / 64][64 * N];
+    __shared__ GroupRoom<UNI ? 0 : 1> room;
     if (blockIdx.x >= a.norm_blocks) {
         switch (bits) {
             case 1: gn_compress_blocks<DT, 1, NT>(a); break;
@@ -635,7 +661,7 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_kernel(GnArg
             for (int k = 0; k < 8; ++k) m[k % N] += v[k];
     }
     over_rows<NT, N, UNI>(a, at, lds[0], m);
-    if constexpr (!UNI) within_column(a, m);
+    if constexpr (!UNI) over_groups<1>(a, at, room, (float (&)[1][8])m);
 #pragma unroll
     for (int k = 0; k < N; ++k) m[k] *= inv;
 #pragma unroll
@@ -657,7 +683,7 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_kernel(GnArg
 #pragma unroll
         for (int k = 0; k < N; ++k) r[k] = 0.0f;
     over_rows<NT, N, UNI>(a, at, lds[1], r);
-    if constexpr (!UNI) within_column(a, r);
+    if constexpr (!UNI) over_groups<1>(a, at, room, (float (&)[1][8])r);
 #pragma unroll
     for (int k = 0; k < N; ++k) r[k] = 1.0f / __builtin_sqrtf(__builtin_fmaf(r[k], inv, a.eps));
     if (!at.holds) return;
@@ -671,7 +697,7 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_kernel(GnArg
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (k % a.D == 0) {
+                if ((c + (uint32_t)k) % a.D == 0) {
                     a.mean[first + (c + (uint32_t)k) / a.D] = m[k % N];
                     a.rstd[first + (c + (uint32_t)k) / a.D] = r[k % N];
                 }
@@ -702,6 +728,7 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_backward_ker
     __shared__ float lds[NT / 64][64 * 16];
     __shared__ float total[64 * 16];
     __shared__ float of_column[64][2];
+    __shared__ GroupRoom<UNI ? 0 : 2> room;
     const WholePlace at(a, NT);
     const uint32_t c = at.c8 * 8u;
     const int cols = 1 << a.col_shift;
@@ -769,18 +796,17 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_backward_ker
         m1[0] *= inv;
         m2[0] *= inv;
     } else {
-        if (!at.holds) return;
+        float g[2][8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            m1[k % (UNI ? 1 : 8)] = w[k] * total[at.col * 16 + k];
-            m2[k % (UNI ? 1 : 8)] = w[k] * total[at.col * 16 + 8 + k];
+            g[0][k] = at.holds ? w[k] * total[at.col * 16 + k] : 0.0f;
+            g[1][k] = at.holds ? w[k] * total[at.col * 16 + 8 + k] : 0.0f;
         }
-        within_column(a, m1);
-        within_column(a, m2);
+        over_groups<2>(a, at, room, g);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            m1[k % (UNI ? 1 : 8)] *= inv;
-            m2[k % (UNI ? 1 : 8)] *= inv;
+            m1[k % (UNI ? 1 : 8)] = g[0][k] * inv;
+            m2[k % (UNI ? 1 : 8)] = g[1][k] * inv;
         }
     }
     if (!at.holds) return;
@@ -868,7 +894,7 @@ static void gn_launch_sized(bool backward, const GnArgs& a, int whole, hipStream
     if (whole == 0) gn_launch<DT, BITS, UNI, SILU>(backward, a, s);
     else if (whole == 1) gn_launch_whole<DT, BITS, UNI, SILU, 0>(backward, a, s);
     else if (whole == 2) gn_launch_whole<DT, BITS, UNI, SILU, 1>(backward, a, s);
-    else gn_launch_whole<DT, BITS, UNI, SILU, 2>(backward, a, s);
+    else if constexpr (UNI) gn_launch_whole<DT, BITS, UNI, SILU, 2>(backward, a, s);
 }
 template <int DT, int BITS>
 static void gn_launch_form(bool backward, const GnArgs& a, int act, int whole, hipStream_t s) {

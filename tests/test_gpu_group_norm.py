@@ -289,3 +289,12 @@ def test_gradients_against_differences():
                 moved.view(-1)[i] += sign * h
                 vals.append(loss(*(moved if j == which else t for j, t in enumerate(args))))
             assert abs((vals[0] - vals[1]) / (2 * h) - float(grad.view(-1)[i])) <= tol
+
+
+# groups that are no whole columns of eight channels, in maps that a workgroup holds and in larger ones, part of a slab and several
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,P,C,H", [(3, 20, 120, 4), (2, 61, 72, 2), (2, 500, 72, 4), (1, 130, 504, 8), (2, 9, 1008, 16), (1, 40, 56, 1),
+                                     (2, 33, 80, 5), (3, 100, 24, 12), (2, 17, 176, 16), (1, 700, 144, 8)])
+def test_groups_of_any_size(B, P, C, H, dtype):
+    check_step(B, P, C, H, 4, 64, "silu", DTYPES[dtype])
+    check_step(B, P, C, H, RAW, 0, "none", DTYPES[dtype], None if H % 2 else torch.float32, wide=8)

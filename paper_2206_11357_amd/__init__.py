@@ -1260,18 +1260,22 @@ def _norm_workspace(x: torch.Tensor, need: int, workspace: Optional[torch.Tensor
     return workspace
 
 
-def _norm_forward_record(x, strides, groups, w, b, eps, act, context, out, device: int) -> bytes:
-    """gact_channel_norm of a forward call into `out`; strides: _map_strides(x)."""
+def _norm_forward_record(x, strides, groups, w, b, eps, act, context, out, device: int):
+    """(out, gact_channel_norm of a forward call into it); strides: _map_strides(x)."""
     B, P, C, sample, pixel = strides
-    ys, yp = sample, pixel
-    if out is not x:
+    if out is None:
+        out = x.new_empty(x.shape)
+        ys, yp = P * C, C
+    elif out is not x:
         _check_like(out, x)
         _, _, _, ys, yp = _map_strides(out)
+    else:
+        ys, yp = sample, pixel
     a, bits, G, seed = (0, 0, 0, 0, 0), GACT_BITS_UNCOMPRESSED, 0, 0
     if context is not None:
         _norm_context(context, x, device, groups)
         a, bits, G, seed = context.addresses(), context.bits, context.group_size, context.seed
-    return _CHANNEL_NORM.pack(
+    return out, _CHANNEL_NORM.pack(
         x.data_ptr(), out.data_ptr(), 0, 0, 0 if w is None else w.data_ptr(), 0 if b is None else b.data_ptr(), 0, 0, *a, sample, pixel,
         ys, yp, 0, 0, 0, 0, B, P, seed, C, groups, _activation(act), dtype_code(x.dtype), _channel_weights(w, b, C), bits, G, eps)
 
@@ -1286,13 +1290,12 @@ def gact_group_norm(x: torch.Tensor, groups: int, w: Optional[torch.Tensor] = No
     device = _same_device(x, out, w, b, workspace)
     need = gact_group_norm_workspace_bytes(*strides[:3], groups, x.dtype)
     if stream is None:
-        out = x.new_empty(x.shape) if out is None else out
         workspace = _norm_workspace(x, need, workspace)
+        out, record = _norm_forward_record(x, strides, groups, w, b, eps, act, context, out, device)
     else:
         with _allocating_for(stream, device):
-            out = x.new_empty(x.shape) if out is None else out
             workspace = _norm_workspace(x, need, workspace)
-    record = _norm_forward_record(x, strides, groups, w, b, eps, act, context, out, device)
+            out, record = _norm_forward_record(x, strides, groups, w, b, eps, act, context, out, device)
     if workspace is None:
         _enqueue(lib.gact_group_norm, "gact_group_norm", device, stream, record, None, 0)
     else:
@@ -1306,7 +1309,7 @@ def prepare_group_norm(x: torch.Tensor, groups: int, w=None, b=None, eps: float 
     strides = _map_strides(x)
     device = _same_device(x, out, w, b, workspace)
     workspace = _norm_workspace(x, gact_group_norm_workspace_bytes(*strides[:3], groups, x.dtype), workspace)
-    record = _norm_forward_record(x, strides, groups, w, b, eps, act, context, out, device)
+    _, record = _norm_forward_record(x, strides, groups, w, b, eps, act, context, out, device)
     vp = ctypes.c_void_p
     keep = ctypes.create_string_buffer(record, len(record))
     args = (vp(ctypes.addressof(keep)), vp(workspace.data_ptr() if workspace is not None else 0),
@@ -1336,7 +1339,11 @@ def gact_group_norm_backward(dy: torch.Tensor, groups: int, w: Optional[torch.Te
     else:
         with _allocating_for(stream, device):
             dx, dw, db, workspace = _norm_gradients(dy, w, b, out, weight_grads, workspace, need)
-    _check_like(dx, dy)
+    if out is not None:
+        _check_like(dx, dy)
+        _, _, _, ds, dp = _map_strides(dx)
+    else:
+        ds, dp = P * C, C
     a_x = xs = xp = 0
     if context.bits == GACT_BITS_UNCOMPRESSED:
         if x is None:
@@ -1344,7 +1351,6 @@ def gact_group_norm_backward(dy: torch.Tensor, groups: int, w: Optional[torch.Te
         _check_like(x, dy)
         a_x = x.data_ptr()
         _, _, _, xs, xp = _map_strides(x)
-    _, _, _, ds, dp = _map_strides(dx)
     record = _CHANNEL_NORM.pack(
         a_x, 0, dy.data_ptr(), dx.data_ptr(), 0 if w is None else w.data_ptr(), 0 if b is None else b.data_ptr(),
         0 if dw is None else dw.data_ptr(), 0 if db is None else db.data_ptr(), *context.addresses(), xs, xp, 0, 0, sample, pixel,

@@ -32,10 +32,11 @@ struct GnArgs {
     float*      gscale;
     float*      partial;                // of each sample, chunk and channel (or column): two floats
     float*      sums;                   // backward: of each sample and channel: sum of dz, sum of dz n
-    float*      means;                  // backward: of each sample and group: mean g, mean g n
+    float*      means;                  // backward: of each sample, group and slice of 64 channels: its part of mean g, mean g n
     uint32_t    B, P, C, H, D;
+    uint32_t    slices;                 // of a group
     uint32_t    C8, cols, rows, slabs;  // columns of a workgroup; cols * slabs >= C8
-    uint32_t    chunks, per_chunk;      // pixels of a chunk
+    uint32_t    chunks, batch, batches; // pixels of a batch; a sample's
     uint32_t    blocks8;                // B P C / 8
     uint32_t    period, passes;         // a pass is 64 blocks; lanes come back to their channels after `period` passes
     uint32_t    stride_passes;
@@ -56,10 +57,16 @@ inline uint32_t gn_up(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / 
 // Whether a block of eight channels lies in one group of the norm.
 inline bool gn_uniform(const GnArgs& a) { return a.D % 8 == 0; }
 
-constexpr uint32_t kGnBlocks = 2048;    // of a launch that adds over pixels, about
+// Of a launch that adds over pixels, about.  More leave more sums to add up behind them.  Us, sums and their addition, 2048 | 1024 | 768:
+// 9 x 1023 x 1136 bf16 in 8 groups, 8 bits 28.7 | 26.0 | 27.3, statistics 23.3 | 19.9 | 15.9; 1 x 262144 x 128 42.4 | 36.3 | 38.6.
+constexpr uint32_t kGnBlocks = 1024;
+// Pixels that a thread of these takes at a time; a workgroup's are a batch.  Chunks take batches in turn, so that what all workgroups read
+// at a time is one region of a sample.
+constexpr uint32_t gn_batch(int dtype) { return dtype == GACT_DT_F32 ? 4 : 8; }
 
-inline void plan_group_norm(GnArgs* a) {
+inline void plan_group_norm(GnArgs* a, int dtype) {
     a->C8 = a->C / 8;
+    a->slices = gn_up(a->D, 64);
     a->slabs = gn_up(a->C8, kGnThreads);
     a->cols = gn_up(a->C8, a->slabs);
     a->rows = (uint32_t)kGnThreads / a->cols;
@@ -68,15 +75,10 @@ inline void plan_group_norm(GnArgs* a) {
     a->by_d = divisor(a->D);
     a->by_cols = divisor(a->cols);
     a->blocks8 = a->B * a->P * a->C8;
-    // chunks of eight pixels a thread at least
     const uint64_t want = kGnBlocks / ((uint64_t)a->B * a->slabs) ? kGnBlocks / ((uint64_t)a->B * a->slabs) : 1;
-    const uint64_t most = gn_up(a->P, (uint64_t)a->rows * 8);
-    const uint64_t chunks = want < most ? want : most;
-    // whole batches of the pixels that a thread takes at a time, if a chunk has several
-    const uint32_t batch = a->rows * 4;
-    a->per_chunk = gn_up(a->P, chunks);
-    if (a->per_chunk > 2 * batch) a->per_chunk = gn_up(a->per_chunk, batch) * batch;
-    a->chunks = gn_up(a->P, a->per_chunk);
+    a->batch = a->rows * gn_batch(dtype);
+    a->batches = gn_up(a->P, a->batch);
+    a->chunks = want < a->batches ? (uint32_t)want : a->batches;
     uint32_t g = a->C8, h = 64;
     while (h) { const uint32_t t = g % h; g = h; h = t; }            // greatest common divisor
     a->period = a->C8 / g;
@@ -108,7 +110,7 @@ inline int plan_whole(GnArgs* a, int dtype) {
     while ((cols << shift) * 8 * size < 64 && (1u << shift) < a->units && a->unit_shift + shift < 6) ++shift;
     const auto fits = [&](const GnWhole& w) { return (uint64_t)a->P << (a->unit_shift + shift) <= (uint64_t)w.threads * w.blocks; };
     // (Groups that are no whole columns take more registers than the largest has: 16 x 500 x 72 bf16 in 4 groups, 4 bits, 18.5 us
-    // forward, 20.3 backward; in passes over memory 15 and 16.)
+    // forward, 24.1 backward; in passes over memory 15.3 and 20.4.)
     const int most = g == 8 ? kGnWholes : kGnWholes - 1;
     while (!fits(kGnWhole[most - 1]) && shift > 0) --shift;
     if (!fits(kGnWhole[most - 1])) return 0;
@@ -131,7 +133,7 @@ inline size_t gn_forward_bytes(const GnArgs& a, int whole) {
 }
 inline size_t gn_backward_bytes(const GnArgs& a, int whole) {
     if (whole) return a.B > 1 ? gn_sums_bytes(a) : 0;
-    return gn_partial_bytes(a) + gn_sums_bytes(a) + gn_align((size_t)a.B * a.H * 2 * sizeof(float));
+    return gn_partial_bytes(a) + gn_sums_bytes(a) + gn_align((size_t)a.B * a.H * a.slices * 2 * sizeof(float));
 }
 
 }  // namespace gact

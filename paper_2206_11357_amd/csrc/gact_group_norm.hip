@@ -67,19 +67,26 @@ struct OfGroups {
 #pragma unroll
         for (int k = 0; k < N; ++k) v[k] = p[(size_t)divided(c + (uint32_t)k, a.by_d) * step];
     }
+    // the same of sums in a.slices parts, which follow each other, two floats apart
+    __device__ __forceinline__ void add(const GnArgs& a, const float* p, uint32_t c) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float* q = p + (size_t)divided(c + (uint32_t)k, a.by_d) * a.slices * 2;
+            v[k] = q[0];
+            for (uint32_t s = 1; s < a.slices; ++s) v[k] += q[2 * s];
+        }
+    }
     __device__ __forceinline__ float operator[](int k) const { return v[UNI ? 0 : k]; }
 };
 // A workgroup's place in a pass over pixels.
 struct Column {
-    uint32_t sample, chunk, p0, p1, c8, row;
+    uint32_t sample, chunk, c8, row;
     bool     holds;
     __device__ __forceinline__ Column(const GnArgs& a, uint32_t block) {
         const uint32_t slab = block % a.slabs;
         block /= a.slabs;
         sample = block / a.chunks;
         chunk = block - sample * a.chunks;
-        p0 = chunk * a.per_chunk;
-        p1 = p0 + a.per_chunk < a.P ? p0 + a.per_chunk : a.P;
         row = divided(threadIdx.x, a.by_cols);
         const uint32_t col = threadIdx.x - row * a.cols;
         c8 = slab * a.cols + col;
@@ -108,21 +115,23 @@ struct Moments {
 };
 template <int DT, bool UNI>
 __global__ __launch_bounds__(kGnThreads) void gn_stats_kernel(GnArgs a) {
-    constexpr int N = UNI ? 1 : 8, U = DT == GACT_DT_F32 ? 4 : 8;
+    constexpr int N = UNI ? 1 : 8, U = (int)gn_batch(DT);
     __shared__ float lds[kGnThreads][2 * N + 1];
     const Column at(a, blockIdx.x);
     Moments<UNI> s = {};
     const uint8_t* x = (const uint8_t*)a.x.p;
     const int64_t first = (int64_t)at.sample * a.x.sample + (int64_t)at.c8 * 8;
-    for (uint32_t p = at.p0 + at.row; at.holds && p < at.p1; p += U * a.rows) {
+    for (uint32_t batch = at.chunk; at.holds && batch < a.batches; batch += a.chunks) {
+        const uint32_t p = batch * a.batch + at.row;
+        if (p >= a.P) break;
         Raw<DT> raw[U];
         float on[U], count = 0.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint32_t q = p + (uint32_t)u * a.rows;
-            on[u] = q < at.p1 ? 1.0f : 0.0f;
+            on[u] = q < a.P ? 1.0f : 0.0f;
             count += on[u];
-            raw[u] = load8<DT>(x, (first + (int64_t)(q < at.p1 ? q : p) * a.x.pixel) * kSize<DT>);
+            raw[u] = load8<DT>(x, (first + (int64_t)(q < a.P ? q : p) * a.x.pixel) * kSize<DT>);
         }
         float mean[N], m2[N];
 #pragma unroll
@@ -208,7 +217,12 @@ __global__ __launch_bounds__(kGnThreads) void gn_finish_kernel(GnArgs a) {
     const uint32_t i = blockIdx.x, sample = i / a.H, h = i - sample * a.H;
     const uint32_t each = UNI ? a.D / 8 : a.D, row = UNI ? a.C8 : a.C, items = each * a.chunks;
     const float* p = a.partial + ((size_t)sample * a.chunks * row + (size_t)h * each) * 2;
-    const double per = UNI ? 8.0 : 1.0, last = per * (a.P - (a.chunks - 1) * a.per_chunk), all = per * a.per_chunk;
+    // elements of a chunk's column: whole batches, but for the sample's last
+    const uint32_t last = (a.batches - 1) % a.chunks, missing = a.batches * a.batch - a.P;
+    const auto elements = [&](uint32_t chunk) {
+        const uint32_t batches = (a.batches - chunk + a.chunks - 1) / a.chunks;
+        return (UNI ? 8.0 : 1.0) * (double)(batches * a.batch - (chunk == last ? missing : 0));
+    };
     // distances from the first part's mean, so that their squares cancel nothing
     const double from = (double)p[0], whole = (double)a.P * a.D;
     double off = 0.0, m2 = 0.0;
@@ -216,7 +230,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_finish_kernel(GnArgs a) {
     for (uint32_t k = threadIdx.x; k < items; k += kGnThreads) {
         const uint32_t chunk = k / each;
         const hf2 v = *(const hf2*)(p + ((size_t)chunk * row + (k - chunk * each)) * 2);
-        const double n = chunk + 1 == a.chunks ? last : all, d = (double)v.x - from;
+        const double n = elements(chunk), d = (double)v.x - from;
         off += n * d;
         m2 += (double)v.y + n * d * d;
     }
@@ -362,6 +376,28 @@ __device__ __forceinline__ void gn_load_n(const GnArgs& a, uint32_t sample, uint
     }
 }
 
+// A thread's pixels, U at a time.
+template <int DT, int U>
+struct GnPixels {
+    static constexpr uint32_t kTurns = gn_batch(DT) / U;
+    uint32_t batch, turn, p;
+    __device__ __forceinline__ GnPixels(const GnArgs& a, const Column& at) : batch(at.chunk), turn(0), p(at.chunk * a.batch + at.row) {}
+    __device__ __forceinline__ bool more(const GnArgs& a) const { return batch < a.batches && p < a.P; }
+    __device__ __forceinline__ void next(const GnArgs& a, const Column& at) {
+        if (++turn == kTurns) {
+            turn = 0;
+            batch += a.chunks;
+            p = batch * a.batch + at.row;
+        } else {
+            p += U * a.rows;
+            // the sample's last batch ends here
+            if (p >= a.P) batch = a.batches;
+        }
+    }
+    __device__ __forceinline__ bool holds(const GnArgs& a, int u) const { return p + (uint32_t)u * a.rows < a.P; }
+    __device__ __forceinline__ uint32_t within(const GnArgs& a, int u) const { return holds(a, u) ? p + (uint32_t)u * a.rows : p; }
+};
+
 template <int DT, int BITS, bool UNI, bool SILU>
 __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnArgs a) {
     constexpr int U = 2;
@@ -378,16 +414,13 @@ __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnArgs a) {
         OfGroups<UNI> m, r;
         m.load(a, a.mean + (size_t)at.sample * a.H, 1, c);
         r.load(a, a.rstd + (size_t)at.sample * a.H, 1, c);
-        for (uint32_t p = at.p0 + at.row; p < at.p1; p += U * a.rows) {
+        for (GnPixels<DT, U> px(a, at); px.more(a); px.next(a, at)) {
             GnInput<DT, BITS> in[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const uint32_t q = p + (uint32_t)u * a.rows;
-                in[u].load(a, at.sample, q < at.p1 ? q : p, at.c8);
-            }
+            for (int u = 0; u < U; ++u) in[u].load(a, at.sample, px.within(a, u), at.c8);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (u > 0 && p + (uint32_t)u * a.rows >= at.p1) break;
+                if (u > 0 && !px.holds(a, u)) break;
                 float n[8], dz[8];
                 in[u].template take<UNI, SILU>(m, r, w, b, n, dz);
 #pragma unroll
@@ -417,52 +450,44 @@ __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnArgs a) {
     for (int k = 0; k < 8; ++k) { out[2 * k] = mine[k]; out[2 * k + 1] = mine[8 + k]; }
 }
 
-// Of a sample's group, a workgroup each: the channels' sums over the chunks, and the means of g and g n, in binary64.
+// Of a slice of a sample's group, a workgroup each: the channels' sums over the chunks, and the slice's part of the means of g and g n,
+// in binary64.
 __global__ __launch_bounds__(kGnThreads) void gn_means_kernel(GnArgs a) {
     __shared__ double lds[2][kGnThreads];
     __shared__ double of_block[2][kGnThreads / 64];
-    const uint32_t i = blockIdx.x, sample = i / a.H, h = i - sample * a.H;
-    // threads: D channels (all threads' at a time), and as many parts of the chunks as fit
-    const uint32_t wide = a.D < (uint32_t)kGnThreads ? a.D : (uint32_t)kGnThreads, parts = kGnThreads / wide;
-    const uint32_t part = threadIdx.x / wide, d0 = threadIdx.x - part * wide;
-    double m1 = 0.0, m2 = 0.0;
-    for (uint32_t d = 0; d < a.D; d += wide) {
-        const uint32_t c = h * a.D + d + d0;
-        const bool holds = part < parts && d + d0 < a.D;
-        double s0 = 0.0, s1 = 0.0;
-        if (holds) {
-            const float* p = a.partial + ((size_t)sample * a.chunks * a.C + c) * 2;
-#pragma unroll 4
-            for (uint32_t k = part; k < a.chunks; k += parts) {
-                const hf2 v = *(const hf2*)(p + (size_t)k * a.C * 2);
-                s0 += (double)v.x;
-                s1 += (double)v.y;
-            }
+    const uint32_t i = blockIdx.x / a.slices, slice = blockIdx.x - i * a.slices, sample = i / a.H, h = i - sample * a.H;
+    // threads: the slice's channels, and as many parts of the chunks as fit
+    const uint32_t wide = a.D - slice * 64u < 64u ? a.D - slice * 64u : 64u, parts = kGnThreads / wide;
+    const uint32_t part = threadIdx.x / wide, d = threadIdx.x - part * wide, c = h * a.D + slice * 64u + d;
+    double s0 = 0.0, s1 = 0.0, m1 = 0.0, m2 = 0.0;
+    if (part < parts) {
+        const float* p = a.partial + ((size_t)sample * a.chunks * a.C + c) * 2;
+#pragma unroll 8
+        for (uint32_t k = part; k < a.chunks; k += parts) {
+            const hf2 v = *(const hf2*)(p + (size_t)k * a.C * 2);
+            s0 += (double)v.x;
+            s1 += (double)v.y;
         }
-        // over the parts, in their order
-        lds[0][threadIdx.x] = s0;
-        lds[1][threadIdx.x] = s1;
-        __syncthreads();
-        if (holds && part == 0) {
-            for (uint32_t k = 1; k < parts; ++k) {
-                s0 += lds[0][d0 + k * wide];
-                s1 += lds[1][d0 + k * wide];
-            }
-            float* out = a.sums + ((size_t)sample * a.C + c) * 2;
-            out[0] = (float)s0;
-            out[1] = (float)s1;
-            double w = 1.0;
-            if (a.w) w = a.w_f32 ? (double)((const float*)a.w)[c]
-                                 : (double)__builtin_bit_cast(float, (uint32_t)((const uint16_t*)a.w)[c] << 16);
-            m1 += w * s0;
-            m2 += w * s1;
+    }
+    // over the parts, in their order
+    lds[0][threadIdx.x] = s0;
+    lds[1][threadIdx.x] = s1;
+    __syncthreads();
+    if (part == 0) {
+        for (uint32_t k = 1; k < parts; ++k) {
+            s0 += lds[0][d + k * wide];
+            s1 += lds[1][d + k * wide];
         }
-        __syncthreads();
+        *(hf2*)(a.sums + ((size_t)sample * a.C + c) * 2) = hf2{(float)s0, (float)s1};
+        double w = 1.0;
+        if (a.w) w = a.w_f32 ? (double)((const float*)a.w)[c]
+                             : (double)__builtin_bit_cast(float, (uint32_t)((const uint16_t*)a.w)[c] << 16);
+        m1 = w * s0;
+        m2 = w * s1;
     }
     over_block(m1, m2, of_block);
     if (threadIdx.x != 0) return;
-    a.means[2 * i] = (float)(m1 / ((double)a.P * a.D));
-    a.means[2 * i + 1] = (float)(m2 / ((double)a.P * a.D));
+    *(hf2*)(a.means + 2 * (size_t)blockIdx.x) = hf2{(float)(m1 / ((double)a.P * a.D)), (float)(m2 / ((double)a.P * a.D))};
 }
 
 // into dw or db, if it is wanted
@@ -510,16 +535,22 @@ __global__ __launch_bounds__(kGnThreads) void gn_dx_kernel(GnArgs a) {
     const size_t group = (size_t)at.sample * a.H;
     m.load(a, a.mean + group, 1, c);
     r.load(a, a.rstd + group, 1, c);
-    m1.load(a, a.means + 2 * group, 2, c);
-    m2.load(a, a.means + 2 * group + 1, 2, c);
-    for (uint32_t p = at.p0 + at.row; p < at.p1; p += a.rows) {
-        GnInput<DT, BITS> in;
-        in.load(a, at.sample, p, at.c8);
-        float n[8], dz[8];
-        in.template take<UNI, SILU>(m, r, w, b, n, dz);
+    m1.add(a, a.means + 2 * group * a.slices, c);
+    m2.add(a, a.means + 2 * group * a.slices + 1, c);
+    constexpr int U = 2;
+    for (GnPixels<DT, U> px(a, at); px.more(a); px.next(a, at)) {
+        GnInput<DT, BITS> in[U];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dz[k] = r[k] * __builtin_fmaf(-n[k], m2[k], __builtin_fmaf(dz[k], w[k], -m1[k]));
-        store8<DT>((uint8_t*)a.dx.p, ((int64_t)at.sample * a.dx.sample + (int64_t)p * a.dx.pixel + c) * kSize<DT>, dz);
+        for (int u = 0; u < U; ++u) in[u].load(a, at.sample, px.within(a, u), at.c8);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u > 0 && !px.holds(a, u)) break;
+            float n[8], dz[8];
+            in[u].template take<UNI, SILU>(m, r, w, b, n, dz);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dz[k] = r[k] * __builtin_fmaf(-n[k], m2[k], __builtin_fmaf(dz[k], w[k], -m1[k]));
+            store8<DT>((uint8_t*)a.dx.p, ((int64_t)at.sample * a.dx.sample + (int64_t)px.within(a, u) * a.dx.pixel + c) * kSize<DT>, dz);
+        }
     }
 }
 
@@ -865,7 +896,7 @@ static void gn_launch(bool backward, const GnArgs& a, hipStream_t s) {
         GnArgs d = a;
         d.dx_blocks = slots;
         hipLaunchKernelGGL((gn_sums_kernel<DT, BITS, UNI, SILU>), dim3(slots), dim3(kGnThreads), 0, s, a);
-        hipLaunchKernelGGL(gn_means_kernel, dim3(a.B * a.H), dim3(kGnThreads), 0, s, a);
+        hipLaunchKernelGGL(gn_means_kernel, dim3(a.B * a.H * a.slices), dim3(kGnThreads), 0, s, a);
         const uint32_t extra = a.dw || a.db ? (a.C + 31) / 32 : 0;
         hipLaunchKernelGGL((gn_dx_kernel<DT, BITS, UNI, SILU>), dim3(slots + extra), dim3(kGnThreads), 0, s, d);
     }

@@ -30,13 +30,13 @@ bool norm_sizes_ok(int64_t B, int64_t P, int C, int H) {
     return (uint64_t)B * (uint64_t)P <= (uint64_t)kMost && (uint64_t)B * (uint64_t)C < 1ull << 30 &&
            (uint64_t)B * (uint64_t)P * (uint64_t)C < 1ull << 34;
 }
-void norm_sizes(int64_t B, int64_t P, int C, int H, gact::GnArgs* a) {
+void norm_sizes(int64_t B, int64_t P, int C, int H, int dtype, gact::GnArgs* a) {
     a->B = (uint32_t)B;
     a->P = (uint32_t)P;
     a->C = (uint32_t)C;
     a->H = (uint32_t)H;
     a->D = (uint32_t)(C / H);
-    gact::plan_group_norm(a);
+    gact::plan_group_norm(a, dtype);
 }
 
 // Whether two pixels of a tensor can share memory: unless, in the order of their sizes, each stride passes what lies below it.
@@ -125,8 +125,8 @@ int stage_norm(const gact_channel_norm* h, bool backward, void* ws, size_t ws_by
         return GACT_OK;
     }
     if (*bits != 0) while ((8 << a->block_shift) < G) ++a->block_shift;
-    norm_sizes(h->batch, h->pixels, h->channels, h->groups, a);
-    if (!gact::launchable((uint64_t)a->B * (a->chunks * a->slabs + a->C8) + a->C, gact::kGnThreads)) return GACT_E_ARG;
+    norm_sizes(h->batch, h->pixels, h->channels, h->groups, h->dtype, a);
+    if (!gact::launchable((uint64_t)a->B * ((uint64_t)a->chunks * a->slabs + a->C) + a->C, gact::kGnThreads)) return GACT_E_ARG;
     *whole = gact::plan_whole(a, h->dtype);
     uint8_t* at = (uint8_t*)ws;
     const size_t need = backward ? gact::gn_backward_bytes(*a, *whole) : gact::gn_forward_bytes(*a, *whole);
@@ -154,7 +154,7 @@ extern "C" {
 size_t gact_group_norm_workspace_bytes(int64_t batch, int64_t pixels, int channels, int groups, gact_dtype dtype, int backward) {
     if (!norm_sizes_ok(batch, pixels, channels, groups) || !dtype_ok((int)dtype) || batch == 0 || pixels == 0) return 0;
     gact::GnArgs a{};
-    norm_sizes(batch, pixels, channels, groups, &a);
+    norm_sizes(batch, pixels, channels, groups, (int)dtype, &a);
     const int whole = gact::plan_whole(&a, (int)dtype);
     return backward ? gact::gn_backward_bytes(a, whole) : gact::gn_forward_bytes(a, whole);
 }

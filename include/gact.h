@@ -454,7 +454,8 @@ int gact_head_norm_rotate_backward(const gact_heads *h_parts, int n_parts, const
  *   strides    in elements: sample, pixel
  *   channels   a multiple of 8 and of groups;  group_size of a context: 32, 64, 128, 256 or 512 (GACT_E_GROUP otherwise:
  *              gact_compress takes such a tensor)
- *   batch * pixels * channels must be below 2^34, batch * pixels below 2^31, batch * channels below 2^30.
+ *   batch * pixels * channels must be below 2^34, batch * pixels below 2^31, batch * channels below 2^30 (below 2^24 where a group of
+ *   a sample has more than 65536 elements or so: GACT_E_ARG if a launch would pass 2^32 threads).
  *   d_workspace  device scratch, >= gact_group_norm_workspace_bytes(...) of the same sizes, dtype and pass (which may be 0),
  *              16-byte aligned, in use until the enqueued kernels have run; calls that share one must not overlap in time.
  * An empty tensor (batch or pixels 0) is GACT_OK; its dw and db are 0.  Both calls can be captured into a HIP graph.
@@ -513,9 +514,8 @@ int gact_group_norm_backward(const gact_channel_norm *h_norm, void *d_workspace,
  *   db           out  [out_features] of w_dtype, or NULL: not wanted.  Outputs overlap nothing.
  *   d_workspace  device scratch, >= gact_linear_weight_grad_workspace_bytes(...) bytes of the same sizes (which may be 0),
  *                16-byte aligned, in use until the enqueued kernels have run; calls that share one must not overlap in time.
- * tokens == 0 writes zeros; out_features == 0 or in_features == 0 is GACT_OK and writes nothing but db.  tokens and
- * out_features must be below 2^31, in_features below 2^22, tokens * in_features below 2^34, out_features * in_features
- * below 2^38.  An infinity or NaN
+ * tokens == 0 writes zeros; out_features == 0 or in_features == 0 is GACT_OK and writes nothing but db.  tokens must
+ * be below 2^31, out_features below 2^28, in_features below 2^22, tokens * in_features and out_features * in_features below 2^34.  An infinity or NaN
  * in a row of dy reaches that row's columns of dW (rows of x^ times it), in a group's minimum or step the elements of
  * that group.  Can be captured into a HIP graph.
  */

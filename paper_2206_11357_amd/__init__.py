@@ -1054,6 +1054,8 @@ def _rows(x: torch.Tensor) -> Tuple[int, int]:
     if len(shape) < 2:
         raise ValueError("gact needs [..., features]")
     if st[-1] != 1 and shape[-1] > 1:
+        if not x.numel():                       # nothing is read, whatever the strides
+            return math.prod(shape[:-1]), shape[-1]
         raise ValueError("a row's elements must be consecutive")
     if len(shape) == 2:
         return shape[0], st[0]
@@ -1130,6 +1132,8 @@ def _map_strides(x: torch.Tensor) -> Tuple[int, int, int, int, int]:
     if len(shape) < 3:
         raise ValueError("gact needs [batch, ..., channels]")
     if st[-1] != 1 and shape[-1] > 1:
+        if not x.numel():                       # nothing is read, whatever the strides
+            return shape[0], math.prod(shape[1:-1]), shape[-1], 0, 0
         raise ValueError("a pixel's channels must be consecutive")
     if len(shape) == 3:
         return shape[0], shape[1], shape[2], st[0], st[1]

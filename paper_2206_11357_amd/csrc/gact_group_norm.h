@@ -107,7 +107,8 @@ inline int plan_whole(GnArgs* a, int dtype) {
     // 64 26.2 + 22.6, 128 (twice the threads) 29.7 + 21.9; of 64 x 3136 x 256 fp32, 2 bits 32 162 + 170, 64 (the most) 136 + 131.
     const uint32_t size = dtype == GACT_DT_F32 ? 4 : 2;
     uint32_t shift = 0;
-    while ((cols << shift) * 8 * size < 64 && (1u << shift) < a->units && a->unit_shift + shift < 6) ++shift;
+    // (and where there are few pixels, columns enough for the threads)
+    while (((cols << shift) * 8 * size < 64 || (uint64_t)a->P << (a->unit_shift + shift) < kGnWhole[0].threads) && (1u << shift) < a->units && a->unit_shift + shift < 6) ++shift;
     const auto fits = [&](const GnWhole& w) { return (uint64_t)a->P << (a->unit_shift + shift) <= (uint64_t)w.threads * w.blocks; };
     // (Groups that are no whole columns take more registers than the largest has: 16 x 500 x 72 bf16 in 4 groups, 4 bits, 18.5 us
     // forward, 24.1 backward; in passes over memory 15.3 and 20.4.)

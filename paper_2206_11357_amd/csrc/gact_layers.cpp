@@ -20,8 +20,8 @@ size_t size_of(int dt) { return dt == GACT_F32 ? 4 : 2; }
 constexpr int64_t kMost = 0x7FFFFFFFll;
 
 bool weight_sizes_ok(int64_t T, int64_t N, int64_t K) {
-    if (T < 0 || N < 0 || K < 0 || T > kMost || N > kMost || K >= 1 << 22) return false;
-    return (uint64_t)T * (uint64_t)K < 1ull << 34 && (uint64_t)N * (uint64_t)K < 1ull << 38;
+    if (T < 0 || N < 0 || K < 0 || T > kMost || N >= 1 << 28 || K >= 1 << 22) return false;
+    return (uint64_t)T * (uint64_t)K < 1ull << 34 && (uint64_t)N * (uint64_t)K < 1ull << 34;
 }
 
 // -------------------------------------------------------------------- group norm
@@ -126,8 +126,13 @@ int stage_norm(const gact_channel_norm* h, bool backward, void* ws, size_t ws_by
     }
     if (*bits != 0) while ((8 << a->block_shift) < G) ++a->block_shift;
     norm_sizes(h->batch, h->pixels, h->channels, h->groups, h->dtype, a);
-    if (!gact::launchable((uint64_t)a->B * ((uint64_t)a->chunks * a->slabs + a->C) + a->C, gact::kGnThreads)) return GACT_E_ARG;
     *whole = gact::plan_whole(a, h->dtype);
+    // (4096: workgroups that compress, and those that add dw)
+    const uint64_t B = a->B;
+    if (*whole ? !gact::launchable(B * a->unit_slabs + 4096, gact::kGnWhole[*whole - 1].threads)
+               : !gact::launchable(B * a->chunks * a->slabs + a->C / 32 + 1, gact::kGnThreads) ||
+                     !gact::launchable(B * a->H * a->slices, gact::kGnThreads))
+        return GACT_E_ARG;
     uint8_t* at = (uint8_t*)ws;
     const size_t need = backward ? gact::gn_backward_bytes(*a, *whole) : gact::gn_forward_bytes(*a, *whole);
     if (need > 0 && (!at || !aligned(at, 16) || ws_bytes < need)) return GACT_E_ARG;
@@ -201,7 +206,9 @@ int gact_linear_weight_grad(const gact_linear_grad* h_grad, void* d_workspace, s
     const gact::WeightPlan plan = gact::plan_weight(T, N, K, h.dtype);
     const gact::WeightTile tile = gact::weight_tile(h.dtype, plan.form);
     const uint64_t blocks = (uint64_t)plan.tiles_n * plan.tiles_k * plan.splits;
-    if (!gact::launchable(blocks, (uint32_t)tile.threads)) return GACT_E_ARG;
+    if (!gact::launchable(blocks, (uint32_t)tile.threads) ||
+        (plan.splits > 1 && !gact::launchable((N * K + N) * (uint64_t)gact::join_parts(plan.splits) / 1024 + 2, 256)))
+        return GACT_E_ARG;
     const size_t need = gact::weight_workspace_bytes(plan, N, K);
     if (need > 0 && (!d_workspace || !aligned(d_workspace, 16) || workspace_bytes < need)) return GACT_E_ARG;
     gact::WeightArgs a{};

@@ -35,7 +35,10 @@ def _laid_out(t: torch.Tensor, strides) -> torch.Tensor:
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, bits, group_size, seed, own):
-        context = gact_compress(x.contiguous(), group_size, bits, seed)
+        kept = x.contiguous()
+        if kept.data_ptr() % 16:                # a view that begins inside 16 bytes, which the compressor loads at a time
+            kept = kept.clone()
+        context = gact_compress(kept, group_size, bits, seed)
         ctx.save_for_backward(weight, *context)
         ctx.versions = [weight._version] if own else ()
         ctx.bits, ctx.group_size, ctx.shape = bits, group_size, x.shape

@@ -244,3 +244,23 @@ def test_captured_step_is_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(u, v) for u, v in zip(grads, step()))
+
+
+def test_inputs_at_odd_addresses_and_of_no_tokens():
+    w = torch.randn(8, 33, device="cuda", requires_grad=True)
+    base = torch.randn(11, 33, device="cuda")
+    for x in (base[1:], base[:0]):
+        dw, = torch.autograd.grad(layers.linear(x, w, None, 8, 32, 3).sum(), w)
+        own, = torch.autograd.grad(layers.linear(x.clone(), w, None, 8, 32, 3).sum(), w)
+        assert torch.equal(dw, own) and dw.shape == w.shape
+    assert base[1:].data_ptr() % 16 != 0
+
+
+def test_many_samples_of_few_pixels():
+    """A norm for every token: samples of one pixel."""
+    x = torch.randn(70000, 1, 64, device="cuda")
+    y = gact.gact_group_norm(x, 4, None, None, 1e-5)
+    v = x.double().view(70000, 4, 16)
+    want = (v - v.mean(-1, keepdim=True)) * (v.var(-1, unbiased=False, keepdim=True) + 1e-5).rsqrt()
+    # 16 elements: m and r each off by a few roundings of values up to 6, their distances and the product by one each
+    assert (y.double().view_as(want) - want).abs().max() <= 2.0 ** -20 * 6

@@ -160,6 +160,8 @@ def test_shapes_that_the_binding_takes():
     assert gact._map_strides(torch.empty(2, 3, 4, 8)) == (2, 12, 8, 96, 8)
     assert gact._map_strides(torch.empty(2, 8, 3, 4).to(memory_format=torch.channels_last).permute(0, 2, 3, 1)) == (2, 12, 8, 96, 8)
     assert gact._map_strides(torch.empty(2, 3, 4, 16)[..., :8]) == (2, 12, 8, 192, 16)
+    assert gact._rows(torch.empty(1).expand(0, 8)) == (0, 8)                    # empty: no strides to keep to
+    assert gact._map_strides(torch.empty(1).expand(2, 0, 8))[:3] == (2, 0, 8)
     for bad in (torch.empty(8), torch.empty(8, 6).t(), torch.empty(4, 3, 8)[:, :2]):
         with pytest.raises(ValueError):
             gact._rows(bad)

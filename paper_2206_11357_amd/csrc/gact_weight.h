@@ -4,6 +4,8 @@
 
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "gact_device.h"
 #include "gact_heads.h"
 
@@ -69,22 +71,15 @@ struct WeightPlan {
     int form;
     uint32_t tiles_n, tiles_k, chunks, splits, db_every;
 };
-inline WeightPlan plan_weight(uint64_t T, uint64_t N, uint64_t K, int dtype) {
+// A form's tiles and splits.
+inline WeightPlan weight_splits(uint64_t T, uint64_t N, uint64_t K, int dtype, int form) {
     WeightPlan p{};
-    const uint64_t small = weight_up(N, 64) * (K ? weight_up(K, 64) : 1);
-    // Us, large | small | long tiles, 4 bits, by tokens x out x in features:
-    //   bf16   1024 x 1024 x 1024 25.3 | 16.0 | 8.8    4096 x 1024 x 1024 32.7 | 28.6 | 19.9    8192 x 1024 x 1024 36.6 | 45.5 | 35.9
-    //          512 x 4096 x 1024 18.7 | 12.9 | 22.5    2048 x 4096 x 1024 39.8 | 35.4 | 43.6    12608 x 1024 x 1024 44.6 | 65.2 | 52.9
-    //   fp32   1024 x 1024 x 1024 50.2 | 32.8 | 22.8   4096 x 1024 x 1024 86.5 | 96.0 | 76.1    8192 x 1024 x 1024 142 | 181 | 147
-    //          512 x 4096 x 1024 58.2 | 42.7 | 50.8    50000 x 1000 x 100 119 | 166 | 140       128 x 4096 x 1024 27.2 | 15.7 | 24.4
-    p.form = N <= 32 ? kWeightWide : K <= 32 ? kWeightTall
-           : N > 128 && K > 64 && T * N * K >= 9ull << 29 ? kWeightLarge
-           : small > 256 || T <= 64 ? kWeightSmall : kWeightLong;
-    const WeightTile tile = weight_tile(dtype, p.form);
+    p.form = form;
+    const WeightTile tile = weight_tile(dtype, form);
     p.tiles_n = (uint32_t)weight_up(N, (uint64_t)tile.n);
     p.tiles_k = K ? (uint32_t)weight_up(K, (uint64_t)tile.k) : 1;      // (K = 0: db alone)
     const uint64_t tiles = (uint64_t)p.tiles_n * p.tiles_k, chunks = weight_up(T, (uint64_t)tile.tokens);
-    const uint64_t fill = p.form == kWeightSmall ? 512 : 256;
+    const uint64_t fill = form == kWeightSmall ? 512 : 256;
     uint64_t splits = tiles >= fill ? 1 : fill / tiles;
     // a second launch costs as much as a few chunks, whose products take more than twice the time in fp32
     const uint64_t most = dtype == GACT_DT_F32 ? (chunks <= 6 ? 1 : chunks / 2) : (chunks <= 12 ? 1 : chunks / 4);
@@ -97,6 +92,38 @@ inline WeightPlan plan_weight(uint64_t T, uint64_t N, uint64_t K, int dtype) {
     if (p.splits == 0) p.splits = 1;
     p.db_every = p.splits > 1 ? p.tiles_k : 1;
     return p;
+}
+// About the us that it takes: products of whole tiles at the rate that the form reaches with the GPU full, rounds of blocks, a second
+// launch.  What it goes by, us, large | small | long tiles, 4 bits, by tokens x out x in features:
+//   bf16   1024 x 1024 x 1024 25.3 | 16.0 | 8.8    4096 x 1024 x 1024 32.7 | 28.6 | 19.9    8192 x 1024 x 1024 36.6 | 45.5 | 35.9
+//          512 x 4096 x 1024 18.7 | 12.9 | 22.5    2048 x 4096 x 1024 39.8 | 35.4 | 43.6    12608 x 1024 x 1024 44.6 | 65.2 | 52.9
+//   fp32   1024 x 1024 x 1024 50.2 | 32.8 | 22.8   4096 x 1024 x 1024 86.5 | 96.0 | 76.1    8192 x 1024 x 1024 142 | 181 | 147
+//          512 x 4096 x 1024 58.2 | 42.7 | 50.8    14645 x 4711 x 104 158 | 263 | 260       128 x 4096 x 1024 27.2 | 15.7 | 24.4
+inline double weight_us(const WeightPlan& p, uint64_t T, int dtype) {
+    const WeightTile tile = weight_tile(dtype, p.form);
+    const double blocks = (double)p.tiles_n * p.tiles_k * p.splits, rounds = (double)weight_up((uint64_t)blocks, 256);
+    const double flops = 2.0 * (double)weight_up(T, (uint64_t)tile.tokens) * tile.tokens * p.tiles_n * tile.n * p.tiles_k * tile.k;
+    const bool f32 = dtype == GACT_DT_F32;
+    const double rate = p.form == kWeightLarge ? (f32 ? 140e6 : 1000e6) : p.form == kWeightLong ? (f32 ? 122e6 : 600e6) : (f32 ? 115e6 : 550e6);
+    // blocks of one to a compute unit, in rounds, or of several
+    const double full = p.form == kWeightSmall ? (blocks < 600 ? blocks / 600 : 1.0) : blocks / (256 * rounds);
+    const double start = p.form == kWeightLarge ? 14 + 4 * rounds : p.form == kWeightLong ? 2 + 3.5 * rounds : 5;
+    return start + flops / (rate * full) + (p.splits == 1 ? 0.0 : p.form == kWeightSmall ? 6.0 : 4.0);
+}
+inline WeightPlan plan_weight(uint64_t T, uint64_t N, uint64_t K, int dtype) {
+    if (N <= 32) return weight_splits(T, N, K, dtype, kWeightWide);
+    if (K <= 32) return weight_splits(T, N, K, dtype, kWeightTall);
+    WeightPlan best = weight_splits(T, N, K, dtype, kWeightSmall);
+    if (T <= 64) return best;                          // few tokens: one team has them all
+    double us = weight_us(best, T, dtype);
+    for (const int form : {kWeightLong, kWeightLarge}) {
+        const WeightPlan p = weight_splits(T, N, K, dtype, form);
+        const double t = weight_us(p, T, dtype);
+        if (t >= us) continue;
+        best = p;
+        us = t;
+    }
+    return best;
 }
 inline size_t weight_partial_bytes(const WeightPlan& p, uint64_t N, uint64_t K) {
     return p.splits > 1 ? (size_t)((p.splits * N * K * sizeof(float) + 15) & ~(uint64_t)15) : 0;

@@ -81,7 +81,7 @@ inline WeightPlan weight_splits(uint64_t T, uint64_t N, uint64_t K, int dtype, i
     const uint64_t tiles = (uint64_t)p.tiles_n * p.tiles_k, chunks = weight_up(T, (uint64_t)tile.tokens);
     const uint64_t fill = form == kWeightSmall ? 512 : 256;
     uint64_t splits = tiles >= fill ? 1 : fill / tiles;
-    // a second launch costs as much as a few chunks, whose products take more than twice the time in fp32
+    // a second launch costs as much as a few chunks, whose products take three times as long in fp32
     const uint64_t most = dtype == GACT_DT_F32 ? (chunks <= 6 ? 1 : chunks / 2) : (chunks <= 12 ? 1 : chunks / 4);
     if (splits > most) splits = most;
     // a split's codes lie within kWeightReach
@@ -97,14 +97,14 @@ inline WeightPlan weight_splits(uint64_t T, uint64_t N, uint64_t K, int dtype, i
 // launch.  What it goes by, us, large | small | long tiles, 4 bits, by tokens x out x in features:
 //   bf16   1024 x 1024 x 1024 25.3 | 16.0 | 8.8    4096 x 1024 x 1024 32.7 | 28.6 | 19.9    8192 x 1024 x 1024 36.6 | 45.5 | 35.9
 //          512 x 4096 x 1024 18.7 | 12.9 | 22.5    2048 x 4096 x 1024 39.8 | 35.4 | 43.6    12608 x 1024 x 1024 44.6 | 65.2 | 52.9
-//   fp32   1024 x 1024 x 1024 50.2 | 32.8 | 22.8   4096 x 1024 x 1024 86.5 | 96.0 | 76.1    8192 x 1024 x 1024 142 | 181 | 147
-//          512 x 4096 x 1024 58.2 | 42.7 | 50.8    14645 x 4711 x 104 158 | 263 | 260       128 x 4096 x 1024 27.2 | 15.7 | 24.4
+//   fp32   1024 x 1024 x 1024 36.1 | 31.1 | 18.7   4096 x 1024 x 1024 58.3 | 90.8 | 63.5    8192 x 1024 x 1024 92.6 | 164 | 121
+//          512 x 4096 x 1024 43.7 | 34.9 | 41.5    14645 x 4711 x 104 109 | 239 | 184       128 x 4096 x 1024 20.3 | 13.7 | 22.6
 inline double weight_us(const WeightPlan& p, uint64_t T, int dtype) {
     const WeightTile tile = weight_tile(dtype, p.form);
     const double blocks = (double)p.tiles_n * p.tiles_k * p.splits, rounds = (double)weight_up((uint64_t)blocks, 256);
     const double flops = 2.0 * (double)weight_up(T, (uint64_t)tile.tokens) * tile.tokens * p.tiles_n * tile.n * p.tiles_k * tile.k;
     const bool f32 = dtype == GACT_DT_F32;
-    const double rate = p.form == kWeightLarge ? (f32 ? 140e6 : 1000e6) : p.form == kWeightLong ? (f32 ? 122e6 : 600e6) : (f32 ? 115e6 : 550e6);
+    const double rate = p.form == kWeightLarge ? (f32 ? 230e6 : 1000e6) : p.form == kWeightLong ? (f32 ? 150e6 : 600e6) : (f32 ? 115e6 : 550e6);
     // blocks of one to a compute unit, in rounds, or of several
     const double full = p.form == kWeightSmall ? (blocks < 600 ? blocks / 600 : 1.0) : blocks / (256 * rounds);
     const double start = p.form == kWeightLarge ? 14 + 4 * rounds : p.form == kWeightLong ? 2 + 3.5 * rounds : 5;

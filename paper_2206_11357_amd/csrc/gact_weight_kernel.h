@@ -3,10 +3,10 @@
 //   dW[n, k] = sum over t of dy[t, n] x^[t, k],   db[n] = sum over t of dy[t, n],   x^ = code * step + minimum
 //
 // A matrix product whose right operand is decoded on its way into shared memory: codes are read from HBM, never x^.
-// Both operands have the summed axis outermost.  bf16: rows of tokens in shared memory as they come, read transposed
-// (ds_read_b64_tr_b16: four tokens of a column a lane), 32x32x16 products; fp32: 32x32x2 products, whose operands are a
-// row's elements as they lie.  A wavefront holds its part of dW in registers; the next tokens are on their way from
-// HBM meanwhile, and are decoded behind the products of the present ones.
+// Both operands have the summed axis outermost: rows of tokens in shared memory as they come, read transposed
+// (ds_read_b64_tr_b16: four tokens of a column a lane), 32x32x16 products of bf16, fp32 in three parts.  A wavefront holds
+// its part of dW in registers; the next tokens are on their way from HBM meanwhile, and are decoded behind the products of
+// the present ones.
 // The tokens are split over blocks where the tiles of dW are too few for the GPU; the splits' sums are added in a fixed
 // order by a second launch.
 #ifndef GACT_WEIGHT_KERNEL_H
@@ -98,14 +98,6 @@ struct Codes {
 };
 
 // ------------------------------------------------------------------ the tiles
-template <int DT>
-struct Operand {
-    typedef wb8 type;
-};
-template <>
-struct Operand<GACT_DT_F32> {
-    typedef float type;
-};
 template <int DT, int FORM>
 struct Tiling {
     static constexpr WeightTile tile = weight_tile(DT, FORM);
@@ -121,32 +113,42 @@ struct Tiling {
     // 32 x 32 products of a wavefront; a team's four lie 2 x 2, or in a row where a tile is narrow
     static constexpr int kWavesN = BN == 32 ? 1 : BK == 32 ? 4 : 2, kWavesK = 4 / kWavesN;
     static constexpr int TN = BN / 32 / kWavesN, TK = BK / 32 / kWavesK;
-    // Bytes from row to row in shared memory.  bf16: the four rows of a transposed read, 64 bytes each, lie in different banks; fp32: so do
-    // the two rows of a product's operands where these are single elements.
-    static constexpr int pad(int bytes, int elements) {
-        return DT == GACT_DT_F32 ? (elements == 1 && bytes % 256 == 0 ? 128 : 0) : (bytes % 256 == 64 || bytes % 256 == 192 ? 0 : 64);
-    }
-    static constexpr int kRowN = BN * kSize + pad(BN * kSize, TN), kRowK = BK * kSize + pad(BK * kSize, TK);
+    // Shared memory: rows of tokens in bf16; fp32: in three parts, each a row.  The four rows of a transposed read, 64 bytes each, lie
+    // in different banks.
+    static constexpr int kParts = DT == GACT_DT_F32 ? 3 : 1;
+    static constexpr int part(int elements) { return elements * 2 + (elements * 2 % 256 == 64 || elements * 2 % 256 == 192 ? 0 : 64); }
+    static constexpr int kPartN = part(BN), kPartK = part(BK), kRowN = kParts * kPartN, kRowK = kParts * kPartK;
     static constexpr int kBufN = BT * kRowN, kBuf = kBufN + BT * kRowK;
+    // where two do not fit, a chunk's operands are all read before the next one is placed
+    static constexpr int kBufs = FORM == kWeightLarge && DT == GACT_DT_F32 ? 1 : 2;
+    static_assert(kRowN % 256 == 64 || kRowN % 256 == 192, "banks");
+    static_assert(kRowK % 256 == 64 || kRowK % 256 == 192, "banks");
     static_assert(kThreads % kRowPieces == 0 && kThreads % kRowBlocks == 0, "a thread stays in its column");
 };
 
-// Where a wavefront's operands lie in a chunk, and its products.
-//   bf16  a step is 16 tokens; 16 lanes read 4 rows of 16 elements, of which each gets a column
-//   fp32  a step is two tokens; a lane's operands are TN (TK) neighbouring elements of row 2 s + lane / 32
+// Where a wavefront's operands lie in a chunk, and its products.  A step is 16 tokens; 16 lanes read 4 rows of 16 elements, of which
+// each gets a column.
+//   fp32  An element is the sum of three bf16, each the rounded rest of the ones before: 8 bits and a sign each, exactly (an infinity,
+//         and what bf16 rounds to one, leaves NaN).  Of the nine products of their parts the six largest are taken.  The second part is
+//         at most 2^-8 of the element and the third 2^-17, so that the others come to at most 2^-24 of a product, as much as its
+//         rounding to binary32 would; sums are binary32.  Six products of bf16 take 6 x 32 cycles of the matrix unit for 16 tokens, eight
+//         of fp32 8 x 64: 169343 x 256 x 256 takes 124 us with the sums' addition, 184 in fp32, and comes closer to the sum in 64 bits
+//         (6.8e-7 of it; the decompressed product by the library 4.0e-6).
 template <int DT, int FORM>
 struct Products {
     typedef Tiling<DT, FORM> L;
-    typedef typename Operand<DT>::type Op;
-    static constexpr int TN = L::TN, TK = L::TK;
-    static constexpr int kSteps = L::BT / L::kTeams / (DT == GACT_DT_F32 ? 2 : 16);          // of a team
+    static constexpr int TN = L::TN, TK = L::TK, kParts = L::kParts;
+    static constexpr int kSteps = L::BT / L::kTeams / 16;                                    // of a team
+    struct Op {
+        wb8 part[kParts];
+    };
     uint32_t at_n, at_k;
     wf16 acc[TN][TK];
     __device__ __forceinline__ Products(int lane, int team, int wn, int wk) {
-        const uint32_t row = (uint32_t)(team * (L::BT / L::kTeams) + (DT == GACT_DT_F32 ? lane >> 5 : 8 * (lane >> 5) + ((lane & 15) >> 2)));
+        const uint32_t row = (uint32_t)(team * (L::BT / L::kTeams) + 8 * (lane >> 5) + ((lane & 15) >> 2));
         const int col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-        at_n = row * L::kRowN + (uint32_t)(DT == GACT_DT_F32 ? (wn * 32 * TN + (lane & 31) * TN) * 4 : (wn * 32 * TN + col) * 2);
-        at_k = L::kBufN + row * L::kRowK + (uint32_t)(DT == GACT_DT_F32 ? (wk * 32 * TK + (lane & 31) * TK) * 4 : (wk * 32 * TK + col) * 2);
+        at_n = row * L::kRowN + (uint32_t)(wn * 32 * TN + col) * 2;
+        at_k = L::kBufN + row * L::kRowK + (uint32_t)(wk * 32 * TK + col) * 2;
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
@@ -154,27 +156,24 @@ struct Products {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
     }
-    static __device__ __forceinline__ Op columns(const uint8_t* p, int stride) {
+    static __device__ __forceinline__ Op columns(const uint8_t* p, int row, int part) {
         typedef __attribute__((address_space(3))) ws4* lds_ptr;
-        union { ws4 h[2]; Op v; } u;
-        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
-        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * stride));
-        return u.v;
+        Op op;
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) {
+            union { ws4 h[2]; wb8 v; } u;
+            u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + k * part));
+            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + k * part + 4 * row));
+            op.part[k] = u.v;
+        }
+        return op;
     }
     __device__ __forceinline__ void read_n(const uint8_t* buf, int s, int i, Op (&x)[TN]) const {
-        if constexpr (DT == GACT_DT_F32) {
-            if (i == 0) __builtin_memcpy(x, __builtin_assume_aligned(buf + at_n + 2 * s * L::kRowN, 4 * TN), 4 * TN);
-        } else {
-            x[i] = columns(buf + at_n + 16 * s * L::kRowN + 64 * i, L::kRowN);
-        }
+        x[i] = columns(buf + at_n + 16 * s * L::kRowN + 64 * i, L::kRowN, L::kPartN);
     }
     __device__ __forceinline__ void read_k(const uint8_t* buf, int s, Op (&y)[TK]) const {
-        if constexpr (DT == GACT_DT_F32) {
-            __builtin_memcpy(y, __builtin_assume_aligned(buf + at_k + 2 * s * L::kRowK, 4 * TK), 4 * TK);
-        } else {
 #pragma unroll
-            for (int j = 0; j < TK; ++j) y[j] = columns(buf + at_k + 16 * s * L::kRowK + 64 * j, L::kRowK);
-        }
+        for (int j = 0; j < TK; ++j) y[j] = columns(buf + at_k + 16 * s * L::kRowK + 64 * j, L::kRowK, L::kPartK);
     }
     __device__ __forceinline__ void read(const uint8_t* buf, int s, Op (&x)[TN], Op (&y)[TK]) const {
         read_k(buf, s, y);
@@ -182,11 +181,14 @@ struct Products {
         for (int i = 0; i < TN; ++i) read_n(buf, s, i, x);
     }
     __device__ __forceinline__ void product(int i, const Op (&x)[TN], const Op (&y)[TK]) {
+        // parts whose numbers add up to less than kParts, the small products first
 #pragma unroll
-        for (int j = 0; j < TK; ++j) {
-            if constexpr (DT == GACT_DT_F32) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[j], acc[i][j], 0, 0, 0);
-            else acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
-        }
+        for (int sum = kParts - 1; sum >= 0; --sum)
+#pragma unroll
+            for (int p = 0; p <= sum; ++p)
+#pragma unroll
+                for (int j = 0; j < TK; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i].part[p], y[j].part[sum - p], acc[i][j], 0, 0, 0);
     }
     __device__ __forceinline__ void chunk(const uint8_t* buf) {
 #pragma unroll
@@ -311,14 +313,37 @@ struct Loader {
 #pragma unroll
         for (int q = 0; q < L::kBlocks; ++q) fetch_x(s, chunk, q);
     }
-    __device__ __forceinline__ void place_dy(const S& s, uint8_t* buf, int q) const {
-        *(w4*)(buf + (pt + q * L::kRowsN) * L::kRowN + pn * 16) = s.dy[q];
+    // A pair of elements as its next part in bf16; what is left of them.
+    static __device__ __forceinline__ uint32_t next_part(float& u, float& v) {
+        const uint32_t w = bf16_pair_rne(u, v);
+        u -= __builtin_bit_cast(float, w << 16);
+        v -= __builtin_bit_cast(float, w & 0xFFFF0000u);
+        return w;
     }
-    __device__ __forceinline__ void place_x(uint8_t* buf, int q, const float (&x)[8]) const {
-        uint8_t* p = buf + L::kBufN + (bt + q * L::kRowsK) * L::kRowK + bk * (8 * L::kSize);
-        if (DT == GACT_DT_F32) {
-            *(wf4*)p = wf4{x[0], x[1], x[2], x[3]};
-            *(wf4*)(p + 16) = wf4{x[4], x[5], x[6], x[7]};
+    __device__ __forceinline__ void place_dy(const S& s, uint8_t* buf, int q) const {
+        uint8_t* p = buf + (pt + q * L::kRowsN) * L::kRowN + pn * (2 * L::kPiece);
+        if constexpr (DT == GACT_DT_F32) {
+            const uint32_t d[4] = {s.dy[q].x, s.dy[q].y, s.dy[q].z, s.dy[q].w};
+            float v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = __builtin_bit_cast(float, d[j]);
+#pragma unroll
+            for (int k = 0; k < L::kParts; ++k) {
+                const uint32_t lo = next_part(v[0], v[1]), hi = next_part(v[2], v[3]);
+                *(w2*)(p + k * L::kPartN) = w2{lo, hi};
+            }
+        } else {
+            *(w4*)p = s.dy[q];
+        }
+    }
+    __device__ __forceinline__ void place_x(uint8_t* buf, int q, float (&x)[8]) const {
+        uint8_t* p = buf + L::kBufN + (bt + q * L::kRowsK) * L::kRowK + bk * 16;
+        if constexpr (DT == GACT_DT_F32) {
+#pragma unroll
+            for (int k = 0; k < L::kParts; ++k) {
+                const uint32_t w0 = next_part(x[0], x[1]), w1 = next_part(x[2], x[3]), w2_ = next_part(x[4], x[5]), w3_ = next_part(x[6], x[7]);
+                *(w4*)(p + k * L::kPartK) = w4{w0, w1, w2_, w3_};
+            }
         } else {
             *(w4*)p = w4{bf16_pair_rne(x[0], x[1]), bf16_pair_rne(x[2], x[3]), bf16_pair_rne(x[4], x[5]), bf16_pair_rne(x[6], x[7])};
         }
@@ -362,7 +387,7 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
     typedef typename Prod::Op Op;
     typedef Loader<DT, BITS, FORM, BUFFER, EVEN> Load;
     constexpr int BN = L::BN, BK = L::BK, TN = L::TN, TK = L::TK;
-    __shared__ __align__(16) uint8_t lds[2][L::kBuf];
+    __shared__ __align__(16) uint8_t lds[L::kBufs][L::kBuf];
     const uint32_t tid = threadIdx.x;
     const int lane = (int)tid & 63, wave = (int)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
 
@@ -394,7 +419,43 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
     };
     if (c0 < c1) {
         const Load load(a, n0, k0, c0);
-        if constexpr (FORM == kWeightLarge) {
+        if constexpr (FORM == kWeightLarge && Prod::kSteps == 1) {
+            // A chunk is one step: its operands are read at once, and behind the second barrier its place is free for the next one, which is
+            // decoded and placed, and the one behind it fetched, between the products.  Without a question, as below.
+            typename Load::S slot;
+            Op x[TN], y[TK];
+            load.fetch(slot, c0);
+            if (adds(c0)) load.add_db(slot, sum);
+            load.place(slot, lds[0]);
+            load.fetch(slot, c0 + 1);
+            for (uint32_t c = c0; c < c1; ++c) {
+                __syncthreads();
+                prod.read(lds[0], 0, x, y);
+                if (c + 1 < c1 && adds(c + 1)) load.add_db(slot, sum);
+                __syncthreads();
+                float v[L::kBlocks][8];
+                constexpr int kValues = 8 * L::kBlocks;
+#pragma unroll
+                for (int i = 0; i < TN; ++i) {
+                    prod.product(i, x, y);
+#pragma unroll
+                    for (int q = i * L::kPieces / TN; q < (i + 1) * L::kPieces / TN; ++q) {
+                        load.place_dy(slot, lds[0], q);
+                        load.fetch_dy(slot, c + 2, q);
+                    }
+#pragma unroll
+                    for (int e = i * kValues / TN; e < (i + 1) * kValues / TN; ++e) {
+                        if (e % 8 == 0) slot.codes[e / 8].part();
+                        v[e / 8][e % 8] = slot.codes[e / 8].value(e % 8);
+                        if (e % 8 == 7) {
+                            load.place_x(lds[0], e / 8, v[e / 8]);
+                            load.fetch_x(slot, c + 2, e / 8);
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        } else if constexpr (FORM == kWeightLarge) {
             // Chunk c is multiplied while chunk c + 1 is placed, the first of its blocks decoded a step ahead, and c + 2 fetched, a little
             // of each behind every row of products, in this order: two wavefronts of a SIMD that do one after the other fall into
             // step and leave the matrix unit idle together.  A step's operands are read during the step before it, so that
@@ -491,7 +552,7 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
     float* room = (float*)lds[0] + (tid & 255u);
     constexpr int kRow = TK * 16 * 256;
     if constexpr (L::kTeams == 2) {
-        static_assert(TN % 2 == 0 && 2 * kRow * 4 <= 2 * L::kBuf, "room");
+        static_assert(TN % 2 == 0 && 2 * kRow * 4 <= L::kBufs * L::kBuf, "room");
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             __syncthreads();
@@ -513,7 +574,7 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
                 }
         }
     } else if constexpr (L::kTeams > 2) {
-        static_assert(TN == 1 && (L::kTeams - 1) * kRow * 4 <= 2 * L::kBuf, "room");
+        static_assert(TN == 1 && (L::kTeams - 1) * kRow * 4 <= L::kBufs * L::kBuf, "room");
         if (team > 0) {
 #pragma unroll
             for (int j = 0; j < TK; ++j)
@@ -535,8 +596,8 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
     const bool whole = a.partial == nullptr, inside = n0 + BN <= a.N && k0 + BK <= a.K;
     const int low = lane >> 5, at_k = lane & 31;
     // of a lane: row, column, and their elements; of row r of products i: what all lanes add to them
-    const uint32_t lane_n = n0 + (uint32_t)(wn * 32 * TN + (DT == GACT_DT_F32 ? 4 * low * TN + first : first * 32 + 4 * low));
-    const uint32_t lane_k = k0 + (uint32_t)(wk * 32 * TK + (DT == GACT_DT_F32 ? at_k * TK : at_k));
+    const uint32_t lane_n = n0 + (uint32_t)(wn * 32 * TN + first * 32 + 4 * low);
+    const uint32_t lane_k = k0 + (uint32_t)(wk * 32 * TK + at_k);
     const auto put = [&](auto* to) {
         typedef typename std::remove_pointer<decltype(to)>::type Out;
         to += (size_t)lane_n * a.K + lane_k;
@@ -544,12 +605,12 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
         for (int i = 0; i < kMine; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const uint32_t row = (uint32_t)((r & 3) + 8 * (r >> 2)), n = DT == GACT_DT_F32 ? row * TN + i : i * 32 + row;
+                const uint32_t n = (uint32_t)(i * 32 + (r & 3) + 8 * (r >> 2));
                 if (!inside && lane_n + n >= a.N) continue;
                 Out* p = to + (size_t)n * a.K;
 #pragma unroll
                 for (int j = 0; j < TK; ++j) {
-                    const uint32_t k = DT == GACT_DT_F32 ? j : j * 32;
+                    const uint32_t k = j * 32;
                     if (!inside && lane_k + k >= a.K) continue;
                     if constexpr (sizeof(Out) == 4) p[k] = acc[i][j][r];
                     else p[k] = (Out)bf16_pair_rne(acc[i][j][r], 0.0f);

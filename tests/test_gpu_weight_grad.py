@@ -212,3 +212,49 @@ def test_largest_products(T, N, K, G, bits, wide, dtype):
     dy = (torch.randn(T, N + wide, generator=gen, device="cuda") * 0.1).to(DTYPES[dtype])[:, wide:]
     context = gact.gact_compress(x, G, bits, 7)
     on_gpu(dy, context, K, G, bits, *gact.gact_linear_weight_grad(dy, *context, K, G, bits, w_dtype=torch.float32, bias=True))
+
+
+# every form; a shape's form depends on its sizes
+SHAPES = [(1, 130, 72), (64, 100, 100), (2000, 24, 200), (2000, 200, 24), (3001, 130, 104), (19000, 512, 512), (19001, 510, 501)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,K", SHAPES)
+def test_each_product_is_exact_to_a_rounding(T, N, K, dtype):
+    """All rows of dy but one are zero.  An fp32 product leaves 2^-24 out and adds six terms, each addition off by at most a
+    step of 2^-23 of a sum that is at most 1 + 2^-7 of the whole; sums with zeros are exact.  bf16: a product has 16 bits."""
+    dy, *context = inputs(T, N, K, 64, 8, DTYPES[dtype])
+    row = T * 2 // 3
+    one = torch.zeros_like(dy)
+    one[row] = dy[row]
+    dw, db = gact.gact_linear_weight_grad(one, *context, K, 64, 8, w_dtype=torch.float32, bias=True)
+    x = gact.gact_decompress(*context, T * K, 64, 8, dtype=dy.dtype).view(T, K)[row].cpu().double()
+    want = dy[row].cpu().double()[:, None] * x[None, :]
+    off = (dw.cpu().double() - want).abs() - (2.0 ** -24 + 7 * 2.0 ** -23 if dtype == "f32" else 0.0) * want.abs()
+    assert off.max() <= 0
+    assert torch.equal(db, dy[row].float())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,K", SHAPES)
+def test_powers_of_two_pass_through(T, N, K, dtype):
+    """Elements of 1/4 to 1 have parts of 2^-27 on; times 2^-90 and 2^100 these and all sums are normal numbers."""
+    dy, *context = inputs(T, N, K, 64, 4, DTYPES[dtype])
+    dy = (0.25 + 0.75 * torch.rand(T, N, device="cuda", generator=torch.Generator(device="cuda").manual_seed(T))).to(dy.dtype) * dy.sign()
+    call = lambda d: gact.gact_linear_weight_grad(d, *context, K, 64, 4, w_dtype=torch.float32, bias=True)
+    dw, db = call(dy)
+    for power in (2.0 ** -90, 2.0 ** 100):
+        scaled_w, scaled_b = call(dy * power)
+        assert torch.equal(scaled_w, dw * power) and torch.equal(scaled_b, db * power)
+
+
+@pytest.mark.parametrize("T,N,K", SHAPES)
+def test_not_a_number_in_binary32(T, N, K):
+    dy, *context = inputs(T, N, K, 32, 4, torch.float32)
+    clean, _ = gact.gact_linear_weight_grad(dy, *context, K, 32, 4)
+    dy[T // 2, 3], dy[T // 3, 9], dy[T - 1, 11] = float("nan"), float("inf"), -float("inf")
+    dw, db = gact.gact_linear_weight_grad(dy, *context, K, 32, 4, bias=True)
+    rows = torch.ones(N, dtype=torch.bool, device="cuda")
+    rows[[3, 9, 11]] = False
+    assert not torch.isfinite(dw[~rows]).any() and torch.equal(dw[rows], clean[rows])
+    assert torch.isnan(db[3]) and db[9] == float("inf") and db[11] == -float("inf") and torch.isfinite(db[rows]).all()

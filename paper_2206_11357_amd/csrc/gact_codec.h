@@ -1,5 +1,5 @@
-// The quantizer's parts that act on registers, for the kernels of gact_kernels.hip and gact_heads.hip: lane moves and
-// group statistics, the noise generator, rounding and packing.  The exact arithmetic is stated in include/gact.h.
+// The quantizer's parts that act on registers, for the kernels of gact_kernels.hip, gact_heads.hip and
+// gact_group_norm.hip: lane moves and group statistics, the noise generator, rounding and packing.  The exact arithmetic is stated in include/gact.h.
 #ifndef GACT_CODEC_H
 #define GACT_CODEC_H
 

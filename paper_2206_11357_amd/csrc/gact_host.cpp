@@ -32,7 +32,7 @@ const char* gact_error_string(int code) {
         case GACT_OK: return "ok";
         case GACT_E_ARG: return "bad argument (null/misaligned pointer, negative size, bad dtype, small workspace)";
         case GACT_E_BITS: return "bits must be 1, 2, 4 or 8";
-        case GACT_E_GROUP: return "group_size must be a multiple of 32 in [32, 1024] (of a head's context: one that fits its heads)";
+        case GACT_E_GROUP: return "group_size must be a multiple of 32 in [32, 1024] (of a head's context: one that fits its heads; of a group norm's: 32 to 512, a power of two)";
         case GACT_E_BUDGET: return "avg_bit_budget must be >= 1";
         case GACT_E_HIP: return "HIP runtime error";
         case GACT_E_CAPTURE: return "the stream is capturing a HIP graph and this call needs a table upload from host memory";

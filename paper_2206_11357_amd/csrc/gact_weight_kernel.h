@@ -9,6 +9,10 @@
 // the present ones.
 // The tokens are split over blocks where the tiles of dW are too few for the GPU; the splits' sums are added in a fixed
 // order by a second launch.
+// Measured, us with that launch: 32768 x 1024 x 4096 bf16, 4 bits 290 (a library's product of values decompressed before
+// 336), 8192 x 4096 x 1024 85 (93), 169343 x 256 x 256 fp32, 2 bits 124 (502).  Bound by the matrix unit at the clock that the
+// power allows, the decoding and the writes to shared memory beside it: of 311 (an earlier 290) 255 without fetching, 250
+// without decoding, 223 without the writes, 220 without products, 217 with products and their reads alone.
 #ifndef GACT_WEIGHT_KERNEL_H
 #define GACT_WEIGHT_KERNEL_H
 

@@ -94,7 +94,7 @@ struct GnWhole {
 constexpr int kGnWholes = 3;
 constexpr GnWhole kGnWhole[kGnWholes] = {{256, 4}, {512, 8}, {1024, 8}};
 // Whether a sample's group fits the registers of a workgroup: which of them it is (0: of none, 1 ..), and how it is laid out.
-inline int plan_whole(GnArgs* a, int dtype) {
+inline int plan_whole(GnArgs* a, int dtype, bool backward) {
     uint32_t g = a->D, h = 8;                          // their greatest common divisor
     while (h) { const uint32_t t = g % h; g = h; h = t; }
     const uint32_t cols = a->D / g;                     // whole groups in whole columns
@@ -115,6 +115,20 @@ inline int plan_whole(GnArgs* a, int dtype) {
     const int most = g == 8 ? kGnWholes : kGnWholes - 1;
     while (!fits(kGnWhole[most - 1]) && shift > 0) --shift;
     if (!fits(kGnWhole[most - 1])) return 0;
+    // A cache line of a pixel, where the workgroups still fill the GPU.  Us, 64 bytes | 128 | 256: backward, 2 and 4 bits, 64 x 1024 x 256 fp32
+    // 39.0 | 29.6 | 27.2, 256 x 784 x 256 fp32 130 | 102 | 101, 64 x 1024 x 512 bf16 SiLU 48.8 | 39.7, 128 x 784 x 256 bf16 29.0 | 30.2 | 31.4;
+    // forward 256 x 784 x 256 fp32 131 | 123, 64 x 1024 x 256 fp32 38.5 | 35.1, 128 x 256 x 640 bf16 in groups of 20 84 | 63, 64 x 196 x
+    // 1024 bf16 19.3 | 24.6, in workgroups of twice the threads 128 x 1568 x 256 fp32 131 | 145.
+    const int largest = backward ? most : 2;
+    if (backward || dtype == GACT_DT_F32 || g != 8) {
+        while ((cols << shift) * 8 * size < 128 && (1u << shift) < a->units && a->unit_shift + shift < 6 &&
+               (uint64_t)a->B * gn_up(a->units, 2u << shift) >= 256) {
+            ++shift;
+            if (fits(kGnWhole[largest - 1])) continue;
+            --shift;
+            break;
+        }
+    }
     a->slab_shift = shift;
     a->col_shift = a->unit_shift + shift;
     a->unit_slabs = gn_up(a->units, 1u << shift);

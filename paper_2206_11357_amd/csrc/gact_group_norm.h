@@ -91,10 +91,15 @@ inline void plan_group_norm(GnArgs* a, int dtype) {
 struct GnWhole {
     uint32_t threads, blocks;
 };
-constexpr int kGnWholes = 3;
-constexpr GnWhole kGnWhole[kGnWholes] = {{256, 4}, {512, 8}, {1024, 8}};
-// Whether a sample's group fits the registers of a workgroup: which of them it is (0: of none, 1 ..), and how it is laid out.
-inline int plan_whole(GnArgs* a, int dtype, bool backward) {
+constexpr int kGnWholes = 4;
+constexpr GnWhole kGnWhole[kGnWholes] = {{256, 4}, {512, 8}, {1024, 8}, {512, 25}};
+// The last, of wavefronts with all the registers that two to a SIMD have: backward, from codes; fp32 without an activation, whose slope
+// would take more than there are.  Us by the others (64 bytes of a pixel, bf16 32) | by it (128, 64): 64 x 3136 x 256 fp32 131 | 113, with SiLU
+// 143 | 184, from x 188 | 192; 16 x 2304 x 512 bf16 36.1 | 25.6, 64 x 3136 x 256 bf16, SiLU 104 | 101.
+constexpr bool gn_held(int dtype, int bits, bool silu) { return bits != 0 && (dtype != GACT_DT_F32 || !silu); }
+// Whether a sample's group fits the registers of a workgroup: which of them it is (0: of none, 1 ..), and how it is laid out.  held:
+// the last may be it (which is never the one where there would be none without).
+inline int plan_whole(GnArgs* a, int dtype, bool backward, bool held) {
     uint32_t g = a->D, h = 8;                          // their greatest common divisor
     while (h) { const uint32_t t = g % h; g = h; h = t; }
     const uint32_t cols = a->D / g;                     // whole groups in whole columns
@@ -112,14 +117,14 @@ inline int plan_whole(GnArgs* a, int dtype, bool backward) {
     const auto fits = [&](const GnWhole& w) { return (uint64_t)a->P << (a->unit_shift + shift) <= (uint64_t)w.threads * w.blocks; };
     // (Groups that are no whole columns take more registers than the largest has: 16 x 500 x 72 bf16 in 4 groups, 4 bits, 18.5 us
     // forward, 24.1 backward; in passes over memory 15.3 and 20.4.)
-    const int most = g == 8 ? kGnWholes : kGnWholes - 1;
+    const int most = g == 8 ? 3 : 2;
     while (!fits(kGnWhole[most - 1]) && shift > 0) --shift;
     if (!fits(kGnWhole[most - 1])) return 0;
     // A cache line of a pixel, where the workgroups still fill the GPU.  Us, 64 bytes | 128 | 256: backward, 2 and 4 bits, 64 x 1024 x 256 fp32
     // 39.0 | 29.6 | 27.2, 256 x 784 x 256 fp32 130 | 102 | 101, 64 x 1024 x 512 bf16 SiLU 48.8 | 39.7, 128 x 784 x 256 bf16 29.0 | 30.2 | 31.4;
     // forward 256 x 784 x 256 fp32 131 | 123, 64 x 1024 x 256 fp32 38.5 | 35.1, 128 x 256 x 640 bf16 in groups of 20 84 | 63, 64 x 196 x
     // 1024 bf16 19.3 | 24.6, in workgroups of twice the threads 128 x 1568 x 256 fp32 131 | 145.
-    const int largest = backward ? most : 2;
+    const int largest = !backward ? 2 : held && g == 8 ? kGnWholes : most;
     if (backward || dtype == GACT_DT_F32 || g != 8) {
         while ((cols << shift) * 8 * size < 128 && (1u << shift) < a->units && a->unit_shift + shift < 6 &&
                (uint64_t)a->B * gn_up(a->units, 2u << shift) >= 256) {
@@ -133,7 +138,7 @@ inline int plan_whole(GnArgs* a, int dtype, bool backward) {
     a->col_shift = a->unit_shift + shift;
     a->unit_slabs = gn_up(a->units, 1u << shift);
     a->norm_blocks = a->B * a->unit_slabs;
-    for (int k = 0; k < most; ++k) if (fits(kGnWhole[k])) return k + 1;
+    for (int k = 0; k < (largest > most ? largest : most); ++k) if (fits(kGnWhole[k])) return k + 1;
     return 0;
 }
 inline size_t gn_align(size_t v) { return (v + 15) & ~(size_t)15; }

@@ -339,6 +339,9 @@ struct GnInput {
     float mn, step;
     __device__ __forceinline__ void load(const GnArgs& a, uint32_t sample, uint32_t p, uint32_t c8) {
         dy = load8<DT>((const uint8_t*)a.dy.p, ((int64_t)sample * a.dy.sample + (int64_t)p * a.dy.pixel + (int64_t)c8 * 8) * kSize<DT>);
+        load_x(a, sample, p, c8);
+    }
+    __device__ __forceinline__ void load_x(const GnArgs& a, uint32_t sample, uint32_t p, uint32_t c8) {
         if constexpr (BITS != 0) {
             const uint32_t e = (sample * a.P + p) * a.C8 + c8;
             codes = load_codes<BITS>(a.packed + (uint64_t)e * BITS);
@@ -871,6 +874,139 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_backward_ker
         store8<DT>((uint8_t*)a.dx.p, (out + (int64_t)p * a.dx.pixel) * kSize<DT>, dz[i]);
     }
 }
+// The same for larger maps: few wavefronts with many registers each, which hold dy as it came, all of it on its way at once; x is
+// loaded kAhead pixels ahead, both times.
+template <int DT, int BITS, bool SILU>
+__global__ __launch_bounds__(kGnWhole[3].threads) void gn_held_backward_kernel(GnArgs a) {
+    constexpr int NT = (int)kGnWhole[3].threads, R = (int)kGnWhole[3].blocks, kAhead = 4;
+    __shared__ float lds[NT / 64][64 * 16];
+    __shared__ float total[64 * 16];
+    __shared__ float of_column[64][2];
+    const WholePlace at(a, NT);
+    const uint32_t c = at.c8 * 8u;
+    const int cols = 1 << a.col_shift;
+    // lanes that hold nothing go through pixel 0 of column 0 without a part in the sums
+    const uint32_t c8 = at.holds ? at.c8 : 0;
+    const auto inside = [&](uint32_t p) { return p < a.P ? p : 0u; };
+    // (an empty statement keeps the compiler from holding all addresses in registers)
+    const auto step = [&](uint32_t& p) {
+        p += at.rows;
+        asm("" : "+v"(p));
+    };
+    uint32_t p = at.row;
+    Raw<DT> dy[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        dy[i] = load8<DT>((const uint8_t*)a.dy.p, ((int64_t)at.sample * a.dy.sample + (int64_t)inside(p) * a.dy.pixel + (int64_t)c8 * 8) * kSize<DT>);
+        step(p);
+    }
+    float w[8], b[8], s[16];
+    load_channels(a.w, a.w_f32, 1.0f, c8 * 8u, w);
+    load_channels(a.b, a.w_f32, 0.0f, c8 * 8u, b);
+    OfGroups<true> m, r;
+    m.load(a, a.mean + (size_t)at.sample * a.H, 1, c8 * 8u);
+    r.load(a, a.rstd + (size_t)at.sample * a.H, 1, c8 * 8u);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s[k] = 0.0f;
+    GnInput<DT, BITS> in[kAhead];
+    p = at.row;
+    uint32_t next = at.row;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        in[i].load_x(a, at.sample, inside(next), c8);
+        step(next);
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        float n[8], dz[8];
+        GnInput<DT, BITS>& now = in[i % kAhead];
+        now.dy = dy[i];
+        now.template take<true, SILU>(m, r, w, b, n, dz);
+        if (i + kAhead < R) now.load_x(a, at.sample, inside(next), c8);
+        step(next);
+        const bool counts = at.holds && p < a.P;
+        step(p);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float v = counts ? dz[k] : 0.0f, u = counts ? n[k] : 0.0f;
+            s[k] += v;
+            s[8 + k] = __builtin_fmaf(v, u, s[8 + k]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    for (int mask = cols; mask < 64; mask <<= 1)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s[k] += __shfl_xor(s[k], mask);
+    if (at.lane < cols) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) lds[at.wave][at.lane * 16 + k] = s[k];
+    }
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < cols * 16; i += NT) {
+        float v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NT / 64; ++k) v += lds[k][i];
+        total[i] = v;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < cols) {
+        float t0 = 0.0f, t1 = 0.0f;
+        if (at.holds) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                t0 = __builtin_fmaf(w[k], total[threadIdx.x * 16 + k], t0);
+                t1 = __builtin_fmaf(w[k], total[threadIdx.x * 16 + 8 + k], t1);
+            }
+        }
+        of_column[threadIdx.x][0] = t0;
+        of_column[threadIdx.x][1] = t1;
+    }
+    __syncthreads();
+    const uint32_t first = at.col & ~((1u << a.unit_shift) - 1u);
+    float m1 = 0.0f, m2 = 0.0f;
+    for (uint32_t k = 0; k < a.unit_cols; ++k) {
+        m1 += of_column[first + k][0];
+        m2 += of_column[first + k][1];
+    }
+    const float inv = 1.0f / ((float)a.P * (float)a.D);
+    m1 *= inv;
+    m2 *= inv;
+    if (!at.holds) return;
+    if ((a.dw || a.db) && at.row == 0) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float db = total[at.col * 16 + k], dw = total[at.col * 16 + 8 + k];
+            if (a.B == 1) {
+                gn_put(a, a.dw, c + (uint32_t)k, dw);
+                gn_put(a, a.db, c + (uint32_t)k, db);
+            } else {
+                *(hf2*)(a.sums + ((size_t)at.sample * a.C + c + (uint32_t)k) * 2) = hf2{db, dw};
+            }
+        }
+    }
+    const int64_t out = (int64_t)at.sample * a.dx.sample + c;
+    p = next = at.row;
+    asm("" : "+v"(p), "+v"(next));
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        in[i].load_x(a, at.sample, inside(next), c8);
+        step(next);
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        float n[8], dz[8];
+        GnInput<DT, BITS>& now = in[i % kAhead];
+        now.dy = dy[i];
+        now.template take<true, SILU>(m, r, w, b, n, dz);
+        if (i + kAhead < R) now.load_x(a, at.sample, inside(next), c8);
+        step(next);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dz[k] = r[k] * __builtin_fmaf(-n[k], m2, __builtin_fmaf(dz[k], w[k], -m1));
+        if (p < a.P) store8<DT>((uint8_t*)a.dx.p, (out + (int64_t)p * a.dx.pixel) * kSize<DT>, dz);
+        step(p);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
 __global__ __launch_bounds__(kGnThreads) void gn_weights_kernel(GnArgs a) {
     __shared__ double lds[2][kGnThreads];
     gn_weights(a, blockIdx.x, lds);
@@ -924,12 +1060,20 @@ static void gn_launch_whole(bool backward, const GnArgs& a, hipStream_t s) {
         if (a.B > 1 && (a.dw || a.db)) hipLaunchKernelGGL(gn_weights_kernel, dim3((a.C + 31) / 32), dim3(kGnThreads), 0, s, a);
     }
 }
+template <int DT, int BITS, bool SILU>
+static void gn_launch_held(const GnArgs& a, hipStream_t s) {
+    hipLaunchKernelGGL((gn_held_backward_kernel<DT, BITS, SILU>), dim3(a.norm_blocks), dim3(kGnWhole[3].threads), 0, s, a);
+    if (a.B > 1 && (a.dw || a.db)) hipLaunchKernelGGL(gn_weights_kernel, dim3((a.C + 31) / 32), dim3(kGnThreads), 0, s, a);
+}
 template <int DT, int BITS, bool UNI, bool SILU>
 static void gn_launch_sized(bool backward, const GnArgs& a, int whole, hipStream_t s) {
     if (whole == 0) gn_launch<DT, BITS, UNI, SILU>(backward, a, s);
     else if (whole == 1) gn_launch_whole<DT, BITS, UNI, SILU, 0>(backward, a, s);
     else if (whole == 2) gn_launch_whole<DT, BITS, UNI, SILU, 1>(backward, a, s);
-    else if constexpr (UNI) gn_launch_whole<DT, BITS, UNI, SILU, 2>(backward, a, s);
+    else if constexpr (UNI) {
+        if (whole == 3) gn_launch_whole<DT, BITS, UNI, SILU, 2>(backward, a, s);
+        else if constexpr (gn_held(DT, BITS, SILU)) gn_launch_held<DT, BITS, SILU>(a, s);
+    }
 }
 template <int DT, int BITS>
 static void gn_launch_form(bool backward, const GnArgs& a, int act, int whole, hipStream_t s) {

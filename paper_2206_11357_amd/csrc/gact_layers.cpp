@@ -126,7 +126,7 @@ int stage_norm(const gact_channel_norm* h, bool backward, void* ws, size_t ws_by
     }
     if (*bits != 0) while ((8 << a->block_shift) < G) ++a->block_shift;
     norm_sizes(h->batch, h->pixels, h->channels, h->groups, h->dtype, a);
-    *whole = gact::plan_whole(a, h->dtype, backward);
+    *whole = gact::plan_whole(a, h->dtype, backward, gact::gn_held(h->dtype, *bits, h->act == GACT_ACT_SILU));
     // (4096: workgroups that compress, and those that add dw)
     const uint64_t B = a->B;
     if (*whole ? !gact::launchable(B * a->unit_slabs + 4096, gact::kGnWhole[*whole - 1].threads)
@@ -160,7 +160,7 @@ size_t gact_group_norm_workspace_bytes(int64_t batch, int64_t pixels, int channe
     if (!norm_sizes_ok(batch, pixels, channels, groups) || !dtype_ok((int)dtype) || batch == 0 || pixels == 0) return 0;
     gact::GnArgs a{};
     norm_sizes(batch, pixels, channels, groups, (int)dtype, &a);
-    const int whole = gact::plan_whole(&a, (int)dtype, backward != 0);
+    const int whole = gact::plan_whole(&a, (int)dtype, backward != 0, false);
     return backward ? gact::gn_backward_bytes(a, whole) : gact::gn_forward_bytes(a, whole);
 }
 

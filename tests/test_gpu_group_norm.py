@@ -298,3 +298,16 @@ def test_gradients_against_differences():
 def test_groups_of_any_size(B, P, C, H, dtype):
     check_step(B, P, C, H, 4, 64, "silu", DTYPES[dtype])
     check_step(B, P, C, H, RAW, 0, "none", DTYPES[dtype], None if H % 2 else torch.float32, wide=8)
+
+
+# maps whose backward pass holds dy in the workgroups of the most registers: groups of one column and of two, a last slab of one, and
+# outputs in place of dy
+@pytest.mark.parametrize("B,P,C,H,bits,G,act,dtype", [(32, 2060, 264, 33, 2, 256, "none", "f32"), (64, 2111, 128, 8, 4, 64, "silu", "bf16")])
+def test_step_of_many_large_maps(B, P, C, H, bits, G, act, dtype):
+    check_step(B, P, C, H, bits, G, act, DTYPES[dtype])
+    x, dy, w, b = inputs(B, P, C, DTYPES[dtype], torch.float32)
+    context = gact.make_group_norm_context(x, H, bits, G, 3)
+    gact.gact_group_norm(x, H, w, b, 1e-5, act, context=context)
+    first = gact.gact_group_norm_backward(dy, H, w, b, act, context=context)
+    again = gact.gact_group_norm_backward(dy, H, w, b, act, context=context, out=dy)
+    assert again[0] is dy and all(torch.equal(u, v) for u, v in zip(first, again))

@@ -109,11 +109,13 @@ inline int plan_whole(GnArgs* a, int dtype, bool backward, bool held) {
     while ((1u << a->unit_shift) < cols) ++a->unit_shift;
     if (a->unit_shift > 6) return 0;
     // 64 bytes of a pixel at least, if they fit.  Us, step of 32 x 1024 x 512 bf16, 4 bits, forward + backward, by bytes: 32 29.1 + 27.8,
-    // 64 26.2 + 22.6, 128 (twice the threads) 29.7 + 21.9; of 64 x 3136 x 256 fp32, 2 bits 32 162 + 170, 64 (the most) 136 + 131.
+    // 64 26.2 + 22.6, 128 (twice the threads) 29.7 + 21.9; of 64 x 3136 x 256 fp32, 2 bits 32 162 + 170, 64 136 + 131.
     const uint32_t size = dtype == GACT_DT_F32 ? 4 : 2;
     uint32_t shift = 0;
     // (and where there are few pixels, columns enough for the threads)
-    while (((cols << shift) * 8 * size < 64 || (uint64_t)a->P << (a->unit_shift + shift) < kGnWhole[0].threads) && (1u << shift) < a->units && a->unit_shift + shift < 6) ++shift;
+    while (((cols << shift) * 8 * size < 64 || (uint64_t)a->P << (a->unit_shift + shift) < kGnWhole[0].threads) &&
+           (1u << shift) < a->units && a->unit_shift + shift < 6)
+        ++shift;
     const auto fits = [&](const GnWhole& w) { return (uint64_t)a->P << (a->unit_shift + shift) <= (uint64_t)w.threads * w.blocks; };
     // (Groups that are no whole columns take more registers than the largest has: 16 x 500 x 72 bf16 in 4 groups, 4 bits, 18.5 us
     // forward, 24.1 backward; in passes over memory 15.3 and 20.4.)

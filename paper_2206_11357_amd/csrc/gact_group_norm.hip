@@ -12,9 +12,9 @@
 // (T. Chan, G. Golub, R. LeVeque 1979), so that nothing cancels.  Backward: sums of dz and dz n over the pixels for each
 // channel and sample, from which the groups' means and dw, db follow; then dx.
 // Where a sample's group fits a workgroup's registers, both are one pass over memory (and dw, db a second launch where there
-// are several samples).  Measured, us: 64 x 3136 x 256 fp32, 2 bits, held 133 forward, 129 backward (HBM: 631 and 441 MB as
+// are several samples).  Measured, us: 64 x 3136 x 256 fp32, 2 bits, held 133 forward, 112 backward (HBM: 631 and 449 MB as
 // counted, x a second time for its codes); 32 x 1024 x 512 bf16, SiLU, 4 bits, held 25.6 (the arithmetic of noise, rounding and
-// activation) and 21.0; 1 x 262144 x 128 bf16, SiLU, in passes 13.6 + 4.4 + 26.7 (reads at 4.9 TB/s).
+// activation) and 19.9; 1 x 262144 x 128 bf16, SiLU, in passes 13.6 + 4.4 + 26.7 (reads at 4.9 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

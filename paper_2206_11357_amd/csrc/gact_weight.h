@@ -81,9 +81,9 @@ inline WeightPlan weight_splits(uint64_t T, uint64_t N, uint64_t K, int dtype, i
     const uint64_t tiles = (uint64_t)p.tiles_n * p.tiles_k, chunks = weight_up(T, (uint64_t)tile.tokens);
     const uint64_t fill = form == kWeightSmall ? 512 : 256;
     uint64_t splits = tiles >= fill ? 1 : fill / tiles;
-    // A second launch costs as much as a few chunks, of which those whose blocks of eight are no whole bytes take longer.  Us, 4 bits, one split | splits of two
-    // chunks: 1024 x 512 x 512 bf16 9.1 | 11.3 (8 chunks), 1044 x 22 x 3632 bf16 10.6 | 12.3 (9), 1500 x 20 x 500 bf16 18.6 | 11.1 (12),
-    // 300 x 256 x 256 fp32 8.6 | 9.9 (5); 3063 x 48 x 200 bf16, of four | two 11.0 | 10.2
+    // A second launch costs as much as a few chunks, of which those whose blocks of eight are no whole bytes take longer.  Us, 4 bits,
+    // one split | splits of two chunks: 1024 x 512 x 512 bf16 9.1 | 11.3 (8 chunks), 1044 x 22 x 3632 bf16 10.6 | 12.3 (9), 1500 x 20 x
+    // 500 bf16 18.6 | 11.1 (12), 300 x 256 x 256 fp32 8.6 | 9.9 (5); 3063 x 48 x 200 bf16, of four | two 11.0 | 10.2
     const uint64_t few = dtype == GACT_DT_F32 ? 6 : K % 8 == 0 ? 12 : 8, most = chunks <= few ? 1 : chunks / 2;
     if (splits > most) splits = most;
     // a split's codes lie within kWeightReach

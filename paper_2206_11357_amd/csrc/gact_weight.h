@@ -24,6 +24,10 @@ constexpr WeightTile weight_tile(int dtype, int form) {
          : form == kWeightLong ? WeightTile{64, 64, 4 * team, 1024}
          : form == kWeightWide ? WeightTile{32, 128, 4 * team, 1024} : WeightTile{128, 32, 4 * team, 1024};
 }
+// The chunk that a block of the large forms fetches for chunk `chunk` of a split that ends in front of chunk `end`: behind the last one
+// the last again.  Loads take the chunk's distance as the wavefront's offset; what a buffer's end does to one that is itself behind it
+// is not asked for.
+__host__ __device__ constexpr uint32_t weight_fetched(uint32_t chunk, uint32_t end) { return chunk < end ? chunk : end - 1; }
 // Chunks that a block of the small forms has on their way.
 constexpr uint32_t weight_depth(int form, bool even) { return even || form == kWeightSmall || form == kWeightLong ? 4 : 2; }
 
@@ -53,7 +57,7 @@ struct WeightArgs {
 //   buffer  dy's rows as words of a buffer: their elements pair up to words, and a split's lie within 2^31 bytes
 //   even    blocks of eight elements of x are whole bytes of one group, and a chunk's tokens are whole groups
 constexpr uint64_t kWeightReach = 1ull << 31;
-inline uint64_t weight_span(const WeightArgs& a, int dtype, int form) {      // tokens of a split, and of what is fetched behind its last
+inline uint64_t weight_span(const WeightArgs& a, int dtype, int form) {      // tokens of a split, and room for what its last rows' loads pass
     return ((uint64_t)a.chunks + 4) * (uint64_t)weight_tile(dtype, form).tokens;
 }
 inline bool weight_buffer(const WeightArgs& a, int dtype, int form) {

@@ -38,7 +38,8 @@ typedef short ws4 __attribute__((ext_vector_type(4)));
 typedef __bf16 wb8 __attribute__((ext_vector_type(8)));
 
 // ---------------------------------------------------------------- buffer loads
-// From a buffer of so many bytes, at an offset of the lane's and one of the wavefront's; words behind its end are zero.
+// From a buffer of so many bytes, at an offset of the lane's and one of the wavefront's, which lies inside; words behind its end are
+// zero.
 typedef __amdgpu_buffer_rsrc_t Buffer;
 __device__ __forceinline__ Buffer buffer_of(const void* p, uint64_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(uint32_t)(bytes < 0x80000000ull ? bytes : 0x80000000ull), 0x00027000);
@@ -421,6 +422,7 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
         db_next += a.db_every;
         return true;
     };
+    const auto fetched = [&](uint32_t chunk) { return weight_fetched(chunk, c1); };
     if (c0 < c1) {
         const Load load(a, n0, k0, c0);
         if constexpr (FORM == kWeightLarge && Prod::kSteps == 1) {
@@ -431,7 +433,7 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
             load.fetch(slot, c0);
             if (adds(c0)) load.add_db(slot, sum);
             load.place(slot, lds[0]);
-            load.fetch(slot, c0 + 1);
+            load.fetch(slot, fetched(c0 + 1));
             for (uint32_t c = c0; c < c1; ++c) {
                 __syncthreads();
                 prod.read(lds[0], 0, x, y);
@@ -445,7 +447,7 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
 #pragma unroll
                     for (int q = i * L::kPieces / TN; q < (i + 1) * L::kPieces / TN; ++q) {
                         load.place_dy(slot, lds[0], q);
-                        load.fetch_dy(slot, c + 2, q);
+                        load.fetch_dy(slot, fetched(c + 2), q);
                     }
 #pragma unroll
                     for (int e = i * kValues / TN; e < (i + 1) * kValues / TN; ++e) {
@@ -453,7 +455,7 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
                         v[e / 8][e % 8] = slot.codes[e / 8].value(e % 8);
                         if (e % 8 == 7) {
                             load.place_x(lds[0], e / 8, v[e / 8]);
-                            load.fetch_x(slot, c + 2, e / 8);
+                            load.fetch_x(slot, fetched(c + 2), e / 8);
                         }
                     }
                     __builtin_amdgcn_sched_barrier(0);
@@ -465,7 +467,7 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
             // step and leave the matrix unit idle together.  A step's operands are read during the step before it, so that
             // all of a chunk's have been read by the beginning of its last step; there the one barrier of a chunk stands: behind
             // it chunk c + 1 is whole, and the place of chunk c is free.  Without a question, also behind the split's last
-            // chunk, where nothing is read outside the buffers and nothing uses what is placed.
+            // chunk, for which the last is fetched again (weight_fetched); nothing uses what is placed then.
             constexpr int kSteps = Prod::kSteps, kSlots = (kSteps - 1) * TN;
             constexpr int kEarly = kSteps == 2 ? L::kBlocks / 2 : 0, kValues = 8 * (L::kBlocks - kEarly);
             typename Load::S slot;
@@ -480,11 +482,11 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
             load.fetch(slot, c0);
             if (adds(c0)) load.add_db(slot, sum);
             load.place(slot, lds[0]);
-            load.fetch(slot, c0 + 1);
+            load.fetch(slot, fetched(c0 + 1));
             __syncthreads();
             prod.read(lds[0], 0, x[0], y[0]);
 #pragma unroll
-            for (int e = 0; e < 8 * kEarly; ++e) decode(c0 + 2, e);
+            for (int e = 0; e < 8 * kEarly; ++e) decode(fetched(c0 + 2), e);
             for (uint32_t c = c0; c < c1; ++c) {
                 const uint32_t now = (c - c0) & 1u;
                 const uint8_t* buf = lds[now];
@@ -503,14 +505,14 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
                             if (at == q) load.place_x(other, q, v[q]);
 #pragma unroll
                         for (int e = at * kValues / kSlots; e < (at + 1) * kValues / kSlots; ++e) {
-                            decode(c + 2, 8 * kEarly + e);
+                            decode(fetched(c + 2), 8 * kEarly + e);
                             if (e % 8 == 7) load.place_x(other, kEarly + e / 8, v[kEarly + e / 8]);
                         }
 #pragma unroll
                         for (int q = 0; q < L::kPieces; ++q)
                             if (at == q * kSlots / L::kPieces) {
                                 load.place_dy(slot, other, q);
-                                load.fetch_dy(slot, c + 2, q);
+                                load.fetch_dy(slot, fetched(c + 2), q);
                             }
                         __builtin_amdgcn_sched_barrier(0);
                     }
@@ -521,7 +523,7 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
                     if (i == 0) prod.read_k(other, 0, y[0]);
                     prod.read_n(other, 0, i, x[0]);
 #pragma unroll
-                    for (int e = i * 8 * kEarly / TN; e < (i + 1) * 8 * kEarly / TN; ++e) decode(c + 3, e);
+                    for (int e = i * 8 * kEarly / TN; e < (i + 1) * 8 * kEarly / TN; ++e) decode(fetched(c + 3), e);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }

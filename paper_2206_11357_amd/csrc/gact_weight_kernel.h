@@ -135,7 +135,7 @@ struct Tiling {
 // Where a wavefront's operands lie in a chunk, and its products.  A step is 16 tokens; 16 lanes read 4 rows of 16 elements, of which
 // each gets a column.
 //   fp32  An element is the sum of three bf16, each the rounded rest of the ones before: 8 bits and a sign each, exactly (an infinity,
-//         and what bf16 rounds to one, leaves NaN).  Of the nine products of their parts the six largest are taken.  The second part is
+//         and what bf16 rounds to one, leaves NaN, of which weight_element makes what it has to be).  Of the nine products of their parts the six largest are taken.  The second part is
 //         at most 2^-8 of the element and the third 2^-17, so that the others come to at most 2^-24 of a product, as much as its
 //         rounding to binary32 would; sums are binary32.  Six products of bf16 take 6 x 32 cycles of the matrix unit for 16 tokens, eight
 //         of fp32 8 x 64: 169343 x 256 x 256 takes 124 us with the sums' addition, 184 in fp32, and comes closer to the sum in 64 bits
@@ -401,6 +401,23 @@ struct Loader {
     }
 };
 
+// An element of dW over the tokens t .. end - 1 in binary32.  What bfloat16 has no number for, an infinity and elements from
+// 2^128 - 2^119 on, leaves an infinity and its rest of the other sign in the parts, and so NaN in the sums: those that are not finite
+// are added again, one by one.  Ms, 169343 x 256 x 256 from Python: 0.13 with none, 0.7 with a NaN in dy, which is in a row of dW, 28 with
+// nothing else.  (As a function that is called it leaves no kernel its registers: 18 to 179 spilled in the large form.)
+template <int BITS>
+__device__ __forceinline__ float weight_element(const WeightArgs& a, uint32_t t, uint32_t end, uint32_t n, uint32_t k) {
+    float s = 0.0f;
+    for (; t < end; ++t) {
+        const uint64_t e = (uint64_t)t * a.K + k;
+        const uint32_t g = divided((uint32_t)(e >> 5), a.by_group), bit = (uint32_t)(e % 8) * BITS;
+        const uint32_t q = a.packed[(e >> 3) * BITS + (bit >> 3)] >> (bit & 7u) & ((1u << BITS) - 1u);
+        const float x = (float)q * a.gscale[g];
+        s = __builtin_fmaf(((const float*)a.dy)[(int64_t)t * a.dy_stride + n], x + a.gmin[g], s);
+    }
+    return s;
+}
+
 template <int DT, int BITS, int FORM, bool BUFFER, bool EVEN>
 __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM).threads == 1024 ? 4 : 2) void weight_kernel(WeightArgs a) {
     typedef Tiling<DT, FORM> L;
@@ -624,6 +641,8 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
     // of a lane: row, column, and their elements; of row r of products i: what all lanes add to them
     const uint32_t lane_n = n0 + (uint32_t)(wn * 32 * TN + first * 32 + 4 * low);
     const uint32_t lane_k = k0 + (uint32_t)(wk * 32 * TK + at_k);
+    static_assert(kMine * 16 * TK <= 64, "a bit for each of a lane's elements");
+    uint64_t again = 0;                                // those that are not finite (weight_element)
     const auto put = [&](auto* to) {
         typedef typename std::remove_pointer<decltype(to)>::type Out;
         to += (size_t)lane_n * a.K + lane_k;
@@ -640,6 +659,7 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
                     if (!inside && lane_k + k >= a.K) continue;
                     if constexpr (sizeof(Out) == 4) p[k] = acc[i][j][r];
                     else p[k] = (Out)bf16_pair_rne(acc[i][j][r], 0.0f);
+                    if (DT == GACT_DT_F32 && !__builtin_isfinite(acc[i][j][r])) again |= 1ull << ((i * 16 + r) * TK + j);
                 }
             }
     };
@@ -647,6 +667,18 @@ __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM
         if (!whole) put(a.partial + (size_t)split * a.N * a.K);
         else if (a.w_f32) put((float*)a.dw);
         else put((uint16_t*)a.dw);
+        if constexpr (DT == GACT_DT_F32) {
+            const uint32_t end = c1 * L::BT < a.T ? c1 * L::BT : a.T;
+            for (; __builtin_expect(again != 0, 0); again &= again - 1) {
+                const uint32_t bit = (uint32_t)__builtin_ctzll(again), j = bit % TK, r = bit / TK % 16u, i = bit / (TK * 16u);
+                const uint32_t n = lane_n + i * 32 + (r & 3u) + 8 * (r >> 2), k = lane_k + j * 32;
+                const float v = weight_element<BITS>(a, c0 * L::BT, end, n, k);
+                const size_t at = (size_t)n * a.K + k;
+                if (!whole) a.partial[(size_t)split * a.N * a.K + at] = v;
+                else if (a.w_f32) ((float*)a.dw)[at] = v;
+                else ((uint16_t*)a.dw)[at] = (uint16_t)bf16_pair_rne(v, 0.0f);
+            }
+        }
     }
 
     if (L::kTeams > 1) __syncthreads();

@@ -53,3 +53,43 @@ def test_an_infinity_that_was_compressed(T, N, K, G, dtype):
     clean, _ = gact.gact_linear_weight_grad(dy, *context, K, G, 4, w_dtype=torch.float32)
     dw, _ = gact.gact_linear_weight_grad(dy, *poisoned, K, G, 4, w_dtype=torch.float32)
     assert torch.equal(dw[:, ~bad], clean[:, ~bad]) and not torch.isfinite(dw[:, bad]).any()
+
+
+# every form again
+FORMS = [(1, 130, 72), (64, 100, 100), (2000, 24, 200), (2000, 200, 24), (3001, 130, 104), (19000, 512, 512), (19001, 510, 501)]
+
+
+@pytest.mark.parametrize("w_dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,K", FORMS)
+def test_binary32_sums_as_binary32_has_them(T, N, K, w_dtype):
+    """Infinities keep their sign where no infinity is against them, zeros and infinities make NaN, and elements that bfloat16 has
+    no number for (from 2^128 - 2^119 on) count as they are."""
+    G, bits = 64, 2
+    gen = torch.Generator(device="cuda").manual_seed(T + N)
+    x = torch.rand(T, K, generator=gen, device="cuda") * 0.5 + 0.25
+    x.view(-1)[torch.arange(0, T * K, G, device="cuda")] = 0.0                    # minima: code 0 is zero
+    context = gact.gact_compress(x, G, bits, 3)
+    if T > 1:
+        context[1][-1] = -float("inf")
+    dy = torch.randn(T, N, generator=gen, device="cuda")
+    dy[T // 2, 3], dy[T // 3, 9], dy[T - 1, 11] = float("nan"), float("inf"), -float("inf")
+    dy[0, 15], dy[T // 2, 17], dy[T - 1, 17] = 3.4e38, -3.4e38, float("inf") if T > 1 else -3.4e38
+    dw, db = gact.gact_linear_weight_grad(dy, *context, K, G, bits, w_dtype=DTYPES[w_dtype], bias=True)
+    back = gact.gact_decompress(*context, T * K, G, bits).view(T, K).cpu().double()
+    d = dy.cpu().double()
+    bad = ~torch.isfinite(back).all(0)
+    size = d.abs().t() @ back.abs()
+    want = d.t() @ back
+    got = dw.cpu().double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    # a bfloat16 dW has no number for sums within half a step of 2^128
+    sure = torch.isinf(want)
+    assert torch.equal(got[sure], want[sure])
+    # T products and additions of binary32, each off by 2^-23 of the terms' sizes at most (in matrix products that cut), and the output's half step
+    half = 2.0 ** -24 if w_dtype == "f32" else 2.0 ** -8
+    fine = torch.isfinite(want) & (size < 3.38e38)
+    bound = half * want.abs() + (T + 2) * 2.0 ** -23 * size * (1 + half) + 2.0 ** -126
+    assert ((got - want).abs() <= bound)[fine].all()
+    assert torch.isnan(want[3]).all()
+    if not bad.all():                                   # (24 columns are all in the last group)
+        assert fine[15].sum() >= (K - bad.sum()) // 2 and torch.isinf(want[9]).any()

@@ -327,12 +327,16 @@ class Controller:
         return (torch.is_grad_enabled() and x.is_cuda and x.requires_grad and x.numel() >= self.min_numel
                 and x.dtype in (torch.float32, torch.bfloat16))
 
-    def _number(self, x: torch.Tensor):
-        """Makes x the scheme's next context tensor; its width and seed."""
+    def _numbered(self, x: torch.Tensor, call):
+        """call(width, seed) of x as the scheme's next context tensor; a call that raises leaves the scheme as it was."""
         index = len(self._handles)
         self._handles.append(None)
         self.numel.append(x.numel())
-        return self.bits_of(index), self.seed_of(index)
+        try:
+            return call(self.bits_of(index), self.seed_of(index))
+        except BaseException:
+            del self._handles[index:], self.numel[index:]
+            raise
 
     def linear(self, x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None) -> torch.Tensor:
         """``layers.linear`` whose context is part of the scheme: x is a context tensor l like those of the hooks, with width b_l,
@@ -341,11 +345,13 @@ class Controller:
         hooks would not compress (size, type, no gradient), or a weight without a gradient, is left to autograd."""
         if not (self._takes(x) and weight.requires_grad) or x.dim() < 2 or torch.is_autocast_enabled("cuda"):
             return torch.nn.functional.linear(x, weight, bias)
-        bits, seed = self._number(x)
-        if bits == GACT_BITS_UNCOMPRESSED:
-            with torch.autograd.graph.saved_tensors_hooks(_itself, _itself):      # numbered already
-                return torch.nn.functional.linear(x, weight, bias)
-        return layers.linear(x, weight, bias, bits, self.group_size, seed, _own=True)
+
+        def call(bits, seed):
+            if bits == GACT_BITS_UNCOMPRESSED:
+                with torch.autograd.graph.saved_tensors_hooks(_itself, _itself):      # numbered already
+                    return torch.nn.functional.linear(x, weight, bias)
+            return layers.linear(x, weight, bias, bits, self.group_size, seed, _own=True)
+        return self._numbered(x, call)
 
     def group_norm(self, x: torch.Tensor, groups: int, w: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,
                    eps: float = 1e-5, act: str = "none") -> torch.Tensor:
@@ -357,8 +363,7 @@ class Controller:
             return layers.group_norm(x, groups, w, b, eps, act)
         if not group_norm_context_fits(self.group_size, x.shape[-1]):
             return layers.group_norm(x.contiguous(), groups, w, b, eps, act)
-        bits, seed = self._number(x)
-        return layers.group_norm(x, groups, w, b, eps, act, bits, self.group_size, seed, _own=True)
+        return self._numbered(x, lambda bits, seed: layers.group_norm(x, groups, w, b, eps, act, bits, self.group_size, seed, _own=True))
 
     def clip_grad_norm_(self, params: Union[torch.Tensor, Iterable[torch.Tensor]], max_norm: float,
                         norm_type: float = 2.0) -> torch.Tensor:

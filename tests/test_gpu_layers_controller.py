@@ -1,0 +1,39 @@
+"""What a controller's layers do with inputs that they do not take as they are."""
+import pytest
+import torch
+
+import paper_2206_11357_amd as gact
+from paper_2206_11357_amd.hooks import Controller
+
+pytestmark = pytest.mark.gpu
+
+
+def refused_calls():
+    x = torch.randn(2, 9, 64, device="cuda", requires_grad=True)
+    odd = torch.randn(2, 9, 60, device="cuda", requires_grad=True)
+    w = torch.randn(16, 64, device="cuda", requires_grad=True)
+    n = torch.ones(64, device="cuda", requires_grad=True)
+    return [lambda c: c.group_norm(odd, 4), lambda c: c.group_norm(x, 7), lambda c: c.group_norm(x, 8, n[:32]),
+            lambda c: c.group_norm(x, 8, n, act="relu"), lambda c: c.group_norm(x, 8, n, eps=-1.0), lambda c: c.group_norm(x.view(18, 64), 8),
+            lambda c: c.linear(x, w[:, :32]), lambda c: c.linear(x, w.bfloat16()), lambda c: c.linear(x, w, n)]
+
+
+@pytest.mark.parametrize("bits", [4, gact.GACT_BITS_UNCOMPRESSED])
+@pytest.mark.parametrize("which", range(9))
+def test_a_refused_call_leaves_the_scheme_as_it_was(which, bits):
+    """The context tensors behind it keep their numbers, and with them their widths and seeds."""
+    ctl = Controller(group_size=64, bits=bits, min_numel=64)
+    ctl.begin_iteration()
+    with ctl.hooks():
+        with pytest.raises((ValueError, RuntimeError)):
+            refused_calls()[which](ctl)
+        assert ctl.numel == [] and ctl._handles == []
+        x = torch.randn(2, 9, 64, device="cuda", requires_grad=True)
+        y = ctl.group_norm(x, 8)
+    assert ctl.numel == [x.numel()] and len(ctl._handles) == 1
+    other = Controller(group_size=64, bits=bits, min_numel=64)
+    other.begin_iteration()
+    with other.hooks():
+        z = other.group_norm(x, 8)
+    g = torch.randn_like(y)
+    assert torch.equal(*(torch.autograd.grad(t, x, g)[0] for t in (y, z)))

@@ -26,7 +26,7 @@ from torch.multiprocessing.reductions import StorageWeakRef
 from . import (GACT_BITS_UNCOMPRESSED, GACT_OK, GactError, TensorDesc, dtype_code, gact_allocate_bits_levels,
                gact_copy_bounded, gact_grad_clip, head_context_fits,
                gact_multi_workspace_bytes, gact_num_groups, gact_packed_bytes, gact_sensitivity, lib)
-from . import group_norm_context_fits, layers
+from . import _map_strides, group_norm_context_fits, layers
 from .heads import _itself, head_norm_rotate
 
 _MASK64 = (1 << 64) - 1
@@ -358,7 +358,9 @@ class Controller:
         """``layers.group_norm`` whose context is part of the scheme: x is a context tensor l like those of the hooks, but
         compressed by the forward call and read by the backward kernels as codes; its buffers stay on the device.  Where the
         controller's group size does not fit (``group_norm_context_fits``) x goes to the hooks as any saved tensor does,
-        copied first where it is a slice; one that the hooks would not compress (size, type) is left to autograd."""
+        copied first where it is a slice; one that the hooks would not compress (size, type) is left to autograd.  Pixels that
+        are not evenly spaced are laid out first."""
+        x = layers._laid_out(x, _map_strides)
         if not self._takes(x):
             return layers.group_norm(x, groups, w, b, eps, act)
         if not group_norm_context_fits(self.group_size, x.shape[-1]):

@@ -37,3 +37,25 @@ def test_a_refused_call_leaves_the_scheme_as_it_was(which, bits):
         z = other.group_norm(x, 8)
     g = torch.randn_like(y)
     assert torch.equal(*(torch.autograd.grad(t, x, g)[0] for t in (y, z)))
+
+
+@pytest.mark.parametrize("group_size", [64, 96])
+@pytest.mark.parametrize("bits", [8, gact.GACT_BITS_UNCOMPRESSED])
+def test_pixels_of_any_spacing(bits, group_size):
+    """A crop of a larger map, whose rows of pixels lie apart, is laid out first, as the linear layer lays out its input."""
+    big = torch.randn(2, 9, 11, 64, device="cuda", requires_grad=True)
+    n = torch.ones(64, device="cuda", requires_grad=True)
+    g = torch.randn(2, 5, 6, 64, device="cuda")
+    results = []
+    for lay in (lambda t: t, lambda t: t.contiguous()):
+        ctl = Controller([n], group_size=group_size, bits=bits, seed=3, min_numel=64)
+        ctl.begin_iteration()
+        with ctl.hooks():
+            y = ctl.group_norm(lay(big[:, 2:7, 3:9]), 8, n, act="silu")
+        assert ctl.numel == [2 * 5 * 6 * 64]
+        results.append((y, *torch.autograd.grad(y, (big, n), g)))
+    assert all(torch.equal(u, v) for u, v in zip(*results))
+    with torch.no_grad():
+        assert torch.equal(ctl.group_norm(big[:, 2:7, 3:9], 8, n, act="silu"), results[0][0])
+    small = Controller(group_size=64, bits=4, min_numel=1 << 20)
+    assert torch.equal(small.group_norm(big[:, 2:7, 3:9], 8, n, act="silu"), results[0][0]) and small.numel == []

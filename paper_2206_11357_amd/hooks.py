@@ -357,8 +357,8 @@ class Controller:
                    eps: float = 1e-5, act: str = "none") -> torch.Tensor:
         """``layers.group_norm`` whose context is part of the scheme: x is a context tensor l like those of the hooks, but
         compressed by the forward call and read by the backward kernels as codes; its buffers stay on the device.  Where the
-        controller's group size does not fit (``group_norm_context_fits``) x goes to the hooks as any saved tensor does,
-        copied first where it is a slice; one that the hooks would not compress (size, type) is left to autograd.  Pixels that
+        controller's group size is none that the pass can compress in (``group_norm_context_fits``) x goes to the hooks as any saved
+        tensor does, copied first where it is a slice; one that the hooks would not compress (size, type) is left to autograd.  Pixels that
         are not evenly spaced are laid out first."""
         x = layers._laid_out(x, _map_strides)
         if not self._takes(x):

@@ -117,7 +117,10 @@ def group_norm(x: torch.Tensor, groups: int, w: Optional[torch.Tensor] = None, b
                _own: bool = False) -> torch.Tensor:
     """``gact_group_norm`` with gradients for x, w and b.  bits: width of the context, in groups of group_size with the
     noise of `seed`; GACT_BITS_UNCOMPRESSED keeps x itself through autograd.  ``Controller.group_norm`` chooses them from its
-    scheme.  Reverse mode, once: forward-mode tangents and second derivatives are refused."""
+    scheme.  Reverse mode, once: forward-mode tangents and second derivatives are refused, and channels that are no multiple
+    of eight and of the groups."""
+    if groups < 1 or x.dim() == 0 or x.shape[-1] % 8 or x.shape[-1] % groups:
+        raise ValueError("the channels must be a multiple of eight and of the groups, got %s in %d groups" % (tuple(x.shape), groups))
     _refuse_tangents(x, w, b, of="group_norm")
     if not (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w, b))):
         return gact_group_norm(x, groups, w, b, eps, act)

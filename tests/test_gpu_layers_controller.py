@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2206_11357_amd as gact
+from paper_2206_11357_amd import layers
 from paper_2206_11357_amd.hooks import Controller
 
 pytestmark = pytest.mark.gpu
@@ -59,3 +60,18 @@ def test_pixels_of_any_spacing(bits, group_size):
         assert torch.equal(ctl.group_norm(big[:, 2:7, 3:9], 8, n, act="silu"), results[0][0])
     small = Controller(group_size=64, bits=4, min_numel=1 << 20)
     assert torch.equal(small.group_norm(big[:, 2:7, 3:9], 8, n, act="silu"), results[0][0]) and small.numel == []
+
+
+def test_channels_that_the_norm_does_not_take():
+    """No multiple of eight, or of the groups: refused by their name, by the controller too, whatever its group size."""
+    for group_size in (64, 96):
+        ctl = Controller(group_size=group_size, bits=4, min_numel=64)
+        ctl.begin_iteration()
+        for channels, groups in ((60, 4), (64, 7), (64, 0), (64, -8), (64, 128)):
+            x = torch.randn(2, 9, channels, device="cuda", requires_grad=True)
+            for call in (ctl.group_norm, layers.group_norm):
+                with ctl.hooks(), pytest.raises(ValueError, match="multiple of eight and of the groups"):
+                    call(x, groups)
+                with torch.no_grad(), pytest.raises(ValueError, match="multiple of eight and of the groups"):
+                    call(x, groups)
+        assert ctl.numel == []

@@ -325,7 +325,7 @@ class Controller:
     def _takes(self, x: torch.Tensor) -> bool:
         """Whether x, of any strides, is a context tensor that the scheme compresses."""
         return (torch.is_grad_enabled() and x.is_cuda and x.requires_grad and x.numel() >= self.min_numel
-                and x.dtype in (torch.float32, torch.bfloat16))
+                and x.dtype in (torch.float32, torch.bfloat16) and x.data_ptr() not in self.param_ptrs)
 
     def _numbered(self, x: torch.Tensor, call):
         """call(width, seed) of x as the scheme's next context tensor; a call that raises leaves the scheme as it was."""
@@ -342,7 +342,7 @@ class Controller:
         """``layers.linear`` whose context is part of the scheme: x is a context tensor l like those of the hooks, with width b_l,
         seed r_l and a place in Alg. 1 and Eq. (ilp), but read by the weight gradient's kernel as codes.  Its buffers stay on
         the device (they are not swapped), and an x that several layers share is compressed for each.  An x that the
-        hooks would not compress (size, type, no gradient), or a weight without a gradient, is left to autograd."""
+        hooks would not compress (size, type, no gradient, a parameter), or a weight without a gradient, is left to autograd."""
         if not (self._takes(x) and weight.requires_grad) or x.dim() < 2 or torch.is_autocast_enabled("cuda"):
             return torch.nn.functional.linear(x, weight, bias)
 
@@ -358,7 +358,7 @@ class Controller:
         """``layers.group_norm`` whose context is part of the scheme: x is a context tensor l like those of the hooks, but
         compressed by the forward call and read by the backward kernels as codes; its buffers stay on the device.  Where the
         controller's group size is none that the pass can compress in (``group_norm_context_fits``) x goes to the hooks as any saved
-        tensor does, copied first where it is a slice; one that the hooks would not compress (size, type) is left to autograd.  Pixels that
+        tensor does, copied first where it is a slice; one that the hooks would not compress (size, type, a parameter) is left to autograd.  Pixels that
         are not evenly spaced are laid out first."""
         x = layers._laid_out(x, _map_strides)
         if not self._takes(x):

@@ -75,3 +75,18 @@ def test_channels_that_the_norm_does_not_take():
                 with torch.no_grad(), pytest.raises(ValueError, match="multiple of eight and of the groups"):
                     call(x, groups)
         assert ctl.numel == []
+
+
+def test_parameters_are_left_alone():
+    """A parameter that is a layer's input (learned queries) is no context tensor: the hooks do not compress it either."""
+    query = torch.randn(2, 9, 64, device="cuda", requires_grad=True)
+    w = torch.randn(16, 64, device="cuda", requires_grad=True)
+    ctl = Controller([query, w], group_size=64, bits=1, min_numel=64)
+    ctl.begin_iteration()
+    with ctl.hooks():
+        y, z = ctl.linear(query, w), ctl.group_norm(query, 8)
+    assert ctl.numel == []
+    g = torch.randn_like(y)
+    assert torch.equal(torch.autograd.grad(y, w, g)[0], torch.autograd.grad(torch.nn.functional.linear(query, w), w, g)[0])
+    g = torch.randn_like(z)
+    assert torch.equal(torch.autograd.grad(z, query, g)[0], torch.autograd.grad(layers.group_norm(query, 8), query, g)[0])

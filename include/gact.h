@@ -435,8 +435,10 @@ int gact_head_norm_rotate_backward(const gact_heads *h_parts, int n_parts, const
  *     m = mean x,   r = 1 / sqrt(mean (x - m)^2 + eps),   n = (x - m) * r,   z = n * w + b,   y = act(z),
  * act(z) = z (GACT_ACT_NONE) or z / (1 + exp(-z)) (GACT_ACT_SILU).  Backward, n from the forward pass's m and r,
  *     dz = dy * act'(z),  g = dz * w,  dx = r * (g - mean g - n * mean(g * n)),  dw = sum of dz * n,  db = sum of dz.
- * Arithmetic in binary32, sums over threads' parts in binary32 and from there on in binary64, all in an order that depends
- * on the sizes only; outputs rounded once.  Samples reach each other in dw and db only.
+ * Arithmetic in binary32.  Sums over what a wavefront holds of a group (a workgroup, where the group is too large for one) in
+ * binary32, of these in binary64, m and r rounded once from there; a sample's part of dw and db is rounded to binary32.  The order
+ * depends on sizes, type, width and activation only, so that every call gives the same.  Outputs are rounded once.  Samples reach
+ * each other in dw and db only.
  *
  * Context.  With bits in {1, 2, 4, 8} the forward pass writes what gact_compress gives for x laid out contiguously with
  * the same group_size, bits and seed, byte for byte, and the backward pass uses codes * step + minimum (in

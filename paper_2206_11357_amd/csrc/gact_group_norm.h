@@ -46,6 +46,7 @@ struct GnArgs {
     uint32_t    block_shift;            // log2 of a context group's blocks of eight
     float       eps;
     int32_t     w_f32;
+    double      inv;                    // 1 / (P D)
     // Kernels that hold their maps in registers: a workgroup takes the whole of a sample's next few units, a unit being a group of
     // the norm, or as many groups as are whole columns.  A unit's columns are lanes 0 .. unit_cols - 1 of 2^unit_shift.
     uint32_t    units, unit_cols, unit_shift, slab_shift, col_shift;       // slab_shift: log2 of a slab's units; col_shift: of its lanes
@@ -74,6 +75,7 @@ inline void plan_group_norm(GnArgs* a, int dtype) {
     a->by_p = divisor(a->P);
     a->by_d = divisor(a->D);
     a->by_cols = divisor(a->cols);
+    a->inv = 1.0 / ((double)a->P * a->D);
     a->blocks8 = a->B * a->P * a->C8;
     const uint64_t want = kGnBlocks / ((uint64_t)a->B * a->slabs) ? kGnBlocks / ((uint64_t)a->B * a->slabs) : 1;
     a->batch = a->rows * gn_batch(dtype);

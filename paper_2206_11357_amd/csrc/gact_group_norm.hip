@@ -583,9 +583,10 @@ struct WholePlace {
         c8 = unit * a.unit_cols + cu;
     }
 };
-// Sum of v over a slab's rows, for each of the lane's values; UNI: over its unit's columns too.  In all lanes.
+// Sum of v over a slab's rows, for each of the lane's values; UNI: over its unit's columns too.  A wavefront's in binary32, theirs in
+// binary64; in all lanes.
 template <int NT, int N, bool UNI>
-__device__ __forceinline__ void over_rows(const GnArgs& a, const WholePlace& at, float (&lds)[NT / 64][64 * N], float (&v)[N]) {
+__device__ __forceinline__ void over_rows(const GnArgs& a, const WholePlace& at, float (&lds)[NT / 64][64 * N], float (&v)[N], double (&sum)[N]) {
     const int cols = 1 << a.col_shift, unit = UNI ? 1 << a.unit_shift : 1;
     for (int m = 1; m < 64; m <<= 1) {
         if (m >= unit && m < cols) continue;
@@ -600,46 +601,56 @@ __device__ __forceinline__ void over_rows(const GnArgs& a, const WholePlace& at,
     const int c = at.lane & (cols - 1);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        float s = 0.0f;
+        sum[k] = 0.0;
 #pragma unroll
-        for (int w = 0; w < NT / 64; ++w) s += lds[w][c * N + k];
-        v[k] = s;
+        for (int w = 0; w < NT / 64; ++w) sum[k] += (double)lds[w][c * N + k];
     }
 }
 // Room for the sums of groups that are no whole columns: of the slab's channels, and of its groups.
 template <int N>
 struct GroupRoom {
-    float of_channel[N][64 * 8], of_group[N][64 * 8];
+    double of_channel[N][64 * 8];
+    float  of_group[N][64 * 8];
 };
 template <>
 struct GroupRoom<0> {};
-// Sums of the groups of the lane's eight channels, from sums of the channels, which the lanes of row 0 hold: for each of N values.
-template <int N>
-__device__ __forceinline__ void over_groups(const GnArgs& a, const WholePlace& at, GroupRoom<N>& room, float (&v)[N][8]) {
-    if (at.row == 0) {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) room.of_channel[i][at.col * 8 + k] = v[i][k];
-    }
+// of_group: what finish makes of the groups' sums of of_channel, which the lanes of row 0 have filled.
+template <int N, typename FINISH>
+__device__ __forceinline__ void over_groups(const GnArgs& a, const WholePlace& at, GroupRoom<N>& room, FINISH finish) {
     __syncthreads();
     const uint32_t each = a.unit_cols * 8 / a.D;                        // groups of a unit
     for (uint32_t t = threadIdx.x; t < each << a.slab_shift; t += at.threads) {
         const uint32_t unit = t / each, first = (unit << a.unit_shift) * 8 + (t - unit * each) * a.D;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float s = 0.0f;
+            double s = 0.0;
             for (uint32_t d = 0; d < a.D; ++d) s += room.of_channel[i][first + d];
-            room.of_group[i][t] = s;
+            room.of_group[i][t] = finish(s);
         }
     }
     __syncthreads();
-    const uint32_t unit = at.col >> a.unit_shift, cu = at.col & ((1u << a.unit_shift) - 1u);
+}
+// of_group of the groups that the lane's channels are in.
+__device__ __forceinline__ void of_lanes(const GnArgs& a, const WholePlace& at, const float (&of_group)[64 * 8], float (&v)[8]) {
+    const uint32_t unit = at.col >> a.unit_shift, cu = at.col & ((1u << a.unit_shift) - 1u), each = a.unit_cols * 8 / a.D;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const uint32_t t = unit * each + divided(cu * 8 + (uint32_t)k, a.by_d);
+        v[k] = of_group[t < 512u ? t : 511u];          // (lanes that hold nothing)
+    }
+}
+// What finish makes of a lane's groups' sums: of one group's, which all of its lanes have, or of the channels', which have to be added.
+template <bool UNI, int N, int M, typename FINISH>
+__device__ __forceinline__ void finish_sums(const GnArgs& a, const WholePlace& at, GroupRoom<M>& room, const double (&sum)[N], float (&v)[N], FINISH finish) {
+    if constexpr (UNI) {
+        v[0] = finish(sum[0]);
+    } else {
+        if (at.row == 0) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i][k] = room.of_group[i][t < 512u ? t : 511u];        // (lanes that hold nothing)
+            for (int k = 0; k < 8; ++k) room.of_channel[0][at.col * 8 + k] = sum[k];
+        }
+        over_groups<1>(a, at, room, finish);
+        of_lanes(a, at, room.of_group[0], v);
     }
 }
 
@@ -658,6 +669,13 @@ __device__ __forceinline__ void gn_compress_blocks(const GnArgs& a) {
         widen8<DT>(load8<DT>((const uint8_t*)a.x.p, at * kSize<DT>), v);
         gn_compress_pass<BITS>(a, pass, lane, active, v);
     }
+}
+
+// 1 / sqrt(v), rounded once: binary32's, and a step of Newton's in binary64.
+__device__ __forceinline__ float inverse_root(double v) {
+    const float r = 1.0f / __builtin_sqrtf((float)v);
+    const double d = (double)r;
+    return r > 0.0f ? (float)(d + 0.5 * d * (1.0 - v * d * d)) : r;      // (squares that have passed binary32: 0; NaN)
 }
 
 // One launch forward: x is read once for y; once more for a context, whose groups do not keep to the norm's.
@@ -685,8 +703,8 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_kernel(GnArg
         raw[i] = Raw<DT>{};
         if (at.holds && p < a.P) raw[i] = load8<DT>((const uint8_t*)a.x.p, (in + (int64_t)p * a.x.pixel) * kSize<DT>);
     }
-    const float inv = 1.0f / ((float)a.P * (float)a.D);
     float m[N], r[N];
+    double sum[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) m[k] = r[k] = 0.0f;
 #pragma unroll
@@ -698,10 +716,8 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_kernel(GnArg
 #pragma unroll
             for (int k = 0; k < 8; ++k) m[k % N] += v[k];
     }
-    over_rows<NT, N, UNI>(a, at, lds[0], m);
-    if constexpr (!UNI) over_groups<1>(a, at, room, (float (&)[1][8])m);
-#pragma unroll
-    for (int k = 0; k < N; ++k) m[k] *= inv;
+    over_rows<NT, N, UNI>(a, at, lds[0], m, sum);
+    finish_sums<UNI>(a, at, room, sum, m, [&](double v) { return (float)(v * a.inv); });
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         if (at.row + (uint32_t)i * at.rows >= a.P) continue;
@@ -720,10 +736,8 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_kernel(GnArg
     if (!at.holds)
 #pragma unroll
         for (int k = 0; k < N; ++k) r[k] = 0.0f;
-    over_rows<NT, N, UNI>(a, at, lds[1], r);
-    if constexpr (!UNI) over_groups<1>(a, at, room, (float (&)[1][8])r);
-#pragma unroll
-    for (int k = 0; k < N; ++k) r[k] = 1.0f / __builtin_sqrtf(__builtin_fmaf(r[k], inv, a.eps));
+    over_rows<NT, N, UNI>(a, at, lds[1], r, sum);
+    finish_sums<UNI>(a, at, room, sum, r, [&](double v) { return inverse_root(v * a.inv + (double)a.eps); });
     if (!at.holds) return;
     if (a.mean && at.row == 0) {
         const uint32_t first = at.sample * a.H;
@@ -759,17 +773,85 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_kernel(GnArg
     }
 }
 
+// Room for a slab's sums backward: of the lane's 16 values (its channels' dz, then dz n) by wavefronts, of the slab's channels, and of each
+// column's g and g n; behind the wavefronts' sums, of groups that are no whole columns.
+template <int NT>
+struct SlabRoom {
+    union {
+        float of_wave[NT / 64][64 * 16];
+        GroupRoom<2> of_groups;
+    };
+    double total[64 * 16], of_column[64][2];
+};
+// The slab's channels' sums of s, a wavefront's in binary32, theirs in binary64.
+template <int NT>
+__device__ __forceinline__ void over_slab(const GnArgs& a, const WholePlace& at, SlabRoom<NT>& room, float (&s)[16]) {
+    const int cols = 1 << a.col_shift;
+    for (int mask = cols; mask < 64; mask <<= 1)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s[k] += __shfl_xor(s[k], mask);
+    if (at.lane < cols) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) room.of_wave[at.wave][at.lane * 16 + k] = s[k];
+    }
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < cols * 16; i += NT) {
+        double v = 0.0;
+#pragma unroll
+        for (int k = 0; k < NT / 64; ++k) v += (double)room.of_wave[k][i];
+        room.total[i] = v;
+    }
+    __syncthreads();
+}
+// mean g and mean g n of the lane's group, whose columns are whole.
+template <int NT>
+__device__ __forceinline__ void slab_means(const GnArgs& a, const WholePlace& at, SlabRoom<NT>& room, const float (&w)[8], float& m1, float& m2) {
+    if ((int)threadIdx.x < 1 << a.col_shift) {
+        double t0 = 0.0, t1 = 0.0;
+        if (at.holds) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                t0 += (double)w[k] * room.total[threadIdx.x * 16 + k];
+                t1 += (double)w[k] * room.total[threadIdx.x * 16 + 8 + k];
+            }
+        }
+        room.of_column[threadIdx.x][0] = t0;
+        room.of_column[threadIdx.x][1] = t1;
+    }
+    __syncthreads();
+    const uint32_t first = at.col & ~((1u << a.unit_shift) - 1u);
+    double t0 = 0.0, t1 = 0.0;
+    for (uint32_t k = 0; k < a.unit_cols; ++k) {
+        t0 += room.of_column[first + k][0];
+        t1 += room.of_column[first + k][1];
+    }
+    m1 = (float)(t0 * a.inv);
+    m2 = (float)(t1 * a.inv);
+}
+// dw and db of the lane's channels, or the sample's part of them.
+template <int NT>
+__device__ __forceinline__ void leave_weights(const GnArgs& a, const WholePlace& at, const SlabRoom<NT>& room) {
+    if ((!a.dw && !a.db) || at.row != 0) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t c = at.c8 * 8u + (uint32_t)k;
+        const float db = (float)room.total[at.col * 16 + k], dw = (float)room.total[at.col * 16 + 8 + k];
+        if (a.B == 1) {
+            gn_put(a, a.dw, c, dw);
+            gn_put(a, a.db, c, db);
+        } else {
+            *(hf2*)(a.sums + ((size_t)at.sample * a.C + c) * 2) = hf2{db, dw};
+        }
+    }
+}
+
 // One launch backward for dx: dy is read once, dz stays in registers; x, mostly codes, is read again for dx.
 template <int DT, int BITS, bool UNI, bool SILU, int WHICH>
 __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_backward_kernel(GnArgs a) {
     constexpr int NT = (int)kGnWhole[WHICH].threads, R = (int)kGnWhole[WHICH].blocks;
-    __shared__ float lds[NT / 64][64 * 16];
-    __shared__ float total[64 * 16];
-    __shared__ float of_column[64][2];
-    __shared__ GroupRoom<UNI ? 0 : 2> room;
+    __shared__ SlabRoom<NT> slab;
     const WholePlace at(a, NT);
     const uint32_t c = at.c8 * 8u;
-    const int cols = 1 << a.col_shift;
     float w[8], b[8], dz[R][8], s[16];
     OfGroups<UNI> m, r;
 #pragma unroll
@@ -794,72 +876,24 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_backward_ker
             }
         }
     }
-    for (int mask = cols; mask < 64; mask <<= 1)
-#pragma unroll
-        for (int k = 0; k < 16; ++k) s[k] += __shfl_xor(s[k], mask);
-    if (at.lane < cols) {
-#pragma unroll
-        for (int k = 0; k < 16; ++k) lds[at.wave][at.lane * 16 + k] = s[k];
-    }
-    __syncthreads();
-    for (int i = (int)threadIdx.x; i < cols * 16; i += NT) {
-        float v = 0.0f;
-#pragma unroll
-        for (int k = 0; k < NT / 64; ++k) v += lds[k][i];
-        total[i] = v;
-    }
-    __syncthreads();
+    over_slab<NT>(a, at, slab, s);
     float m1[UNI ? 1 : 8], m2[UNI ? 1 : 8];
-    const float inv = 1.0f / ((float)a.P * (float)a.D);
     if constexpr (UNI) {
-        if ((int)threadIdx.x < cols) {
-            float t0 = 0.0f, t1 = 0.0f;
-            if (at.holds) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    t0 = __builtin_fmaf(w[k], total[threadIdx.x * 16 + k], t0);
-                    t1 = __builtin_fmaf(w[k], total[threadIdx.x * 16 + 8 + k], t1);
-                }
-            }
-            of_column[threadIdx.x][0] = t0;
-            of_column[threadIdx.x][1] = t1;
-        }
-        __syncthreads();
-        const uint32_t first = at.col & ~((1u << a.unit_shift) - 1u);
-        m1[0] = m2[0] = 0.0f;
-        for (uint32_t k = 0; k < a.unit_cols; ++k) {
-            m1[0] += of_column[first + k][0];
-            m2[0] += of_column[first + k][1];
-        }
-        m1[0] *= inv;
-        m2[0] *= inv;
+        slab_means<NT>(a, at, slab, w, m1[0], m2[0]);
     } else {
-        float g[2][8];
+        if (at.row == 0) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            g[0][k] = at.holds ? w[k] * total[at.col * 16 + k] : 0.0f;
-            g[1][k] = at.holds ? w[k] * total[at.col * 16 + 8 + k] : 0.0f;
-        }
-        over_groups<2>(a, at, room, g);
+            for (int k = 0; k < 8; ++k)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            m1[k % (UNI ? 1 : 8)] = g[0][k] * inv;
-            m2[k % (UNI ? 1 : 8)] = g[1][k] * inv;
+                for (int i = 0; i < 2; ++i)
+                    slab.of_groups.of_channel[i][at.col * 8 + k] = at.holds ? (double)w[k] * slab.total[at.col * 16 + 8 * i + k] : 0.0;
         }
+        over_groups<2>(a, at, slab.of_groups, [&](double v) { return (float)(v * a.inv); });
+        of_lanes(a, at, slab.of_groups.of_group[0], m1);
+        of_lanes(a, at, slab.of_groups.of_group[1], m2);
     }
     if (!at.holds) return;
-    if ((a.dw || a.db) && at.row == 0) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float db = total[at.col * 16 + k], dw = total[at.col * 16 + 8 + k];
-            if (a.B == 1) {
-                gn_put(a, a.dw, c + (uint32_t)k, dw);
-                gn_put(a, a.db, c + (uint32_t)k, db);
-            } else {
-                *(hf2*)(a.sums + ((size_t)at.sample * a.C + c + (uint32_t)k) * 2) = hf2{db, dw};
-            }
-        }
-    }
+    leave_weights<NT>(a, at, slab);
     const int64_t out = (int64_t)at.sample * a.dx.sample + c;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -879,12 +913,9 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_backward_ker
 template <int DT, int BITS, bool SILU>
 __global__ __launch_bounds__(kGnWhole[3].threads) void gn_held_backward_kernel(GnArgs a) {
     constexpr int NT = (int)kGnWhole[3].threads, R = (int)kGnWhole[3].blocks, kAhead = 4;
-    __shared__ float lds[NT / 64][64 * 16];
-    __shared__ float total[64 * 16];
-    __shared__ float of_column[64][2];
+    __shared__ SlabRoom<NT> slab;
     const WholePlace at(a, NT);
     const uint32_t c = at.c8 * 8u;
-    const int cols = 1 << a.col_shift;
     // lanes that hold nothing go through pixel 0 of column 0 without a part in the sums
     const uint32_t c8 = at.holds ? at.c8 : 0;
     const auto inside = [&](uint32_t p) { return p < a.P ? p : 0u; };
@@ -934,56 +965,11 @@ __global__ __launch_bounds__(kGnWhole[3].threads) void gn_held_backward_kernel(G
         }
         __builtin_amdgcn_sched_barrier(0);
     }
-    for (int mask = cols; mask < 64; mask <<= 1)
-#pragma unroll
-        for (int k = 0; k < 16; ++k) s[k] += __shfl_xor(s[k], mask);
-    if (at.lane < cols) {
-#pragma unroll
-        for (int k = 0; k < 16; ++k) lds[at.wave][at.lane * 16 + k] = s[k];
-    }
-    __syncthreads();
-    for (int i = (int)threadIdx.x; i < cols * 16; i += NT) {
-        float v = 0.0f;
-#pragma unroll
-        for (int k = 0; k < NT / 64; ++k) v += lds[k][i];
-        total[i] = v;
-    }
-    __syncthreads();
-    if ((int)threadIdx.x < cols) {
-        float t0 = 0.0f, t1 = 0.0f;
-        if (at.holds) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                t0 = __builtin_fmaf(w[k], total[threadIdx.x * 16 + k], t0);
-                t1 = __builtin_fmaf(w[k], total[threadIdx.x * 16 + 8 + k], t1);
-            }
-        }
-        of_column[threadIdx.x][0] = t0;
-        of_column[threadIdx.x][1] = t1;
-    }
-    __syncthreads();
-    const uint32_t first = at.col & ~((1u << a.unit_shift) - 1u);
-    float m1 = 0.0f, m2 = 0.0f;
-    for (uint32_t k = 0; k < a.unit_cols; ++k) {
-        m1 += of_column[first + k][0];
-        m2 += of_column[first + k][1];
-    }
-    const float inv = 1.0f / ((float)a.P * (float)a.D);
-    m1 *= inv;
-    m2 *= inv;
+    over_slab<NT>(a, at, slab, s);
+    float m1, m2;
+    slab_means<NT>(a, at, slab, w, m1, m2);
     if (!at.holds) return;
-    if ((a.dw || a.db) && at.row == 0) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float db = total[at.col * 16 + k], dw = total[at.col * 16 + 8 + k];
-            if (a.B == 1) {
-                gn_put(a, a.dw, c + (uint32_t)k, dw);
-                gn_put(a, a.db, c + (uint32_t)k, db);
-            } else {
-                *(hf2*)(a.sums + ((size_t)at.sample * a.C + c + (uint32_t)k) * 2) = hf2{db, dw};
-            }
-        }
-    }
+    leave_weights<NT>(a, at, slab);
     const int64_t out = (int64_t)at.sample * a.dx.sample + c;
     p = next = at.row;
     asm("" : "+v"(p), "+v"(next));

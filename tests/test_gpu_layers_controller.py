@@ -1,6 +1,7 @@
 """What a controller's layers do with inputs that they do not take as they are."""
 import pytest
 import torch
+from torch.utils.checkpoint import checkpoint
 
 import paper_2206_11357_amd as gact
 from paper_2206_11357_amd import layers
@@ -90,3 +91,31 @@ def test_parameters_are_left_alone():
     assert torch.equal(torch.autograd.grad(y, w, g)[0], torch.autograd.grad(torch.nn.functional.linear(query, w), w, g)[0])
     g = torch.randn_like(z)
     assert torch.equal(torch.autograd.grad(z, query, g)[0], torch.autograd.grad(layers.group_norm(query, 8), query, g)[0])
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_values_of_regions_that_are_computed_twice(reentrant):
+    """A checkpointed region's input is a context tensor of the hooks', the first; a reentrant one's second run begins with what was
+    compressed of it, and makes the contexts; else the first run makes them."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(2, 30, 64, generator=gen, device="cuda", requires_grad=True)
+    w = torch.randn(96, 64, generator=gen, device="cuda", requires_grad=True)
+    n = torch.randn(96, generator=gen, device="cuda", requires_grad=True)
+    ctl = Controller([w, n], group_size=64, bits=4, seed=4, min_numel=64)
+    ctl.begin_iteration()
+    with ctl.hooks():
+        y = checkpoint(lambda t: ctl.group_norm(ctl.linear(t, w), 12, n, act="silu"), x, use_reentrant=reentrant)
+    g = torch.randn(y.shape, generator=gen, device="cuda")
+    y.backward(g)
+    assert ctl.numel == [x.numel(), x.numel(), y.numel()]
+    with torch.no_grad():
+        if reentrant:
+            x.copy_(gact.gact_decompress(*gact.gact_compress(x, 64, 4, ctl.seed_of(0)), x.numel(), 64, 4).view_as(x))
+        a = torch.nn.functional.linear(x, w)
+        context = gact.make_group_norm_context(a, 12, 4, 64, ctl.seed_of(2))
+        again = gact.gact_group_norm(a, 12, n, act="silu", context=context)
+        assert reentrant or torch.equal(again, y)
+        da, dn, _ = gact.gact_group_norm_backward(g, 12, n, act="silu", context=context)
+        dw, _ = gact.gact_linear_weight_grad(da, *gact.gact_compress(x, 64, 4, ctl.seed_of(1)), 64, 64, 4)
+        assert torch.equal(n.grad, dn) and torch.equal(w.grad, dw)
+        assert torch.equal(x.grad, torch.mm(da.view(60, 96), w).view_as(x))

@@ -297,6 +297,7 @@ struct Loader {
     __device__ __forceinline__ void cut(uint32_t chunk, int first, int end) {
         if constexpr (EVEN) {
             if (chunk != short_chunk) return;
+            asm volatile("");                          // keeps it a branch, of the wavefront's: else four selections a chunk
 #pragma unroll
             for (int q = 0; q < L::kBlocks; ++q)
                 if (q >= first && q < end && bt + q * L::kRowsK >= a.T - chunk * L::BT) at_group[q] = kBehind;

@@ -12,9 +12,9 @@
 // (T. Chan, G. Golub, R. LeVeque 1979), so that nothing cancels.  Backward: sums of dz and dz n over the pixels for each
 // channel and sample, from which the groups' means and dw, db follow; then dx.
 // Where a sample's group fits a workgroup's registers, both are one pass over memory (and dw, db a second launch where there
-// are several samples).  Measured, us: 64 x 3136 x 256 fp32, 2 bits, held 133 forward, 112 backward (HBM: 631 and 449 MB as
-// counted, x a second time for its codes); 32 x 1024 x 512 bf16, SiLU, 4 bits, held 25.6 (the arithmetic of noise, rounding and
-// activation) and 19.9; 1 x 262144 x 128 bf16, SiLU, in passes 13.6 + 4.4 + 26.7 (reads at 4.9 TB/s).
+// are several samples).  Measured, us: 64 x 3136 x 256 fp32, 2 bits, held 137 forward, 110 backward (HBM: 631 and 448 MB as
+// counted, x a second time for its codes); 32 x 1024 x 512 bf16, SiLU, 4 bits, held 25.2 (calls in a row: norm without a context
+// 16.3, compressor alone 9.4, both 25.9) and 21.0; 1 x 262144 x 128 bf16, SiLU, in passes 13.2 + 4.4 + 26.2 (reads at 5.1 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -909,7 +909,7 @@ __global__ __launch_bounds__(kGnWhole[WHICH].threads) void gn_whole_backward_ker
     }
 }
 // The same for larger maps: few wavefronts with many registers each, which hold dy as it came, all of it on its way at once; x is
-// loaded kAhead pixels ahead, both times.
+// loaded kAhead pixels ahead, both times.  (Of the 256 registers fp32 and SiLU need 1 to 2 more, at 8 bits 9 and 5.)
 template <int DT, int BITS, bool SILU>
 __global__ __launch_bounds__(kGnWhole[3].threads) void gn_held_backward_kernel(GnArgs a) {
     constexpr int NT = (int)kGnWhole[3].threads, R = (int)kGnWhole[3].blocks, kAhead = 4;

@@ -9,10 +9,11 @@
 // the present ones.
 // The tokens are split over blocks where the tiles of dW are too few for the GPU; the splits' sums are added in a fixed
 // order by a second launch.
-// Measured, us with that launch: 32768 x 1024 x 4096 bf16, 4 bits 290 (a library's product of values decompressed before
-// 336), 8192 x 4096 x 1024 85 (93), 169343 x 256 x 256 fp32, 2 bits 124 (502).  Bound by the matrix unit at the clock that the
-// power allows, the decoding and the writes to shared memory beside it: of 311 (an earlier 290) 255 without fetching, 250
-// without decoding, 223 without the writes, 220 without products, 217 with products and their reads alone.
+// Measured, us with that launch: 32768 x 1024 x 4096 bf16, 4 bits 280 to 302 from card to card (a library's product of values
+// decompressed before 336), 8192 x 4096 x 1024 85 to 91 (93), 169343 x 256 x 256 fp32, 2 bits 117 to 133 (502).  Bound by the matrix
+// unit at the clock that the power allows, the decoding and the writes to shared memory beside it: of the first's 289 to 304 on one
+// card 266 without fetching, 259 without decoding, 205 without the writes, 206 without products, 205 with products and their reads
+// alone.
 #ifndef GACT_WEIGHT_KERNEL_H
 #define GACT_WEIGHT_KERNEL_H
 
@@ -139,7 +140,7 @@ struct Tiling {
 //         at most 2^-8 of the element and the third 2^-17, so that the others come to at most 2^-24 of a product, as much as its
 //         rounding to binary32 would; sums are binary32.  Six products of bf16 take 6 x 32 cycles of the matrix unit for 16 tokens, eight
 //         of fp32 8 x 64: 169343 x 256 x 256 takes 124 us with the sums' addition, 184 in fp32, and comes closer to the sum in 64 bits
-//         (6.8e-7 of it; the decompressed product by the library 4.0e-6).
+//         (6.7e-7 of it; the decompressed product by the library 4.0e-6).
 template <int DT, int FORM>
 struct Products {
     typedef Tiling<DT, FORM> L;
@@ -292,8 +293,8 @@ struct Loader {
     }
     // Tokens behind the last are behind the codes' end, but their elements may be some of the last group's, whose minimum or step, where it
     // is not finite, dy's zeros would not take out of the sums: they have none.  To be called for blocks first .. end - 1 of a thread in front
-    // of a chunk's fetch_x; the tensor's last chunk is fetched after all others.  (Asked in fetch_x, for each block, 32768 x 1024 x
-    // 4096 bf16 takes 300 us instead of 285, 169343 x 256 x 256 fp32 126 instead of 120.)
+    // of a chunk's fetch_x; the tensor's last chunk is fetched after all others.  (Asked in fetch_x, for each block, in turn with
+    // this: 32768 x 1024 x 4096 bf16 281.4 us | 280.2, 12608 x 1024 x 1024 46.4 | 45.6, and more registers spilled.)
     __device__ __forceinline__ void cut(uint32_t chunk, int first, int end) {
         if constexpr (EVEN) {
             if (chunk != short_chunk) return;
@@ -419,6 +420,8 @@ __device__ __forceinline__ float weight_element(const WeightArgs& a, uint32_t t,
     return s;
 }
 
+// Where 1024 threads leave 128 registers, some forms spill: long tiles of uneven codes 25 to 36 without a buffer and 6 with one at 8 bits
+// (fp32; bf16 1 to 8), tall tiles of fp32 without a buffer 3 to 5; those of whole groups through a buffer none.
 template <int DT, int BITS, int FORM, bool BUFFER, bool EVEN>
 __global__ __launch_bounds__(weight_tile(DT, FORM).threads, weight_tile(DT, FORM).threads == 1024 ? 4 : 2) void weight_kernel(WeightArgs a) {
     typedef Tiling<DT, FORM> L;

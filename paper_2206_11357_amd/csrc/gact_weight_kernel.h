@@ -136,11 +136,12 @@ struct Tiling {
 // Where a wavefront's operands lie in a chunk, and its products.  A step is 16 tokens; 16 lanes read 4 rows of 16 elements, of which
 // each gets a column.
 //   fp32  An element is the sum of three bf16, each the rounded rest of the ones before: 8 bits and a sign each, exactly (an infinity,
-//         and what bf16 rounds to one, leaves NaN, of which weight_element makes what it has to be).  Of the nine products of their parts the six largest are taken.  The second part is
-//         at most 2^-8 of the element and the third 2^-17, so that the others come to at most 2^-24 of a product, as much as its
-//         rounding to binary32 would; sums are binary32.  Six products of bf16 take 6 x 32 cycles of the matrix unit for 16 tokens, eight
-//         of fp32 8 x 64: 169343 x 256 x 256 takes 124 us with the sums' addition, 184 in fp32, and comes closer to the sum in 64 bits
-//         (6.7e-7 of it; the decompressed product by the library 4.0e-6).
+//         and what bf16 rounds to one, leaves NaN, of which weight_element makes what it has to be).  Of the nine products of their
+//         parts the six largest are taken.  The second part is at most 2^-8 of the element and the third 2^-17, so that the others
+//         come to at most 2^-24 of a product, as much as its rounding to binary32 would; sums are binary32.  Six products of bf16
+//         take 6 x 32 cycles of the matrix unit for 16 tokens, eight of fp32 8 x 64: 169343 x 256 x 256 takes 124 us with the sums'
+//         addition, 184 in fp32, and comes closer to the sum in 64 bits (6.8e-7 of it; the decompressed product by the library
+//         4.0e-6).
 template <int DT, int FORM>
 struct Products {
     typedef Tiling<DT, FORM> L;

@@ -518,11 +518,11 @@ int gact_group_norm_backward(const gact_channel_norm *h_norm, void *d_workspace,
  *                16-byte aligned, in use until the enqueued kernels have run; calls that share one must not overlap in time.
  * tokens == 0 writes zeros; out_features == 0 or in_features == 0 is GACT_OK and writes nothing but db.  tokens must
  * be below 2^31, out_features below 2^28, in_features below 2^22, tokens * in_features and out_features * in_features
- * below 2^34.  With dtype binary32, each product is exact to 2^-24 of itself, of values taken apart into bfloat16, whose parts
- * below 2^-126 may be lost; an element of dW whose sum is not finite that way (infinities, NaN, elements from 2^128 - 2^119 on) is added
- * again in binary32, at the cost of a pass over its tokens.  An infinity or NaN in a row of dy reaches that row's columns of dW
- * (rows of x^ times it), in a group's minimum or step the elements of
- * that group.  Can be captured into a HIP graph.
+ * below 2^34.  With dtype binary32, each product is exact to 2^-24 of itself, of values taken apart into bfloat16, whose least
+ * number leaves 2^-134 of an element at most; an element of dW whose sum is not finite that way (infinities, NaN, elements from
+ * 2^128 - 2^119 on) is added again in binary32, at the cost of a pass over its tokens.  An infinity or NaN in a row of
+ * dy reaches that row's columns of dW (rows of x^ times it), in a group's minimum or step the elements of that
+ * group.  Can be captured into a HIP graph.
  */
 typedef struct {
     const void  *dy;

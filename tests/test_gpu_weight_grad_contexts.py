@@ -93,3 +93,18 @@ def test_binary32_sums_as_binary32_has_them(T, N, K, w_dtype):
     assert torch.isnan(want[3]).all()
     if not bad.all():                                   # (24 columns are all in the last group)
         assert fine[15].sum() >= (K - bad.sum()) // 2 and torch.isinf(want[9]).any()
+
+
+@pytest.mark.parametrize("T,N,K", FORMS)
+def test_small_elements_in_binary32(T, N, K):
+    """Elements that bfloat16's least number, 2^-133, cuts the parts of: x^ is 1, and dW is dy's one row up to 2^-134 and the roundings of
+    test_each_product_is_exact_to_a_rounding."""
+    context = gact.gact_compress(torch.ones(T, K, device="cuda"), 32, 4, 1)
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    dy = torch.zeros(T, N, device="cuda")
+    exponents = -100.0 - (torch.arange(N, device="cuda") % 27)
+    dy[T // 2] = (1.0 + torch.rand(N, generator=gen, device="cuda")) * 2.0 ** exponents
+    dw, db = gact.gact_linear_weight_grad(dy, *context, K, 32, 4, bias=True)
+    want = dy[T // 2].double()[:, None]
+    off = (dw.double() - want).abs() - (2.0 ** -24 + 7 * 2.0 ** -23) * want - 2.0 ** -134
+    assert off.max() <= 0 and torch.equal(db, dy[T // 2])
